@@ -33,7 +33,7 @@ typedef enum {
   NGG_ENOMEM = -5     /* device or host allocation failed */
 } ngg_status;
 
-typedef enum { NGG_F32 = 0, NGG_BF16 = 1 } ngg_dtype;
+typedef enum { NGG_F32 = 0, NGG_BF16 = 1, NGG_FP8 = 2 /* cached keys and values of ngg_kv_pages only */ } ngg_dtype;
 
 /* Decoder shape.  The base model M of Section 4.1 is a pre-norm decoder with
  * RMSNorm, rotary multi-head attention (rotate-half pairing: element i pairs
@@ -312,6 +312,160 @@ ngg_status ngg_debug_peek(ngg_ctx *ctx, const char *name, void *dst, int64_t cap
 ngg_status ngg_debug_plan(int32_t dtype, int32_t gemm, int32_t tokens, int32_t n, int32_t k, int32_t *plan);
 ngg_status ngg_debug_gemm_kernel(int32_t dtype, int32_t gemm, int32_t tokens, int32_t n, int32_t k, int32_t shape, int32_t *kernel);
 ngg_status ngg_debug_tiles(ngg_ctx *ctx, int32_t shape);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Operators of a batched tree verification.  Drafts that form a tree share the tokens of their common beginnings: one
+ * model call on the tree's tokens verifies all of its paths at once, for many sequences side by side.  A program that
+ * runs its own projections chains, per layer, ngg_rotary and ngg_kv_write (or the latter alone, which can rotate the
+ * keys on the way) and ngg_tree_attention, and behind the output embedding ngg_token_logprobs.
+ *
+ * No context object.  Pointers are DEVICE pointers unless a comment says HOST; strides count elements, and the
+ * innermost dimension is contiguous.  Every call checks its arguments on the host, queues its kernels on hip_stream (a
+ * hipStream_t, NULL = the default stream) and returns without synchronising and without allocating; it may be captured
+ * into a HIP graph.  What lies in device memory (positions, slots, page numbers, lengths, targets) is not seen by
+ * the host: the kernels check it, and each call says what becomes of an entry out of range.  Errors are reported
+ * through ngg_last_error(NULL).  dtype: NGG_F32 or NGG_BF16 unless stated.
+ * --------------------------------------------------------------------------------------------------------------- */
+
+/* Rotary tables.  Pair i of the first rotary_dim elements of a head turns by the angle position * f_i, with
+ * f_i = theta^(-2i / rotary_dim) or, where a model runs past the length it was trained on, one of
+ *   LINEAR  f_i / factor
+ *   BASE    theta' = theta * factor^(rotary_dim / (rotary_dim - 2)) in the place of theta
+ *   BANDS   with n_i = original * f_i / 2 pi, the turns of the pair over the original length: f_i where n_i >= high,
+ *           f_i / factor where n_i <= low, and between the two the mean weighted by (n_i - low) / (high - low)
+ *   RAMP    the same mean, with a weight linear in the pair's index: 1 up to the pair that makes `high` turns (its index
+ *           rounded down), 0 from the one that makes `low` (rounded up).
+ * cos and sin are multiplied by `amplitude` (0 stands for 1). */
+enum { NGG_ROPE_PLAIN = 0, NGG_ROPE_LINEAR = 1, NGG_ROPE_BASE = 2, NGG_ROPE_BANDS = 3, NGG_ROPE_RAMP = 4 };
+typedef struct {
+  int32_t kind;
+  int32_t original; /* BANDS, RAMP: positions of the original training */
+  double factor;    /* >= 1; all kinds but PLAIN */
+  double low, high; /* BANDS, RAMP: 0 < low < high, in turns */
+  double amplitude;
+} ngg_rope_scaling;
+
+/* Fills cos and sin (HOST, [n_positions][rotary_dim / 2]), computed in 64 bits and rounded once.  No GPU.  rotary_dim
+ * even, 2 .. 1024; theta > 1; scaling may be NULL. */
+ngg_status ngg_rope_table(double theta, int32_t rotary_dim, int32_t n_positions, const ngg_rope_scaling *scaling,
+                          float *cos, float *sin);
+
+/* A table on the device and how it is applied. */
+typedef struct {
+  const float *cos, *sin; /* [n_positions][rotary_dim / 2] */
+  int32_t n_positions, rotary_dim;
+  int32_t interleaved;    /* 0: element i pairs with i + rotary_dim / 2; 1: element 2i with 2i + 1 */
+} ngg_rope;
+
+/* One tensor to rotate: [n_tokens][n_heads][head_dim].  in == out (with equal strides) rotates in place; otherwise the
+ * two must not overlap. */
+typedef struct {
+  const void *in;
+  void *out;
+  int64_t in_token, in_head, out_token, out_head;
+  int32_t n_heads;
+} ngg_rotary_rows;
+
+/* Rotary positions: every pair (x, y) of the first rotary_dim elements of a head becomes
+ * (x cos - y sin, y cos + x sin), the elements behind them are copied.  b may be NULL (queries and keys
+ * go in one launch as a and b).  inverse != 0 turns back by the same angle, which (amplitude 1) also is the gradient's
+ * direction.  A token whose position is outside 0 .. n_positions - 1 gets NaN in its pairs.  n_tokens >= 0;
+ * rotary_dim <= head_dim <= 1024. */
+ngg_status ngg_rotary(const ngg_rope *rope, const int32_t *positions, int32_t n_tokens, int32_t head_dim, int32_t dtype,
+                      const ngg_rotary_rows *a, const ngg_rotary_rows *b, int32_t inverse, void *hip_stream);
+
+/* A pool of pages of page_size positions each (a multiple of 32), shared by any number of sequences.  The caller owns the
+ * memory: k and v of the bytes that ngg_kv_bytes returns, 16-byte aligned, with no value that has to be set before
+ * the first write.  Slot s is position s % page_size of page s / page_size.  dtype NGG_F32, NGG_BF16, or NGG_FP8:
+ * every element in 8 bits (1 sign, 4 exponent, 3 fraction bits, largest magnitude 448, no infinities), times a power of
+ * two for each (position, head) of keys and of values, the smallest that brings the head's largest magnitude to 448 or
+ * below (2^-126 at least; 1 for a head of zeros), kept as its exponent + 127 in k_exp and v_exp.  Rounding is to nearest even; an element that is not
+ * finite is kept as NaN.  Writing what was read changes nothing.
+ * Layout (the library's own): page by page, head by head, tiles of 32 positions in matrix operand order, as the caches of ngg_debug_peek. */
+typedef struct {
+  void *k, *v;
+  uint8_t *k_exp, *v_exp; /* NGG_FP8: [n_pages][n_kv_heads][page_size]; otherwise NULL */
+  int32_t n_pages, page_size, n_kv_heads;
+  int32_t head_dim;       /* 32, 64 or 128 */
+  int32_t dtype;
+} ngg_kv_pages;
+
+/* Bytes of k (and of v), and of k_exp (and of v_exp; 0 without).  Host only; reads the sizes alone. */
+ngg_status ngg_kv_bytes(const ngg_kv_pages *pages, int64_t *values, int64_t *exponents);
+
+/* Writes keys and values [n_tokens][n_kv_heads][head_dim] of `dtype` (the pool's own, or any into NGG_FP8) to the slots
+ * [n_tokens], which are distinct; a token whose slot is negative or beyond the pool is not written.  rope
+ * not NULL: keys are rotated to `positions` on the way and rounded to `dtype` as ngg_rotary does (rotary_dim <= head_dim).  stride:
+ * HOST, of k's token and head and of v's token and head. */
+ngg_status ngg_kv_write(const ngg_kv_pages *pages, const void *k, const void *v, int32_t dtype, const int64_t *stride,
+                        const int32_t *slots, int32_t n_tokens, const ngg_rope *rope, const int32_t *positions,
+                        void *hip_stream);
+
+/* Reads slots [n_tokens] back into k and v, [n_tokens][n_kv_heads][head_dim] of `dtype` (the pool's own, or any from
+ * NGG_FP8); either may be NULL.  A slot outside the pool reads as zeros.  stride as in ngg_kv_write. */
+ngg_status ngg_kv_read(const ngg_kv_pages *pages, const int32_t *slots, int32_t n_tokens, int32_t dtype, void *k, void *v,
+                       const int64_t *stride, void *hip_stream);
+
+/* The mask and depths of a tree of n tokens.  parents: HOST [n], parents[j] < j, -1 for a token that follows the context
+ * directly.  mask: HOST [n][(n + 63) / 64], bit j % 64 of word j / 64 of row t set where j is t or one of its
+ * ancestors.  depth: HOST [n] or NULL, the number of ancestors (the token's position is the context's length plus
+ * it).  Host only; n <= NGG_TREE_MAX. */
+#define NGG_TREE_MAX 1024
+ngg_status ngg_tree_mask(const int32_t *parents, int32_t n, uint64_t *mask, int32_t *depth);
+
+/* Attention of a tree of tokens (a chain, a single new token: tree = 1) of every sequence over its cached positions.
+ * Sequence b has context_lens[b] cached positions; its tree's own keys and values are cached behind them, token j of the tree at position
+ * context_lens[b] + j whatever its depth.  Position p lies in slot pages[b][p / page_size] * page_size + p % page_size.  Token t
+ * sees every position of the context and the tree's tokens j <= t whose bit is set in row t of the mask (NULL: all j <= t).
+ *   out[b][t][h] = sum_p softmax_p(scale * q[b][t][h] . k[p][h'])  v[p][h'],   h' = h / (n_heads / n_kv_heads)
+ * with scores, sums and outputs held in 32 bits; for NGG_BF16 the probabilities become bf16 for the product
+ * with the values.  lse[b][t][h], if not NULL, is the logarithm of the sum of exp(scale * q . k).  A token that
+ * sees nothing, and a token behind the sequence's own tree_lens[b], gets zeros and an lse of minus infinity.
+ * Bits of positions, lengths and pages out of range: negative lengths count as 0, tree_lens is cut to
+ * `tree`, positions beyond the page list and those on a page outside the pool are not seen.  What lies behind the last
+ * position, or is masked, has no influence, NaN and infinities included. */
+typedef struct {
+  const void *q;
+  void *out;
+  float *lse;                              /* [batch][tree][n_heads] contiguous, or NULL */
+  int64_t q_batch, q_token, q_head, out_batch, out_token, out_head;
+  const int32_t *pages;                    /* [batch][max_pages] */
+  int64_t pages_batch;
+  const int32_t *context_lens, *tree_lens; /* [batch]; tree_lens NULL: `tree` each */
+  const uint64_t *mask;                    /* [batch][tree][(tree + 63) / 64], or NULL */
+  int64_t mask_batch, mask_token;          /* mask_batch 0: one mask for all */
+  int32_t max_pages, batch, tree, n_heads; /* batch 1 .. NGG_TREE_MAX, tree 1 .. NGG_TREE_MAX; n_heads <= 1024;
+                                              max_pages * page_size <= 2^30, times batch <= 2^36 */
+  int32_t dtype;                           /* of q and out; the pool's own, or any with NGG_FP8 */
+  float scale;                             /* > 0 */
+} ngg_tree_args;
+
+/* Bytes of workspace a call with these sizes needs (its pointers are not read).  Host only.  The workspace belongs to one
+ * call at a time: calls on one stream may share it. */
+ngg_status ngg_tree_attention_workspace(const ngg_kv_pages *pages, const ngg_tree_args *args, int64_t *bytes);
+ngg_status ngg_tree_attention(const ngg_kv_pages *pages, const ngg_tree_args *args, void *workspace, int64_t workspace_bytes,
+                              void *hip_stream);
+
+/* Log probabilities of given tokens.  With x = scale * logits[r] (scale the inverse of the temperature) and
+ * lse = log sum_v exp(x_v):  logprobs[r][i] = x[targets[r][i]] - lse;  entropy[r] = -sum_v p_v log p_v, p = exp(x - lse);
+ * top_ids[r], top_logprobs[r]: the top_n largest in falling order, equal ones by rising id (NaN counts as the largest).
+ * Ruled-out tokens (logits of minus infinity) have no share in the sums.  A target below 0 gives 0 (no token), one
+ * beyond the vocabulary NaN.  A row whose logits are all minus infinity has an lse and log probabilities of minus infinity and entropy 0; a row
+ * with NaN or plus infinity has NaN in lse, entropy and log probabilities.  Outputs are [n_rows][..] contiguous; lse, entropy and, without
+ * targets or top_n, the others may be NULL.  Sums are held in 32 bits.  0 <= top_n <= min(64, vocab), 0 <= n_targets <= 64. */
+typedef struct {
+  const void *logits;          /* [n_rows][vocab] */
+  int64_t row_stride;
+  int32_t dtype, n_rows, vocab;
+  float scale;                 /* > 0 */
+  const int32_t *targets;      /* [n_rows][n_targets] contiguous */
+  int32_t n_targets, top_n;
+  float *logprobs, *entropy, *lse, *top_logprobs;
+  int32_t *top_ids;
+} ngg_score_args;
+
+ngg_status ngg_token_logprobs_workspace(const ngg_score_args *args, int64_t *bytes);
+ngg_status ngg_token_logprobs(const ngg_score_args *args, void *workspace, int64_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -16,7 +16,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "csrc", "libngg.so")
 
 NGG_OK, NGG_EINVAL, NGG_ECAPACITY, NGG_ESTATE, NGG_EHIP, NGG_ENOMEM = 0, -1, -2, -3, -4, -5
-NGG_F32, NGG_BF16 = 0, 1
+NGG_F32, NGG_BF16, NGG_FP8 = 0, 1, 2
 PROF_CLASSES = ("gemm_qkv", "gemm_o", "gemm_gateup", "gemm_down", "gemm_unembed", "attention", "norm", "drafts",
                 "accept_commit", "other")
 
@@ -24,7 +24,8 @@ EXPORTS = ("ngg_create", "ngg_destroy", "ngg_prefill", "ngg_build_drafts", "ngg_
            "ngg_greedy_decode", "ngg_get_tokens", "ngg_last_error", "ngg_profile_enable", "ngg_profile_reset",
            "ngg_profile_read", "ngg_debug_peek", "ngg_bigram_table_build", "ngg_bigram_source", "ngg_profile_bracket_overhead", "ngg_unigram_build", "ngg_decode_more", "ngg_profile_sample",
            "ngg_context_drafts_static", "ngg_allocation", "ngg_profile_read_bandwidth", "ngg_step_graphs", "ngg_debug_plan", "ngg_debug_tiles",
-           "ngg_debug_gemm_kernel")
+           "ngg_debug_gemm_kernel", "ngg_rope_table", "ngg_rotary", "ngg_kv_bytes", "ngg_kv_write", "ngg_kv_read", "ngg_tree_mask",
+           "ngg_tree_attention_workspace", "ngg_tree_attention", "ngg_token_logprobs_workspace", "ngg_token_logprobs")
 NGG_STATIC_MAX_TOKENS = 32768
 
 
@@ -60,6 +61,38 @@ class ngg_stats(C.Structure):
                 ("ms_prefill", C.c_double), ("ms_drafts", C.c_double), ("ms_verify", C.c_double),
                 ("ms_commit", C.c_double), ("accept_hist", (C.c_int64 * 34) * 2), ("rank_hist", (C.c_int64 * 32) * 2),
                 ("alloc_hist", C.c_int64 * 33)]
+
+
+class ngg_rope_scaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("original", C.c_int32)] + [(n, C.c_double) for n in ("factor", "low", "high", "amplitude")]
+
+
+class ngg_rope(C.Structure):
+    _fields_ = [("cos", C.c_void_p), ("sin", C.c_void_p)] + [(n, C.c_int32) for n in ("n_positions", "rotary_dim", "interleaved")]
+
+
+class ngg_rotary_rows(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p)] + [(n, C.c_int64) for n in ("in_token", "in_head", "out_token", "out_head")] + \
+               [("n_heads", C.c_int32)]
+
+
+class ngg_kv_pages(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_exp", "v_exp")] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")]
+
+
+class ngg_tree_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "out", "lse")] + \
+               [(n, C.c_int64) for n in ("q_batch", "q_token", "q_head", "out_batch", "out_token", "out_head")] + \
+               [("pages", C.c_void_p), ("pages_batch", C.c_int64), ("context_lens", C.c_void_p), ("tree_lens", C.c_void_p),
+                ("mask", C.c_void_p), ("mask_batch", C.c_int64), ("mask_token", C.c_int64)] + \
+               [(n, C.c_int32) for n in ("max_pages", "batch", "tree", "n_heads", "dtype")] + [("scale", C.c_float)]
+
+
+class ngg_score_args(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("row_stride", C.c_int64)] + [(n, C.c_int32) for n in ("dtype", "n_rows", "vocab")] + \
+               [("scale", C.c_float), ("targets", C.c_void_p), ("n_targets", C.c_int32), ("top_n", C.c_int32)] + \
+               [(n, C.c_void_p) for n in ("logprobs", "entropy", "lse", "top_logprobs", "top_ids")]
 
 
 _lib = None
@@ -103,6 +136,17 @@ def load_library():
     lib.ngg_debug_gemm_kernel.argtypes = [C.c_int32] * 6 + [i32p]
     lib.ngg_debug_tiles.argtypes = [vp, C.c_int32]
     lib.ngg_context_drafts_static.argtypes = [vp, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp]
+    ref = C.POINTER
+    lib.ngg_rope_table.argtypes = [C.c_double, C.c_int32, C.c_int32, ref(ngg_rope_scaling), vp, vp]
+    lib.ngg_rotary.argtypes = [ref(ngg_rope), vp, C.c_int32, C.c_int32, C.c_int32, ref(ngg_rotary_rows), ref(ngg_rotary_rows), C.c_int32, vp]
+    lib.ngg_kv_bytes.argtypes = [ref(ngg_kv_pages), ref(C.c_int64), ref(C.c_int64)]
+    lib.ngg_kv_write.argtypes = [ref(ngg_kv_pages), vp, vp, C.c_int32, vp, vp, C.c_int32, ref(ngg_rope), vp, vp]
+    lib.ngg_kv_read.argtypes = [ref(ngg_kv_pages), vp, C.c_int32, C.c_int32, vp, vp, vp, vp]
+    lib.ngg_tree_mask.argtypes = [vp, C.c_int32, vp, vp]
+    lib.ngg_tree_attention_workspace.argtypes = [ref(ngg_kv_pages), ref(ngg_tree_args), ref(C.c_int64)]
+    lib.ngg_tree_attention.argtypes = [ref(ngg_kv_pages), ref(ngg_tree_args), vp, C.c_int64, vp]
+    lib.ngg_token_logprobs_workspace.argtypes = [ref(ngg_score_args), ref(C.c_int64)]
+    lib.ngg_token_logprobs.argtypes = [ref(ngg_score_args), vp, C.c_int64, vp]
     for name in EXPORTS:
         if name != "ngg_last_error":
             getattr(lib, name).restype = C.c_int32
@@ -353,3 +397,15 @@ def context_drafts_static(tokens, w, k_ctx_max, q_min, q_max, rows, n_rows, stre
                                        int(q_min), int(q_max), rows.data_ptr(), n_rows.data_ptr(), s.cuda_stream)
     if st != NGG_OK:
         raise NggError(st, lib.ngg_last_error(None).decode())
+
+
+_OPERATORS = ("KVPages", "Rope", "TokenLogprobs", "rotary", "token_logprobs", "tree_attention", "tree_mask")
+
+
+def __getattr__(name):
+    """The operators of a batched tree verification (operators.py), which import torch, on their first use."""
+    if name not in _OPERATORS:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    from . import operators
+    globals().update({n: getattr(operators, n) for n in _OPERATORS})
+    return globals()[name]

@@ -2,6 +2,7 @@
 // one verify step and the decode loop.  Host logic only; every step of the path runs in kernels.
 #include "ngg.h"
 #include "ngg_internal.h"
+#include "ngg_operators.h"
 
 #include <algorithm>
 #include <chrono>
@@ -134,6 +135,25 @@ ngg_status fail(ngg_ctx *c, ngg_status st, const char *fmt, ...) {
   else g_create_error = buf;
   return st;
 }
+
+}  // namespace
+
+namespace ngg {
+ngg_status fail_global(ngg_status st, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  try {
+    return fail(nullptr, st, "%s", buf);
+  } catch (...) {                                         // no memory for the message: the status stands
+    return st;
+  }
+}
+}  // namespace ngg
+
+namespace {
 
 #define NGG_HIP(c, call)                                                                                  \
   do {                                                                                                    \
