@@ -452,7 +452,7 @@ ngg_status ngg_tree_attention(const ngg_kv_pages *pages, const ngg_tree_args *ar
  * Ruled-out tokens (logits of minus infinity) have no share in the sums.  A target below 0 gives 0 (no token), one
  * beyond the vocabulary NaN.  A row whose logits are all minus infinity has an lse and log probabilities of minus infinity and entropy 0; a row
  * with NaN or plus infinity has NaN in lse, entropy and log probabilities.  Outputs are [n_rows][..] contiguous; lse, entropy and, without
- * targets or top_n, the others may be NULL.  Sums are held in 32 bits.  0 <= top_n <= min(64, vocab), 0 <= n_targets <= 64. */
+ * targets or top_n, the others may be NULL.  Sums are held in 32 bits.  0 <= top_n <= min(64, vocab), 0 <= n_targets <= 64, vocab <= 2^30. */
 typedef struct {
   const void *logits;          /* [n_rows][vocab] */
   int64_t row_stride;

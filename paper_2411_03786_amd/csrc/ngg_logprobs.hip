@@ -1,8 +1,21 @@
 // Log probabilities of given tokens under rows of logits, with the entropy and the likeliest alternatives.
 //   m = max x,  s = sum e^(x - m),  lse = m + log s,  entropy = log s - (sum e^(x - m) (x - m)) / s
+// All of it in one pass over the logits: every lane keeps sums against a reference of its own, every wave a list of candidates
+// for the likeliest tokens.  A row is cut into slices where the rows alone would not fill the chip; a second kernel joins them.
 #include "ngg_operators.h"
 
+#include <algorithm>
+
 namespace ngg {
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.6931471805599453f;
+constexpr int NV = 4;            // vectors of 16 bytes that a lane takes at a time: a batch of a wave is 4 KB
+constexpr int kList = 512;       // places in a wave's list of candidates
+constexpr int kMaxSlices = 64;   // of a row: the joining wave has a lane for each
+
+typedef unsigned long long key_t64;
 
 // A float as an unsigned integer of the same order (-0 and 0 alike), NaN above everything.
 __device__ __forceinline__ unsigned order_key(float x) {
@@ -10,89 +23,304 @@ __device__ __forceinline__ unsigned order_key(float x) {
   if (x != x) return 0xfffffffeu;
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ float key_value(unsigned k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+// Larger for larger values, among equal ones for lower places: no two places share a key
+__device__ __forceinline__ key_t64 place_key(float x, int v) { return (key_t64)order_key(x) << 32 | (unsigned)~v; }
+__device__ __forceinline__ int key_place(key_t64 k) { return (int)~(unsigned)k; }
 
-template <typename T>
-__global__ __launch_bounds__(256) void logprobs_row_kernel(const ScoreArgs a) {
-  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const T *x = (const T *)a.x + (int64_t)r * a.row_stride;
-  __shared__ float red[4][3];
-  __shared__ unsigned long long best[4];
-  float m = -__builtin_inff(), s = 0.0f, t = 0.0f;
-  bool bad = false;
-  for (int v = tid; v < a.V; v += 256) {
-    const float y = to_f32(x[v]) * a.scale;
-    bad |= !(y < __builtin_inff());
-    if (y > m) {
-      const float d = m - y, f = m == -__builtin_inff() ? 0.0f : expf(d);
-      t = f > 0.0f ? f * (t + s * d) : 0.0f;
-      s *= f;
-      m = y;
+// Sums against a reference in units of the logits: s = sum 2^d, t = sum 2^d d with d = (x - m) c, c = scale log2(e).  The reference
+// starts at the lowest finite float, so that a row of those has sums too; minus infinity adds nothing.
+struct Sums { float m, s, t; };
+__device__ __forceinline__ Sums no_sums() { return {-3.402823466e38f, 0.0f, 0.0f}; }
+__device__ __forceinline__ void move_to(Sums &a, float m, float c) {
+  const float d = (a.m - m) * c, f = __builtin_amdgcn_exp2f(d);
+  a.t = f > 0.0f ? f * (a.t + a.s * d) : 0.0f;
+  a.s *= f;
+  a.m = m;
+}
+__device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  move_to(a, m, c);
+  move_to(b, m, c);
+  return {m, a.s + b.s, a.t + b.t};
+}
+
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+  static constexpr int n = 4;
+  static __device__ __forceinline__ void load(const float *p, float *x) {
+    const f32x4 v = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = v[e];
+  }
+};
+template <> struct Vec<bf16_t> {
+  static constexpr int n = 8;
+  static __device__ __forceinline__ void load(const bf16_t *p, float *x) {
+    const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16);
+  }
+};
+
+// The n largest of a wave's cnt candidates (cnt <= kList), sorted to the front of its list.  Every candidate counts those above it.
+__device__ __forceinline__ void select(key_t64 *list, int cnt, int n, int lane) {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  key_t64 own[kList / 64];
+  int rank[kList / 64];
+#pragma unroll
+  for (int i = 0; i < kList / 64; ++i) {
+    own[i] = lane + 64 * i < cnt ? list[lane + 64 * i] : 0;
+    rank[i] = 0;
+  }
+  if (cnt <= 128) {
+    for (int j = 0; j < cnt; ++j) {
+      const key_t64 k = list[j];
+      rank[0] += k > own[0];
+      rank[1] += k > own[1];
     }
-    if (y > -__builtin_inff()) {
-      const float e = expf(y - m);
-      s += e;
-      if (e > 0.0f) t += e * (y - m);
+  } else {
+    for (int j = 0; j < cnt; ++j) {
+      const key_t64 k = list[j];
+#pragma unroll
+      for (int i = 0; i < kList / 64; ++i) rank[i] += k > own[i];
     }
   }
-  auto join = [](float &m, float &s, float &t, float m2, float s2, float t2) {
-    const float n = fmaxf(m, m2);
-    if (n == -__builtin_inff()) return;
-    const float d = m - n, d2 = m2 - n, f = m == -__builtin_inff() ? 0.0f : expf(d), f2 = m2 == -__builtin_inff() ? 0.0f : expf(d2);
-    t = (f > 0.0f ? f * (t + s * d) : 0.0f) + (f2 > 0.0f ? f2 * (t2 + s2 * d2) : 0.0f);
-    s = s * f + s2 * f2;
-    m = n;
-  };
-  if (bad) s = __builtin_nanf("");
-  for (int o = 1; o < 64; o <<= 1) {
-    const float m2 = __shfl_xor(m, o), s2 = __shfl_xor(s, o), t2 = __shfl_xor(t, o);
-    const bool b2 = s != s || s2 != s2;
-    join(m, s, t, m2, s2, t2);
-    if (b2) s = __builtin_nanf("");
-  }
-  if (lane == 0) { red[wave][0] = m; red[wave][1] = s; red[wave][2] = t; }
-  __syncthreads();
-  m = red[0][0]; s = red[0][1]; t = red[0][2];
-  bad = s != s;
-  for (int w = 1; w < 4; ++w) {
-    bad |= red[w][1] != red[w][1];
-    join(m, s, t, red[w][0], red[w][1], red[w][2]);
-  }
-  const float ls = logf(s), lse = bad ? __builtin_nanf("") : s > 0.0f ? m + ls : -__builtin_inff();
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+  for (int i = 0; i < kList / 64; ++i)
+    if (lane + 64 * i < cnt && rank[i] < n) list[rank[i]] = own[i];
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// Results of a row from its sums; a thread each for the targets.
+struct RowResult { float lse; bool bad; };
+__device__ __forceinline__ RowResult finish_row(const ScoreArgs &a, int r, const Sums &q, int tid) {
+  RowResult o;
+  o.bad = q.s != q.s;                                      // NaN, or plus infinity less itself
+  const float ls = kLn2 * __builtin_log2f(q.s);
+  o.lse = o.bad ? __builtin_nanf("") : q.s > 0.0f ? q.m * a.scale + ls : -__builtin_inff();
   if (tid == 0) {
-    if (a.lse) a.lse[r] = lse;
-    if (a.entropy) a.entropy[r] = bad ? __builtin_nanf("") : s > 0.0f ? ls - t / s : 0.0f;
+    if (a.lse) a.lse[r] = o.lse;
+    if (a.entropy) a.entropy[r] = o.bad ? o.lse : q.s > 0.0f ? ls - kLn2 * q.t / q.s : 0.0f;
   }
-  auto logp = [&](float y) { return y == -__builtin_inff() && !bad ? y : y - lse; };
-  for (int i = tid; i < a.m; i += 256) {
+  return o;
+}
+__device__ __forceinline__ float logp(const ScoreArgs &a, const RowResult &o, float x) {
+  const float y = x * a.scale;
+  return y == -__builtin_inff() && !o.bad ? y : y - o.lse;
+}
+template <typename T>
+__device__ __forceinline__ void score_targets(const ScoreArgs &a, const RowResult &o, const T *x, int r, int tid, int threads) {
+  for (int i = tid; i < a.m; i += threads) {
     const int v = a.targets[(int64_t)r * a.m + i];
-    a.logprobs[(int64_t)r * a.m + i] = v < 0 ? 0.0f : v >= a.V ? __builtin_nanf("") : logp(to_f32(x[v]) * a.scale);
+    a.logprobs[(int64_t)r * a.m + i] = v < 0 ? 0.0f : v >= a.V ? __builtin_nanf("") : logp(a, o, to_f32(x[v]));
   }
-  unsigned long long prev = ~0ull;
+}
+__device__ __forceinline__ void put_top(const ScoreArgs &a, const RowResult &o, int r, int i, key_t64 k, float x) {
+  a.top_ids[(int64_t)r * a.top + i] = key_place(k);
+  a.top_logprobs[(int64_t)r * a.top + i] = logp(a, o, x);
+}
+// The likeliest tokens of a row that holds NaN: the lists leave those out, so the row is searched again, once for each place
+template <typename T>
+__device__ void top_with_nan(const ScoreArgs &a, const RowResult &o, const T *x, int r, int lane) {
+  key_t64 prev = ~0ull;
   for (int i = 0; i < a.top; ++i) {
-    unsigned long long b = 0;
-    for (int v = tid; v < a.V; v += 256) {
-      const unsigned long long k = (unsigned long long)order_key(to_f32(x[v]) * a.scale) << 32 | (unsigned)~v;
+    key_t64 b = 0;
+    for (int v = lane; v < a.V; v += 64) {
+      const key_t64 k = place_key(to_f32(x[v]), v);
       if (k < prev && k > b) b = k;
     }
-    for (int o = 1; o < 64; o <<= 1) { const unsigned long long c = __shfl_xor(b, o); b = c > b ? c : b; }
-    __syncthreads();
-    if (lane == 0) best[wave] = b;
-    __syncthreads();
-    for (int w = 0; w < 4; ++w) b = best[w] > b ? best[w] : b;
+    for (int off = 1; off < 64; off <<= 1) { const key_t64 c = __shfl_xor(b, off); b = c > b ? c : b; }
     prev = b;
-    if (tid == 0) {
-      const int v = (int)~(unsigned)b;
-      a.top_ids[(int64_t)r * a.top + i] = v;
-      a.top_logprobs[(int64_t)r * a.top + i] = logp(to_f32(x[v]) * a.scale);
-    }
+    if (lane == 0) put_top(a, o, r, i, b, to_f32(x[key_place(b)]));
   }
 }
 
-size_t score_workspace(int, int, int, int, int) { return 0; }
+// One workgroup per (row, slice).  TOP: with a list of the likeliest.
+template <typename T, bool TOP>
+__global__ __launch_bounds__(256) void logprobs_kernel(const ScoreArgs a, int slices) {
+  constexpr int VE = Vec<T>::n, K = NV * VE;               // elements of a vector, of a lane's batch
+  __shared__ key_t64 lists[TOP ? 4 : 1][TOP ? kList : 1];
+  __shared__ Sums wsum[4];
+  __shared__ int counts[4];
+  const int r = blockIdx.x / slices, slice = blockIdx.x % slices;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const T *x = (const T *)a.x + (int64_t)r * a.row_stride;
+  // vectors of the row lie on 16-byte boundaries of memory: the first may begin before it, the last end behind it
+  const int off = (int)(((uintptr_t)x / sizeof(T)) % VE);
+  const int n_vec = (a.V + off + VE - 1) / VE, batches = (n_vec + 64 * NV - 1) / (64 * NV);
+  const int b0 = (int)((int64_t)batches * slice / slices), b1 = (int)((int64_t)batches * (slice + 1) / slices);
+  const float c = a.scale * kLog2e;
+  Sums q = no_sums();
+  key_t64 *list = lists[TOP ? wave : 0];
+  int cnt = 0;
+  float tau = -__builtin_inff();                           // candidates have at least this value ...
+  key_t64 tau_key = 0;                                     // ... and a key above this
+  bool first = true;
+  for (int b = b0 + wave; b < b1; b += 4) {
+    float y[K];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int at = ((b * NV + i) * 64 + lane) * VE - off;
+      if (at >= 0 && at + VE <= a.V) Vec<T>::load(x + at, y + i * VE);
+      else
+#pragma unroll
+        for (int e = 0; e < VE; ++e) y[i * VE + e] = at + e >= 0 && at + e < a.V ? to_f32(x[at + e]) : -__builtin_inff();
+    }
+    float top = y[0];
+#pragma unroll
+    for (int e = 1; e < K; ++e) top = fmaxf(top, y[e]);
+    // the reference follows the largest value so far at a distance: sums of up to 2^16 more lose nothing
+    if (__ballot((top - q.m) * c > 16.0f) != 0 && top > q.m) move_to(q, top, c);
+#pragma unroll
+    for (int e = 0; e < K; ++e) {
+      const float d = (y[e] - q.m) * c, p = __builtin_amdgcn_exp2f(d);
+      q.s += p;
+      q.t += p * fmaxf(d, -1000.0f);                       // 2^-1000 is 0: minus infinity adds nothing
+    }
+    if constexpr (TOP) {
+      if (first) {
+        // the top-th largest of the lanes' maxima: as many elements at least are no smaller
+        first = false;
+        int rank = 0;
+#pragma unroll
+        for (int j = 0; j < 64; ++j) {
+          const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(top), j));
+          rank += o > top || (o == top && j < lane);
+        }
+        const uint64_t who = __ballot(rank == a.top - 1);
+        tau = who ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(top), __builtin_ctzll(who))) : -__builtin_inff();
+        tau_key = (key_t64)order_key(tau) << 32;
+      }
+      if (__ballot(top >= tau) != 0) {
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            float z = y[e];                                // (i is not unrolled: K copies of this would not fit the instruction cache)
+#pragma unroll
+            for (int j = 1; j < NV; ++j) z = i == j ? y[j * VE + e] : z;
+            const int v = ((b * NV + i) * 64 + lane) * VE - off + e;
+            bool in = z >= tau && v >= 0 && v < a.V;
+            if (__ballot(in) == 0) continue;
+            const key_t64 k = place_key(z, v);
+            in = in && k > tau_key;
+            const uint64_t m = __ballot(in);
+            if (in) list[cnt + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = k;
+            cnt += __builtin_popcountll(m);
+            if (cnt + 64 > kList) {                        // full: the top-th best becomes the bar
+              select(list, cnt, a.top, lane);
+              cnt = min(cnt, a.top);
+              if (cnt == a.top) {
+                tau_key = list[cnt - 1];
+                tau = key_value((unsigned)(tau_key >> 32));
+              }
+            }
+          }
+      }
+    }
+  }
+  // the lanes' sums, then the waves'
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) q = join(q, {__shfl_xor(q.m, o), __shfl_xor(q.s, o), __shfl_xor(q.t, o)}, c);
+  if (lane == 0) wsum[wave] = q;
+  if constexpr (TOP) {
+    select(list, cnt, a.top, lane);
+    if (lane == 0) counts[wave] = min(cnt, a.top);
+  }
+  __syncthreads();
+  q = join(join(wsum[0], wsum[1], c), join(wsum[2], wsum[3], c), c);
+  // the four lists' entries count those above them: 4 top <= 256
+  key_t64 mine = 0;
+  int rank = 0;
+  if constexpr (TOP) {
+    const int w = tid / a.top, i = tid % a.top;
+    if (w < 4 && i < counts[w]) {
+      mine = lists[w][i];
+      for (int j = 0; j < 4; ++j)
+        for (int k = 0; k < counts[j]; ++k) rank += lists[j][k] > mine;
+    }
+  }
+  if (slices > 1) {
+    Sums *ws = (Sums *)a.ws;
+    if (tid == 0) ws[(size_t)r * slices + slice] = q;
+    if constexpr (TOP) {
+      key_t64 *wl = (key_t64 *)((char *)a.ws + ((size_t)a.N * slices * sizeof(Sums) + 15) / 16 * 16) + ((size_t)r * slices + slice) * a.top;
+      if (mine && rank < a.top) wl[rank] = mine;
+      const int have = counts[0] + counts[1] + counts[2] + counts[3];
+      if (tid >= have && tid < a.top) wl[tid] = 0;
+    }
+    return;
+  }
+  const RowResult o = finish_row(a, r, q, tid);
+  score_targets(a, o, x, r, tid, 256);
+  if constexpr (TOP) {
+    if (!o.bad) {
+      if (mine && rank < a.top) put_top(a, o, r, rank, mine, to_f32(x[key_place(mine)]));
+    } else if (wave == 0) top_with_nan(a, o, x, r, lane);
+  }
+}
+
+// Joins the slices of a row: a lane for each, whose sorted list it holds by its head.  One wave per row.
+template <typename T>
+__global__ __launch_bounds__(64) void logprobs_join_kernel(const ScoreArgs a, int slices) {
+  const int r = blockIdx.x, lane = threadIdx.x;
+  const T *x = (const T *)a.x + (int64_t)r * a.row_stride;
+  const float c = a.scale * kLog2e;
+  Sums q = no_sums();
+  if (lane < slices) q = ((const Sums *)a.ws)[(size_t)r * slices + lane];
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) q = join(q, {__shfl_xor(q.m, o), __shfl_xor(q.s, o), __shfl_xor(q.t, o)}, c);
+  const RowResult o = finish_row(a, r, q, lane);
+  score_targets(a, o, x, r, lane, 64);
+  if (a.top == 0) return;
+  if (o.bad) {
+    top_with_nan(a, o, x, r, lane);
+    return;
+  }
+  const key_t64 *wl = (const key_t64 *)((const char *)a.ws + ((size_t)a.N * slices * sizeof(Sums) + 15) / 16 * 16) + ((size_t)r * slices + lane) * a.top;
+  int at = 0;
+  key_t64 head = lane < slices ? wl[0] : 0, next = lane < slices && a.top > 1 ? wl[1] : 0;
+  key_t64 found = 0;                                       // lane i keeps the i-th best
+  for (int i = 0; i < a.top; ++i) {
+    key_t64 b = head;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) { const key_t64 k = __shfl_xor(b, off); b = k > b ? k : b; }
+    if (i == lane) found = b;
+    if (head == b) {                                       // (keys differ, so one lane moves on)
+      head = next;
+      ++at;
+      next = at + 1 < a.top ? wl[at + 1] : 0;
+    }
+  }
+  if (lane < a.top) put_top(a, o, r, lane, found, to_f32(x[key_place(found)]));
+}
+
+// Slices of a row: as many as bring the rows to four workgroups for each of the 256 CUs, of a batch for every wave at least.
+int row_slices(int dtype, int N, int V) {
+  const int per = (dtype == NGG_F32 ? 4 : 8) * 64 * NV * 4;
+  return std::max(1, std::min({kMaxSlices, (1024 + N - 1) / N, V / per}));
+}
+
+}  // namespace
+
+size_t score_workspace(int dtype, int N, int V, int m, int top) {
+  (void)m;
+  const int s = N > 0 ? row_slices(dtype, N, V) : 1;
+  return s == 1 ? 0 : ((size_t)N * s * sizeof(Sums) + 15) / 16 * 16 + (size_t)N * s * top * sizeof(key_t64);
+}
+
+template <typename T>
+static void launch(const ScoreArgs &a, int slices, hipStream_t s) {
+  if (a.top) hipLaunchKernelGGL((logprobs_kernel<T, true>), dim3(a.N * slices), dim3(256), 0, s, a, slices);
+  else hipLaunchKernelGGL((logprobs_kernel<T, false>), dim3(a.N * slices), dim3(256), 0, s, a, slices);
+  if (slices > 1) hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3(a.N), dim3(64), 0, s, a, slices);
+}
 
 void launch_token_logprobs(int dtype, const ScoreArgs &a, hipStream_t s) {
-  if (dtype == NGG_F32) hipLaunchKernelGGL(logprobs_row_kernel<float>, dim3(a.N), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(logprobs_row_kernel<bf16_t>, dim3(a.N), dim3(256), 0, s, a);
+  const int slices = row_slices(dtype, a.N, a.V);
+  if (dtype == NGG_F32) launch<float>(a, slices, s);
+  else launch<bf16_t>(a, slices, s);
 }
 
 }  // namespace ngg

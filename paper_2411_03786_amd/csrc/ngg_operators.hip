@@ -81,7 +81,7 @@ ngg_status check_tree(const char *what, const ngg_kv_pages *p, const ngg_tree_ar
 ngg_status check_score(const char *what, const ngg_score_args *a, bool pointers) {
   if (!a) return fail_global(NGG_EINVAL, "%s: null arguments", what);
   if (!element_type(a->dtype)) return fail_global(NGG_EINVAL, "%s: dtype must be NGG_F32 or NGG_BF16", what);
-  if (a->n_rows < 0 || a->vocab < 1) return fail_global(NGG_EINVAL, "%s: %d rows of %d logits", what, a->n_rows, a->vocab);
+  if (a->n_rows < 0 || a->vocab < 1 || a->vocab > (1 << 30)) return fail_global(NGG_EINVAL, "%s: %d rows of %d logits", what, a->n_rows, a->vocab);
   if (a->top_n < 0 || a->top_n > 64 || a->top_n > a->vocab) return fail_global(NGG_EINVAL, "%s: top_n %d must be 0 .. min(64, vocab)", what, a->top_n);
   if (a->n_targets < 0 || a->n_targets > 64) return fail_global(NGG_EINVAL, "%s: n_targets %d must be 0 .. 64", what, a->n_targets);
   if (!pointers) return NGG_OK;
