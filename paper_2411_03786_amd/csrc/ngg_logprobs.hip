@@ -13,7 +13,7 @@ namespace {
 constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.6931471805599453f;
 constexpr int NV = 4;            // vectors of 16 bytes that a lane takes at a time: a batch of a wave is 4 KB
 constexpr int kList = 512;       // places in a wave's list of candidates
-constexpr int kMaxSlices = 64;   // of a row: the joining wave has a lane for each
+constexpr int kMaxSlices = 64;   // of a row: a joining wave has a lane for each
 
 typedef unsigned long long key_t64;
 
@@ -45,6 +45,20 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
   return {m, a.s + b.s, a.t + b.t};
 }
 
+// The sums of a wave, on every lane
+__device__ __forceinline__ Sums wave_sums(Sums a, float c) {
+  float m = a.m;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+  move_to(a, m, c);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    a.s += __shfl_xor(a.s, o);
+    a.t += __shfl_xor(a.t, o);
+  }
+  return a;
+}
+
 template <typename T> struct Vec;
 template <> struct Vec<float> {
   static constexpr int n = 4;
@@ -73,7 +87,9 @@ __device__ __forceinline__ void select(key_t64 *list, int cnt, int n, int lane) 
     own[i] = lane + 64 * i < cnt ? list[lane + 64 * i] : 0;
     rank[i] = 0;
   }
-  if (cnt <= 128) {
+  if (cnt <= 64) {
+    for (int j = 0; j < cnt; ++j) rank[0] += list[j] > own[0];
+  } else if (cnt <= 128) {
     for (int j = 0; j < cnt; ++j) {
       const key_t64 k = list[j];
       rank[0] += k > own[0];
@@ -91,6 +107,31 @@ __device__ __forceinline__ void select(key_t64 *list, int cnt, int n, int lane) 
   for (int i = 0; i < kList / 64; ++i)
     if (lane + 64 * i < cnt && rank[i] < n) list[rank[i]] = own[i];
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+__device__ __forceinline__ key_t64 uniform(key_t64 k) {
+  const unsigned hi = __builtin_amdgcn_readfirstlane((unsigned)(k >> 32)), lo = __builtin_amdgcn_readfirstlane((unsigned)k);   // (returned as int)
+  return (key_t64)hi << 32 | lo;
+}
+// Keeps the n best of the list and makes the n-th of them the bar; how many are left
+__device__ __forceinline__ int raise_bar(key_t64 *list, int cnt, int n, int lane, key_t64 &bar) {
+  select(list, cnt, n, lane);
+  if (cnt < n) return cnt;
+  bar = uniform(list[n - 1]);
+  return n;
+}
+// A value that n lanes at least, and mostly not many more, are no smaller than: bit by bit from the highest
+__device__ __forceinline__ unsigned lane_bar(unsigned k, int n) {
+  unsigned t = 0;
+  for (int bit = 31; bit >= 0; --bit) {
+    const unsigned u = t | 1u << bit;
+    const int have = __builtin_popcountll(__ballot(k >= u));
+    if (have >= n) {
+      t = u;
+      if (have <= n + 2) break;
+    }
+  }
+  return t;
 }
 
 // Results of a row from its sums; a thread each for the targets.
@@ -144,6 +185,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const ScoreArgs a, int sl
   __shared__ key_t64 lists[TOP ? 4 : 1][TOP ? kList : 1];
   __shared__ Sums wsum[4];
   __shared__ int counts[4];
+  __shared__ key_t64 shared_bar;                           // the best of the waves' bars: the top-th of a part is none of the row's best
   const int r = blockIdx.x / slices, slice = blockIdx.x % slices;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const T *x = (const T *)a.x + (int64_t)r * a.row_stride;
@@ -155,11 +197,21 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const ScoreArgs a, int sl
   Sums q = no_sums();
   key_t64 *list = lists[TOP ? wave : 0];
   int cnt = 0;
-  float tau = -__builtin_inff();                           // candidates have at least this value ...
-  key_t64 tau_key = 0;                                     // ... and a key above this
+  key_t64 bar = 0;                                         // candidates have a key above this (0: as a value, NaN)
   bool first = true;
+  // a wave sorts its list and raises the bar when that many are in it
+  const int raise_at = a.top + 16 > 2 * a.top ? a.top + 16 : 2 * a.top;
+  if constexpr (TOP) {
+    if (tid == 0) shared_bar = 0;
+    __syncthreads();
+  }
   for (int b = b0 + wave; b < b1; b += 4) {
     float y[K];
+    if constexpr (TOP) {                                   // another wave may have raised the bar
+      const key_t64 o = *(volatile key_t64 *)&shared_bar;
+      if (o > bar) bar = o;
+      bar = uniform(bar);
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int at = ((b * NV + i) * 64 + lane) * VE - off;
@@ -181,48 +233,49 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const ScoreArgs a, int sl
     }
     if constexpr (TOP) {
       if (first) {
-        // the top-th largest of the lanes' maxima: as many elements at least are no smaller
         first = false;
-        int rank = 0;
-#pragma unroll
-        for (int j = 0; j < 64; ++j) {
-          const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(top), j));
-          rank += o > top || (o == top && j < lane);
-        }
-        const uint64_t who = __ballot(rank == a.top - 1);
-        tau = who ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(top), __builtin_ctzll(who))) : -__builtin_inff();
-        tau_key = (key_t64)order_key(tau) << 32;
+        const key_t64 k = (key_t64)lane_bar(order_key(top), a.top) << 32;   // the bar of what this batch brings
+        if (k > bar) bar = k;
       }
-      if (__ballot(top >= tau) != 0) {
-        for (int i = 0; i < NV; ++i)
+      const float tau = key_value((unsigned)(bar >> 32));  // (a bar of 0 is NaN: nothing is below it)
+      const uint64_t who = __ballot(!(top < tau));
+      if (who != 0) {
+        if (cnt + K * __builtin_popcountll(who) <= kList) {
+          // few lanes hold candidates: they fit whatever there are
 #pragma unroll
-          for (int e = 0; e < VE; ++e) {
-            float z = y[e];                                // (i is not unrolled: K copies of this would not fit the instruction cache)
-#pragma unroll
-            for (int j = 1; j < NV; ++j) z = i == j ? y[j * VE + e] : z;
-            const int v = ((b * NV + i) * 64 + lane) * VE - off + e;
-            bool in = z >= tau && v >= 0 && v < a.V;
-            if (__ballot(in) == 0) continue;
-            const key_t64 k = place_key(z, v);
-            in = in && k > tau_key;
-            const uint64_t m = __ballot(in);
-            if (in) list[cnt + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = k;
+          for (int e = 0; e < K; ++e) {
+            if (__ballot(!(y[e] < tau)) == 0) continue;
+            const int v = ((b * NV + e / VE) * 64 + lane) * VE - off + e % VE;
+            const key_t64 k = place_key(y[e], v);
+            const uint64_t m = __ballot(k > bar && v >= 0 && v < a.V);
+            if (m >> lane & 1) list[cnt + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = k;
             cnt += __builtin_popcountll(m);
-            if (cnt + 64 > kList) {                        // full: the top-th best becomes the bar
-              select(list, cnt, a.top, lane);
-              cnt = min(cnt, a.top);
-              if (cnt == a.top) {
-                tau_key = list[cnt - 1];
-                tau = key_value((unsigned)(tau_key >> 32));
-              }
-            }
           }
+        } else {
+          for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+              float z = y[e];                              // (i is not unrolled: K copies of this would not fit the instruction cache)
+#pragma unroll
+              for (int j = 1; j < NV; ++j) z = i == j ? y[j * VE + e] : z;
+              const int v = ((b * NV + i) * 64 + lane) * VE - off + e;
+              const key_t64 k = place_key(z, v);
+              const uint64_t m = __ballot(k > bar && v >= 0 && v < a.V);
+              if (m == 0) continue;
+              if (m >> lane & 1) list[cnt + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = k;
+              cnt += __builtin_popcountll(m);
+              if (cnt + 64 > kList) cnt = raise_bar(list, cnt, a.top, lane, bar);
+            }
+        }
+        if (cnt >= raise_at) {
+          cnt = raise_bar(list, cnt, a.top, lane, bar);
+          if (lane == 0) atomicMax(&shared_bar, bar);
+        }
       }
     }
   }
   // the lanes' sums, then the waves'
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) q = join(q, {__shfl_xor(q.m, o), __shfl_xor(q.s, o), __shfl_xor(q.t, o)}, c);
+  q = wave_sums(q, c);
   if (lane == 0) wsum[wave] = q;
   if constexpr (TOP) {
     select(list, cnt, a.top, lane);
@@ -261,39 +314,44 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const ScoreArgs a, int sl
   }
 }
 
-// Joins the slices of a row: a lane for each, whose sorted list it holds by its head.  One wave per row.
+// Joins the slices of a row.  One workgroup per row.
 template <typename T>
-__global__ __launch_bounds__(64) void logprobs_join_kernel(const ScoreArgs a, int slices) {
-  const int r = blockIdx.x, lane = threadIdx.x;
+__global__ __launch_bounds__(256) void logprobs_join_kernel(const ScoreArgs a, int slices) {
+  __shared__ key_t64 kept[kMaxSlices * 64];
+  __shared__ int n_kept;
+  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const T *x = (const T *)a.x + (int64_t)r * a.row_stride;
   const float c = a.scale * kLog2e;
+  const key_t64 *wl = (const key_t64 *)((const char *)a.ws + ((size_t)a.N * slices * sizeof(Sums) + 15) / 16 * 16) + (size_t)r * slices * a.top;
   Sums q = no_sums();
   if (lane < slices) q = ((const Sums *)a.ws)[(size_t)r * slices + lane];
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) q = join(q, {__shfl_xor(q.m, o), __shfl_xor(q.s, o), __shfl_xor(q.t, o)}, c);
-  const RowResult o = finish_row(a, r, q, lane);
-  score_targets(a, o, x, r, lane, 64);
+  key_t64 low = ~0ull;
+  if (a.top && lane < slices) low = wl[(size_t)lane * a.top + (a.top + slices - 1) / slices - 1];
+  q = wave_sums(q, c);
+  const RowResult o = finish_row(a, r, q, tid);
+  score_targets(a, o, x, r, tid, 256);
   if (a.top == 0) return;
   if (o.bad) {
-    top_with_nan(a, o, x, r, lane);
+    if (tid < 64) top_with_nan(a, o, x, r, lane);
     return;
   }
-  const key_t64 *wl = (const key_t64 *)((const char *)a.ws + ((size_t)a.N * slices * sizeof(Sums) + 15) / 16 * 16) + ((size_t)r * slices + lane) * a.top;
-  int at = 0;
-  key_t64 head = lane < slices ? wl[0] : 0, next = lane < slices && a.top > 1 ? wl[1] : 0;
-  key_t64 found = 0;                                       // lane i keeps the i-th best
-  for (int i = 0; i < a.top; ++i) {
-    key_t64 b = head;
+  // the first top / slices entries of every list are `top` together: what is below the last of all of those is out
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) { const key_t64 k = __shfl_xor(b, off); b = k > b ? k : b; }
-    if (i == lane) found = b;
-    if (head == b) {                                       // (keys differ, so one lane moves on)
-      head = next;
-      ++at;
-      next = at + 1 < a.top ? wl[at + 1] : 0;
-    }
+  for (int off = 1; off < 64; off <<= 1) { const key_t64 k = __shfl_xor(low, off); low = k < low ? k : low; }
+  if (tid == 0) n_kept = 0;
+  __syncthreads();
+  for (int i = tid; i < slices * a.top; i += 256) {
+    const key_t64 k = wl[i];
+    if (k >= low && k) kept[atomicAdd(&n_kept, 1)] = k;
   }
-  if (lane < a.top) put_top(a, o, r, lane, found, to_f32(x[key_place(found)]));
+  __syncthreads();
+  const int n = n_kept;
+  for (int i = tid; i < n; i += 256) {
+    const key_t64 mine = kept[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += kept[j] > mine;
+    if (rank < a.top) put_top(a, o, r, rank, mine, to_f32(x[key_place(mine)]));
+  }
 }
 
 // Slices of a row: as many as bring the rows to four workgroups for each of the 256 CUs, of a batch for every wave at least.
@@ -314,7 +372,7 @@ template <typename T>
 static void launch(const ScoreArgs &a, int slices, hipStream_t s) {
   if (a.top) hipLaunchKernelGGL((logprobs_kernel<T, true>), dim3(a.N * slices), dim3(256), 0, s, a, slices);
   else hipLaunchKernelGGL((logprobs_kernel<T, false>), dim3(a.N * slices), dim3(256), 0, s, a, slices);
-  if (slices > 1) hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3(a.N), dim3(64), 0, s, a, slices);
+  if (slices > 1) hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3(a.N), dim3(256), 0, s, a, slices);
 }
 
 void launch_token_logprobs(int dtype, const ScoreArgs &a, hipStream_t s) {
