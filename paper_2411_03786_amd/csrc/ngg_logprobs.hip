@@ -28,29 +28,31 @@ __device__ __forceinline__ float key_value(unsigned k) { return __uint_as_float(
 __device__ __forceinline__ key_t64 place_key(float x, int v) { return (key_t64)order_key(x) << 32 | (unsigned)~v; }
 __device__ __forceinline__ int key_place(key_t64 k) { return (int)~(unsigned)k; }
 
-// Sums against a reference in units of the logits: s = sum 2^d, t = sum 2^d d with d = (x - m) c, c = scale log2(e).  The reference
-// starts at the lowest finite float, so that a row of those has sums too; minus infinity adds nothing.
+// Sums in the base-2 domain against a reference m: s = sum 2^d, t = sum 2^d d with d = x c - m, c = scale log2(e).  m is a whole number
+// wherever that is exact (up to 2^24), so that d is rounded once and a change of reference costs nothing.  A row that leaves s = 0
+// (nothing above -1e38), NaN or m >= 1e38 is summed again by odd_row.
 struct Sums { float m, s, t; };
-__device__ __forceinline__ Sums no_sums() { return {-3.402823466e38f, 0.0f, 0.0f}; }
-__device__ __forceinline__ void move_to(Sums &a, float m, float c) {
-  const float d = (a.m - m) * c, f = __builtin_amdgcn_exp2f(d);
+constexpr float kHuge = 1e38f;
+__device__ __forceinline__ Sums no_sums() { return {-kHuge, 0.0f, 0.0f}; }
+__device__ __forceinline__ void move_to(Sums &a, float m) {
+  const float d = a.m - m, f = __builtin_amdgcn_exp2f(d);
   a.t = f > 0.0f ? f * (a.t + a.s * d) : 0.0f;
   a.s *= f;
   a.m = m;
 }
-__device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
+__device__ __forceinline__ Sums join(Sums a, Sums b) {
   const float m = fmaxf(a.m, b.m);
-  move_to(a, m, c);
-  move_to(b, m, c);
+  move_to(a, m);
+  move_to(b, m);
   return {m, a.s + b.s, a.t + b.t};
 }
 
 // The sums of a wave, on every lane
-__device__ __forceinline__ Sums wave_sums(Sums a, float c) {
+__device__ __forceinline__ Sums wave_sums(Sums a) {
   float m = a.m;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-  move_to(a, m, c);
+  move_to(a, m);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     a.s += __shfl_xor(a.s, o);
@@ -62,51 +64,55 @@ __device__ __forceinline__ Sums wave_sums(Sums a, float c) {
 template <typename T> struct Vec;
 template <> struct Vec<float> {
   static constexpr int n = 4;
-  static __device__ __forceinline__ void load(const float *p, float *x) {
-    const f32x4 v = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p));
+  static __device__ __forceinline__ void widen(const u32x4 &v, float *x) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = v[e];
+    for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(v[e]);
   }
 };
 template <> struct Vec<bf16_t> {
   static constexpr int n = 8;
-  static __device__ __forceinline__ void load(const bf16_t *p, float *x) {
-    const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
+  static __device__ __forceinline__ void widen(const u32x4 &v, float *x) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16);
   }
 };
 
-// The n largest of a wave's cnt candidates (cnt <= kList), sorted to the front of its list.  Every candidate counts those above it.
-__device__ __forceinline__ void select(key_t64 *list, int cnt, int n, int lane) {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  key_t64 own[kList / 64];
-  int rank[kList / 64];
+// How many of n keys are above each of N, STEP at a time (the list is padded to eight with zeros)
+template <int STEP, int N>
+__device__ __forceinline__ void count_above(const key_t64 *list, int n, const key_t64 (&own)[N], int (&rank)[N]) {
+  for (int j = 0; j < n; j += STEP) {
+    key_t64 k[STEP];
 #pragma unroll
-  for (int i = 0; i < kList / 64; ++i) {
+    for (int u = 0; u < STEP; ++u) k[u] = list[j + u];
+#pragma unroll
+    for (int u = 0; u < STEP; ++u)
+#pragma unroll
+      for (int i = 0; i < N; ++i) rank[i] += k[u] > own[i];
+  }
+}
+// The n largest of a wave's cnt candidates (cnt <= 64 N), sorted to the front of its list: each counts those above it
+template <int N>
+__device__ __forceinline__ void select_of(key_t64 *list, int cnt, int n, int lane) {
+  key_t64 own[N];
+  int rank[N];
+  if (lane < 8) list[cnt + lane] = 0;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
     own[i] = lane + 64 * i < cnt ? list[lane + 64 * i] : 0;
     rank[i] = 0;
   }
-  if (cnt <= 64) {
-    for (int j = 0; j < cnt; ++j) rank[0] += list[j] > own[0];
-  } else if (cnt <= 128) {
-    for (int j = 0; j < cnt; ++j) {
-      const key_t64 k = list[j];
-      rank[0] += k > own[0];
-      rank[1] += k > own[1];
-    }
-  } else {
-    for (int j = 0; j < cnt; ++j) {
-      const key_t64 k = list[j];
-#pragma unroll
-      for (int i = 0; i < kList / 64; ++i) rank[i] += k > own[i];
-    }
-  }
+  count_above<(N > 2 ? 1 : 8)>(list, cnt, own, rank);
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-  for (int i = 0; i < kList / 64; ++i)
+  for (int i = 0; i < N; ++i)
     if (lane + 64 * i < cnt && rank[i] < n) list[rank[i]] = own[i];
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+__device__ __forceinline__ void select(key_t64 *list, int cnt, int n, int lane) {
+  if (cnt <= 64) select_of<1>(list, cnt, n, lane);
+  else if (cnt <= 128) select_of<2>(list, cnt, n, lane);
+  else select_of<kList / 64>(list, cnt, n, lane);
 }
 
 __device__ __forceinline__ key_t64 uniform(key_t64 k) {
@@ -134,16 +140,48 @@ __device__ __forceinline__ unsigned lane_bar(unsigned k, int n) {
   return t;
 }
 
-// Results of a row from its sums; a thread each for the targets.
+// A row whose sums the fast way cannot hold, by the definition: m = max x, then the sums against it.  256 threads.
+template <typename T>
+__device__ __forceinline__ Sums odd_row(const ScoreArgs &a, const T *x, Sums *part) {
+  const int tid = threadIdx.x;
+  float m = -__builtin_inff();
+  bool nan = false;
+  for (int v = tid; v < a.V; v += 256) {
+    const float y = to_f32(x[v]) * a.scale;
+    m = fmaxf(m, y);
+    nan |= y != y;
+  }
+  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+  __syncthreads();
+  if (tid % 64 == 0) part[tid / 64].m = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(part[0].m, part[1].m), fmaxf(part[2].m, part[3].m));
+  float s = nan ? __builtin_nanf("") : 0.0f, t = 0.0f;
+  if (m > -__builtin_inff())
+    for (int v = tid; v < a.V; v += 256) {
+      const float d = (to_f32(x[v]) * a.scale - m) * kLog2e, p = __builtin_amdgcn_exp2f(d);
+      s += p;                                              // NaN from plus infinity less itself
+      if (p > 0.0f) t += p * d;
+    }
+  for (int o = 1; o < 64; o <<= 1) { s += __shfl_xor(s, o); t += __shfl_xor(t, o); }
+  if (tid % 64 == 0) { part[tid / 64].s = s; part[tid / 64].t = t; }
+  __syncthreads();
+  return {m, part[0].s + part[1].s + part[2].s + part[3].s, part[0].t + part[1].t + part[2].t + part[3].t};
+}
+
+// Results of a row from its sums.  256 threads.
 struct RowResult { float lse; bool bad; };
-__device__ __forceinline__ RowResult finish_row(const ScoreArgs &a, int r, const Sums &q, int tid) {
+template <typename T>
+__device__ __forceinline__ RowResult finish_row(const ScoreArgs &a, int r, Sums q, const T *x, Sums *part) {
   RowResult o;
-  o.bad = q.s != q.s;                                      // NaN, or plus infinity less itself
-  const float ls = kLn2 * __builtin_log2f(q.s);
-  o.lse = o.bad ? __builtin_nanf("") : q.s > 0.0f ? q.m * a.scale + ls : -__builtin_inff();
-  if (tid == 0) {
+  const bool odd = !(q.s > 0.0f && q.m < kHuge);           // (the same for every thread)
+  if (odd) q = odd_row(a, x, part);
+  o.bad = q.s != q.s;
+  const float l2 = __builtin_log2f(q.s);
+  o.lse = o.bad ? __builtin_nanf("") : !(q.s > 0.0f) ? -__builtin_inff() : odd ? q.m + kLn2 * l2 : kLn2 * (q.m + l2);
+  if (threadIdx.x == 0) {
     if (a.lse) a.lse[r] = o.lse;
-    if (a.entropy) a.entropy[r] = o.bad ? o.lse : q.s > 0.0f ? ls - kLn2 * q.t / q.s : 0.0f;
+    if (a.entropy) a.entropy[r] = o.bad ? o.lse : q.s > 0.0f ? kLn2 * (l2 - q.t / q.s) : 0.0f;
   }
   return o;
 }
@@ -152,8 +190,8 @@ __device__ __forceinline__ float logp(const ScoreArgs &a, const RowResult &o, fl
   return y == -__builtin_inff() && !o.bad ? y : y - o.lse;
 }
 template <typename T>
-__device__ __forceinline__ void score_targets(const ScoreArgs &a, const RowResult &o, const T *x, int r, int tid, int threads) {
-  for (int i = tid; i < a.m; i += threads) {
+__device__ __forceinline__ void score_targets(const ScoreArgs &a, const RowResult &o, const T *x, int r) {
+  for (int i = threadIdx.x; i < a.m; i += 256) {
     const int v = a.targets[(int64_t)r * a.m + i];
     a.logprobs[(int64_t)r * a.m + i] = v < 0 ? 0.0f : v >= a.V ? __builtin_nanf("") : logp(a, o, to_f32(x[v]));
   }
@@ -180,9 +218,9 @@ __device__ void top_with_nan(const ScoreArgs &a, const RowResult &o, const T *x,
 
 // One workgroup per (row, slice).  TOP: with a list of the likeliest.
 template <typename T, bool TOP>
-__global__ __launch_bounds__(256) void logprobs_kernel(const ScoreArgs a, int slices) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 6 : 5) void logprobs_kernel(const ScoreArgs a, int slices) {
   constexpr int VE = Vec<T>::n, K = NV * VE;               // elements of a vector, of a lane's batch
-  __shared__ key_t64 lists[TOP ? 4 : 1][TOP ? kList : 1];
+  __shared__ __align__(16) key_t64 lists[TOP ? 4 : 1][TOP ? kList + 8 : 1];
   __shared__ Sums wsum[4];
   __shared__ int counts[4];
   __shared__ key_t64 shared_bar;                           // the best of the waves' bars: the top-th of a part is none of the row's best
@@ -205,31 +243,58 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const ScoreArgs a, int sl
     if (tid == 0) shared_bar = 0;
     __syncthreads();
   }
+  // the next batch is on its way while one is worked on; vectors that reach over the row's ends are read by element
+  u32x4 raw[NV];
+  auto fetch = [&](int b) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int at = ((b * NV + i) * 64 + lane) * VE - off;
+      if (at >= 0 && at + VE <= a.V) raw[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(x + at));
+    }
+  };
+  bool plain = true;                                       // (uniform) no minus infinity so far: its 0 times infinity needs a clamp
+  if (b0 + wave < b1) fetch(b0 + wave);
   for (int b = b0 + wave; b < b1; b += 4) {
     float y[K];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) Vec<T>::widen(raw[i], y + i * VE);
+    if (b == 0 || b == batches - 1)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int at = ((b * NV + i) * 64 + lane) * VE - off;
+        if (!(at >= 0 && at + VE <= a.V))
+#pragma unroll
+          for (int e = 0; e < VE; ++e) y[i * VE + e] = at + e >= 0 && at + e < a.V ? to_f32(x[at + e]) : -__builtin_inff();
+      }
+    if (b + 4 < b1) fetch(b + 4);
     if constexpr (TOP) {                                   // another wave may have raised the bar
       const key_t64 o = *(volatile key_t64 *)&shared_bar;
       if (o > bar) bar = o;
       bar = uniform(bar);
     }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int at = ((b * NV + i) * 64 + lane) * VE - off;
-      if (at >= 0 && at + VE <= a.V) Vec<T>::load(x + at, y + i * VE);
-      else
-#pragma unroll
-        for (int e = 0; e < VE; ++e) y[i * VE + e] = at + e >= 0 && at + e < a.V ? to_f32(x[at + e]) : -__builtin_inff();
-    }
     float top = y[0];
 #pragma unroll
     for (int e = 1; e < K; ++e) top = fmaxf(top, y[e]);
     // the reference follows the largest value so far at a distance: sums of up to 2^16 more lose nothing
-    if (__ballot((top - q.m) * c > 16.0f) != 0 && top > q.m) move_to(q, top, c);
+    if (__ballot(top * c - q.m > 16.0f) != 0 && top * c > q.m) move_to(q, ceilf(top * c));
+    const float s0 = q.s, t0 = q.t;
+    if (plain) {
 #pragma unroll
-    for (int e = 0; e < K; ++e) {
-      const float d = (y[e] - q.m) * c, p = __builtin_amdgcn_exp2f(d);
-      q.s += p;
-      q.t += p * fmaxf(d, -1000.0f);                       // 2^-1000 is 0: minus infinity adds nothing
+      for (int e = 0; e < K; ++e) {
+        const float d = __builtin_fmaf(y[e], c, -q.m), p = __builtin_amdgcn_exp2f(d);
+        q.s += p;
+        q.t = __builtin_fmaf(p, d, q.t);
+      }
+      plain = __ballot(q.t != q.t) == 0;
+    }
+    if (!plain) {
+      q.s = s0; q.t = t0;
+#pragma unroll
+      for (int e = 0; e < K; ++e) {
+        const float d = __builtin_fmaf(y[e], c, -q.m), p = __builtin_amdgcn_exp2f(d);
+        q.s += p;
+        q.t = __builtin_fmaf(p, fmaxf(d, -1000.0f), q.t);  // 2^-1000 is 0
+      }
     }
     if constexpr (TOP) {
       if (first) {
@@ -275,41 +340,42 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const ScoreArgs a, int sl
     }
   }
   // the lanes' sums, then the waves'
-  q = wave_sums(q, c);
+  q = wave_sums(q);
   if (lane == 0) wsum[wave] = q;
   if constexpr (TOP) {
-    select(list, cnt, a.top, lane);
-    if (lane == 0) counts[wave] = min(cnt, a.top);
+    if (cnt > 64) {
+      select(list, cnt, a.top, lane);
+      cnt = min(cnt, a.top);
+    }
+    if (lane < 8) list[cnt + lane] = 0;
+    if (lane == 0) counts[wave] = cnt;
   }
   __syncthreads();
-  q = join(join(wsum[0], wsum[1], c), join(wsum[2], wsum[3], c), c);
-  // the four lists' entries count those above them: 4 top <= 256
-  key_t64 mine = 0;
-  int rank = 0;
+  q = join(join(wsum[0], wsum[1]), join(wsum[2], wsum[3]));
+  // every entry of the four lists counts those above it
+  key_t64 mine[1] = {0};
+  int rank[1] = {0};
   if constexpr (TOP) {
-    const int w = tid / a.top, i = tid % a.top;
-    if (w < 4 && i < counts[w]) {
-      mine = lists[w][i];
-      for (int j = 0; j < 4; ++j)
-        for (int k = 0; k < counts[j]; ++k) rank += lists[j][k] > mine;
-    }
+    if (lane < counts[wave]) mine[0] = list[lane];
+    for (int j = 0; j < 4; ++j) count_above<8>(lists[j], counts[j], mine, rank);
   }
   if (slices > 1) {
     Sums *ws = (Sums *)a.ws;
     if (tid == 0) ws[(size_t)r * slices + slice] = q;
     if constexpr (TOP) {
       key_t64 *wl = (key_t64 *)((char *)a.ws + ((size_t)a.N * slices * sizeof(Sums) + 15) / 16 * 16) + ((size_t)r * slices + slice) * a.top;
-      if (mine && rank < a.top) wl[rank] = mine;
+      if (mine[0] && rank[0] < a.top) wl[rank[0]] = mine[0];
       const int have = counts[0] + counts[1] + counts[2] + counts[3];
       if (tid >= have && tid < a.top) wl[tid] = 0;
     }
     return;
   }
-  const RowResult o = finish_row(a, r, q, tid);
-  score_targets(a, o, x, r, tid, 256);
+  __syncthreads();
+  const RowResult o = finish_row(a, r, q, x, wsum);
+  score_targets(a, o, x, r);
   if constexpr (TOP) {
     if (!o.bad) {
-      if (mine && rank < a.top) put_top(a, o, r, rank, mine, to_f32(x[key_place(mine)]));
+      if (mine[0] && rank[0] < a.top) put_top(a, o, r, rank[0], mine[0], to_f32(x[key_place(mine[0])]));
     } else if (wave == 0) top_with_nan(a, o, x, r, lane);
   }
 }
@@ -317,8 +383,9 @@ __global__ __launch_bounds__(256) void logprobs_kernel(const ScoreArgs a, int sl
 // Joins the slices of a row.  One workgroup per row.
 template <typename T>
 __global__ __launch_bounds__(256) void logprobs_join_kernel(const ScoreArgs a, int slices) {
-  __shared__ key_t64 kept[kMaxSlices * 64];
+  __shared__ __align__(16) key_t64 kept[kMaxSlices * 64 + 8];
   __shared__ int n_kept;
+  __shared__ Sums part[4];
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const T *x = (const T *)a.x + (int64_t)r * a.row_stride;
   const float c = a.scale * kLog2e;
@@ -327,9 +394,9 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(const ScoreArgs a, i
   if (lane < slices) q = ((const Sums *)a.ws)[(size_t)r * slices + lane];
   key_t64 low = ~0ull;
   if (a.top && lane < slices) low = wl[(size_t)lane * a.top + (a.top + slices - 1) / slices - 1];
-  q = wave_sums(q, c);
-  const RowResult o = finish_row(a, r, q, tid);
-  score_targets(a, o, x, r, tid, 256);
+  q = wave_sums(q);
+  const RowResult o = finish_row(a, r, q, x, part);
+  score_targets(a, o, x, r);
   if (a.top == 0) return;
   if (o.bad) {
     if (tid < 64) top_with_nan(a, o, x, r, lane);
@@ -346,11 +413,13 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(const ScoreArgs a, i
   }
   __syncthreads();
   const int n = n_kept;
+  if (tid < 8) kept[n + tid] = 0;
+  __syncthreads();
   for (int i = tid; i < n; i += 256) {
-    const key_t64 mine = kept[i];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += kept[j] > mine;
-    if (rank < a.top) put_top(a, o, r, rank, mine, to_f32(x[key_place(mine)]));
+    const key_t64 mine[1] = {kept[i]};
+    int rank[1] = {0};
+    count_above<8>(kept, n, mine, rank);
+    if (rank[0] < a.top) put_top(a, o, r, rank[0], mine[0], to_f32(x[key_place(mine[0])]));
   }
 }
 
