@@ -12,7 +12,7 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.6931471805599453f;
 constexpr int NV = 4;            // vectors of 16 bytes that a lane takes at a time: a batch of a wave is 4 KB
-constexpr int kList = 512;       // places in a wave's list of candidates
+constexpr int kList = 192;       // places in a wave's list of candidates
 constexpr int kMaxSlices = 64;   // of a row: a joining wave has a lane for each
 
 typedef unsigned long long key_t64;
@@ -102,7 +102,7 @@ __device__ __forceinline__ void select_of(key_t64 *list, int cnt, int n, int lan
     own[i] = lane + 64 * i < cnt ? list[lane + 64 * i] : 0;
     rank[i] = 0;
   }
-  count_above<(N > 2 ? 1 : 8)>(list, cnt, own, rank);
+  count_above<(N > 1 ? 2 : 8)>(list, cnt, own, rank);
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
   for (int i = 0; i < N; ++i)
@@ -111,7 +111,6 @@ __device__ __forceinline__ void select_of(key_t64 *list, int cnt, int n, int lan
 }
 __device__ __forceinline__ void select(key_t64 *list, int cnt, int n, int lane) {
   if (cnt <= 64) select_of<1>(list, cnt, n, lane);
-  else if (cnt <= 128) select_of<2>(list, cnt, n, lane);
   else select_of<kList / 64>(list, cnt, n, lane);
 }
 
@@ -119,22 +118,18 @@ __device__ __forceinline__ key_t64 uniform(key_t64 k) {
   const unsigned hi = __builtin_amdgcn_readfirstlane((unsigned)(k >> 32)), lo = __builtin_amdgcn_readfirstlane((unsigned)k);   // (returned as int)
   return (key_t64)hi << 32 | lo;
 }
-// Keeps the n best of the list and makes the n-th of them the bar; how many are left
-__device__ __forceinline__ int raise_bar(key_t64 *list, int cnt, int n, int lane, key_t64 &bar) {
-  select(list, cnt, n, lane);
-  if (cnt < n) return cnt;
-  bar = uniform(list[n - 1]);
-  return n;
-}
-// A value that n lanes at least, and mostly not many more, are no smaller than: bit by bit from the highest
-__device__ __forceinline__ unsigned lane_bar(unsigned k, int n) {
+// A value that n of the 256 keys of the four waves (four on every lane) at least, and mostly not many more, are no smaller than: bit
+// by bit from the highest
+__device__ __forceinline__ unsigned first_bar(const unsigned (&k)[4], int n) {
   unsigned t = 0;
   for (int bit = 31; bit >= 0; --bit) {
     const unsigned u = t | 1u << bit;
-    const int have = __builtin_popcountll(__ballot(k >= u));
+    int have = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) have += __builtin_popcountll(__ballot(k[i] >= u));
     if (have >= n) {
       t = u;
-      if (have <= n + 2) break;
+      if (have <= n + n / 8) break;
     }
   }
   return t;
@@ -218,12 +213,13 @@ __device__ void top_with_nan(const ScoreArgs &a, const RowResult &o, const T *x,
 
 // One workgroup per (row, slice).  TOP: with a list of the likeliest.
 template <typename T, bool TOP>
-__global__ __launch_bounds__(256, sizeof(T) == 4 ? 6 : 5) void logprobs_kernel(const ScoreArgs a, int slices) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprobs_kernel(const ScoreArgs a, int slices) {
   constexpr int VE = Vec<T>::n, K = NV * VE;               // elements of a vector, of a lane's batch
   __shared__ __align__(16) key_t64 lists[TOP ? 4 : 1][TOP ? kList + 8 : 1];
   __shared__ Sums wsum[4];
   __shared__ int counts[4];
-  __shared__ key_t64 shared_bar;                           // the best of the waves' bars: the top-th of a part is none of the row's best
+  __shared__ key_t64 held[4];                              // (TOP) of every wave's candidates the (top / 4)-th best
+  __shared__ unsigned firsts[TOP ? 256 : 1];
   const int r = blockIdx.x / slices, slice = blockIdx.x % slices;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const T *x = (const T *)a.x + (int64_t)r * a.row_stride;
@@ -236,24 +232,50 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 6 : 5) void logprobs_kernel(c
   key_t64 *list = lists[TOP ? wave : 0];
   int cnt = 0;
   key_t64 bar = 0;                                         // candidates have a key above this (0: as a value, NaN)
-  bool first = true;
-  // a wave sorts its list and raises the bar when that many are in it
-  const int raise_at = a.top + 16 > 2 * a.top ? a.top + 16 : 2 * a.top;
-  if constexpr (TOP) {
-    if (tid == 0) shared_bar = 0;
-    __syncthreads();
-  }
+  const int share = (a.top + 3) / 4;
+  int raise_at = share + 16;
+  // Sorts the list, keeps the best and raises the bar: the waves' own share-th best are `top` entries together that are no smaller
+  // than the last of them
+  auto raise = [&]() {
+    select(list, cnt, a.top, lane);
+    if (cnt >= a.top) { const key_t64 k = uniform(list[a.top - 1]); bar = k > bar ? k : bar; }
+    if (cnt >= share && lane == 0) *(volatile key_t64 *)&held[wave] = list[share - 1];
+    cnt = min(cnt, a.top);
+    cnt = __builtin_popcountll(__ballot(lane < cnt && list[lane] >= bar));
+    raise_at = cnt + share + 8;
+  };
   // the next batch is on its way while one is worked on; vectors that reach over the row's ends are read by element
   u32x4 raw[NV];
+  constexpr unsigned kNone = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;   // minus infinity
   auto fetch = [&](int b) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int at = ((b * NV + i) * 64 + lane) * VE - off;
       if (at >= 0 && at + VE <= a.V) raw[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(x + at));
+      else raw[i] = u32x4{kNone, kNone, kNone, kNone};
     }
   };
   bool plain = true;                                       // (uniform) no minus infinity so far: its 0 times infinity needs a clamp
   if (b0 + wave < b1) fetch(b0 + wave);
+  if constexpr (TOP) {
+    // the first bar: from the largest elements of the lanes' first batches
+    unsigned k[4] = {0, 0, 0, 0};
+    if (b0 + wave < b1) {
+      float y[K];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) Vec<T>::widen(raw[i], y + i * VE);
+      float m = y[0];
+#pragma unroll
+      for (int e = 1; e < K; ++e) m = fmaxf(m, y[e]);
+      k[0] = order_key(m);
+    }
+    if (tid < 4) held[tid] = 0;
+    firsts[tid] = k[0];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) k[i] = firsts[i * 64 + lane];
+    bar = (key_t64)first_bar(k, a.top) << 32;
+  }
   for (int b = b0 + wave; b < b1; b += 4) {
     float y[K];
 #pragma unroll
@@ -268,13 +290,21 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 6 : 5) void logprobs_kernel(c
       }
     if (b + 4 < b1) fetch(b + 4);
     if constexpr (TOP) {                                   // another wave may have raised the bar
-      const key_t64 o = *(volatile key_t64 *)&shared_bar;
-      if (o > bar) bar = o;
-      bar = uniform(bar);
-    }
-    float top = y[0];
+      const key_t64 h = *(volatile key_t64 *)&held[lane & 3];
+      key_t64 o = h;
 #pragma unroll
-    for (int e = 1; e < K; ++e) top = fmaxf(top, y[e]);
+      for (int i = 1; i < 4; i <<= 1) { const key_t64 k = __shfl_xor(o, i); o = k < o ? k : o; }
+      o = uniform(o);
+      bar = o > bar ? o : bar;
+    }
+    float most[NV], top;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      most[i] = y[i * VE];
+#pragma unroll
+      for (int e = 1; e < VE; ++e) most[i] = fmaxf(most[i], y[i * VE + e]);
+      top = i ? fmaxf(top, most[i]) : most[0];
+    }
     // the reference follows the largest value so far at a distance: sums of up to 2^16 more lose nothing
     if (__ballot(top * c - q.m > 16.0f) != 0 && top * c > q.m) move_to(q, ceilf(top * c));
     const float s0 = q.s, t0 = q.t;
@@ -297,24 +327,26 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 6 : 5) void logprobs_kernel(c
       }
     }
     if constexpr (TOP) {
-      if (first) {
-        first = false;
-        const key_t64 k = (key_t64)lane_bar(order_key(top), a.top) << 32;   // the bar of what this batch brings
-        if (k > bar) bar = k;
-      }
-      const float tau = key_value((unsigned)(bar >> 32));  // (a bar of 0 is NaN: nothing is below it)
-      const uint64_t who = __ballot(!(top < tau));
-      if (who != 0) {
-        if (cnt + K * __builtin_popcountll(who) <= kList) {
-          // few lanes hold candidates: they fit whatever there are
+      const float tau = key_value((unsigned)(bar >> 32));
+      if (__ballot(!(top < tau)) != 0) {
+        int room = cnt;
 #pragma unroll
-          for (int e = 0; e < K; ++e) {
-            if (__ballot(!(y[e] < tau)) == 0) continue;
-            const int v = ((b * NV + e / VE) * 64 + lane) * VE - off + e % VE;
-            const key_t64 k = place_key(y[e], v);
-            const uint64_t m = __ballot(k > bar && v >= 0 && v < a.V);
-            if (m >> lane & 1) list[cnt + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = k;
-            cnt += __builtin_popcountll(m);
+        for (int i = 0; i < NV; ++i) room += VE * __builtin_popcountll(__ballot(!(most[i] < tau)));
+        if (room <= kList) {
+          // few vectors hold candidates: they fit whatever there are
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            if (__ballot(!(most[i] < tau)) == 0) continue;
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+              const float z = y[i * VE + e];
+              if (__ballot(!(z < tau)) == 0) continue;
+              const int v = ((b * NV + i) * 64 + lane) * VE - off + e;
+              const key_t64 k = place_key(z, v);
+              const uint64_t m = __ballot(k > bar && v >= 0 && v < a.V);
+              if (m >> lane & 1) list[cnt + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = k;
+              cnt += __builtin_popcountll(m);
+            }
           }
         } else {
           for (int i = 0; i < NV; ++i)
@@ -329,13 +361,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 6 : 5) void logprobs_kernel(c
               if (m == 0) continue;
               if (m >> lane & 1) list[cnt + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = k;
               cnt += __builtin_popcountll(m);
-              if (cnt + 64 > kList) cnt = raise_bar(list, cnt, a.top, lane, bar);
+              if (cnt + 64 > kList) raise();
             }
         }
-        if (cnt >= raise_at) {
-          cnt = raise_bar(list, cnt, a.top, lane, bar);
-          if (lane == 0) atomicMax(&shared_bar, bar);
-        }
+        if (cnt >= raise_at) raise();
       }
     }
   }
