@@ -213,7 +213,7 @@ __device__ void top_with_nan(const ScoreArgs &a, const RowResult &o, const T *x,
 
 // One workgroup per (row, slice).  TOP: with a list of the likeliest.
 template <typename T, bool TOP>
-__global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprobs_kernel(const ScoreArgs a, int slices) {
+__global__ __launch_bounds__(256, 5) void logprobs_kernel(const ScoreArgs a, int slices) {
   constexpr int VE = Vec<T>::n, K = NV * VE;               // elements of a vector, of a lane's batch
   __shared__ __align__(16) key_t64 lists[TOP ? 4 : 1][TOP ? kList + 8 : 1];
   __shared__ Sums wsum[4];
@@ -452,10 +452,10 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(const ScoreArgs a, i
   }
 }
 
-// Slices of a row: as many as bring the rows to four workgroups for each of the 256 CUs, of a batch for every wave at least.
+// Slices of a row: as many as the 1280 workgroups that the chip holds at a time allow for, of a batch for every wave at least.
 int row_slices(int dtype, int N, int V) {
   const int per = (dtype == NGG_F32 ? 4 : 8) * 64 * NV * 4;
-  return std::max(1, std::min({kMaxSlices, (1024 + N - 1) / N, V / per}));
+  return std::max(1, std::min({kMaxSlices, 1280 / N, V / per}));
 }
 
 }  // namespace
