@@ -31,19 +31,19 @@ __device__ __forceinline__ void pack_frag(Frag<bf16_t> &f, const float *p) {
   for (int e = 0; e < 8; ++e) f.v[e] = (bf16_t)p[e];
 }
 
-// Eight 8-bit elements as a fragment of either type; exact in both.
-__device__ __forceinline__ void widen(Frag<bf16_t> &f, unsigned lo, unsigned hi) {
+// Eight 8-bit elements times a power of two as a fragment of either type; exact in both.
+__device__ __forceinline__ void widen(Frag<bf16_t> &f, unsigned lo, unsigned hi, float scale) {
   bf16x2 *d = reinterpret_cast<bf16x2 *>(&f.v);
-  d[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
-  d[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-  d[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
-  d[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+  d[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+  d[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  d[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+  d[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
 }
-__device__ __forceinline__ void widen(Frag<float> &f, unsigned lo, unsigned hi) {
-  f.v[0] = __builtin_amdgcn_cvt_f32_fp8(lo, 0); f.v[1] = __builtin_amdgcn_cvt_f32_fp8(lo, 1);
-  f.v[2] = __builtin_amdgcn_cvt_f32_fp8(lo, 2); f.v[3] = __builtin_amdgcn_cvt_f32_fp8(lo, 3);
-  f.v[4] = __builtin_amdgcn_cvt_f32_fp8(hi, 0); f.v[5] = __builtin_amdgcn_cvt_f32_fp8(hi, 1);
-  f.v[6] = __builtin_amdgcn_cvt_f32_fp8(hi, 2); f.v[7] = __builtin_amdgcn_cvt_f32_fp8(hi, 3);
+__device__ __forceinline__ void widen(Frag<float> &f, unsigned lo, unsigned hi, float scale) {
+  f.v[0] = __builtin_amdgcn_cvt_f32_fp8(lo, 0) * scale; f.v[1] = __builtin_amdgcn_cvt_f32_fp8(lo, 1) * scale;
+  f.v[2] = __builtin_amdgcn_cvt_f32_fp8(lo, 2) * scale; f.v[3] = __builtin_amdgcn_cvt_f32_fp8(lo, 3) * scale;
+  f.v[4] = __builtin_amdgcn_cvt_f32_fp8(hi, 0) * scale; f.v[5] = __builtin_amdgcn_cvt_f32_fp8(hi, 1) * scale;
+  f.v[6] = __builtin_amdgcn_cvt_f32_fp8(hi, 2) * scale; f.v[7] = __builtin_amdgcn_cvt_f32_fp8(hi, 3) * scale;
 }
 
 // The sequence's cached and tree tokens, cut to what the page list can hold.
@@ -59,19 +59,21 @@ __device__ __forceinline__ int seq_keys(const TreeArgs &a, const SeqLens &s) {
   return s.tree ? min(s.ctx + s.tree, a.max_pages * a.p.page_size) : 0;
 }
 
-// Running totals of the sequences' steps (of one head): pre[b] steps lie before sequence b, pre[B] in all.  A sequence has one step at
-// least, so that someone writes its rows.  256 threads, four sequences each.
-static_assert(NGG_TREE_MAX == 1024, "step_totals takes four sequences per thread");
+// Steps of KS keys of a sequence (of one head): one at least, so that someone writes its rows
 template <int KS>
+__device__ __forceinline__ int seq_steps(const TreeArgs &a, int b) { return max(1, (seq_keys(a, seq_lens(a, b)) + KS - 1) / KS); }
+
+// Running totals of those: pre[b] steps lie before sequence b, pre[B] in all.  NT threads.
+template <int KS, int NT>
 __device__ __forceinline__ void step_totals(const TreeArgs &a, int *pre) {
-  __shared__ int wsum[4];
+  constexpr int PER = NGG_TREE_MAX / NT;
+  __shared__ int wsum[NT / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int n[4], sum = 0;
+  int n[PER], sum = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int b = tid * 4 + i;
-    n[i] = 0;
-    if (b < a.B) n[i] = max(1, (seq_keys(a, seq_lens(a, b)) + KS - 1) / KS);
+  for (int i = 0; i < PER; ++i) {
+    const int b = tid * PER + i;
+    n[i] = b < a.B ? seq_steps<KS>(a, b) : 0;
     sum += n[i];
   }
   int inc = sum;
@@ -85,8 +87,8 @@ __device__ __forceinline__ void step_totals(const TreeArgs &a, int *pre) {
   int at = inc - sum;
   for (int w = 0; w < wave; ++w) at += wsum[w];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int b = tid * 4 + i;
+  for (int i = 0; i < PER; ++i) {
+    const int b = tid * PER + i;
     if (b < a.B) pre[b] = at;
     at += n[i];
     if (b == a.B - 1) pre[a.B] = at;
@@ -96,6 +98,55 @@ __device__ __forceinline__ void step_totals(const TreeArgs &a, int *pre) {
 
 // The number of workgroups that share the list: as many as were launched, but no fewer than two steps each.
 __device__ __forceinline__ int64_t shares(const TreeArgs &a, int64_t total) { return min((int64_t)a.ranges, max((int64_t)1, total / 2)); }
+
+// A workgroup's place and share of the list, one (sequence, head) after the other.
+template <int KS, int NT>
+struct Work {
+  const TreeArgs &a;
+  int *pre;
+  int z;
+  int64_t range, u, u_end;
+  // of the part at hand: steps s_begin .. s_end - 1 of `steps`
+  int b, hk, s_begin, s_end, steps;
+
+  __device__ __forceinline__ Work(const TreeArgs &args, int *totals) : a(args), pre(totals), b(0) {
+    // the row tiles of a share run next to each other on one die: its keys come from memory once
+    const bool dealt = a.ranges % 8 == 0;
+    z = (int)(dealt ? blockIdx.x / 8 : blockIdx.x) % a.Z;
+    range = dealt ? (int64_t)(blockIdx.x / 8) / a.Z * 8 + blockIdx.x % 8 : blockIdx.x / a.Z;
+    if (a.whole) {                                         // a (sequence, head) for each
+      u = range;
+      u_end = min(range + 1, (int64_t)a.B * a.p.Hkv);
+      return;
+    }
+    step_totals<KS, NT>(a, pre);
+    const int64_t total = (int64_t)pre[a.B] * a.p.Hkv, R = shares(a, total);
+    u = range < R ? total * range / R : 0;
+    u_end = range < R ? total * (range + 1) / R : 0;
+  }
+  __device__ __forceinline__ bool next() {
+    if (u >= u_end) return false;
+    if (a.whole) {
+      b = (int)(u / a.p.Hkv);
+      hk = (int)(u % a.p.Hkv);
+      s_begin = 0;
+      steps = s_end = seq_steps<KS>(a, b);
+      ++u;
+      return true;
+    }
+    while ((int64_t)pre[b + 1] * a.p.Hkv <= u) ++b;
+    steps = pre[b + 1] - pre[b];
+    const int64_t in_b = u - (int64_t)pre[b] * a.p.Hkv;
+    hk = (int)(in_b / steps);
+    s_begin = (int)(in_b % steps);
+    s_end = (int)min((int64_t)steps, s_begin + (u_end - u));
+    u += s_end - s_begin;
+    return true;
+  }
+  __device__ __forceinline__ bool is_whole() const { return s_begin == 0 && s_end == steps; }
+  // where a part goes: one that begins inside a (sequence, head) is the first of its share, one that ends inside it the last
+  __device__ __forceinline__ size_t part() const { return ((size_t)range * a.Z + z) * 2 + (s_begin == 0 ? 1 : 0); }
+};
 
 // Eight bits, bit e set if token t of the tree sees position ctx + at + e (at may be negative: the context); keys: positions there are
 __device__ __forceinline__ unsigned visible8(const uint64_t *row, int words, int t, int at, int tree_keys) {
@@ -114,12 +165,14 @@ __device__ __forceinline__ unsigned visible8(const uint64_t *row, int words, int
   return n >= 8 ? v : n <= 0 ? 0u : v & ((1u << n) - 1);
 }
 
-// Takes zeros in the place of a fragment's elements that are not finite; true if there were any.
+// Takes zeros in the place of values of positions that are not there (pos + e >= n) and of those that are not finite; true if there
+// were any of the latter.
 template <typename T>
-__device__ __forceinline__ bool drop_not_finite(Frag<T> &f) {
+__device__ __forceinline__ bool only_there(Frag<T> &f, int pos, int n) {
   bool bad = false;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
+    if (pos + e >= n) f.v[e] = (T)0.0f;
     const bool b = !(fabsf((float)f.v[e]) < __builtin_inff());
     f.v[e] = b ? (T)0.0f : f.v[e];
     bad |= b;
@@ -154,22 +207,10 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
   int *pre = reinterpret_cast<int *>(lml + NW * QF * 32);  // [B + 1]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, g4 = lane >> 4;
-  // the row tiles of a share run next to each other on one die: its keys come from memory once
-  const bool dealt = a.ranges % 8 == 0;
-  const int z = (int)(dealt ? blockIdx.x / 8 : blockIdx.x) % a.Z;
-  const int64_t range = dealt ? (int64_t)(blockIdx.x / 8) / a.Z * 8 + blockIdx.x % 8 : blockIdx.x / a.Z;
-  step_totals<KS>(a, pre);
   const int Hkv = a.p.Hkv, words = (a.T + 63) / 64;
-  const int64_t total = (int64_t)pre[a.B] * Hkv, R = shares(a, total);
-  if (range >= R) return;
-  const int64_t u_begin = total * range / R, u_end = total * (range + 1) / R;
-  int b = 0;
-  for (int64_t u = u_begin; u < u_end;) {
-    while ((int64_t)pre[b + 1] * Hkv <= u) ++b;
-    const int steps = pre[b + 1] - pre[b];
-    const int64_t in_b = u - (int64_t)pre[b] * Hkv;
-    const int hk = (int)(in_b / steps), s_begin = (int)(in_b % steps);
-    const int s_end = (int)min((int64_t)steps, s_begin + (u_end - u));
+  Work<KS, 256> w(a, pre);
+  while (w.next()) {
+    const int b = w.b, hk = w.hk, z = w.z;
     const SeqLens len = seq_lens(a, b);
     const int n_keys = seq_keys(a, len);
 
@@ -202,7 +243,7 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
       for (int d = 0; d < DF; ++d) O[f][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    for (int tile = s_begin * NW + wave; tile < s_end * NW && tile * 32 < keys_seen; tile += NW) {
+    for (int tile = w.s_begin * NW + wave; tile < w.s_end * NW && tile * 32 < keys_seen; tile += NW) {
       const int pos0 = tile * 32;
       const int page = a.pages[b * a.pages_batch + pos0 / a.p.page_size];
       if (page < 0 || page >= a.p.n_pages) continue;
@@ -210,25 +251,23 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
       const int off = pos0 % a.p.page_size;
       const CT *kt = (const CT *)a.p.k + (head * a.p.page_size + off) * HD, *vt = (const CT *)a.p.v + (head * a.p.page_size + off) * HD;
       Frag<T> K[2][DS], V[DF];
-      float ks[8], vs[8];
+      float vs[8];
       if constexpr (sizeof(CT) == 1) {
+        const u32x2 ke = *reinterpret_cast<const u32x2 *>(a.p.k_exp + head * a.p.page_size + off + (c >> 2) * 8);
+        const float k0 = exp_scale(ke[0] >> (c & 3) * 8 & 0xff), k1 = exp_scale(ke[1] >> (c & 3) * 8 & 0xff);
 #pragma unroll
         for (int d = 0; d < DS; ++d) {
-          const u32x4 w = *reinterpret_cast<const u32x4 *>((const uint8_t *)kt + d * 1024 + lane * 16);
-          widen(K[0][d], w[0], w[1]); widen(K[1][d], w[2], w[3]);
+          const u32x4 x = *reinterpret_cast<const u32x4 *>((const uint8_t *)kt + d * 1024 + lane * 16);
+          widen(K[0][d], x[0], x[1], k0); widen(K[1][d], x[2], x[3], k1);
         }
 #pragma unroll
         for (int d = 0; d < DF; d += 2) {
-          const u32x4 w = *reinterpret_cast<const u32x4 *>((const uint8_t *)vt + d * 512 + lane * 16);
-          widen(V[d], w[0], w[1]); widen(V[d + 1], w[2], w[3]);
+          const u32x4 x = *reinterpret_cast<const u32x4 *>((const uint8_t *)vt + d * 512 + lane * 16);
+          widen(V[d], x[0], x[1], 1.0f); widen(V[d + 1], x[2], x[3], 1.0f);
         }
-        const u32x2 ke = *reinterpret_cast<const u32x2 *>(a.p.k_exp + head * a.p.page_size + off + g4 * 8);
         const u32x2 ve = *reinterpret_cast<const u32x2 *>(a.p.v_exp + head * a.p.page_size + off + g4 * 8);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          ks[e] = exp_scale(ke[e >> 2] >> (e & 3) * 8 & 0xff);
-          vs[e] = exp_scale(ve[e >> 2] >> (e & 3) * 8 & 0xff);
-        }
+        for (int e = 0; e < 8; ++e) vs[e] = exp_scale(ve[e >> 2] >> (e & 3) * 8 & 0xff);
       } else {
 #pragma unroll
         for (int f = 0; f < 2; ++f)
@@ -242,12 +281,7 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
       if (!full) {
         // what lies behind the last position is anything: values there are taken as zeros
 #pragma unroll
-        for (int d = 0; d < DF; ++d) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (pos0 + g4 * 8 + e >= n_keys) V[d].v[e] = (T)0.0f;
-          poison |= drop_not_finite(V[d]);
-        }
+        for (int d = 0; d < DF; ++d) poison |= only_there(V[d], pos0 + g4 * 8, n_keys);
         if constexpr (sizeof(CT) == 1)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -266,7 +300,6 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           s[e] = S[e >> 2][e & 3] * a.sfac;
-          if constexpr (sizeof(CT) == 1) s[e] *= ks[e];
           if (!(vis >> e & 1)) s[e] = -__builtin_inff();
           mx = fmaxf(mx, s[e]);
         }
@@ -324,22 +357,22 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
       if (g4 == 0) { lml[((wave * QF + f) * 16 + c) * 2] = m[f]; lml[((wave * QF + f) * 16 + c) * 2 + 1] = lsum; }
     }
     __syncthreads();
-    const bool whole = s_begin == 0 && s_end == steps;
-    const size_t part = ((size_t)range * a.Z + z) * 2 + (s_begin == 0 ? 1 : 0);
+    const bool whole = w.is_whole();
+    const size_t part = w.part();
     for (int i = tid; i < QF * DF * 64; i += 256) {
       const int f = i / (DF * 64), d = i / 64 % DF, ln = i & 63, cc = ln & 15;
       float mm = -__builtin_inff(), ll = 0.0f;
       f32x4 o{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < NW; ++w) mm = fmaxf(mm, lml[((w * QF + f) * 16 + cc) * 2]);
+      for (int v = 0; v < NW; ++v) mm = fmaxf(mm, lml[((v * QF + f) * 16 + cc) * 2]);
       const float ref = mm == -__builtin_inff() ? 0.0f : mm;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const float x = __builtin_amdgcn_exp2f(lml[((w * QF + f) * 16 + cc) * 2] - ref);
-        ll += x * lml[((w * QF + f) * 16 + cc) * 2 + 1];
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(lo + (((w * QF + f) * DF + d) * 64 + ln) * 4);
+      for (int v = 0; v < NW; ++v) {
+        const float x = __builtin_amdgcn_exp2f(lml[((v * QF + f) * 16 + cc) * 2] - ref);
+        ll += x * lml[((v * QF + f) * 16 + cc) * 2 + 1];
+        const f32x4 y = *reinterpret_cast<const f32x4 *>(lo + (((v * QF + f) * DF + d) * 64 + ln) * 4);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] += x * v[k];
+        for (int k = 0; k < 4; ++k) o[k] += x * y[k];
       }
       const int r = f * 16 + cc, rr = z * ROWS + r, t = rr / a.G, dim = d * 16 + (ln >> 4) * 4;
       if (t >= a.T) continue;
@@ -352,75 +385,380 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
       write_row4<T>(a, b, t, hk * a.G + rr % a.G, dim, o, mm, ll);
     }
     __syncthreads();
-    u += s_end - s_begin;
   }
 }
 
-// Joins the parts of every (sequence, head) that more than one workgroup worked on, in their order.
+// Row tiles of more than 32 rows on 16-bit operands: the waves of a workgroup own 32 rows each and share the keys, two tiles (64 keys)
+// per step, through LDS, where 8-bit tiles arrive widened (keys with their powers of two; those of the values go to the probabilities).
+// 32x32x16 products: row 8 j + 4 h + i of a key tile is key 16 (j % 2) + 8 h + 4 (j / 2) + i, so lane (row, h) ends up with keys
+// 16 u + 8 h .. + 7 of every 16, its operand of the second product.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <typename CT, int HD, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a) {
+  typedef bf16_t T;
+  constexpr int DS = HD / 32, KQ = HD / 16, DB = HD / 32, TILE = 32 * HD, KT = 2, KS = 32 * KT, ROWS = 32 * NW, NT = 64 * NW;
+  constexpr bool C8 = sizeof(CT) == 1;
+  constexpr int PIECES = TILE * (int)sizeof(CT) / 16, PPT = (PIECES + NT - 1) / NT;   // 16-byte pieces of a tile, of a thread
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  T *kl = reinterpret_cast<T *>(smem);                     // [2][KT][TILE]
+  T *vl = kl + 2 * KT * TILE;                              // [2][KT][TILE]
+  float *vsl = reinterpret_cast<float *>(vl + 2 * KT * TILE);   // [2][KS] powers of two of the values
+  int *odd = reinterpret_cast<int *>(vsl + 2 * KS);        // [3][KT] a tile holds values that are not finite
+  int *pre = odd + 3 * KT;                                 // [B + 1]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r32 = lane & 31, h = lane >> 5;
+  const int Hkv = a.p.Hkv, words = (a.T + 63) / 64;
+  const int loff = (h * 16 + (r32 & 15)) * 8, koff = (r32 >> 4) * DS * 512 + loff, voff = (r32 >> 4) * 512 + loff;
+  Work<KS, NT> w(a, pre);
+  while (w.next()) {
+    const int b = w.b, hk = w.hk, z = w.z;
+    const SeqLens len = seq_lens(a, b);
+    const int n_keys = seq_keys(a, len);
+    auto seen = [&](int r0, int rows) {                    // positions that rows r0 .. r0 + rows - 1 can see some of
+      const int t_last = min(len.tree, (r0 + rows - 1) / a.G + 1) - 1;
+      return (t_last + 1) * a.G > r0 ? min(n_keys, len.ctx + t_last + 1) : 0;
+    };
+    const int group_keys = seen(z * ROWS, ROWS), wave_keys = seen(z * ROWS + wave * 32, 32);
+    const int t_begin = w.s_begin * KT, t_end = min(w.s_end * KT, (group_keys + 31) / 32);
+
+    u32x4 kst[KT][PPT], vst[KT][PPT];                      // the next step's tiles, on their way
+    u32x2 kex[KT][C8 ? PPT : 1];
+    unsigned vex = 0;
+    bool there[KT];                                        // (uniform) the tile's page is one of the pool's
+    auto stage_load = [&](int t) {
+#pragma unroll
+      for (int k = 0; k < KT; ++k) {
+        const int pos0 = (t + k) * 32;
+        there[k] = t + k < t_end;
+        int page = there[k] ? a.pages[b * a.pages_batch + pos0 / a.p.page_size] : -1;
+        there[k] = page >= 0 && page < a.p.n_pages;
+        page = there[k] ? page : 0;
+        const int off = there[k] ? pos0 % a.p.page_size : 0;
+        const size_t head = ((size_t)page * Hkv + hk) * a.p.page_size + off;
+        const uint8_t *kp = (const uint8_t *)a.p.k + head * HD * sizeof(CT), *vp = (const uint8_t *)a.p.v + head * HD * sizeof(CT);
+#pragma unroll
+        for (int i = 0; i < PPT; ++i) {
+          const int pc = min(tid + NT * i, PIECES - 1);
+          kst[k][i] = reinterpret_cast<const u32x4 *>(kp)[pc];
+          vst[k][i] = reinterpret_cast<const u32x4 *>(vp)[pc];
+          if constexpr (C8) kex[k][i] = *reinterpret_cast<const u32x2 *>(a.p.k_exp + head + (pc % 16 / 4) * 8);
+        }
+        if constexpr (C8)
+          if (tid / 32 == k) vex = a.p.v_exp[head + tid % 32];
+      }
+    };
+    auto stage_store = [&](int t, int buf, int o3) {
+#pragma unroll
+      for (int k = 0; k < KT; ++k) {
+        T *kt = kl + (buf * KT + k) * TILE, *vt = vl + (buf * KT + k) * TILE;
+        const int pos0 = (t + k) * 32;
+        const bool full = there[k] && pos0 + 32 <= len.ctx;
+        const int limit = there[k] ? n_keys : 0;
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < PPT; ++i) {
+          const int pc = min(tid + NT * i, PIECES - 1), slot = pc % 64, blk = pc / 64;
+          if constexpr (C8) {
+            const int sh = slot % 4 * 8;
+            Frag<T> f0, f1;
+            widen(f0, kst[k][i][0], kst[k][i][1], exp_scale(kex[k][i][0] >> sh & 0xff));
+            widen(f1, kst[k][i][2], kst[k][i][3], exp_scale(kex[k][i][1] >> sh & 0xff));
+            *reinterpret_cast<bf16x8 *>(kt + blk * 512 + slot * 8) = f0.v;
+            *reinterpret_cast<bf16x8 *>(kt + (DS + blk) * 512 + slot * 8) = f1.v;
+            widen(f0, vst[k][i][0], vst[k][i][1], 1.0f);
+            widen(f1, vst[k][i][2], vst[k][i][3], 1.0f);
+            if (!full) {
+              bad |= only_there(f0, pos0 + slot / 16 * 8, limit);
+              bad |= only_there(f1, pos0 + slot / 16 * 8, limit);
+            }
+            *reinterpret_cast<bf16x8 *>(vt + 2 * blk * 512 + slot * 8) = f0.v;
+            *reinterpret_cast<bf16x8 *>(vt + (2 * blk + 1) * 512 + slot * 8) = f1.v;
+          } else {
+            Frag<T> f;
+            f.v = __builtin_bit_cast(bf16x8, vst[k][i]);
+            if (!full) bad |= only_there(f, pos0 + slot / 16 * 8, limit);
+            reinterpret_cast<u32x4 *>(kt)[pc] = kst[k][i];
+            reinterpret_cast<bf16x8 *>(vt)[pc] = f.v;
+          }
+        }
+        if (bad) odd[o3 * KT + k] = 1;
+        if constexpr (C8)
+          if (tid / 32 == k) vsl[buf * KS + tid] = pos0 + tid % 32 < limit ? exp_scale(vex) : 1.0f;
+      }
+    };
+    if (tid < 3 * KT) odd[tid] = 0;
+    stage_load(t_begin);
+
+    const int row = z * ROWS + wave * 32 + r32, tok = row / a.G;
+    const bool live = tok < len.tree;
+    bf16x8 Q[KQ];
+    {
+      const T *q = (const T *)a.q + b * a.q_batch + (live ? tok : 0) * a.q_token + (int64_t)(hk * a.G + row % a.G) * a.q_head;
+#pragma unroll
+      for (int d = 0; d < KQ; ++d) {
+        if (!live) Q[d] = zero_frag<T>().v;
+        else if (a.q_vec) Q[d] = *reinterpret_cast<const bf16x8 *>(q + d * 16 + h * 8);
+        else
+#pragma unroll
+          for (int e = 0; e < 8; ++e) Q[d][e] = q[d * 16 + h * 8 + e];
+      }
+    }
+    float m = -__builtin_inff(), l = 0.0f;
+    f32x16 O[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) O[d][r] = 0.0f;
+    __syncthreads();                                       // (odd is clear)
+
+    bool here[KT];
+    auto compute = [&](int t, int buf, int o3) {
+      if (t * 32 >= wave_keys) return;                     // (uniform per wave)
+      const T *kt = kl + buf * KT * TILE + koff, *vt = vl + buf * KT * TILE + voff;
+      f32x16 S[KT];
+#pragma unroll
+      for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[k][r] = 0.0f;
+#pragma unroll
+      for (int q = 0; q < KQ; ++q)
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+          const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(kt + k * TILE + (q >> 1) * 512 + (q & 1) * 256);
+          S[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, Q[q], S[k], 0, 0, 0);
+        }
+      unsigned vis[KT][2];
+      float mx = -__builtin_inff();
+#pragma unroll
+      for (int k = 0; k < KT; ++k) {
+        const int pos0 = (t + k) * 32;
+        vis[k][0] = vis[k][1] = 0xff;
+        if (pos0 + 32 > len.ctx || !here[k]) {             // (uniform)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            vis[k][u] = here[k] ? visible8(a.mask ? a.mask + b * a.mask_batch + min(tok, a.T - 1) * a.mask_token : nullptr, words, tok,
+                                           pos0 + 16 * u + 8 * h - len.ctx, n_keys - len.ctx) : 0u;
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (!(vis[k][r >> 2 & 1] >> ((r >> 3) * 4 + (r & 3)) & 1)) S[k][r] = -__builtin_inff();
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, S[k][r]);
+      }
+      mx *= a.sfac;                                        // sfac > 0: the maximum commutes with the scaling
+      // the reference is brought up to date only when a score is far above it: sums and outputs use the same one, whichever it is
+      if (__ballot(mx > m + 8.0f) != 0) {
+        const float mnew = fmaxf(m, fmaxf(mx, other_half(mx)));
+        const float alpha = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
+        l *= alpha;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) O[d][r] *= alpha;
+        m = mnew;
+      }
+      const float ref = m == -__builtin_inff() ? 0.0f : m;
+      bf16x8 P[KT][2];
+      float ps[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float vs[8];
+          if constexpr (C8)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) vs[e] = vsl[buf * KS + k * 32 + u * 16 + h * 8 + e];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int r = 4 * (u + 2 * (e >> 2)) + (e & 3);
+            float p = __builtin_amdgcn_exp2f(__builtin_fmaf(S[k][r], a.sfac, -ref));
+            ps[e & 3] += p;
+            if constexpr (C8) p *= vs[e];
+            P[k][u][e] = (T)p;
+          }
+        }
+      l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+#pragma unroll
+      for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int d = 0; d < DB; ++d) {
+            const bf16x8 vf = *reinterpret_cast<const bf16x8 *>(vt + k * TILE + d * 1024 + u * 256);
+            O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, P[k][u], O[d], 0, 0, 0);
+          }
+      // values that are not finite were left out, because 0 times them must stay 0 where their key is masked
+#pragma unroll
+      for (int k = 0; k < KT; ++k) {
+        if (!here[k] || !odd[o3 * KT + k]) continue;      // (uniform)
+        const int pos0 = (t + k) * 32;
+        const int page = a.pages[b * a.pages_batch + pos0 / a.p.page_size];
+        const CT *vg = (const CT *)a.p.v + (((size_t)page * Hkv + hk) * a.p.page_size + pos0 % a.p.page_size) * HD;
+        for (int j = 0; j < 32 && pos0 + j < n_keys; ++j) {
+          float pj = 0.0f;
+          unsigned vj = 0;
+#pragma unroll
+          for (int uu = 0; uu < 2; ++uu)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float x = __shfl((float)P[k][uu][e], (j >> 3 & 1) * 32 + r32);
+              const unsigned y = __shfl(vis[k][uu], (j >> 3 & 1) * 32 + r32);
+              if ((j & 7) == e && j >> 4 == uu) { pj = x; vj = y; }
+            }
+#pragma unroll
+          for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const CT x = vg[page_v_offset<CT>(j, d * 32 + 8 * (r >> 2) + 4 * h + (r & 3), HD)];
+              float v;
+              if constexpr (C8) v = fp8_to_f32(x.bits);
+              else v = to_f32(x);
+              if ((vj >> (j & 7) & 1) && !(fabsf(v) < __builtin_inff())) O[d][r] += pj * v;
+            }
+        }
+      }
+    };
+
+    int buf = 0, o3 = 0;
+    for (int t = t_begin; t < t_end; t += KT) {            // barriers are uniform
+      stage_store(t, buf, o3);
+#pragma unroll
+      for (int k = 0; k < KT; ++k) here[k] = there[k];
+      __syncthreads();
+      // the marks of the step before this one: every wave has left it, and none sets them again before the next barrier
+      const int last = o3 == 0 ? 2 : o3 - 1;
+      if (tid < KT) odd[last * KT + tid] = 0;
+      stage_load(t + KT);
+      compute(t, buf, o3);
+      buf ^= 1;
+      o3 = o3 == 2 ? 0 : o3 + 1;
+    }
+
+    const float lsum = l + other_half(l);
+    const bool whole = w.is_whole();
+    const size_t part = w.part();
+    if (tok < a.T) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          f32x4 o = {O[d][4 * j], O[d][4 * j + 1], O[d][4 * j + 2], O[d][4 * j + 3]};
+          float mm = m, ll = lsum;
+          if (!live) { o = f32x4{0.f, 0.f, 0.f, 0.f}; ll = 0.0f; mm = -__builtin_inff(); }   // not a token of this sequence
+          const int dim = d * 32 + 8 * j + 4 * h, r = wave * 32 + r32;
+          if (whole) write_row4<T>(a, b, tok, hk * a.G + row % a.G, dim, o, mm, ll);
+          else {
+            *reinterpret_cast<f32x4 *>(a.part_o + (part * ROWS + r) * HD + dim) = o;
+            if (dim == 0) { a.part_ml[(part * ROWS + r) * 2] = mm; a.part_ml[(part * ROWS + r) * 2 + 1] = ll; }
+          }
+        }
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the parts of every (sequence, head) that more than one workgroup worked on, in their order.  A thread takes four elements of a
+// row, a workgroup 256 of those.
 template <typename T, int HD, int ROWS, int KS>
 __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
   __shared__ int pre[NGG_TREE_MAX + 1];
-  step_totals<KS>(a, pre);
+  step_totals<KS, 256>(a, pre);
   const int z = blockIdx.y, b = blockIdx.x / a.p.Hkv, hk = blockIdx.x % a.p.Hkv;
   const int64_t total = (int64_t)pre[a.B] * a.p.Hkv, R = shares(a, total);
   const int64_t steps = pre[b + 1] - pre[b], u0 = (int64_t)pre[b] * a.p.Hkv + hk * steps, u1 = u0 + steps;
   const int64_t first = ((u0 + 1) * R + total - 1) / total - 1, last = (u1 * R + total - 1) / total - 1;   // the shares that hold u0 and u1 - 1
   if (first == last) return;
-  for (int i = threadIdx.x; i < ROWS * HD / 4; i += 256) {
-    const int r = i / (HD / 4), dim = i % (HD / 4) * 4, rr = z * ROWS + r, t = rr / a.G;
-    if (t >= a.T) break;
-    float mm = -__builtin_inff(), ll = 0.0f;
-    f32x4 o{0.f, 0.f, 0.f, 0.f};
-    for (int64_t w = first; w <= last; ++w) {
-      const size_t part = ((size_t)w * a.Z + z) * 2 + (total * w / R <= u0 ? 1 : 0);
-      const float m2 = a.part_ml[(part * ROWS + r) * 2], l2 = a.part_ml[(part * ROWS + r) * 2 + 1];
-      const f32x4 v = *reinterpret_cast<const f32x4 *>(a.part_o + (part * ROWS + r) * HD + dim);
-      const float mn = fmaxf(mm, m2), ref = mn == -__builtin_inff() ? 0.0f : mn;
-      const float x = __builtin_amdgcn_exp2f(mm - ref), y = __builtin_amdgcn_exp2f(m2 - ref);
-      mm = mn;
-      ll = ll * x + l2 * y;
+  const int i = blockIdx.z * 256 + threadIdx.x;
+  const int r = i / (HD / 4), dim = i % (HD / 4) * 4, rr = z * ROWS + r, t = rr / a.G;
+  if (r >= ROWS || t >= a.T) return;
+  const int slot0 = total * first / R <= u0 ? 1 : 0;       // the first share may have begun before
+  float mm = -__builtin_inff(), ll = 0.0f;
+  f32x4 o{0.f, 0.f, 0.f, 0.f};
+  for (int64_t w = first; w <= last; w += 8) {             // eight parts on their way at a time
+    f32x2 ml[8];
+    f32x4 v[8];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = o[k] * x + v[k] * y;
+    for (int j = 0; j < 8; ++j) {
+      const int64_t x = min(w + j, last);
+      const size_t part = (((size_t)x * a.Z + z) * 2 + (x == first ? slot0 : 0)) * ROWS + r;
+      ml[j] = *reinterpret_cast<const f32x2 *>(a.part_ml + part * 2);
+      v[j] = *reinterpret_cast<const f32x4 *>(a.part_o + part * HD + dim);
     }
-    write_row4<T>(a, b, t, hk * a.G + rr % a.G, dim, o, mm, ll);
+    float mn = mm;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mn = fmaxf(mn, ml[j][0]);
+    const float ref = mn == -__builtin_inff() ? 0.0f : mn, x = __builtin_amdgcn_exp2f(mm - ref);
+    mm = mn;
+    ll *= x;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] *= x;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float y = w + j <= last ? __builtin_amdgcn_exp2f(ml[j][0] - ref) : 0.0f;
+      if (w + j > last) continue;
+      ll += ml[j][1] * y;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] += v[j][k] * y;
+    }
   }
+  write_row4<T>(a, b, t, hk * a.G + rr % a.G, dim, o, mm, ll);
 }
 
-// Rows of a tile: the smallest of 16, 32 and 64 (fp32: 16 and 32, whose fragments are twice as large) that holds all of them, else the largest.
-static int row_frags(int dtype, int rows) { return rows <= 16 ? 1 : rows <= 32 || dtype == NGG_F32 ? 2 : 4; }
+// Which kernel and rows of a tile: up to 16 and 32 rows (fp32: any number) are tree_stream_kernel's, above that two waves of 32 rows or
+// four are tree_block_kernel's.
+static int tile_rows(int dtype, int rows) { return rows <= 16 ? 16 : rows <= 32 || dtype == NGG_F32 ? 32 : rows <= 64 ? 64 : 128; }
+static int step_keys(int rows) { return rows <= 32 ? 128 : 64; }
 
 TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, int64_t max_positions) {
   (void)cache;
   TreePlan p;
-  p.rows = 16 * row_frags(dtype, T * G);
+  p.rows = tile_rows(dtype, T * G);
   p.Z = (T * G + p.rows - 1) / p.rows;
-  const int64_t steps = (max_positions + 127) / 128 * B * Hkv;
-  const int64_t want = (512 + p.Z - 1) / p.Z, r = std::max<int64_t>(1, std::min(want, steps));
-  p.ranges = (int)(r >= 8 ? r / 8 * 8 : r);
-  const size_t rows = (size_t)p.ranges * p.Z * 2 * p.rows;
+  const int64_t steps = (max_positions + step_keys(p.rows) - 1) / step_keys(p.rows);
+  p.whole = steps <= 4;
+  const int64_t want = (512 + p.Z - 1) / p.Z, r = p.whole ? (int64_t)B * Hkv : std::max<int64_t>(1, std::min(want, steps * B * Hkv));
+  p.ranges = (int)(p.whole ? r : r >= 8 ? r / 8 * 8 : r);
+  const size_t rows = p.whole ? 0 : (size_t)p.ranges * p.Z * 2 * p.rows;
   p.o_bytes = rows * hd * 4;
   p.ml_bytes = rows * 8;
   return p;
 }
 
+template <typename K>
+static void allow_lds(K kernel, size_t bytes) {
+  if (bytes > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+template <typename T, int HD, int ROWS, int KS>
+static void merge(const TreeArgs &a, hipStream_t s) {
+  if (a.whole) return;
+  const int rows = std::min(ROWS, a.T * a.G);
+  hipLaunchKernelGGL((tree_merge_kernel<T, HD, ROWS, KS>), dim3(a.B * a.p.Hkv, a.Z, (rows * HD / 4 + 255) / 256), dim3(256), 0, s, a);
+}
 template <typename T, typename CT, int HD, int QF>
-static void launch(const TreeArgs &a, hipStream_t s) {
-  constexpr int NW = 4;
-  const size_t lds = (size_t)NW * QF * (HD / 16 * 256 + 32) * 4 + (a.B + 1) * 4;
-  constexpr size_t most = (size_t)NW * QF * (HD / 16 * 256 + 32) * 4 + (NGG_TREE_MAX + 1) * 4;
-  if (most > 64 * 1024) {
-    static const hipError_t opted = hipFuncSetAttribute(reinterpret_cast<const void *>(&tree_stream_kernel<T, CT, HD, QF>),
-                                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)most);
-    (void)opted;
-  }
-  hipLaunchKernelGGL((tree_stream_kernel<T, CT, HD, QF>), dim3(a.ranges * a.Z), dim3(256), lds, s, a);
-  hipLaunchKernelGGL((tree_merge_kernel<T, HD, 16 * QF, 32 * NW>), dim3(a.B * a.p.Hkv, a.Z), dim3(256), 0, s, a);
+static void launch_stream(const TreeArgs &a, hipStream_t s) {
+  constexpr size_t lds = (size_t)4 * QF * (HD / 16 * 256 + 32) * 4;
+  static const bool once = (allow_lds(&tree_stream_kernel<T, CT, HD, QF>, lds + (NGG_TREE_MAX + 1) * 4), true);
+  (void)once;
+  hipLaunchKernelGGL((tree_stream_kernel<T, CT, HD, QF>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
+  merge<T, HD, 16 * QF, 128>(a, s);
+}
+template <typename CT, int HD, int NW>
+static void launch_block(const TreeArgs &a, hipStream_t s) {
+  constexpr size_t lds = (size_t)8 * 32 * HD * 2 + 2 * 64 * 4 + 3 * 2 * 4;
+  static const bool once = (allow_lds(&tree_block_kernel<CT, HD, NW>, lds + (NGG_TREE_MAX + 1) * 4), true);
+  (void)once;
+  hipLaunchKernelGGL((tree_block_kernel<CT, HD, NW>), dim3(a.ranges * a.Z), dim3(64 * NW), lds + (a.B + 1) * 4, s, a);
+  merge<bf16_t, HD, 32 * NW, 64>(a, s);
 }
 template <typename T, typename CT, int HD>
 static void by_rows(const TreeArgs &a, int rows, hipStream_t s) {
-  if (rows == 16) launch<T, CT, HD, 1>(a, s);
-  else if (rows == 32) launch<T, CT, HD, 2>(a, s);
-  else if constexpr (sizeof(T) == 2) launch<T, CT, HD, 4>(a, s);
+  if (rows == 16) launch_stream<T, CT, HD, 1>(a, s);
+  else if (rows == 32) launch_stream<T, CT, HD, 2>(a, s);
+  else if constexpr (sizeof(T) == 2) {
+    if (rows == 64) launch_block<CT, HD, 2>(a, s);
+    else launch_block<CT, HD, 4>(a, s);
+  }
 }
 template <typename T, typename CT>
 static void by_head(const TreeArgs &a, int rows, hipStream_t s) {
