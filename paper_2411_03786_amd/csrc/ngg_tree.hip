@@ -8,6 +8,7 @@
 // workgroups (per row tile) take equal shares of it, whatever the lengths of the sequences; a share that ends inside a (sequence,
 // head) leaves a partial result, at most one at either end, and tree_merge_kernel joins those.  The lengths are read on the device.
 #include "ngg_operators.h"
+#include "ngg_epilogues.h"
 
 #include <algorithm>
 
@@ -96,8 +97,9 @@ __device__ __forceinline__ void step_totals(const TreeArgs &a, int *pre) {
   __syncthreads();
 }
 
-// The number of workgroups that share the list: as many as were launched, but no fewer than two steps each.
-__device__ __forceinline__ int64_t shares(const TreeArgs &a, int64_t total) { return min((int64_t)a.ranges, max((int64_t)1, total / 2)); }
+// The number of workgroups that share the list: as many as were launched, but no fewer steps each than make 256 keys.
+template <int KS>
+__device__ __forceinline__ int64_t shares(const TreeArgs &a, int64_t total) { return min((int64_t)a.ranges, max((int64_t)1, total * KS / 256)); }
 
 // A workgroup's place and share of the list, one (sequence, head) after the other.
 template <int KS, int NT>
@@ -120,10 +122,12 @@ struct Work {
       return;
     }
     step_totals<KS, NT>(a, pre);
-    const int64_t total = (int64_t)pre[a.B] * a.p.Hkv, R = shares(a, total);
+    const int64_t total = (int64_t)before(a.B) * a.p.Hkv, R = shares<KS>(a, total);
     u = range < R ? total * range / R : 0;
     u_end = range < R ? total * (range + 1) / R : 0;
   }
+  // (uniform: what comes from LDS does not look it, and would keep every address in vector registers)
+  __device__ __forceinline__ int before(int i) const { return __builtin_amdgcn_readfirstlane(pre[i]); }
   __device__ __forceinline__ bool next() {
     if (u >= u_end) return false;
     if (a.whole) {
@@ -134,9 +138,9 @@ struct Work {
       ++u;
       return true;
     }
-    while ((int64_t)pre[b + 1] * a.p.Hkv <= u) ++b;
-    steps = pre[b + 1] - pre[b];
-    const int64_t in_b = u - (int64_t)pre[b] * a.p.Hkv;
+    while ((int64_t)before(b + 1) * a.p.Hkv <= u) ++b;
+    steps = before(b + 1) - before(b);
+    const int64_t in_b = u - (int64_t)before(b) * a.p.Hkv;
     hk = (int)(in_b / steps);
     s_begin = (int)(in_b % steps);
     s_end = (int)min((int64_t)steps, s_begin + (u_end - u));
@@ -399,13 +403,13 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
   typedef bf16_t T;
   constexpr int DS = HD / 32, KQ = HD / 16, DB = HD / 32, TILE = 32 * HD, KT = 2, KS = 32 * KT, ROWS = 32 * NW, NT = 64 * NW;
   constexpr bool C8 = sizeof(CT) == 1;
-  constexpr int PIECES = TILE * (int)sizeof(CT) / 16, PPT = (PIECES + NT - 1) / NT;   // 16-byte pieces of a tile, of a thread
+  constexpr int PIECES = TILE / 16, PPT = (PIECES + NT - 1) / NT;   // (8 bits) 16-byte pieces of a tile, of a thread
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   T *kl = reinterpret_cast<T *>(smem);                     // [2][KT][TILE]
   T *vl = kl + 2 * KT * TILE;                              // [2][KT][TILE]
   float *vsl = reinterpret_cast<float *>(vl + 2 * KT * TILE);   // [2][KS] powers of two of the values
-  int *odd = reinterpret_cast<int *>(vsl + 2 * KS);        // [3][KT] a tile holds values that are not finite
-  int *pre = odd + 3 * KT;                                 // [B + 1]
+  int *odd = reinterpret_cast<int *>(vsl + 2 * KS);        // [KT] a tile of this step holds values that are not finite
+  int *pre = odd + KT;                                     // [B + 1]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r32 = lane & 31, h = lane >> 5;
   const int Hkv = a.p.Hkv, words = (a.T + 63) / 64;
@@ -422,45 +426,67 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
     const int group_keys = seen(z * ROWS, ROWS), wave_keys = seen(z * ROWS + wave * 32, 32);
     const int t_begin = w.s_begin * KT, t_end = min(w.s_end * KT, (group_keys + 31) / 32);
 
-    u32x4 kst[KT][PPT], vst[KT][PPT];                      // the next step's tiles, on their way
-    u32x2 kex[KT][C8 ? PPT : 1];
-    unsigned vex = 0;
-    bool there[KT];                                        // (uniform) the tile's page is one of the pool's
-    auto stage_load = [&](int t) {
+    // Tiles are taken in order; the pages of a step are looked up a step before its keys are asked for.
+    int pg[KT], pg_off[KT];
+    int at_page = t_begin * 32 / a.p.page_size, at_off = t_begin * 32 % a.p.page_size, at_tile = t_begin;
+    auto look_up = [&]() {
 #pragma unroll
       for (int k = 0; k < KT; ++k) {
-        const int pos0 = (t + k) * 32;
-        there[k] = t + k < t_end;
-        int page = there[k] ? a.pages[b * a.pages_batch + pos0 / a.p.page_size] : -1;
-        there[k] = page >= 0 && page < a.p.n_pages;
-        page = there[k] ? page : 0;
-        const int off = there[k] ? pos0 % a.p.page_size : 0;
-        const size_t head = ((size_t)page * Hkv + hk) * a.p.page_size + off;
-        const uint8_t *kp = (const uint8_t *)a.p.k + head * HD * sizeof(CT), *vp = (const uint8_t *)a.p.v + head * HD * sizeof(CT);
-#pragma unroll
-        for (int i = 0; i < PPT; ++i) {
-          const int pc = min(tid + NT * i, PIECES - 1);
-          kst[k][i] = reinterpret_cast<const u32x4 *>(kp)[pc];
-          vst[k][i] = reinterpret_cast<const u32x4 *>(vp)[pc];
-          if constexpr (C8) kex[k][i] = *reinterpret_cast<const u32x2 *>(a.p.k_exp + head + (pc % 16 / 4) * 8);
-        }
-        if constexpr (C8)
-          if (tid / 32 == k) vex = a.p.v_exp[head + tid % 32];
+        pg[k] = at_tile < t_end ? a.pages[b * a.pages_batch + at_page] : -1;
+        pg_off[k] = at_off;
+        ++at_tile;
+        at_off += 32;
+        if (at_off == a.p.page_size) { at_off = 0; ++at_page; }
       }
     };
-    auto stage_store = [&](int t, int buf, int o3) {
+    // 16-bit tiles go straight to LDS, 1 KB per wave and instruction; 8-bit ones by way of registers
+    u32x4 kst[C8 ? KT : 1][C8 ? PPT : 1], vst[C8 ? KT : 1][C8 ? PPT : 1];
+    u32x2 kex[C8 ? KT : 1][C8 ? PPT : 1];
+    unsigned vex = 0;
+    bool there[KT];                                        // (uniform) the tile's page is one of the pool's
+    auto stage_load = [&](int buf) {
+      const uint8_t *kp[KT], *vp[KT];
+      size_t head[KT];
 #pragma unroll
       for (int k = 0; k < KT; ++k) {
-        T *kt = kl + (buf * KT + k) * TILE, *vt = vl + (buf * KT + k) * TILE;
-        const int pos0 = (t + k) * 32;
-        const bool full = there[k] && pos0 + 32 <= len.ctx;
-        const int limit = there[k] ? n_keys : 0;
-        bool bad = false;
+        const int page = __builtin_amdgcn_readfirstlane(pg[k]);
+        there[k] = page >= 0 && page < a.p.n_pages;
+        head[k] = there[k] ? ((size_t)page * Hkv + hk) * a.p.page_size + pg_off[k] : 0;
+        kp[k] = (const uint8_t *)a.p.k + head[k] * HD * sizeof(CT);
+        vp[k] = (const uint8_t *)a.p.v + head[k] * HD * sizeof(CT);
+      }
+      if constexpr (C8) {
 #pragma unroll
-        for (int i = 0; i < PPT; ++i) {
-          const int pc = min(tid + NT * i, PIECES - 1), slot = pc % 64, blk = pc / 64;
-          if constexpr (C8) {
-            const int sh = slot % 4 * 8;
+        for (int k = 0; k < KT; ++k) {
+#pragma unroll
+          for (int i = 0; i < PPT; ++i) {
+            const int pc = min(tid + NT * i, PIECES - 1);
+            kst[k][i] = reinterpret_cast<const u32x4 *>(kp[k])[pc];
+            vst[k][i] = reinterpret_cast<const u32x4 *>(vp[k])[pc];
+            kex[k][i] = *reinterpret_cast<const u32x2 *>(a.p.k_exp + head[k] + (pc % 16 / 4) * 8);
+          }
+          if (tid / 32 == k) vex = a.p.v_exp[head[k] + tid % 32];
+        }
+      } else {
+        constexpr int KB = TILE * 2 / 1024, PER = 2 * KT * KB / NW;      // of a tile, of a wave
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int n = i * NW + wave, x = n / KB, kb = n % KB;          // x: keys of tile 0, 1, then values
+          const uint8_t *src = x == 0 ? kp[0] : x == 1 ? kp[1] : x == 2 ? vp[0] : vp[1];
+          T *dst = (x < KT ? kl + buf * KT * TILE : vl + buf * KT * TILE) + (x % KT) * TILE;
+          lds_dma16<false>(src + kb * 1024, lane * 16, (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)dst + kb * 1024);
+        }
+      }
+      look_up();
+    };
+    auto stage_store = [&](int t, int buf) {
+      if constexpr (C8) {
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+          T *kt = kl + (buf * KT + k) * TILE, *vt = vl + (buf * KT + k) * TILE;
+#pragma unroll
+          for (int i = 0; i < PPT; ++i) {
+            const int pc = min(tid + NT * i, PIECES - 1), slot = pc % 64, blk = pc / 64, sh = slot % 4 * 8;
             Frag<T> f0, f1;
             widen(f0, kst[k][i][0], kst[k][i][1], exp_scale(kex[k][i][0] >> sh & 0xff));
             widen(f1, kst[k][i][2], kst[k][i][3], exp_scale(kex[k][i][1] >> sh & 0xff));
@@ -468,27 +494,15 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
             *reinterpret_cast<bf16x8 *>(kt + (DS + blk) * 512 + slot * 8) = f1.v;
             widen(f0, vst[k][i][0], vst[k][i][1], 1.0f);
             widen(f1, vst[k][i][2], vst[k][i][3], 1.0f);
-            if (!full) {
-              bad |= only_there(f0, pos0 + slot / 16 * 8, limit);
-              bad |= only_there(f1, pos0 + slot / 16 * 8, limit);
-            }
             *reinterpret_cast<bf16x8 *>(vt + 2 * blk * 512 + slot * 8) = f0.v;
             *reinterpret_cast<bf16x8 *>(vt + (2 * blk + 1) * 512 + slot * 8) = f1.v;
-          } else {
-            Frag<T> f;
-            f.v = __builtin_bit_cast(bf16x8, vst[k][i]);
-            if (!full) bad |= only_there(f, pos0 + slot / 16 * 8, limit);
-            reinterpret_cast<u32x4 *>(kt)[pc] = kst[k][i];
-            reinterpret_cast<bf16x8 *>(vt)[pc] = f.v;
           }
+          if (tid / 32 == k) vsl[buf * KS + tid] = (t + k) * 32 + tid % 32 < (there[k] ? n_keys : 0) ? exp_scale(vex) : 1.0f;
         }
-        if (bad) odd[o3 * KT + k] = 1;
-        if constexpr (C8)
-          if (tid / 32 == k) vsl[buf * KS + tid] = pos0 + tid % 32 < limit ? exp_scale(vex) : 1.0f;
-      }
+      } else __builtin_amdgcn_s_waitcnt(0x0F70);           // vmcnt(0): this wave's transfers to LDS have landed
     };
-    if (tid < 3 * KT) odd[tid] = 0;
-    stage_load(t_begin);
+    look_up();
+    stage_load(0);
 
     const int row = z * ROWS + wave * 32 + r32, tok = row / a.G;
     const bool live = tok < len.tree;
@@ -510,59 +524,57 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r) O[d][r] = 0.0f;
-    __syncthreads();                                       // (odd is clear)
-
     bool here[KT];
-    auto compute = [&](int t, int buf, int o3) {
+    // all: every row sees every key of the step (one body for both: two of them cost more registers than there are)
+    auto compute = [&](bool all, int t, int buf) {
       if (t * 32 >= wave_keys) return;                     // (uniform per wave)
-      const T *kt = kl + buf * KT * TILE + koff, *vt = vl + buf * KT * TILE + voff;
-      f32x16 S[KT];
-#pragma unroll
-      for (int k = 0; k < KT; ++k)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) S[k][r] = 0.0f;
-#pragma unroll
-      for (int q = 0; q < KQ; ++q)
-#pragma unroll
-        for (int k = 0; k < KT; ++k) {
-          const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(kt + k * TILE + (q >> 1) * 512 + (q & 1) * 256);
-          S[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, Q[q], S[k], 0, 0, 0);
-        }
-      unsigned vis[KT][2];
-      float mx = -__builtin_inff();
 #pragma unroll
       for (int k = 0; k < KT; ++k) {
+        const T *kt = kl + (buf * KT + k) * TILE + koff, *vt = vl + (buf * KT + k) * TILE + voff;
         const int pos0 = (t + k) * 32;
-        vis[k][0] = vis[k][1] = 0xff;
-        if (pos0 + 32 > len.ctx || !here[k]) {             // (uniform)
+        f32x16 S;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[r] = 0.0f;
+        // (left to itself the compiler fetches one fragment, waits, and multiplies: the fences keep the fetches together and ahead)
+        bf16x8 kf[KQ], vf[2][DB];
+#pragma unroll
+        for (int q = 0; q < KQ; ++q) kf[q] = *reinterpret_cast<const bf16x8 *>(kt + (q >> 1) * 512 + (q & 1) * 256);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int q = 0; q < KQ; ++q) S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[q], Q[q], S, 0, 0, 0);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int d = 0; d < DB; ++d) vf[u][d] = *reinterpret_cast<const bf16x8 *>(vt + d * 1024 + u * 256);
+        __builtin_amdgcn_sched_barrier(0);
+        unsigned vis[2] = {0xff, 0xff};
+        if (!all) {
 #pragma unroll
           for (int u = 0; u < 2; ++u)
-            vis[k][u] = here[k] ? visible8(a.mask ? a.mask + b * a.mask_batch + min(tok, a.T - 1) * a.mask_token : nullptr, words, tok,
-                                           pos0 + 16 * u + 8 * h - len.ctx, n_keys - len.ctx) : 0u;
+            vis[u] = here[k] ? visible8(a.mask ? a.mask + b * a.mask_batch + min(tok, a.T - 1) * a.mask_token : nullptr, words, tok,
+                                        pos0 + 16 * u + 8 * h - len.ctx, n_keys - len.ctx) : 0u;
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if (!(vis[k][r >> 2 & 1] >> ((r >> 3) * 4 + (r & 3)) & 1)) S[k][r] = -__builtin_inff();
+            if (!(vis[r >> 2 & 1] >> ((r >> 3) * 4 + (r & 3)) & 1)) S[r] = -__builtin_inff();
         }
+        float mx = S[0];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, S[k][r]);
-      }
-      mx *= a.sfac;                                        // sfac > 0: the maximum commutes with the scaling
-      // the reference is brought up to date only when a score is far above it: sums and outputs use the same one, whichever it is
-      if (__ballot(mx > m + 8.0f) != 0) {
-        const float mnew = fmaxf(m, fmaxf(mx, other_half(mx)));
-        const float alpha = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
-        l *= alpha;
+        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, S[r]);
+        mx *= a.sfac;                                      // sfac > 0: the maximum commutes with the scaling
+        // the reference is brought up to date only when a score is far above it: sums and outputs use the same one, whichever it is
+        if (__ballot(mx > m + 8.0f) != 0) {
+          const float mnew = fmaxf(m, fmaxf(mx, other_half(mx)));
+          const float alpha = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
+          l *= alpha;
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+          for (int d = 0; d < DB; ++d)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) O[d][r] *= alpha;
-        m = mnew;
-      }
-      const float ref = m == -__builtin_inff() ? 0.0f : m;
-      bf16x8 P[KT][2];
-      float ps[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < KT; ++k)
+            for (int r = 0; r < 16; ++r) O[d][r] *= alpha;
+          m = mnew;
+        }
+        const float ref = m == -__builtin_inff() ? 0.0f : m;
+        bf16x8 P[2];
+        float ps[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           float vs[8];
@@ -570,70 +582,90 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
 #pragma unroll
             for (int e = 0; e < 8; ++e) vs[e] = vsl[buf * KS + k * 32 + u * 16 + h * 8 + e];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int r = 4 * (u + 2 * (e >> 2)) + (e & 3);
-            float p = __builtin_amdgcn_exp2f(__builtin_fmaf(S[k][r], a.sfac, -ref));
-            ps[e & 3] += p;
-            if constexpr (C8) p *= vs[e];
-            P[k][u][e] = (T)p;
+          for (int e = 0; e < 8; e += 2) {
+            f32x2 p;
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+              p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[4 * (u + 2 * (e >> 2)) + (e & 3) + v], a.sfac, -ref));
+              ps[v] += p[v];
+              if constexpr (C8) p[v] *= vs[e + v];
+            }
+            const bf16x2 q = __builtin_convertvector(p, bf16x2);
+            P[u][e] = q[0];
+            P[u][e + 1] = q[1];
           }
         }
-      l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
-#pragma unroll
-      for (int k = 0; k < KT; ++k)
+        l += ps[0] + ps[1];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int d = 0; d < DB; ++d) {
-            const bf16x8 vf = *reinterpret_cast<const bf16x8 *>(vt + k * TILE + d * 1024 + u * 256);
-            O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, P[k][u], O[d], 0, 0, 0);
-          }
-      // values that are not finite were left out, because 0 times them must stay 0 where their key is masked
-#pragma unroll
-      for (int k = 0; k < KT; ++k) {
-        if (!here[k] || !odd[o3 * KT + k]) continue;      // (uniform)
-        const int pos0 = (t + k) * 32;
-        const int page = a.pages[b * a.pages_batch + pos0 / a.p.page_size];
-        const CT *vg = (const CT *)a.p.v + (((size_t)page * Hkv + hk) * a.p.page_size + pos0 % a.p.page_size) * HD;
-        for (int j = 0; j < 32 && pos0 + j < n_keys; ++j) {
-          float pj = 0.0f;
-          unsigned vj = 0;
-#pragma unroll
-          for (int uu = 0; uu < 2; ++uu)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float x = __shfl((float)P[k][uu][e], (j >> 3 & 1) * 32 + r32);
-              const unsigned y = __shfl(vis[k][uu], (j >> 3 & 1) * 32 + r32);
-              if ((j & 7) == e && j >> 4 == uu) { pj = x; vj = y; }
-            }
-#pragma unroll
           for (int d = 0; d < DB; ++d)
+            O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[u][d], P[u], O[d], 0, 0, 0);
+        if (!all) {
+          // values that are not finite were left out, because 0 times them must stay 0 where their key is masked
+          if (odd[k]) {                                    // (uniform)
+            const int page = a.pages[b * a.pages_batch + pos0 / a.p.page_size];
+            const CT *vg = (const CT *)a.p.v + (((size_t)page * Hkv + hk) * a.p.page_size + pos0 % a.p.page_size) * HD;
+            for (int j = 0; j < 32 && pos0 + j < n_keys; ++j) {
+              unsigned pair = 0, vj = 0;                   // the probability of key j is half of a register of lane (row, j / 8 % 2)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const CT x = vg[page_v_offset<CT>(j, d * 32 + 8 * (r >> 2) + 4 * h + (r & 3), HD)];
-              float v;
-              if constexpr (C8) v = fp8_to_f32(x.bits);
-              else v = to_f32(x);
-              if ((vj >> (j & 7) & 1) && !(fabsf(v) < __builtin_inff())) O[d][r] += pj * v;
+              for (int u = 0; u < 2; ++u) {
+                const u32x4 w = __builtin_bit_cast(u32x4, P[u]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if ((j & 7) >> 1 == e && j >> 4 == u) { pair = w[e]; vj = vis[u]; }
+              }
+              int hh = h;
+              asm volatile("" : "+v"(hh));                 // the addresses below are made here, not kept in registers from the start
+              pair = __shfl(pair, (j >> 3 & 1) * 32 + r32);
+              vj = __shfl(vj, (j >> 3 & 1) * 32 + r32);
+              const float pj = __uint_as_float(j & 1 ? pair & 0xffff0000u : pair << 16);
+#pragma unroll
+              for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                  const CT x = vg[page_v_offset<CT>(j, d * 32 + 8 * (r >> 2) + 4 * hh + (r & 3), HD)];
+                  float v;
+                  if constexpr (C8) v = fp8_to_f32(x.bits);
+                  else v = to_f32(x);
+                  if ((vj >> (j & 7) & 1) && !(fabsf(v) < __builtin_inff())) O[d][r] += pj * v;
+                  if ((r & 3) == 3) asm volatile("" ::: "memory");       // few loads at a time: this path must not cost the other registers
+                }
             }
+          }
         }
       }
     };
 
-    int buf = 0, o3 = 0;
+    // the queries have landed before the loop: waited for inside it, they would take the tiles on their way with them
+    __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0)
+    int buf = 0;
     for (int t = t_begin; t < t_end; t += KT) {            // barriers are uniform
-      stage_store(t, buf, o3);
+      stage_store(t, buf);
 #pragma unroll
       for (int k = 0; k < KT; ++k) here[k] = there[k];
       __syncthreads();
-      // the marks of the step before this one: every wave has left it, and none sets them again before the next barrier
-      const int last = o3 == 0 ? 2 : o3 - 1;
-      if (tid < KT) odd[last * KT + tid] = 0;
-      stage_load(t + KT);
-      compute(t, buf, o3);
+      stage_load(buf ^ 1);
+      const bool all = (t + KT) * 32 <= len.ctx && here[0] && here[1];
+      if (!all) {
+        // a step at the end of the list: values that are not there become zeros, and those that are not finite
+        if (tid < KT) odd[tid] = 0;
+        __syncthreads();
+        for (int i = tid; i < KT * TILE / 8; i += NT) {
+          const int k = i / (TILE / 8);
+          Frag<T> f;
+          bf16x8 *at = reinterpret_cast<bf16x8 *>(vl + buf * KT * TILE) + i;
+          f.v = *at;
+          if (only_there(f, (t + k) * 32 + i % 64 / 16 * 8, here[k] ? n_keys : 0)) odd[k] = 1;
+          *at = f.v;
+        }
+        __syncthreads();
+      }
+      compute(all, t, buf);
       buf ^= 1;
-      o3 = o3 == 2 ? 0 : o3 + 1;
     }
+    // (the last transfers, of no step's tiles, have landed before LDS is used again)
+    if constexpr (!C8) __builtin_amdgcn_s_waitcnt(0x0F70);
 
     const float lsum = l + other_half(l);
     const bool whole = w.is_whole();
@@ -665,7 +697,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
   __shared__ int pre[NGG_TREE_MAX + 1];
   step_totals<KS, 256>(a, pre);
   const int z = blockIdx.y, b = blockIdx.x / a.p.Hkv, hk = blockIdx.x % a.p.Hkv;
-  const int64_t total = (int64_t)pre[a.B] * a.p.Hkv, R = shares(a, total);
+  const int64_t total = (int64_t)pre[a.B] * a.p.Hkv, R = shares<KS>(a, total);
   const int64_t steps = pre[b + 1] - pre[b], u0 = (int64_t)pre[b] * a.p.Hkv + hk * steps, u1 = u0 + steps;
   const int64_t first = ((u0 + 1) * R + total - 1) / total - 1, last = (u1 * R + total - 1) / total - 1;   // the shares that hold u0 and u1 - 1
   if (first == last) return;
@@ -745,7 +777,7 @@ static void launch_stream(const TreeArgs &a, hipStream_t s) {
 }
 template <typename CT, int HD, int NW>
 static void launch_block(const TreeArgs &a, hipStream_t s) {
-  constexpr size_t lds = (size_t)8 * 32 * HD * 2 + 2 * 64 * 4 + 3 * 2 * 4;
+  constexpr size_t lds = (size_t)8 * 32 * HD * 2 + 2 * 64 * 4 + 2 * 4;
   static const bool once = (allow_lds(&tree_block_kernel<CT, HD, NW>, lds + (NGG_TREE_MAX + 1) * 4), true);
   (void)once;
   hipLaunchKernelGGL((tree_block_kernel<CT, HD, NW>), dim3(a.ranges * a.Z), dim3(64 * NW), lds + (a.B + 1) * 4, s, a);
