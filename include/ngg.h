@@ -435,7 +435,7 @@ typedef struct {
   const uint64_t *mask;                    /* [batch][tree][(tree + 63) / 64], or NULL */
   int64_t mask_batch, mask_token;          /* mask_batch 0: one mask for all */
   int32_t max_pages, batch, tree, n_heads; /* batch 1 .. NGG_TREE_MAX, tree 1 .. NGG_TREE_MAX; n_heads <= 1024;
-                                              max_pages * page_size <= 2^30, times batch <= 2^36 */
+                                              max_pages * page_size <= 2^30, (that / 64 + 1) * batch * n_kv_heads <= 2^30 */
   int32_t dtype;                           /* of q and out; the pool's own, or any with NGG_FP8 */
   float scale;                             /* > 0 */
 } ngg_tree_args;

@@ -70,8 +70,8 @@ ngg_status check_tree(const char *what, const ngg_kv_pages *p, const ngg_tree_ar
     return fail_global(NGG_EINVAL, "%s: %d heads over %d key heads", what, a->n_heads, p->n_kv_heads);
   if (a->max_pages < 1 || (int64_t)a->max_pages * p->page_size > (1 << 30))
     return fail_global(NGG_EINVAL, "%s: %d pages of %d positions per sequence", what, a->max_pages, p->page_size);
-  if ((int64_t)a->max_pages * p->page_size * a->batch > (int64_t)1 << 36)
-    return fail_global(NGG_EINVAL, "%s: %d sequences of up to %d pages", what, a->batch, a->max_pages);
+  if (((int64_t)a->max_pages * p->page_size / 64 + 1) * a->batch * p->n_kv_heads > 1 << 30)   // the kernels count steps of 64 keys in 32 bits
+    return fail_global(NGG_EINVAL, "%s: %d sequences of up to %d pages and %d key heads", what, a->batch, a->max_pages, p->n_kv_heads);
   if (!pointers) return NGG_OK;
   if (!(a->scale > 0.0f) || !std::isfinite(a->scale)) return fail_global(NGG_EINVAL, "%s: scale must be positive and finite", what);
   if (!a->q || !a->out || !a->pages || !a->context_lens) return fail_global(NGG_EINVAL, "%s: null pointer", what);

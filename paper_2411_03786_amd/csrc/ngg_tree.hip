@@ -64,86 +64,88 @@ __device__ __forceinline__ int seq_keys(const TreeArgs &a, const SeqLens &s) {
 template <int KS>
 __device__ __forceinline__ int seq_steps(const TreeArgs &a, int b) { return max(1, (seq_keys(a, seq_lens(a, b)) + KS - 1) / KS); }
 
-// Running totals of those: pre[b] steps lie before sequence b, pre[B] in all.  NT threads.
-template <int KS, int NT>
+// Running totals of those: pre[b] steps lie before sequence b, pre[B] in all.  The first wave's work.
+template <int KS>
 __device__ __forceinline__ void step_totals(const TreeArgs &a, int *pre) {
-  constexpr int PER = NGG_TREE_MAX / NT;
-  __shared__ int wsum[NT / 64];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int n[PER], sum = 0;
+  const int tid = threadIdx.x;
+  if (tid < 64) {
+    int carry = 0;
+#pragma unroll 1
+    for (int first = 0; first < a.B; first += 64) {
+      const int b = first + tid, n = b < a.B ? seq_steps<KS>(a, b) : 0;
+      int inc = n;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int b = tid * PER + i;
-    n[i] = b < a.B ? seq_steps<KS>(a, b) : 0;
-    sum += n[i];
-  }
-  int inc = sum;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int up = __shfl_up(inc, o);
-    if (lane >= o) inc += up;
-  }
-  if (lane == 63) wsum[wave] = inc;
-  __syncthreads();
-  int at = inc - sum;
-  for (int w = 0; w < wave; ++w) at += wsum[w];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int b = tid * PER + i;
-    if (b < a.B) pre[b] = at;
-    at += n[i];
-    if (b == a.B - 1) pre[a.B] = at;
+      for (int o = 1; o < 64; o <<= 1) {
+        const int up = __shfl_up(inc, o);
+        if (tid >= o) inc += up;
+      }
+      if (b < a.B) pre[b] = carry + inc - n;
+      carry += __builtin_amdgcn_readlane(inc, 63);
+    }
+    if (tid == 0) pre[a.B] = carry;
   }
   __syncthreads();
 }
 
-// The number of workgroups that share the list: as many as were launched, but no fewer steps each than make 256 keys.
+// Steps of a share of the list: as many shares as workgroups were launched for, but of 256 keys at least
 template <int KS>
-__device__ __forceinline__ int64_t shares(const TreeArgs &a, int64_t total) { return min((int64_t)a.ranges, max((int64_t)1, total * KS / 256)); }
+__device__ __forceinline__ int share_steps(const TreeArgs &a, int total) { return max((int)((unsigned)(total + a.ranges - 1) / (unsigned)a.ranges), 256 / KS); }
 
-// A workgroup's place and share of the list, one (sequence, head) after the other.
-template <int KS, int NT>
+// A workgroup's place and share of the list, one (sequence, head) after the other.  Whole numbers of 32 bits (the host sees to that):
+// what runs once costs a launch its instruction fetches.
+template <int KS>
 struct Work {
   const TreeArgs &a;
   int *pre;
-  int z;
-  int64_t range, u, u_end;
+  int z, range, u, u_end;
   // of the part at hand: steps s_begin .. s_end - 1 of `steps`
   int b, hk, s_begin, s_end, steps;
 
   __device__ __forceinline__ Work(const TreeArgs &args, int *totals) : a(args), pre(totals), b(0) {
     // the row tiles of a share run next to each other on one die: its keys come from memory once
-    const bool dealt = a.ranges % 8 == 0;
-    z = (int)(dealt ? blockIdx.x / 8 : blockIdx.x) % a.Z;
-    range = dealt ? (int64_t)(blockIdx.x / 8) / a.Z * 8 + blockIdx.x % 8 : blockIdx.x / a.Z;
+    if (a.Z == 1) {
+      z = 0;
+      range = blockIdx.x;
+    } else {
+      const bool dealt = a.ranges % 8 == 0;
+      const int slot = dealt ? blockIdx.x / 8 : blockIdx.x;
+      range = slot / a.Z;
+      z = slot - range * a.Z;
+      if (dealt) range = range * 8 + blockIdx.x % 8;
+    }
     if (a.whole) {                                         // a (sequence, head) for each
       u = range;
-      u_end = min(range + 1, (int64_t)a.B * a.p.Hkv);
+      u_end = range + 1;
       return;
     }
-    step_totals<KS, NT>(a, pre);
-    const int64_t total = (int64_t)before(a.B) * a.p.Hkv, R = shares<KS>(a, total);
-    u = range < R ? total * range / R : 0;
-    u_end = range < R ? total * (range + 1) / R : 0;
+    step_totals<KS>(a, pre);
+    const int total = before(a.B) * a.p.Hkv, per = share_steps<KS>(a, total);
+    u = range * per;
+    u_end = min(u + per, total);
   }
   // (uniform: what comes from LDS does not look it, and would keep every address in vector registers)
   __device__ __forceinline__ int before(int i) const { return __builtin_amdgcn_readfirstlane(pre[i]); }
   __device__ __forceinline__ bool next() {
     if (u >= u_end) return false;
     if (a.whole) {
-      b = (int)(u / a.p.Hkv);
-      hk = (int)(u % a.p.Hkv);
+      b = u / a.p.Hkv;
+      hk = u - b * a.p.Hkv;
       s_begin = 0;
       steps = s_end = seq_steps<KS>(a, b);
       ++u;
       return true;
     }
-    while ((int64_t)before(b + 1) * a.p.Hkv <= u) ++b;
-    steps = before(b + 1) - before(b);
-    const int64_t in_b = u - (int64_t)before(b) * a.p.Hkv;
-    hk = (int)(in_b / steps);
-    s_begin = (int)(in_b % steps);
-    s_end = (int)min((int64_t)steps, s_begin + (u_end - u));
+    int p0 = before(b), p1 = before(b + 1);
+    while (p1 * a.p.Hkv <= u) {
+      ++b;
+      p0 = p1;
+      p1 = before(b + 1);
+    }
+    steps = p1 - p0;
+    const int in_b = u - p0 * a.p.Hkv;
+    hk = in_b / steps;
+    s_begin = in_b - hk * steps;
+    s_end = min(steps, s_begin + (u_end - u));
     u += s_end - s_begin;
     return true;
   }
@@ -152,18 +154,28 @@ struct Work {
   __device__ __forceinline__ size_t part() const { return ((size_t)range * a.Z + z) * 2 + (s_begin == 0 ? 1 : 0); }
 };
 
-// Eight bits, bit e set if token t of the tree sees position ctx + at + e (at may be negative: the context); keys: positions there are
-__device__ __forceinline__ unsigned visible8(const uint64_t *row, int words, int t, int at, int tree_keys) {
+// Two words of a token's row of the mask, from the one that holds tree position at (or the first): enough for the 64 positions from
+// there.  Without a mask every bit is set.
+struct MaskWindow { uint64_t lo, hi; };
+__device__ __forceinline__ MaskWindow mask_window(const TreeArgs &a, int b, int tok, int at) {
+  MaskWindow w = {~0ull, ~0ull};
+  if (!a.mask) return w;
+  const int words = (a.T + 63) / 64, i = max(at, 0) >> 6;
+  const uint64_t *row = a.mask + b * a.mask_batch + min(tok, a.T - 1) * a.mask_token;
+  w.lo = row[min(i, words - 1)];
+  w.hi = row[min(i + 1, words - 1)];                       // (words that are not there are of positions behind every token)
+  return w;
+}
+// Eight bits, bit e set if token t sees tree position at + e (negative: the context).  w: the window from tree position from;
+// tree_keys: how many tree positions there are
+__device__ __forceinline__ unsigned visible8(const MaskWindow &w, int from, int t, int at, int tree_keys) {
   unsigned v = 0xff;
-  if (at + 7 >= 0 && row) {
-    const int lo = max(at, 0), w = lo >> 6, sh = lo & 63;
-    if (w >= words) v = 0;
-    else {
-      uint64_t x = row[w] >> sh;
-      if (sh > 56 && w + 1 < words) x |= row[w + 1] << (64 - sh);
-      v = (unsigned)(x & 0xff);
-      if (at < 0) v = ((v << -at) | ((1u << -at) - 1)) & 0xff;
-    }
+  if (at + 7 >= 0) {
+    const int sh = max(at, 0) - (max(from, 0) & ~63);      // 0 .. 127
+    uint64_t x = sh >= 64 ? w.hi >> (sh & 63) : w.lo >> sh;
+    if (sh > 0 && sh < 64) x |= w.hi << (64 - sh);
+    v = (unsigned)(x & 0xff);
+    if (at < 0) v = ((v << -at) | ((1u << -at) - 1)) & 0xff;
   }
   const int n = min(t + 1, tree_keys) - at;                // positions at .. at + n - 1 are there and not behind t
   return n >= 8 ? v : n <= 0 ? 0u : v & ((1u << n) - 1);
@@ -188,16 +200,20 @@ __device__ __forceinline__ bool only_there(Frag<T> &f, int pos, int n) {
 __device__ __forceinline__ Frag<bf16_t> load_frag_row(const bf16_t *p) { return load_frag_tiled(p); }
 __device__ __forceinline__ Frag<float> load_frag_row(const float *p) { return load_frag(p); }
 
+__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? -__builtin_inff() : kLn2 * (m + __builtin_log2f(l)); }
+template <typename T>
+__device__ __forceinline__ void put4(T *out, const f32x4 &o, int vec) {
+  if (vec) store4(out, o[0], o[1], o[2], o[3]);
+  else
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = from_f32<T>(o[i]);
+}
 // Four elements of an output row from their sum o with its running maximum (base 2) and sum; a row that saw nothing is zero.
 template <typename T>
 __device__ __forceinline__ void write_row4(const TreeArgs &a, int b, int t, int h, int dim, const f32x4 &o, float m, float l) {
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  T *out = (T *)a.out + b * a.out_batch + t * a.out_token + h * a.out_head + dim;
-  if (a.out_vec) store4(out, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-  else
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = from_f32<T>(o[i] * inv);
-  if (dim == 0 && a.lse) a.lse[((int64_t)b * a.T + t) * a.H + h] = l == 0.0f ? -__builtin_inff() : kLn2 * (m + __builtin_log2f(l));
+  put4((T *)a.out + b * a.out_batch + t * a.out_token + h * a.out_head + dim, f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv}, a.out_vec);
+  if (dim == 0 && a.lse) a.lse[((int64_t)b * a.T + t) * a.H + h] = log_sum(m, l);
 }
 
 // One workgroup: one row tile (16 QF rows) over its share of the list.  The waves take the tiles of 32 keys of a (sequence, head) in
@@ -211,8 +227,8 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
   int *pre = reinterpret_cast<int *>(lml + NW * QF * 32);  // [B + 1]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, g4 = lane >> 4;
-  const int Hkv = a.p.Hkv, words = (a.T + 63) / 64;
-  Work<KS, 256> w(a, pre);
+  const int Hkv = a.p.Hkv;
+  Work<KS> w(a, pre);
   while (w.next()) {
     const int b = w.b, hk = w.hk, z = w.z;
     const SeqLens len = seq_lens(a, b);
@@ -221,10 +237,12 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
     // rows of this lane's queries
     Frag<T> Q[QF][DS];
     int tok[QF];
+    MaskWindow see[QF];                                    // of trees of up to 64 tokens the whole row
 #pragma unroll
     for (int f = 0; f < QF; ++f) {
       const int r = z * ROWS + f * 16 + c;
       tok[f] = r / a.G;
+      see[f] = mask_window(a, b, tok[f], 0);
       const bool live = tok[f] < len.tree;
       const T *q = (const T *)a.q + b * a.q_batch + (live ? tok[f] : 0) * a.q_token + (int64_t)(hk * a.G + r % a.G) * a.q_head;
 #pragma unroll
@@ -298,8 +316,11 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
 #pragma unroll
         for (int d = 0; d < DS; ++d) { mma(S[0], K[0][d], Q[f][d]); mma(S[1], K[1][d], Q[f][d]); }
         unsigned vis = 0xff;
-        if (!full) vis = visible8(a.mask ? a.mask + b * a.mask_batch + min(tok[f], a.T - 1) * a.mask_token : nullptr, words, tok[f],
-                                  pos0 + g4 * 8 - len.ctx, n_keys - len.ctx);
+        if (!full) {
+          const int from = a.T > 64 ? pos0 - len.ctx : 0;
+          if (a.T > 64) see[f] = mask_window(a, b, tok[f], from);
+          vis = visible8(see[f], from, tok[f], pos0 + g4 * 8 - len.ctx, n_keys - len.ctx);
+        }
         float s[8], p[8], mx = -__builtin_inff();
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -412,9 +433,9 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
   int *pre = odd + KT;                                     // [B + 1]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r32 = lane & 31, h = lane >> 5;
-  const int Hkv = a.p.Hkv, words = (a.T + 63) / 64;
+  const int Hkv = a.p.Hkv;
   const int loff = (h * 16 + (r32 & 15)) * 8, koff = (r32 >> 4) * DS * 512 + loff, voff = (r32 >> 4) * 512 + loff;
-  Work<KS, NT> w(a, pre);
+  Work<KS> w(a, pre);
   while (w.next()) {
     const int b = w.b, hk = w.hk, z = w.z;
     const SeqLens len = seq_lens(a, b);
@@ -444,7 +465,13 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
     u32x2 kex[C8 ? KT : 1][C8 ? PPT : 1];
     unsigned vex = 0;
     bool there[KT];                                        // (uniform) the tile's page is one of the pool's
+    const int tok = (z * ROWS + wave * 32 + r32) / a.G;
+    const bool live = tok < len.tree;
+    MaskWindow see_next;                                   // ... and what the rows see of a step that holds tree tokens
+    int at_step = t_begin;
     auto stage_load = [&](int buf) {
+      if (at_step * 32 + KS > len.ctx) see_next = mask_window(a, b, tok, at_step * 32 - len.ctx);
+      at_step += KT;
       const uint8_t *kp[KT], *vp[KT];
       size_t head[KT];
 #pragma unroll
@@ -503,28 +530,43 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
     };
     look_up();
     stage_load(0);
-
-    const int row = z * ROWS + wave * 32 + r32, tok = row / a.G;
-    const bool live = tok < len.tree;
     bf16x8 Q[KQ];
     {
+      const int row = z * ROWS + wave * 32 + r32;
       const T *q = (const T *)a.q + b * a.q_batch + (live ? tok : 0) * a.q_token + (int64_t)(hk * a.G + row % a.G) * a.q_head;
 #pragma unroll
-      for (int d = 0; d < KQ; ++d) {
-        if (!live) Q[d] = zero_frag<T>().v;
-        else if (a.q_vec) Q[d] = *reinterpret_cast<const bf16x8 *>(q + d * 16 + h * 8);
-        else
+      for (int d = 0; d < KQ; ++d) Q[d] = zero_frag<T>().v;
+      if (live) {
+        if (a.q_vec) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) Q[d][e] = q[d * 16 + h * 8 + e];
+          for (int d = 0; d < KQ; ++d) Q[d] = *reinterpret_cast<const bf16x8 *>(q + d * 16 + h * 8);
+        } else {
+#pragma unroll
+          for (int d = 0; d < KQ; ++d)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) Q[d][e] = q[d * 16 + h * 8 + e];
+        }
       }
     }
+    bool here[KT];
+    MaskWindow see;
+    auto arrive = [&]() {                                  // what was asked for last becomes the step at hand
+#pragma unroll
+      for (int k = 0; k < KT; ++k) here[k] = there[k];
+      see = see_next;
+    };
+    if constexpr (!C8) {                                   // both buffers are empty: the second step's tiles may come at once
+      arrive();
+      stage_load(1);
+    }
+
     float m = -__builtin_inff(), l = 0.0f;
     f32x16 O[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r) O[d][r] = 0.0f;
-    bool here[KT];
+
     // all: every row sees every key of the step (one body for both: two of them cost more registers than there are)
     auto compute = [&](bool all, int t, int buf) {
       if (t * 32 >= wave_keys) return;                     // (uniform per wave)
@@ -532,14 +574,14 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
       for (int k = 0; k < KT; ++k) {
         const T *kt = kl + (buf * KT + k) * TILE + koff, *vt = vl + (buf * KT + k) * TILE + voff;
         const int pos0 = (t + k) * 32;
-        f32x16 S;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) S[r] = 0.0f;
         // (left to itself the compiler fetches one fragment, waits, and multiplies: the fences keep the fetches together and ahead)
         bf16x8 kf[KQ], vf[2][DB];
 #pragma unroll
         for (int q = 0; q < KQ; ++q) kf[q] = *reinterpret_cast<const bf16x8 *>(kt + (q >> 1) * 512 + (q & 1) * 256);
         __builtin_amdgcn_sched_barrier(0);
+        f32x16 S;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[r] = 0.0f;
 #pragma unroll
         for (int q = 0; q < KQ; ++q) S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[q], Q[q], S, 0, 0, 0);
 #pragma unroll
@@ -551,8 +593,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
         if (!all) {
 #pragma unroll
           for (int u = 0; u < 2; ++u)
-            vis[u] = here[k] ? visible8(a.mask ? a.mask + b * a.mask_batch + min(tok, a.T - 1) * a.mask_token : nullptr, words, tok,
-                                        pos0 + 16 * u + 8 * h - len.ctx, n_keys - len.ctx) : 0u;
+            vis[u] = here[k] ? visible8(see, t * 32 - len.ctx, tok, pos0 + 16 * u + 8 * h - len.ctx, n_keys - len.ctx) : 0u;
 #pragma unroll
           for (int r = 0; r < 16; ++r)
             if (!(vis[r >> 2 & 1] >> ((r >> 3) * 4 + (r & 3)) & 1)) S[r] = -__builtin_inff();
@@ -563,8 +604,9 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
         mx *= a.sfac;                                      // sfac > 0: the maximum commutes with the scaling
         // the reference is brought up to date only when a score is far above it: sums and outputs use the same one, whichever it is
         if (__ballot(mx > m + 8.0f) != 0) {
-          const float mnew = fmaxf(m, fmaxf(mx, other_half(mx)));
-          const float alpha = mnew == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
+          // (each row by itself: its result must not hang on its neighbours')
+          const float top = fmaxf(mx, other_half(mx)), mnew = top > m + 8.0f ? top : m;
+          const float alpha = mnew == m ? 1.0f : __builtin_amdgcn_exp2f(m - mnew);
           l *= alpha;
 #pragma unroll
           for (int d = 0; d < DB; ++d)
@@ -599,39 +641,36 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int d = 0; d < DB; ++d)
-            O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[u][d], P[u], O[d], 0, 0, 0);
-        if (!all) {
+          for (int d = 0; d < DB; ++d) O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[u][d], P[u], O[d], 0, 0, 0);
+        if (!all && odd[k]) {                              // (uniform)
           // values that are not finite were left out, because 0 times them must stay 0 where their key is masked
-          if (odd[k]) {                                    // (uniform)
-            const int page = a.pages[b * a.pages_batch + pos0 / a.p.page_size];
-            const CT *vg = (const CT *)a.p.v + (((size_t)page * Hkv + hk) * a.p.page_size + pos0 % a.p.page_size) * HD;
-            for (int j = 0; j < 32 && pos0 + j < n_keys; ++j) {
-              unsigned pair = 0, vj = 0;                   // the probability of key j is half of a register of lane (row, j / 8 % 2)
+          const int page = a.pages[b * a.pages_batch + pos0 / a.p.page_size];
+          const CT *vg = (const CT *)a.p.v + (((size_t)page * Hkv + hk) * a.p.page_size + pos0 % a.p.page_size) * HD;
+          for (int j = 0; j < 32 && pos0 + j < n_keys; ++j) {
+            unsigned pair = 0, vj = 0;                     // the probability of key j is half of a register of lane (row, j / 8 % 2)
 #pragma unroll
-              for (int u = 0; u < 2; ++u) {
-                const u32x4 w = __builtin_bit_cast(u32x4, P[u]);
+            for (int u = 0; u < 2; ++u) {
+              const u32x4 w = __builtin_bit_cast(u32x4, P[u]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if ((j & 7) >> 1 == e && j >> 4 == u) { pair = w[e]; vj = vis[u]; }
-              }
-              int hh = h;
-              asm volatile("" : "+v"(hh));                 // the addresses below are made here, not kept in registers from the start
-              pair = __shfl(pair, (j >> 3 & 1) * 32 + r32);
-              vj = __shfl(vj, (j >> 3 & 1) * 32 + r32);
-              const float pj = __uint_as_float(j & 1 ? pair & 0xffff0000u : pair << 16);
-#pragma unroll
-              for (int d = 0; d < DB; ++d)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                  const CT x = vg[page_v_offset<CT>(j, d * 32 + 8 * (r >> 2) + 4 * hh + (r & 3), HD)];
-                  float v;
-                  if constexpr (C8) v = fp8_to_f32(x.bits);
-                  else v = to_f32(x);
-                  if ((vj >> (j & 7) & 1) && !(fabsf(v) < __builtin_inff())) O[d][r] += pj * v;
-                  if ((r & 3) == 3) asm volatile("" ::: "memory");       // few loads at a time: this path must not cost the other registers
-                }
+              for (int e = 0; e < 4; ++e)
+                if ((j & 7) >> 1 == e && j >> 4 == u) { pair = w[e]; vj = vis[u]; }
             }
+            int hh = h;
+            asm volatile("" : "+v"(hh));                   // the addresses below are made here, not kept in registers from the start
+            pair = __shfl(pair, (j >> 3 & 1) * 32 + r32);
+            vj = __shfl(vj, (j >> 3 & 1) * 32 + r32);
+            const float pj = __uint_as_float(j & 1 ? pair & 0xffff0000u : pair << 16);
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                const CT x = vg[page_v_offset<CT>(j, d * 32 + 8 * (r >> 2) + 4 * hh + (r & 3), HD)];
+                float v;
+                if constexpr (C8) v = fp8_to_f32(x.bits);
+                else v = to_f32(x);
+                if ((vj >> (j & 7) & 1) && !(fabsf(v) < __builtin_inff())) O[d][r] += pj * v;
+                if ((r & 3) == 3) asm volatile("" ::: "memory");         // few loads at a time: this path must not cost the other registers
+              }
           }
         }
       }
@@ -642,22 +681,27 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
     int buf = 0;
     for (int t = t_begin; t < t_end; t += KT) {            // barriers are uniform
       stage_store(t, buf);
-#pragma unroll
-      for (int k = 0; k < KT; ++k) here[k] = there[k];
+      if (C8 || t > t_begin) arrive();
       __syncthreads();
-      stage_load(buf ^ 1);
+      if (C8 || t > t_begin) stage_load(buf ^ 1);
       const bool all = (t + KT) * 32 <= len.ctx && here[0] && here[1];
       if (!all) {
         // a step at the end of the list: values that are not there become zeros, and those that are not finite
         if (tid < KT) odd[tid] = 0;
         __syncthreads();
+#pragma unroll 2
         for (int i = tid; i < KT * TILE / 8; i += NT) {
-          const int k = i / (TILE / 8);
-          Frag<T> f;
-          bf16x8 *at = reinterpret_cast<bf16x8 *>(vl + buf * KT * TILE) + i;
-          f.v = *at;
-          if (only_there(f, (t + k) * 32 + i % 64 / 16 * 8, here[k] ? n_keys : 0)) odd[k] = 1;
-          *at = f.v;
+          const int k = i / (TILE / 8), pos = (t + k) * 32 + i % 64 / 16 * 8, left = (here[k] ? n_keys : 0) - pos;
+          u32x4 *at = reinterpret_cast<u32x4 *>(vl + buf * KT * TILE) + i, x = *at;
+          unsigned top = 0;                                // an exponent of ones, plus one, carries into the sign's place
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top |= (x[e] & 0x7f807f80u) + 0x00800080u;
+          if (left < 8 || (top & 0x80008000u)) {
+            Frag<T> f;
+            f.v = __builtin_bit_cast(bf16x8, x);
+            if (only_there(f, pos, pos + left)) odd[k] = 1;
+            *at = __builtin_bit_cast(u32x4, f.v);
+          }
         }
         __syncthreads();
       }
@@ -667,24 +711,39 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
     // (the last transfers, of no step's tiles, have landed before LDS is used again)
     if constexpr (!C8) __builtin_amdgcn_s_waitcnt(0x0F70);
 
-    const float lsum = l + other_half(l);
     const bool whole = w.is_whole();
-    const size_t part = w.part();
+    float lsum = l + other_half(l);
     if (tok < a.T) {
+      if (!live) lsum = 0.0f;                              // not a token of this sequence
+      const int r = wave * 32 + r32;
+      if (whole) {
+        const int head = hk * a.G + (z * ROWS + r) % a.G;
+        const float inv = lsum == 0.0f ? 0.0f : 1.0f / lsum;
+        T *out = (T *)a.out + b * a.out_batch + tok * a.out_token + head * a.out_head + 4 * h;
 #pragma unroll
-      for (int d = 0; d < DB; ++d)
+        for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          f32x4 o = {O[d][4 * j], O[d][4 * j + 1], O[d][4 * j + 2], O[d][4 * j + 3]};
-          float mm = m, ll = lsum;
-          if (!live) { o = f32x4{0.f, 0.f, 0.f, 0.f}; ll = 0.0f; mm = -__builtin_inff(); }   // not a token of this sequence
-          const int dim = d * 32 + 8 * j + 4 * h, r = wave * 32 + r32;
-          if (whole) write_row4<T>(a, b, tok, hk * a.G + row % a.G, dim, o, mm, ll);
-          else {
-            *reinterpret_cast<f32x4 *>(a.part_o + (part * ROWS + r) * HD + dim) = o;
-            if (dim == 0) { a.part_ml[(part * ROWS + r) * 2] = mm; a.part_ml[(part * ROWS + r) * 2 + 1] = ll; }
+          for (int j = 0; j < 4; ++j) {
+            f32x4 o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = live ? O[d][4 * j + i] * inv : 0.0f;
+            put4(out + d * 32 + 8 * j, o, a.out_vec);
           }
-        }
+        if (h == 0 && a.lse) a.lse[((int64_t)b * a.T + tok) * a.H + head] = log_sum(m, lsum);
+      } else {
+        const size_t at = w.part() * ROWS + r;
+        float *po = a.part_o + at * HD + 4 * h;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            f32x4 o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = live ? O[d][4 * j + i] : 0.0f;
+            *reinterpret_cast<f32x4 *>(po + d * 32 + 8 * j) = o;
+          }
+        if (h == 0) *reinterpret_cast<f32x2 *>(a.part_ml + at * 2) = f32x2{live ? m : -__builtin_inff(), lsum};
+      }
     }
     __syncthreads();
   }
@@ -695,25 +754,24 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
 template <typename T, int HD, int ROWS, int KS>
 __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
   __shared__ int pre[NGG_TREE_MAX + 1];
-  step_totals<KS, 256>(a, pre);
+  step_totals<KS>(a, pre);
   const int z = blockIdx.y, b = blockIdx.x / a.p.Hkv, hk = blockIdx.x % a.p.Hkv;
-  const int64_t total = (int64_t)pre[a.B] * a.p.Hkv, R = shares<KS>(a, total);
-  const int64_t steps = pre[b + 1] - pre[b], u0 = (int64_t)pre[b] * a.p.Hkv + hk * steps, u1 = u0 + steps;
-  const int64_t first = ((u0 + 1) * R + total - 1) / total - 1, last = (u1 * R + total - 1) / total - 1;   // the shares that hold u0 and u1 - 1
+  const int per = share_steps<KS>(a, pre[a.B] * a.p.Hkv), steps = pre[b + 1] - pre[b], u0 = pre[b] * a.p.Hkv + hk * steps;
+  const int first = u0 / per, last = (u0 + steps - 1) / per;   // the shares that hold its first and its last step
   if (first == last) return;
   const int i = blockIdx.z * 256 + threadIdx.x;
   const int r = i / (HD / 4), dim = i % (HD / 4) * 4, rr = z * ROWS + r, t = rr / a.G;
   if (r >= ROWS || t >= a.T) return;
-  const int slot0 = total * first / R <= u0 ? 1 : 0;       // the first share may have begun before
+  // (the last part of its first share, the first of the others)
   float mm = -__builtin_inff(), ll = 0.0f;
   f32x4 o{0.f, 0.f, 0.f, 0.f};
-  for (int64_t w = first; w <= last; w += 8) {             // eight parts on their way at a time
+  for (int w = first; w <= last; w += 8) {                 // eight parts on their way at a time
     f32x2 ml[8];
     f32x4 v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int64_t x = min(w + j, last);
-      const size_t part = (((size_t)x * a.Z + z) * 2 + (x == first ? slot0 : 0)) * ROWS + r;
+      const int x = min(w + j, last);
+      const size_t part = (((size_t)x * a.Z + z) * 2 + (x == first ? 1 : 0)) * ROWS + r;
       ml[j] = *reinterpret_cast<const f32x2 *>(a.part_ml + part * 2);
       v[j] = *reinterpret_cast<const f32x4 *>(a.part_o + part * HD + dim);
     }
@@ -737,15 +795,24 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
   write_row4<T>(a, b, t, hk * a.G + rr % a.G, dim, o, mm, ll);
 }
 
-// Which kernel and rows of a tile: up to 16 and 32 rows (fp32: any number) are tree_stream_kernel's, above that two waves of 32 rows or
-// four are tree_block_kernel's.
-static int tile_rows(int dtype, int rows) { return rows <= 16 ? 16 : rows <= 32 || dtype == NGG_F32 ? 32 : rows <= 64 ? 64 : 128; }
+// Rows of a tile, and with them the kernel: 16 and 32 rows are tree_stream_kernel's, 128 tree_block_kernel's (16-bit operands).  Short
+// lists take the smaller tiles, whose workgroups start and end quicker, though every tile reads the keys again (from the L2); the
+// rule goes by the positions of all (sequence, key head) together.  Measured with 32 heads of 128 (us; tiles of 16, 32, 128 rows):
+//   51 rows, 32 x 2048 positions 23, 25, 28; 32 x 8000: 41, 39, 42; 32 x 24000: 123, 100, 93
+//   128 rows, 64 x 500: 18, 28, 32; 64 x 2048: 37, 41, 44; 64 x 8000: 104, 100, 81
+//   244 rows, 64 x 500: 30, 25, 41; 64 x 2048: 64, 51, 58; 64 x 8000: 193, 151, 118
+static int tile_rows(int dtype, int rows, int64_t positions) {
+  if (rows <= 16) return 16;
+  if (dtype == NGG_F32) return 32;
+  if (positions < 160 * 1024) return rows <= 128 ? 16 : 32;
+  return rows <= 32 || positions < 400 * 1024 ? 32 : 128;
+}
 static int step_keys(int rows) { return rows <= 32 ? 128 : 64; }
 
 TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, int64_t max_positions) {
   (void)cache;
   TreePlan p;
-  p.rows = tile_rows(dtype, T * G);
+  p.rows = tile_rows(dtype, T * G, max_positions * B * Hkv);
   p.Z = (T * G + p.rows - 1) / p.rows;
   const int64_t steps = (max_positions + step_keys(p.rows) - 1) / step_keys(p.rows);
   p.whole = steps <= 4;
@@ -788,8 +855,7 @@ static void by_rows(const TreeArgs &a, int rows, hipStream_t s) {
   if (rows == 16) launch_stream<T, CT, HD, 1>(a, s);
   else if (rows == 32) launch_stream<T, CT, HD, 2>(a, s);
   else if constexpr (sizeof(T) == 2) {
-    if (rows == 64) launch_block<CT, HD, 2>(a, s);
-    else launch_block<CT, HD, 4>(a, s);
+    launch_block<CT, HD, 4>(a, s);
   }
 }
 template <typename T, typename CT>

@@ -304,7 +304,7 @@ def check_attention(out, lse, want, want_lse, mag, qk, dtype):
 class Case:
     """Sequences of random keys and values in a pool of shuffled pages whose unwritten places hold NaN."""
 
-    def __init__(self, ctx, trees, T, H, Hkv, hd, dtype="bf16", cache=None, page=32, seed=0, spare=1, sharp=1.0):
+    def __init__(self, ctx, trees, T, H, Hkv, hd, dtype="bf16", cache=None, page=32, seed=0, spare=1, sharp=1.0, wide=False):
         cache = cache or dtype
         rng = np.random.default_rng(seed)
         B = len(ctx)
@@ -318,6 +318,9 @@ class Case:
             self.kv.k_exps.fill_(255)
             self.kv.v_exps.fill_(255)
         self.table = ints(rng.permutation(pool)[:B * per].reshape(B, per))
+        if wide:                                                        # a page list long enough for the kernels of long contexts
+            more = -(-(1 << 19) // (page * B * Hkv))
+            self.table = torch.cat([self.table, torch.full((B, more), -1, dtype=torch.int32, device="cuda")], 1)
         self.ks, self.vs = [], []
         for b in range(B):
             n = max(ctx[b], 0) + trees[b]
@@ -363,18 +366,20 @@ TYPES = [("f32", "f32"), ("bf16", "bf16"), ("f32", "fp8"), ("bf16", "fp8")]
 @pytest.mark.parametrize("dtype,cache", TYPES)
 @pytest.mark.parametrize("H,Hkv,hd", [(4, 4, 32), (6, 2, 64), (8, 2, 128), (3, 3, 128)])
 @pytest.mark.parametrize("T,ctx", [(1, 0), (1, 1), (1, 31), (1, 300), (2, 127), (5, 0), (13, 128), (17, 65), (33, 200), (65, 97), (70, 1000)])
-def test_tree_attention_one_sequence(dtype, cache, H, Hkv, hd, T, ctx):
-    c = Case([ctx], [T], T, H, Hkv, hd, dtype, cache, seed=T + ctx)
+@pytest.mark.parametrize("wide", [False, True])
+def test_tree_attention_one_sequence(dtype, cache, H, Hkv, hd, T, ctx, wide):
+    c = Case([ctx], [T], T, H, Hkv, hd, dtype, cache, seed=T + ctx, wide=wide)
     see, words = c.masks(seed=T)
     c.check(words, see)
 
 
 @pytest.mark.parametrize("dtype,cache", TYPES)
 @pytest.mark.parametrize("page", [32, 64, 160])
-def test_tree_attention_ragged_batch(dtype, cache, page):
+@pytest.mark.parametrize("wide", [False, True])
+def test_tree_attention_ragged_batch(dtype, cache, page, wide):
     ctx = [0, 1, 31, 32, 33, 500, 1999, 64, 5]
     trees = [3, 19, 0, 19, 1, 7, 18, 19, 2]
-    c = Case(ctx, trees, 19, 8, 2, 64, dtype, cache, page=page, seed=3)
+    c = Case(ctx, trees, 19, 8, 2, 64, dtype, cache, page=page, seed=3, wide=wide)
     see, words = c.masks(seed=4)
     c.check(words, see)
     c.check(None, None)                                                 # a chain each
@@ -391,9 +396,10 @@ def test_tree_attention_many_short_sequences(dtype, cache):
 
 @pytest.mark.parametrize("dtype,cache", TYPES)
 @pytest.mark.parametrize("H,Hkv,hd,T,ctx", [(4, 1, 128, 64, 3000), (2, 2, 64, 150, 513), (8, 1, 32, 33, 700), (1, 1, 128, 300, 100)])
-def test_tree_attention_wide_trees(dtype, cache, H, Hkv, hd, T, ctx):
+@pytest.mark.parametrize("wide", [False, True])
+def test_tree_attention_wide_trees(dtype, cache, H, Hkv, hd, T, ctx, wide):
     """More rows than a tile, masks of several words."""
-    c = Case([ctx, ctx // 3], [T, T - 5], T, H, Hkv, hd, dtype, cache, page=64, seed=T)
+    c = Case([ctx, ctx // 3], [T, T - 5], T, H, Hkv, hd, dtype, cache, page=64, seed=T, wide=wide)
     see, words = c.masks(seed=T + 1)
     c.check(words, see)
     c.check()
@@ -407,16 +413,18 @@ def test_tree_attention_long_context(dtype, cache):
 
 
 @pytest.mark.parametrize("dtype,cache", TYPES)
-def test_tree_attention_sharp_scores(dtype, cache):
+@pytest.mark.parametrize("wide", [False, True])
+def test_tree_attention_sharp_scores(dtype, cache, wide):
     """Scores in the hundreds: the running maximum moves, and single keys carry rows."""
-    c = Case([700, 33], [20, 20], 20, 4, 2, 128, dtype, cache, seed=9, sharp=30.0)
+    c = Case([700, 33], [20, 20], 20, 4, 2, 128, dtype, cache, seed=9, sharp=30.0, wide=wide)
     see, words = c.masks(seed=9)
     c.check(words, see)
 
 
 @pytest.mark.parametrize("dtype,cache", TYPES)
-def test_tree_attention_rows_that_see_nothing(dtype, cache):
-    c = Case([0, 40], [9, 9], 9, 4, 2, 64, dtype, cache, seed=10)
+@pytest.mark.parametrize("wide", [False, True])
+def test_tree_attention_rows_that_see_nothing(dtype, cache, wide):
+    c = Case([0, 40], [9, 9], 9, 8, 2, 64, dtype, cache, seed=10, wide=wide)
     see, words = c.masks(seed=10, empty=(0, 4, 8))
     c.check(words, see)
     c = Case([-5, 0], [0, 4], 4, 4, 2, 64, dtype, cache, seed=10)       # a sequence that is not there
@@ -425,10 +433,11 @@ def test_tree_attention_rows_that_see_nothing(dtype, cache):
 
 @pytest.mark.parametrize("dtype,cache", TYPES)
 @pytest.mark.parametrize("bad", [NAN, INF, -INF])
-def test_tree_attention_masked_numbers_that_are_not_finite(dtype, cache, bad):
+@pytest.mark.parametrize("wide", [False, True])
+def test_tree_attention_masked_numbers_that_are_not_finite(dtype, cache, bad, wide):
     """One tree token's key, then another's value, is not finite: the rows that do not see it are as they were."""
     T, ctx = 21, 50
-    c = Case([ctx], [T], T, 4, 2, 64, dtype, cache, seed=11)
+    c = Case([ctx], [T], T, 4, 2, 64, dtype, cache, seed=11, wide=wide)
     see, words = c.masks(seed=11)
     clean, clean_lse = c.check(words, see)
     for j, which in ((7, "k"), (12, "v")):
@@ -452,8 +461,9 @@ def test_tree_attention_masked_numbers_that_are_not_finite(dtype, cache, bad):
     assert torch.equal(ngg.tree_attention(c.q, c.kv, c.table, ints([ctx]), mask=words), clean)
 
 
-def test_tree_attention_a_bad_number_in_the_context_reaches_every_row():
-    c = Case([100], [5], 5, 2, 2, 64, "bf16", seed=12)
+@pytest.mark.parametrize("wide,T", [(False, 5), (True, 40)])
+def test_tree_attention_a_bad_number_in_the_context_reaches_every_row(wide, T):
+    c = Case([100], [T], T, 2, 2, 64, "bf16", seed=12, wide=wide)
     k, v = c.ks[0][10:11].clone(), c.vs[0][10:11].clone()
     v[..., 0] = NAN
     c.kv.write(k, v, (c.table[0, 0] * 32 + 10)[None].int())
@@ -462,10 +472,11 @@ def test_tree_attention_a_bad_number_in_the_context_reaches_every_row():
 
 
 @pytest.mark.parametrize("dtype,cache", TYPES)
-def test_tree_attention_pages_and_lengths_out_of_range(dtype, cache):
+@pytest.mark.parametrize("H", [4, 24])
+def test_tree_attention_pages_and_lengths_out_of_range(dtype, cache, H):
     """A page outside the pool hides its positions; lengths past the page list are cut."""
     T, ctx = 3, 150
-    c = Case([ctx], [T], T, 4, 2, 64, dtype, cache, seed=13, spare=0)
+    c = Case([ctx], [T], T, H, 2, 64, dtype, cache, seed=13, spare=0)
     for wrong in (-1, c.kv.n_pages, 2 ** 31 - 1, -2 ** 31):
         table = c.table.clone()
         table[0, 2] = wrong                                             # positions 64 .. 95
@@ -474,6 +485,12 @@ def test_tree_attention_pages_and_lengths_out_of_range(dtype, cache):
         check_attention(out, lse, *attention64(c.q, [c.ks[0][keep]], [c.vs[0][keep]], [ctx - 32], [T], None, c.scale), dtype)
     out, lse = ngg.tree_attention(c.q, c.kv, torch.full_like(c.table, -1), ints([ctx]), want_lse=True)
     assert (out == 0).all() and (lse == -INF).all()
+    # the same with the kernels of long contexts
+    w = Case([ctx], [40], 40, H, 2, 64, dtype, cache, seed=21, wide=True)
+    w.table[0, 2] = -1
+    out, lse = ngg.tree_attention(w.q, w.kv, w.table, ints([ctx]), want_lse=True)
+    keep = torch.cat([torch.arange(64), torch.arange(96, ctx + 40)]).cuda()
+    check_attention(out, lse, *attention64(w.q, [w.ks[0][keep]], [w.vs[0][keep]], [ctx - 32], [40], None, w.scale), dtype)
     n = c.table.shape[1] * 32                                           # 160 places, 153 of them written
     x = randn(7, 2, 64, seed=14, dtype=dtype)
     c.kv.write(x, x, (c.table[0, -1] * 32 + torch.arange(25, 32, device="cuda")).int())
@@ -488,10 +505,11 @@ def test_tree_attention_pages_and_lengths_out_of_range(dtype, cache):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_tree_attention_strides(dtype):
+@pytest.mark.parametrize("T,wide", [(5, False), (20, True)])
+def test_tree_attention_strides(dtype, T, wide):
     """Queries and outputs as slices of something larger, at odd offsets, and a page list with a stride."""
-    B, T, H, Hkv, hd = 3, 5, 4, 2, 64
-    c = Case([40, 7, 130], [T] * 3, T, H, Hkv, hd, dtype, seed=15)
+    B, H, Hkv, hd = 3, 4, 2, 64
+    c = Case([40, 7, 130], [T] * 3, T, H, Hkv, hd, dtype, seed=15, wide=wide)
     want = c.check()[0]
     for gap in (0, 1, 2, 8):
         big = torch.zeros(T, B, H, hd + gap, dtype=DT[dtype], device="cuda")
@@ -566,8 +584,9 @@ def test_operators_on_another_stream_and_in_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
-def test_tree_attention_repeats_itself():
-    c = Case([3000, 100, 900], [40, 11, 33], 40, 8, 2, 128, "bf16", "fp8", page=64, seed=19)
+@pytest.mark.parametrize("wide", [False, True])
+def test_tree_attention_repeats_itself(wide):
+    c = Case([3000, 100, 900], [40, 11, 33], 40, 8, 2, 128, "bf16", "fp8", page=64, seed=19, wide=wide)
     see, words = c.masks(seed=19)
     a = c.check(words, see)
     for _ in range(5):
