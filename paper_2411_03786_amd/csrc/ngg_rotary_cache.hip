@@ -83,11 +83,11 @@ __global__ __launch_bounds__(256) void rotary_rows_kernel(const RotaryArgs a, in
     for (int i = 0; i < U; ++i) {
       const int hh = h0 + i * lanes;
       if (hh >= H) continue;
-      const bool second = hh >= a.rows[0].n_heads;
-      const RotaryArgs::Rows &r = a.rows[second ? 1 : 0];
-      const int h = second ? hh - a.rows[0].n_heads : hh;
-      const T *in = (const T *)r.in + t * r.in_token + h * r.in_head;
-      out[i] = (T *)r.out + t * r.out_token + h * r.out_head;
+      // (both tensors' addresses, then one of them: an index into the arguments would be a load of its own)
+      const RotaryArgs::Rows &r = a.rows[0], &q = a.rows[1];
+      const int h = hh - r.n_heads;
+      const T *in = h < 0 ? (const T *)r.in + t * r.in_token + hh * r.in_head : (const T *)q.in + t * q.in_token + h * q.in_head;
+      out[i] = h < 0 ? (T *)r.out + t * r.out_token + hh * r.out_head : (T *)q.out + t * q.out_token + h * q.out_head;
       x[i] = *reinterpret_cast<const u32x4 *>(in + e0);
       if (!INTER && turns) y[i] = *reinterpret_cast<const u32x4 *>(in + e1);
     }
@@ -214,7 +214,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(const CacheArgs a) {
       if (d >= hd) continue;
       const size_t at = kv ? page_v_offset<CT>(pos, d, hd) : page_k_offset<CT>(pos, d, hd);
       if constexpr (sizeof(CT) == 1)
-        dst[at].bits = fabsf(x[j]) < __builtin_inff() ? (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[j] * un, 0.0f, 0, false) : 0x7f;
+        dst[at].bits = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[j] * un, 0.0f, 0, false);   // what is not finite becomes NaN
       else dst[at] = from_f32<CT>(x[j]);
     }
   }
@@ -284,8 +284,8 @@ __global__ __launch_bounds__(256) void kv_write_group_kernel(const CacheArgs a, 
   __shared__ float un[2][kGroup];
   __shared__ GroupSlots g;
   const int tid = threadIdx.x, h = blockIdx.y, t0 = blockIdx.x * kGroup, m = min(kGroup, a.n_tokens - t0), hd = a.p.hd, ps = a.p.page_size;
-  load_slots(a, g, t0, m);
   const int per = hd / VE;
+#pragma unroll 4
   for (int i = tid; i < 2 * m * per; i += 256) {
     const int kv = i >= m * per, j = kv ? i - m * per : i, t = j / per, e = j % per * VE;
     const T *src = (kv ? (const T *)a.v + (t0 + t) * a.v_token + h * a.v_head : (const T *)a.k + (t0 + t) * a.k_token + h * a.k_head) + e;
@@ -294,6 +294,7 @@ __global__ __launch_bounds__(256) void kv_write_group_kernel(const CacheArgs a, 
 #pragma unroll
       for (int x = 0; x < VE; ++x) rows[kv][t][e + x] = src[x];
   }
+  load_slots(a, g, t0, m);
   __syncthreads();
   if (a.cos) {
     const int half = a.rd / 2;
@@ -331,7 +332,10 @@ __global__ __launch_bounds__(256) void kv_write_group_kernel(const CacheArgs a, 
     }
     __syncthreads();
   }
-  auto eight = [&](float v) { return fabsf(v) < __builtin_inff() ? __builtin_amdgcn_cvt_pk_fp8_f32(v, 0.0f, 0, false) & 0xff : 0x7f; };
+  // (what is not finite converts to NaN)
+  auto four = [&](const float (&v)[8], int i) {
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(v[i + 2], v[i + 3], __builtin_amdgcn_cvt_pk_fp8_f32(v[i], v[i + 1], 0, false), true);
+  };
   // keys: eight dimensions of a position lie side by side (fp32: four)
   for (int i = tid; i < kGroup * (hd / 8); i += 256) {
     const int t = i % kGroup, d = i / kGroup * 8, slot = g.slot[t];
@@ -339,10 +343,10 @@ __global__ __launch_bounds__(256) void kv_write_group_kernel(const CacheArgs a, 
     CT *dst = (CT *)a.p.k + slot_head(a, slot, h) * hd;
     const T *src = &rows[0][t][d];
     if constexpr (sizeof(CT) == 1) {
-      u32x2 w = {0, 0};
+      float v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e >> 2] |= (unsigned)eight(to_f32(src[e]) * un[0][t]) << (e & 3) * 8;
-      *reinterpret_cast<u32x2 *>(dst + page_k_offset<CT>(slot % ps, d, hd)) = w;
+      for (int e = 0; e < 8; ++e) v[e] = to_f32(src[e]) * un[0][t];
+      *reinterpret_cast<u32x2 *>(dst + page_k_offset<CT>(slot % ps, d, hd)) = u32x2{four(v, 0), four(v, 4)};
     } else {
       *reinterpret_cast<u32x4 *>(dst + page_k_offset<CT>(slot % ps, d, hd)) = *reinterpret_cast<const u32x4 *>(src);
       if constexpr (sizeof(CT) == 4)
@@ -351,27 +355,45 @@ __global__ __launch_bounds__(256) void kv_write_group_kernel(const CacheArgs a, 
   }
   // values: eight positions of a dimension do
   auto value = [&](int t, int d) -> CT {
-    if constexpr (sizeof(CT) == 1) return {(uint8_t)eight(to_f32(rows[1][t][d]) * un[1][t])};
+    if constexpr (sizeof(CT) == 1) return {(uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(to_f32(rows[1][t][d]) * un[1][t], 0.0f, 0, false)};
     else return rows[1][t][d];
   };
   if (g.run) {
     const int s0 = g.slot[0], lead = s0 % 8, groups = (lead + m + 7) / 8;
-    for (int i = tid; i < groups * hd; i += 256) {
-      const int q = i / hd, d = i % hd, first = q * 8 - lead;
+    // a thread takes two neighbouring dimensions
+    for (int i = tid; i < groups * hd / 2; i += 256) {
+      const int q = i / (hd / 2), d = i % (hd / 2) * 2, first = q * 8 - lead;
       const int from = max(first, 0), to = min(first + 8, m), slot = s0 + from;
       CT *dst = (CT *)a.p.v + slot_head(a, slot, h) * hd;
-      if (to - from == 8) {
-        CT x[8];
+      const int pos = slot % ps;
+      if (to - from < 8) {
+        for (int t = from; t < to; ++t)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = value(first + e, d);
-        if constexpr (sizeof(CT) == 1) *reinterpret_cast<u32x2 *>(dst + page_v_offset<CT>(slot % ps, d, hd)) = __builtin_bit_cast(u32x2, x);
-        else if constexpr (sizeof(CT) == 2) *reinterpret_cast<u32x4 *>(dst + page_v_offset<CT>(slot % ps, d, hd)) = __builtin_bit_cast(u32x4, x);
+          for (int x = 0; x < 2; ++x) dst[page_v_offset<CT>(pos + t - from, d + x, hd)] = value(t, d + x);
+        continue;
+      }
+      T v[2][8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        struct alignas(2 * sizeof(T)) Two { T x[2]; };
+        const Two w = *reinterpret_cast<const Two *>(&rows[1][first + e][d]);
+        v[0][e] = w.x[0];
+        v[1][e] = w.x[1];
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        CT *to8 = dst + page_v_offset<CT>(pos, d + x, hd);
+        if constexpr (sizeof(CT) == 1) {
+          float y[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = to_f32(v[x][e]) * un[1][first + e];
+          *reinterpret_cast<u32x2 *>(to8) = u32x2{four(y, 0), four(y, 4)};
+        } else if constexpr (sizeof(CT) == 2) *reinterpret_cast<u32x4 *>(to8) = __builtin_bit_cast(u32x4, v[x]);
         else {
-          *reinterpret_cast<f32x4 *>(dst + page_v_offset<CT>(slot % ps, d, hd)) = f32x4{x[0], x[1], x[2], x[3]};
-          *reinterpret_cast<f32x4 *>(dst + page_v_offset<CT>(slot % ps + 4, d, hd)) = f32x4{x[4], x[5], x[6], x[7]};
+          *reinterpret_cast<f32x4 *>(to8) = f32x4{v[x][0], v[x][1], v[x][2], v[x][3]};
+          *reinterpret_cast<f32x4 *>(dst + page_v_offset<CT>(pos + 4, d + x, hd)) = f32x4{v[x][4], v[x][5], v[x][6], v[x][7]};
         }
-      } else
-        for (int t = from; t < to; ++t) dst[page_v_offset<CT>(slot % ps + t - from, d, hd)] = value(t, d);
+      }
     }
   } else
     for (int i = tid; i < m * hd; i += 256) {
@@ -456,8 +478,10 @@ __global__ __launch_bounds__(256) void kv_read_group_kernel(const CacheArgs a, i
   }
 }
 
-// Calls of few tokens have a wave for each (token, head), whose chain of loads is the shorter one: 32 tokens of 8 heads took WWW.
-constexpr int kFewTokens = 64;
+// Calls of few rows have a wave for each (token, head), whose chain of loads is the shorter one: 256 rows of 128 written to a 16-bit
+// cache 3.4 us against 5.2, 7800 to an 8-bit one 8.5 against 7.5.
+constexpr int kFewRows = 4096;
+static bool few_rows(const CacheArgs &a) { return (int64_t)a.n_tokens * a.p.Hkv <= kFewRows; }
 template <typename T>
 static bool rows_of_vectors(const CacheArgs &a, const void *k, const void *v) {
   constexpr int VE = Vec16<T>::n;
@@ -474,14 +498,14 @@ static void by_types(int dtype, int cache, const CacheArgs &a, hipStream_t s) {
 }
 template <typename T, typename CT> struct WriteLaunch {
   static void go(const CacheArgs &a, hipStream_t s) {
-    if (a.n_tokens > kFewTokens)
+    if (!few_rows(a))
       hipLaunchKernelGGL((kv_write_group_kernel<T, CT>), dim3((a.n_tokens + kGroup - 1) / kGroup, a.p.Hkv), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k, a.v));
     else hipLaunchKernelGGL((kv_write_kernel<T, CT>), dim3((a.n_tokens * a.p.Hkv + 3) / 4), dim3(256), 0, s, a);
   }
 };
 template <typename T, typename CT> struct ReadLaunch {
   static void go(const CacheArgs &a, hipStream_t s) {
-    if (a.n_tokens > kFewTokens)
+    if (!few_rows(a))
       hipLaunchKernelGGL((kv_read_group_kernel<T, CT>), dim3((a.n_tokens + kGroup - 1) / kGroup, a.p.Hkv), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k_out, a.v_out));
     else hipLaunchKernelGGL((kv_read_kernel<T, CT>), dim3((a.n_tokens * a.p.Hkv + 3) / 4), dim3(256), 0, s, a);
   }

@@ -121,13 +121,10 @@ def eight_bits(x):
     x = x.double().cpu().numpy()
     fin = np.where(np.isfinite(x), x, 0.0)
     top = np.abs(fin).max(-1, keepdims=True)
-    e = np.zeros_like(top)
-    for idx in np.ndindex(top.shape):
-        if top[idx] > 0:
-            k = -126
-            while 448.0 * 2.0 ** k < top[idx]:
-                k += 1
-            e[idx] = k
+    e = np.full_like(top, -126.0)
+    for k in range(-126, 120):
+        e = np.where(448.0 * 2.0 ** k < top, k + 1.0, e)
+    e = np.where(top > 0, e, 0.0)
     y = np.abs(fin) / 2.0 ** e
     hi = np.clip(np.searchsorted(grid, y), 0, len(grid) - 1)
     lo = np.maximum(hi - 1, 0)
@@ -137,7 +134,7 @@ def eight_bits(x):
 
 
 @pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("bf16", "bf16"), ("f32", "fp8"), ("bf16", "fp8")])
-@pytest.mark.parametrize("hd,Hkv,page", [(32, 4, 32), (64, 3, 96), (128, 8, 64)])
+@pytest.mark.parametrize("hd,Hkv,page", [(32, 4, 32), (64, 3, 96), (128, 8, 64), (64, 90, 32), (32, 200, 64), (128, 200, 32)])
 @pytest.mark.parametrize("n,order", [(1, "run"), (5, "run"), (32, "run"), (61, "run"), (200, "run"), (97, "shuffled"), (130, "halves")])
 def test_cache_holds_what_was_written(dtype, cache, hd, Hkv, page, n, order):
     pool = 300 // page + 3
@@ -187,20 +184,26 @@ def test_eight_bit_corners():
     rows[9, 0] = torch.linspace(1e-38, 3e-36, hd)
     rows[10, 0, :5] = torch.tensor([448.0, 2.0 ** -9, 2.0 ** -10, 3 * 2.0 ** -10, 5 * 2.0 ** -10])
     rows[11, 0] = torch.linspace(-1, 1, hd)
-    x = rows.cuda()
-    kv = ngg.KVPages(2, 32, 1, hd, "fp8")
-    slots = ints(range(20, 32))
-    kv.write(x, x.flip(0).contiguous(), slots)
-    k, v = kv.read(slots, torch.float32)
+    for heads in (1, 400):
+        x = rows.expand(-1, heads, -1).contiguous().cuda()
+        kv = ngg.KVPages(2, 32, heads, hd, "fp8")
+        slots = ints(range(20, 32))
+        kv.write(x, x.flip(0).contiguous(), slots)
+        k, v = (t[:, -1:] for t in kv.read(slots, torch.float32))
+        check_corners(rows.cuda(), k, v)
+
+
+def check_corners(x, k, v):
     want = eight_bits(x).float()
     assert torch.equal(torch.nan_to_num(k, nan=-77.0), torch.nan_to_num(want, nan=-77.0))
     assert torch.equal(torch.nan_to_num(v, nan=-77.0), torch.nan_to_num(want.flip(0), nan=-77.0))
 
 
 @pytest.mark.parametrize("cache", ["bf16", "fp8"])
-def test_cache_slots_out_of_range(cache):
-    kv = ngg.KVPages(2, 32, 2, 64, cache)
-    x = randn(6, 2, 64, seed=1, dtype="bf16")
+@pytest.mark.parametrize("H", [2, 2100])
+def test_cache_slots_out_of_range(cache, H):
+    kv = ngg.KVPages(2, 32, H, 64, cache)
+    x = randn(6, H, 64, seed=1, dtype="bf16")
     kv.write(x[:2], x[2:4], ints([5, 6]))
     before = [t.clone() for t in (kv.k_bytes, kv.v_bytes)]
     kv.write(x[:4], x[2:6], ints([-1, 64, 2 ** 31 - 1, -2 ** 31]))
@@ -214,13 +217,13 @@ def test_cache_slots_out_of_range(cache):
     want = torch.cat([x[:3], x[3:]])
     assert torch.equal(k2, want if cache == "bf16" else eight_bits(want).bfloat16())
     kv.write(x[:0], x[:0], ints([]))
-    assert kv.read(ints([]))[0].shape == (0, 2, 64)
+    assert kv.read(ints([]))[0].shape == (0, H, 64)
 
 
 @pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("bf16", "bf16"), ("f32", "fp8"), ("bf16", "fp8")])
 @pytest.mark.parametrize("hd,rd,inter", [(32, 32, False), (64, 32, True), (128, 128, True), (128, 128, False), (128, 34, False), (64, 6, True)])
-def test_cache_rotates_as_rotary_does(dtype, cache, hd, rd, inter):
-    Hkv, n = 3, 75
+@pytest.mark.parametrize("Hkv,n", [(3, 75), (60, 75)])
+def test_cache_rotates_as_rotary_does(dtype, cache, hd, rd, inter, Hkv, n):
     rope, pos = ngg.Rope(rd, 300, interleaved=inter), ints(np.random.default_rng(2).integers(0, 300, n))
     x = randn(n, 2 * Hkv * hd + 2, seed=hd, dtype=dtype)
     k, v = x[:, :Hkv * hd].view(n, Hkv, hd), x[:, Hkv * hd:2 * Hkv * hd].view(n, Hkv, hd)
