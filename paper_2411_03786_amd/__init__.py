@@ -14,6 +14,7 @@ import numpy as np
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "csrc", "libngg.so")
+BINDING_PATH = os.path.join(_HERE, "csrc", "ngg_torch.so")
 
 NGG_OK, NGG_EINVAL, NGG_ECAPACITY, NGG_ESTATE, NGG_EHIP, NGG_ENOMEM = 0, -1, -2, -3, -4, -5
 NGG_F32, NGG_BF16, NGG_FP8 = 0, 1, 2
@@ -152,6 +153,28 @@ def load_library():
             getattr(lib, name).restype = C.c_int32
     _lib = lib
     return lib
+
+
+_binding = None
+
+
+def load_binding():
+    """Loads csrc/ngg_torch.so, the operators' binding to torch tensors (it imports torch).  Raises if it was not built."""
+    global _binding
+    if _binding is None:
+        import importlib.machinery
+        import importlib.util
+
+        import torch  # noqa: F401  (the binding's symbols)
+        load_library()
+        if not os.path.exists(BINDING_PATH):
+            raise RuntimeError(f"{BINDING_PATH} is missing: run `python __graft_entry__.py` first; there is no fallback path")
+        loader = importlib.machinery.ExtensionFileLoader("ngg_torch", BINDING_PATH)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("ngg_torch", loader))
+        loader.exec_module(module)
+        module.set_error(NggError)
+        _binding = module
+    return _binding
 
 
 class NggError(RuntimeError):
