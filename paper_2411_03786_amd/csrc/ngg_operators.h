@@ -109,7 +109,7 @@ struct TreeArgs {
   int ranges, Z;              // workgroups along the list of key steps, row tiles
   int whole;                  // a workgroup for every (sequence, head) instead: no parts, no merge
 };
-struct TreePlan { int rows, ranges, Z; bool whole; size_t o_bytes, ml_bytes; };
+struct TreePlan { int rows, ranges, Z; bool whole, stream; size_t o_bytes, ml_bytes; };
 TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, int64_t max_positions);
 void launch_tree_attention(int dtype, int cache, const TreeArgs &a, const TreePlan &p, hipStream_t s);
 

@@ -16,11 +16,6 @@ namespace ngg {
 
 constexpr float kLn2 = 0.6931471805599453f;
 
-__device__ __forceinline__ Frag<bf16_t> load_frag_tiled(const bf16_t *p) {
-  Frag<bf16_t> f;
-  f.v = *reinterpret_cast<const bf16x8 *>(p);
-  return f;
-}
 template <> __device__ __forceinline__ Frag<bf16_t> zero_frag<bf16_t>() {
   Frag<bf16_t> f;
 #pragma unroll
@@ -30,6 +25,13 @@ template <> __device__ __forceinline__ Frag<bf16_t> zero_frag<bf16_t>() {
 __device__ __forceinline__ void pack_frag(Frag<bf16_t> &f, const float *p) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) f.v[e] = (bf16_t)p[e];
+}
+
+// A fragment from the 16-byte parts of a tile as they lie in memory.
+__device__ __forceinline__ void raw_frag(Frag<bf16_t> &f, const u32x4 *r) { f.v = __builtin_bit_cast(bf16x8, r[0]); }
+__device__ __forceinline__ void raw_frag(Frag<float> &f, const u32x4 *r) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f.v[e] = __uint_as_float(r[e >> 2][e & 3]);
 }
 
 // Eight 8-bit elements times a power of two as a fragment of either type; exact in both.
@@ -197,7 +199,11 @@ __device__ __forceinline__ bool only_there(Frag<T> &f, int pos, int n) {
 }
 
 // Elements of a query row, 16-byte aligned.
-__device__ __forceinline__ Frag<bf16_t> load_frag_row(const bf16_t *p) { return load_frag_tiled(p); }
+__device__ __forceinline__ Frag<bf16_t> load_frag_row(const bf16_t *p) {
+  Frag<bf16_t> f;
+  f.v = *reinterpret_cast<const bf16x8 *>(p);
+  return f;
+}
 __device__ __forceinline__ Frag<float> load_frag_row(const float *p) { return load_frag(p); }
 
 __device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? -__builtin_inff() : kLn2 * (m + __builtin_log2f(l)); }
@@ -218,7 +224,8 @@ __device__ __forceinline__ void write_row4(const TreeArgs &a, int b, int t, int 
 
 // One workgroup: one row tile (16 QF rows) over its share of the list.  The waves take the tiles of 32 keys of a (sequence, head) in
 // turn, each straight from memory, and are joined through LDS at its end.
-template <typename T, typename CT, int HD, int QF>
+// NT: keys that nobody reads again stay out of the caches.
+template <typename T, typename CT, int HD, int QF, bool NT>
 __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
   constexpr int NW = 4, DS = HD / 32, DF = HD / 16, TILE = 32 * HD, ROWS = 16 * QF, KS = 32 * NW;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -274,29 +281,34 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
       const CT *kt = (const CT *)a.p.k + (head * a.p.page_size + off) * HD, *vt = (const CT *)a.p.v + (head * a.p.page_size + off) * HD;
       Frag<T> K[2][DS], V[DF];
       float vs[8];
+      constexpr int NR = HD * (int)sizeof(CT) / 32;        // 1 KB parts of a tile
+      u32x4 kr[NR], vr[NR];
+      const uint8_t *kp = (const uint8_t *)kt + lane * 16, *vp = (const uint8_t *)vt + lane * 16;
+      auto part = [](const uint8_t *from) {
+        if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from));
+        else return *reinterpret_cast<const u32x4 *>(from);
+      };
+#pragma unroll
+      for (int r = 0; r < NR; ++r) kr[r] = part(kp + r * 1024);
+#pragma unroll
+      for (int r = 0; r < NR; ++r) vr[r] = part(vp + r * 1024);
       if constexpr (sizeof(CT) == 1) {
         const u32x2 ke = *reinterpret_cast<const u32x2 *>(a.p.k_exp + head * a.p.page_size + off + (c >> 2) * 8);
+        const u32x2 ve = *reinterpret_cast<const u32x2 *>(a.p.v_exp + head * a.p.page_size + off + g4 * 8);
         const float k0 = exp_scale(ke[0] >> (c & 3) * 8 & 0xff), k1 = exp_scale(ke[1] >> (c & 3) * 8 & 0xff);
 #pragma unroll
-        for (int d = 0; d < DS; ++d) {
-          const u32x4 x = *reinterpret_cast<const u32x4 *>((const uint8_t *)kt + d * 1024 + lane * 16);
-          widen(K[0][d], x[0], x[1], k0); widen(K[1][d], x[2], x[3], k1);
-        }
+        for (int d = 0; d < DS; ++d) { widen(K[0][d], kr[d][0], kr[d][1], k0); widen(K[1][d], kr[d][2], kr[d][3], k1); }
 #pragma unroll
-        for (int d = 0; d < DF; d += 2) {
-          const u32x4 x = *reinterpret_cast<const u32x4 *>((const uint8_t *)vt + d * 512 + lane * 16);
-          widen(V[d], x[0], x[1], 1.0f); widen(V[d + 1], x[2], x[3], 1.0f);
-        }
-        const u32x2 ve = *reinterpret_cast<const u32x2 *>(a.p.v_exp + head * a.p.page_size + off + g4 * 8);
+        for (int d = 0; d < DF; d += 2) { widen(V[d], vr[d / 2][0], vr[d / 2][1], 1.0f); widen(V[d + 1], vr[d / 2][2], vr[d / 2][3], 1.0f); }
 #pragma unroll
         for (int e = 0; e < 8; ++e) vs[e] = exp_scale(ve[e >> 2] >> (e & 3) * 8 & 0xff);
       } else {
 #pragma unroll
         for (int f = 0; f < 2; ++f)
 #pragma unroll
-          for (int d = 0; d < DS; ++d) K[f][d] = load_frag_tiled(kt + (f * DS + d) * 512 + lane * (sizeof(CT) == 2 ? 8 : 4));
+          for (int d = 0; d < DS; ++d) raw_frag(K[f][d], &kr[(f * DS + d) * (sizeof(CT) / 2)]);
 #pragma unroll
-        for (int d = 0; d < DF; ++d) V[d] = load_frag_tiled(vt + d * 512 + lane * (sizeof(CT) == 2 ? 8 : 4));
+        for (int d = 0; d < DF; ++d) raw_frag(V[d], &vr[d * (sizeof(CT) / 2)]);
       }
       const bool full = pos0 + 32 <= len.ctx;              // (uniform) every row sees every key
       bool poison = false;
@@ -809,13 +821,21 @@ static int tile_rows(int dtype, int rows, int64_t positions) {
 }
 static int step_keys(int rows) { return rows <= 32 ? 128 : 64; }
 
+// Short lists go whole to a workgroup each: no parts, no merge.  Measured (us, whole and shared): 32 heads, 51 rows, 800 positions
+// 13.5 and 17.9, 1300 positions 17.5 and 20.0, 1900 positions 22.8 and 18.8; 256 heads of one row, 1900 positions 41.5 and 46.9.
+static bool whole_lists(int64_t steps, int64_t workgroups) { return steps <= 8 || (steps <= 12 && workgroups >= 128) || (steps <= 16 && workgroups >= 256); }
+
 TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, int64_t max_positions) {
-  (void)cache;
   TreePlan p;
-  p.rows = tile_rows(dtype, T * G, max_positions * B * Hkv);
+  const int64_t positions = max_positions * B * Hkv;
+  p.rows = tile_rows(dtype, T * G, positions);
   p.Z = (T * G + p.rows - 1) / p.rows;
   const int64_t steps = (max_positions + step_keys(p.rows) - 1) / step_keys(p.rows);
-  p.whole = steps <= 4;
+  p.whole = p.rows <= 32 && whole_lists(steps, (int64_t)B * Hkv * p.Z);
+  // A single tile of 16 rows reads the keys once.  Past what the last cache holds, non-temporal loads: 32 single tokens over 16000 positions 332 us
+  // instead of 372; below, a list that is read again soon is better kept (1900 positions 46.9, non-temporal 49.7).
+  const int64_t bytes = 2 * positions * hd * (cache == NGG_F32 ? 4 : cache == NGG_BF16 ? 2 : 1);
+  p.stream = p.rows == 16 && p.Z == 1 && bytes > (int64_t)400 << 20;
   const int64_t want = (512 + p.Z - 1) / p.Z, r = p.whole ? (int64_t)B * Hkv : std::max<int64_t>(1, std::min(want, steps * B * Hkv));
   p.ranges = (int)(p.whole ? r : r >= 8 ? r / 8 * 8 : r);
   const size_t rows = p.whole ? 0 : (size_t)p.ranges * p.Z * 2 * p.rows;
@@ -834,12 +854,12 @@ static void merge(const TreeArgs &a, hipStream_t s) {
   const int rows = std::min(ROWS, a.T * a.G);
   hipLaunchKernelGGL((tree_merge_kernel<T, HD, ROWS, KS>), dim3(a.B * a.p.Hkv, a.Z, (rows * HD / 4 + 255) / 256), dim3(256), 0, s, a);
 }
-template <typename T, typename CT, int HD, int QF>
+template <typename T, typename CT, int HD, int QF, bool NT>
 static void launch_stream(const TreeArgs &a, hipStream_t s) {
   constexpr size_t lds = (size_t)4 * QF * (HD / 16 * 256 + 32) * 4;
-  static const bool once = (allow_lds(&tree_stream_kernel<T, CT, HD, QF>, lds + (NGG_TREE_MAX + 1) * 4), true);
+  static const bool once = (allow_lds(&tree_stream_kernel<T, CT, HD, QF, NT>, lds + (NGG_TREE_MAX + 1) * 4), true);
   (void)once;
-  hipLaunchKernelGGL((tree_stream_kernel<T, CT, HD, QF>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
+  hipLaunchKernelGGL((tree_stream_kernel<T, CT, HD, QF, NT>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
   merge<T, HD, 16 * QF, 128>(a, s);
 }
 template <typename CT, int HD, int NW>
@@ -851,25 +871,26 @@ static void launch_block(const TreeArgs &a, hipStream_t s) {
   merge<bf16_t, HD, 32 * NW, 64>(a, s);
 }
 template <typename T, typename CT, int HD>
-static void by_rows(const TreeArgs &a, int rows, hipStream_t s) {
-  if (rows == 16) launch_stream<T, CT, HD, 1>(a, s);
-  else if (rows == 32) launch_stream<T, CT, HD, 2>(a, s);
+static void by_rows(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
+  if (p.rows == 16 && p.stream) launch_stream<T, CT, HD, 1, true>(a, s);
+  else if (p.rows == 16) launch_stream<T, CT, HD, 1, false>(a, s);
+  else if (p.rows == 32) launch_stream<T, CT, HD, 2, false>(a, s);
   else if constexpr (sizeof(T) == 2) {
     launch_block<CT, HD, 4>(a, s);
   }
 }
 template <typename T, typename CT>
-static void by_head(const TreeArgs &a, int rows, hipStream_t s) {
-  if (a.p.hd == 32) by_rows<T, CT, 32>(a, rows, s);
-  else if (a.p.hd == 64) by_rows<T, CT, 64>(a, rows, s);
-  else by_rows<T, CT, 128>(a, rows, s);
+static void by_head(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
+  if (a.p.hd == 32) by_rows<T, CT, 32>(a, p, s);
+  else if (a.p.hd == 64) by_rows<T, CT, 64>(a, p, s);
+  else by_rows<T, CT, 128>(a, p, s);
 }
 
 void launch_tree_attention(int dtype, int cache, const TreeArgs &a, const TreePlan &p, hipStream_t s) {
-  if (dtype == NGG_F32 && cache == NGG_F32) by_head<float, float>(a, p.rows, s);
-  else if (dtype == NGG_F32) by_head<float, fp8_t>(a, p.rows, s);
-  else if (cache == NGG_BF16) by_head<bf16_t, bf16_t>(a, p.rows, s);
-  else by_head<bf16_t, fp8_t>(a, p.rows, s);
+  if (dtype == NGG_F32 && cache == NGG_F32) by_head<float, float>(a, p, s);
+  else if (dtype == NGG_F32) by_head<float, fp8_t>(a, p, s);
+  else if (cache == NGG_BF16) by_head<bf16_t, bf16_t>(a, p, s);
+  else by_head<bf16_t, fp8_t>(a, p, s);
 }
 
 }  // namespace ngg
