@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256) void rotary_rows_kernel(const RotaryArgs a, in
   const int H = a.rows[0].n_heads + a.rows[1].n_heads;
   float cs[NA], sn[NA];
   bool have = false;
-  for (int h0 = in_t / chunks + blockIdx.y * lanes * U; h0 < H; h0 += lanes * U * gridDim.y) {
+  for (int h0 = in_t / chunks; h0 < H; h0 += lanes * U) {
     u32x4 x[U], y[U];
     T *out[U];
 #pragma unroll
@@ -140,21 +140,24 @@ static void launch_rotary_type(const RotaryArgs &a, hipStream_t s) {
     rows = rows && (r.n_heads == 0 || (aligned16(r.in) && aligned16(r.out) && r.in_token % VE == 0 && r.in_head % VE == 0 &&
                                        r.out_token % VE == 0 && r.out_head % VE == 0));
   const int chunks = a.interleaved ? a.hd / VE : a.rd / (2 * VE) + (a.hd - a.rd) / VE;
-  if (rows && chunks <= 256) {
-    // a wave or so for a token, whose lanes take several heads each; calls of few tokens (51: 3.4 us by elements, 2.9 so) spread the heads
-    const int H = a.rows[0].n_heads + a.rows[1].n_heads;
+  const int H = a.rows[0].n_heads + a.rows[1].n_heads;
+  // Calls of little work go by elements, whose code is shorter to start (64 heads of 128, us, by elements and by vectors: 1 token 2.9
+  // and 5.0, 51 tokens 3.5 and 6.4, 128 tokens 4.6 and 6.4, 512 tokens 10.3 and 7.2).
+  const int64_t work = (int64_t)a.n_tokens * H * (a.hd - a.rd / 2);
+  if (rows && chunks <= 256 && work > 1 << 20 && a.n_tokens < 1 << 23) {
+    // a wave or so for a token, whose lanes take several heads each
     int lanes = 1;
-    while (lanes * 2 * chunks <= (a.n_tokens < 1024 ? 256 : 64) && lanes < H) lanes *= 2;
+    while (lanes * 2 * chunks <= 64 && lanes < H) lanes *= 2;
     const int tokens = 256 / (chunks * lanes);
-    const int spread = a.n_tokens < 1024 ? (H + 4 * lanes - 1) / (4 * lanes) : 1;
-    const dim3 grid((a.n_tokens + tokens - 1) / tokens, spread);
+    const dim3 grid((a.n_tokens + tokens - 1) / tokens);
     if (a.interleaved) hipLaunchKernelGGL((rotary_rows_kernel<T, true>), grid, dim3(256), 0, s, a, chunks, lanes);
     else hipLaunchKernelGGL((rotary_rows_kernel<T, false>), grid, dim3(256), 0, s, a, chunks, lanes);
     return;
   }
   const int heads = a.rows[0].n_heads > a.rows[1].n_heads ? a.rows[0].n_heads : a.rows[1].n_heads;
   const int64_t total = (int64_t)a.n_tokens * heads * (a.hd - a.rd / 2), blocks = (total + 255) / 256;
-  hipLaunchKernelGGL(rotary_kernel<T>, dim3((unsigned)(blocks < 8192 ? blocks : 8192), a.rows[1].n_heads ? 2 : 1), dim3(256), 0, s, a);
+  const dim3 grid((unsigned)(blocks < 8192 ? blocks : 8192), a.rows[1].n_heads ? 2 : 1);
+  hipLaunchKernelGGL(rotary_kernel<T>, grid, dim3(256), 0, s, a);
 }
 
 void launch_rotary(int dtype, const RotaryArgs &a, hipStream_t s) {

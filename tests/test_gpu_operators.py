@@ -70,6 +70,30 @@ def test_rotary_of_strided_rows(dtype, n, H, Hkv, hd, rd, inter):
     assert (apart[..., hd:] == 7.0).all() and torch.equal(x[:, (H + Hkv) * hd:], before[:, (H + Hkv) * hd:])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,H,Hkv,hd,rd,inter,pad", [(700, 32, 8, 128, 128, False, 8), (1025, 32, 8, 64, 64, True, 0), (900, 24, 8, 128, 64, False, 16),
+                                                     (901, 40, 8, 96, 32, True, 8), (3000, 7, 1, 80, 48, False, 8), (2050, 9, 0, 256, 128, True, 0),
+                                                     (4100, 3, 2, 112, 112, False, 24), (140, 100, 3, 192, 16, False, 8)])
+def test_rotary_of_many_aligned_rows(dtype, n, H, Hkv, hd, rd, inter, pad):
+    x = randn(n, (H + Hkv) * hd + pad, seed=n, dtype=dtype)
+    q, k = x[:, :H * hd].view(n, H, hd), x[:, H * hd:(H + Hkv) * hd].view(n, Hkv, hd)
+    rope = ngg.Rope(rd, 900, interleaved=inter)
+    pos = torch.randint(0, 900, (n,), dtype=torch.int32, generator=torch.Generator().manual_seed(n)).cuda()
+    pos[n // 2] = 900                                                   # behind the table: NaN
+    live = torch.arange(n, device="cuda") != n // 2
+    for inverse in (False, True):
+        got = ngg.rotary(rope, pos, q, k, inverse=inverse) if Hkv else (ngg.rotary(rope, pos, q, inverse=inverse),)
+        for g, t in zip(got, (q, k)):
+            want, slack = rotate64(t[live], pos[live], rope, inverse)
+            assert ((g[live].double() - want).abs() <= slack + want.abs() * ROUND[dtype] * 1.01).all()
+            assert torch.equal(g[..., rd:], t[..., rd:]) and torch.isnan(g[n // 2, :, :rd]).all()
+        few = ngg.rotary(rope, pos[5:8], q[5:8], inverse=inverse)
+        assert torch.equal(few, got[0][5:8])                            # a few rows as many
+    want = got[0]
+    ngg.rotary(rope, pos, q, inverse=True, out=q)
+    assert torch.equal(q[live], want[live])
+
+
 def test_rotary_inverse_is_the_gradient():
     """d/dx <w, R x> = R^T w, by differences in 64 bits of the fp32 kernel's own results (which are linear in x)."""
     n, H, hd = 4, 2, 16
@@ -411,6 +435,18 @@ def test_tree_attention_wide_trees(dtype, cache, H, Hkv, hd, T, ctx, wide):
 @pytest.mark.parametrize("dtype,cache", TYPES)
 def test_tree_attention_long_context(dtype, cache):
     c = Case([40000, 9, 17001], [6, 6, 6], 6, 4, 1, 64, dtype, cache, page=256, seed=8)
+    see, words = c.masks(seed=8)
+    c.check(words, see)
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("H,Hkv,hd,T", [(4, 2, 128, 1), (8, 1, 64, 2), (3, 3, 32, 13), (16, 1, 128, 1)])
+def test_tree_attention_page_lists_beyond_the_caches(dtype, cache, H, Hkv, hd, T):
+    """Few rows and page lists of more keys than any cache holds."""
+    ctx = [0, 1000, 63]
+    c = Case(ctx, [T] * 3, T, H, Hkv, hd, dtype, cache, seed=hd + T)
+    room = (1 << 29) // (2 * hd * Hkv * 3)                              # positions, one byte an element
+    c.table = torch.cat([c.table, torch.full((3, room // 32), -1, dtype=torch.int32, device="cuda")], 1)
     see, words = c.masks(seed=8)
     c.check(words, see)
 
