@@ -252,182 +252,303 @@ __global__ __launch_bounds__(256) void kv_read_kernel(const CacheArgs a) {
   }
 }
 
-// Runs of tokens.  One workgroup per (32 tokens, head): the rows pass through LDS, so that they are read and written whole, and eight
-// positions of a value's dimension lie in one store where the tokens' slots follow each other (a prompt, a tree); others go
-// element by element.  HBM bound.
+// Runs of tokens.  One workgroup per (32 tokens, head, keys or values): the rows pass through LDS, so that they are read and written
+// whole, and eight positions of a value's dimension lie in one store where the tokens' slots follow each other (a prompt, a tree);
+// others go element by element.  HBM bound: 16000 tokens of 8 heads of 128 are written in 22 us and read in 21 at 16 bits (6 TB/s,
+// reading and writing), in 27 and 21 at 8 bits (3.7 and 4.7 TB/s; there the conversion is what is left).
 constexpr int kGroup = 32, kRowPad = 16;                   // tokens of a workgroup; bytes behind a row in LDS (banks)
 
+// A workgroup's tokens t0 .. t0 + m - 1 (none: false).  Groups begin where eights of positions do if all slots follow each other, so
+// that no chunk (below) lies in two of them: 16000 tokens of 8 heads from position 37, 16 bits, are written in 22 us, from groups
+// that begin at token 0 in 30.
+__device__ __forceinline__ bool group_tokens(const CacheArgs &a, int &t0, int &m) {
+  const int64_t begin = (int64_t)blockIdx.x * kGroup - (a.slots[0] & 7);
+  t0 = (int)max(begin, (int64_t)0);
+  m = (int)(min(begin + kGroup, (int64_t)a.n_tokens) - t0);
+  return m > 0;
+}
+
+// The slots of a workgroup's tokens, in every wave by itself, and their chunks: tokens whose slots follow each other inside eight
+// positions, which lie in one place of a value's dimension.
 struct GroupSlots {
-  int slot[kGroup];                                        // -1: not there
-  int run;                                                 // the slots follow each other
-};
-__device__ __forceinline__ void load_slots(const CacheArgs &a, GroupSlots &g, int t0, int m) {
-  const int tid = threadIdx.x;
-  if (tid < 64) {
-    int s = -1;
-    if (tid < m) {
-      s = a.slots[t0 + tid];
-      if (s < 0 || s / a.p.page_size >= a.p.n_pages) s = -1;
+  int slot;                                                // of token lane % 32; -1: not there
+  int chunk;                                               // of chunk lane % 32: its first token
+  int chunks;
+  __device__ __forceinline__ GroupSlots(const CacheArgs &a, int t0, int m) {
+    const int lane = threadIdx.x & 63, t = lane % kGroup;
+    slot = -1;
+    if (t < m) {
+      slot = a.slots[t0 + t];
+      if (slot < 0 || slot / a.p.page_size >= a.p.n_pages) slot = -1;
     }
-    if (tid < kGroup) g.slot[tid] = s;
-    const int first = __builtin_amdgcn_readfirstlane(s);
-    const bool ok = tid >= m || (first >= 0 && s == first + tid);
-    const bool run = __ballot(ok) == ~0ull;
-    if (tid == 0) g.run = run;
+    const int before = __shfl_up(slot, 1);
+    const bool leads = lane < m && (t == 0 || slot < 0 || slot % 8 == 0 || before < 0 || slot != before + 1);
+    const unsigned mask = (unsigned)__ballot(leads);
+    chunks = __builtin_popcount(mask);
+    // (every other lane sends to one that nobody reads)
+    chunk = __builtin_amdgcn_ds_permute((leads ? __builtin_popcount(mask & ((1u << t) - 1)) : 63) * 4, t);
+    chunk = lane < chunks ? chunk : m;
   }
+};
+// Chunk q's tokens first .. last - 1 and the slot of the first; all lanes take part.
+struct Chunk { int first, last, slot; };
+__device__ __forceinline__ Chunk chunk_at(const GroupSlots &g, int q) {
+  Chunk c;
+  c.first = __shfl(g.chunk, min(q, 62));
+  c.last = __shfl(g.chunk, min(q + 1, 62));
+  c.slot = __shfl(g.slot, c.first);
+  return c;
 }
 __device__ __forceinline__ size_t slot_head(const CacheArgs &a, int slot, int h) {   // first position of the slot's (page, head)
   return ((size_t)(slot / a.p.page_size) * a.p.Hkv + h) * a.p.page_size;
 }
 
+// Eight positions of value dimensions d and d + 1 (y[0], y[1]) to and from the cache, d even, by the lanes of a group of 16 that hold
+// dimensions 32 i + 2 (lane % 16) at the same positions: they trade one of the two, so that the lanes of a load or store follow each
+// other in memory.  tile: position 0 of the page and head.
+__device__ __forceinline__ u32x4 from_lane_xor1(const u32x4 &v) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = (unsigned)__builtin_amdgcn_mov_dpp((int)v[i], 0xb1, 0xf, 0xf, true);      // quad_perm 1 0 3 2
+  return r;
+}
+__device__ __forceinline__ u32x2 from_lane_xor8(const u32x2 &v) {
+  u32x2 r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) r[i] = (unsigned)__builtin_amdgcn_mov_dpp((int)v[i], 0x128, 0xf, 0xf, true);     // row_ror 8
+  return r;
+}
+__device__ __forceinline__ void put_values(bf16_t *tile, int pos, int d, int hd, const u32x4 (&y)[2]) {        // 32 bytes of a lane
+  const bool odd = threadIdx.x & 1;
+  const u32x4 got = from_lane_xor1(odd ? y[0] : y[1]);
+  u32x4 *to = reinterpret_cast<u32x4 *>(tile + page_v_offset<bf16_t>(pos, d & ~2, hd)) + odd;
+  to[0] = odd ? got : y[0];
+  to[2] = odd ? y[1] : got;
+}
+__device__ __forceinline__ void get_values(const bf16_t *tile, int pos, int d, int hd, u32x4 (&y)[2]) {
+  const bool odd = threadIdx.x & 1;
+  const u32x4 *from = reinterpret_cast<const u32x4 *>(tile + page_v_offset<bf16_t>(pos, d & ~2, hd)) + odd;
+  const u32x4 u = from[0], v = from[2], got = from_lane_xor1(odd ? u : v);
+  y[0] = odd ? got : u;
+  y[1] = odd ? v : got;
+}
+__device__ __forceinline__ void put_values(fp8_t *tile, int pos, int d, int hd, const u32x2 (&y)[2]) {         // dimensions d and d + 16: 16 bytes
+  const bool upper = threadIdx.x & 8;
+  const u32x2 got = from_lane_xor8(upper ? y[0] : y[1]), u = upper ? got : y[0], v = upper ? y[1] : got;
+  *reinterpret_cast<u32x4 *>(tile + page_v_offset<fp8_t>(pos, upper ? d - 15 : d, hd)) = u32x4{u[0], u[1], v[0], v[1]};
+}
+__device__ __forceinline__ void get_values(const fp8_t *tile, int pos, int d, int hd, u32x2 (&y)[2]) {
+  const bool upper = threadIdx.x & 8;
+  const u32x4 x = *reinterpret_cast<const u32x4 *>(tile + page_v_offset<fp8_t>(pos, upper ? d - 15 : d, hd));
+  const u32x2 u{x[0], x[1]}, v{x[2], x[3]}, got = from_lane_xor8(upper ? u : v);
+  y[0] = upper ? got : u;
+  y[1] = upper ? v : got;
+}
+
+// Two bytes each of eight positions to eight bytes of each of two dimensions, and back.
+__device__ __forceinline__ void turn_bytes(const unsigned (&w)[8], u32x2 (&y)[2]) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const unsigned u = __builtin_amdgcn_perm(w[4 * k + 1], w[4 * k], 0x05010400), v = __builtin_amdgcn_perm(w[4 * k + 3], w[4 * k + 2], 0x05010400);
+    y[0][k] = __builtin_amdgcn_perm(v, u, 0x05040100);
+    y[1][k] = __builtin_amdgcn_perm(v, u, 0x07060302);
+  }
+}
+__device__ __forceinline__ void turn_bytes(const u32x2 (&y)[2], unsigned (&w)[4]) {   // positions 2 i and 2 i + 1 in a word
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    w[2 * k] = __builtin_amdgcn_perm(y[1][k], y[0][k], 0x05010400);
+    w[2 * k + 1] = __builtin_amdgcn_perm(y[1][k], y[0][k], 0x07030602);
+  }
+}
+
 template <typename T, typename CT>
 __global__ __launch_bounds__(256) void kv_write_group_kernel(const CacheArgs a, int vec) {
   constexpr int VE = Vec16<T>::n, ROW = 128 + kRowPad / (int)sizeof(T);
-  __shared__ __align__(16) T rows[2][kGroup][ROW];
-  __shared__ float un[2][kGroup];
-  __shared__ GroupSlots g;
-  const int tid = threadIdx.x, h = blockIdx.y, t0 = blockIdx.x * kGroup, m = min(kGroup, a.n_tokens - t0), hd = a.p.hd, ps = a.p.page_size;
+  constexpr int PARTS = kGroup * 128 / VE / 256;           // of a thread, at most
+  constexpr bool C8 = sizeof(CT) == 1;
+  __shared__ __align__(16) T rows[kGroup][ROW];
+  __shared__ __align__(16) uint8_t bytes[C8 ? kGroup : 1][128 + 8];   // rows in 8 bits
+  __shared__ uint8_t ex[kGroup];                           // their exponents
+  const int tid = threadIdx.x, h = blockIdx.y, hd = a.p.hd, ps = a.p.page_size;
+  int t0, m;
+  if (!group_tokens(a, t0, m)) return;
+  const bool values = blockIdx.z, turns = a.cos && !values;
   const int per = hd / VE;
-#pragma unroll 4
-  for (int i = tid; i < 2 * m * per; i += 256) {
-    const int kv = i >= m * per, j = kv ? i - m * per : i, t = j / per, e = j % per * VE;
-    const T *src = (kv ? (const T *)a.v + (t0 + t) * a.v_token + h * a.v_head : (const T *)a.k + (t0 + t) * a.k_token + h * a.k_head) + e;
-    if (vec) *reinterpret_cast<u32x4 *>(&rows[kv][t][e]) = *reinterpret_cast<const u32x4 *>(src);
-    else
+  const int64_t stride = values ? a.v_token : a.k_token;
+  const T *in = (values ? (const T *)a.v + h * a.v_head : (const T *)a.k + h * a.k_head) + t0 * stride;
+  u32x4 part[PARTS];
 #pragma unroll
-      for (int x = 0; x < VE; ++x) rows[kv][t][e + x] = src[x];
+  for (int j = 0; j < PARTS; ++j) {
+    const int i = tid + 256 * j;
+    if (i >= m * per) continue;
+    const T *src = in + i / per * stride + i % per * VE;
+    if (vec) part[j] = *reinterpret_cast<const u32x4 *>(src);
+    else {
+      struct alignas(16) { T x[VE]; } one;
+#pragma unroll
+      for (int e = 0; e < VE; ++e) one.x[e] = src[e];
+      part[j] = __builtin_bit_cast(u32x4, one);
+    }
   }
-  load_slots(a, g, t0, m);
-  __syncthreads();
-  if (a.cos) {
+  const GroupSlots g(a, t0, m);
+  if (turns || !C8) {
+#pragma unroll
+    for (int j = 0; j < PARTS; ++j) {
+      const int i = tid + 256 * j;
+      if (i < m * per) *reinterpret_cast<u32x4 *>(&rows[i / per][i % per * VE]) = part[j];
+    }
+    __syncthreads();
+  }
+  if (turns) {
     const int half = a.rd / 2;
     for (int i = tid; i < m * half; i += 256) {
       const int t = i / half, p = i % half, pos = a.positions[t0 + t];
       const bool ok = pos >= 0 && pos < a.n_positions;
       const float c = ok ? a.cos[(int64_t)pos * half + p] : __builtin_nanf(""), s = ok ? a.sin[(int64_t)pos * half + p] : 0.0f;
-      T &x = rows[0][t][a.interleaved ? 2 * p : p], &y = rows[0][t][a.interleaved ? 2 * p + 1 : p + half];
+      T &x = rows[t][a.interleaved ? 2 * p : p], &y = rows[t][a.interleaved ? 2 * p + 1 : p + half];
       const float u = to_f32(x), v = to_f32(y);
       x = from_f32<T>(turned(u, v, c, -s));
       y = from_f32<T>(turned(v, u, c, s));
     }
     __syncthreads();
   }
-  if constexpr (sizeof(CT) == 1) {
-    const int t = tid >> 3;                                // eight threads to a token
+  if constexpr (C8) {
+    // a row's exponent from the threads that hold it, which sit side by side, and its bytes
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      float top = 0.0f;
-      if (t < m)
-        for (int d = (tid & 7) * 2; d < hd; d += 16)
+    for (int j = 0; j < PARTS; ++j) {
+      const int i = tid + 256 * j;
+      if (i >= m * per) continue;
+      if (turns) part[j] = *reinterpret_cast<const u32x4 *>(&rows[i / per][i % per * VE]);
+      float x[VE], top = 0.0f;
+      Vec16<T>::get(part[j], x);
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const float v = fabsf(to_f32(rows[kv][t][d + x]));
-            if (v < __builtin_inff()) top = fmaxf(top, v);
-          }
+      for (int e = 0; e < VE; ++e) top = fmaxf(top, fabsf(x[e]));          // (a NaN is passed over)
+      if (!(top < __builtin_inff())) {
+        top = 0.0f;
 #pragma unroll
-      for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-      const unsigned e = fp8_exponent(top);
-      if ((tid & 7) == 0) {
-        un[kv][t] = exp_unscale(e);
-        const int slot = g.slot[t];
-        if (slot >= 0) (kv ? a.p.v_exp : a.p.k_exp)[slot_head(a, slot, h) + slot % ps] = (uint8_t)e;
+        for (int e = 0; e < VE; ++e) top = fmaxf(top, fabsf(x[e]) < __builtin_inff() ? fabsf(x[e]) : 0.0f);
       }
+      for (int o = 1; o < per; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+      const unsigned exp = fp8_exponent(top);
+      const float un = exp_unscale(exp);
+      if (i % per == 0) ex[i / per] = (uint8_t)exp;
+      unsigned w[VE / 4];
+#pragma unroll
+      for (int e = 0; e < VE; e += 4)                      // (what is not finite converts to NaN)
+        w[e / 4] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(x[e + 2] * un, x[e + 3] * un, __builtin_amdgcn_cvt_pk_fp8_f32(x[e] * un, x[e + 1] * un, 0, false), true);
+#pragma unroll
+      for (int e = 0; e < VE / 4; ++e) *reinterpret_cast<unsigned *>(&bytes[i / per][i % per * VE + e * 4]) = w[e];
     }
     __syncthreads();
+    if (tid < m && g.slot >= 0) (values ? a.p.v_exp : a.p.k_exp)[slot_head(a, g.slot, h) + g.slot % ps] = ex[tid];
   }
-  // (what is not finite converts to NaN)
-  auto four = [&](const float (&v)[8], int i) {
-    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(v[i + 2], v[i + 3], __builtin_amdgcn_cvt_pk_fp8_f32(v[i], v[i + 1], 0, false), true);
-  };
-  // keys: eight dimensions of a position lie side by side (fp32: four)
-  for (int i = tid; i < kGroup * (hd / 8); i += 256) {
-    const int t = i % kGroup, d = i / kGroup * 8, slot = g.slot[t];
-    if (slot < 0) continue;
-    CT *dst = (CT *)a.p.k + slot_head(a, slot, h) * hd;
-    const T *src = &rows[0][t][d];
-    if constexpr (sizeof(CT) == 1) {
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = to_f32(src[e]) * un[0][t];
-      *reinterpret_cast<u32x2 *>(dst + page_k_offset<CT>(slot % ps, d, hd)) = u32x2{four(v, 0), four(v, 4)};
-    } else {
-      *reinterpret_cast<u32x4 *>(dst + page_k_offset<CT>(slot % ps, d, hd)) = *reinterpret_cast<const u32x4 *>(src);
-      if constexpr (sizeof(CT) == 4)
-        *reinterpret_cast<u32x4 *>(dst + page_k_offset<CT>(slot % ps, d + 4, hd)) = *reinterpret_cast<const u32x4 *>(src + 4);
+  if (!values) {
+    // eight dimensions of a key's position lie side by side (fp32: four)
+    const int slot = g.slot, t = tid % kGroup;             // (of every turn)
+    if (slot < 0) return;
+    for (int i = tid; i < kGroup * (hd / 8); i += 256) {
+      const int d = i / kGroup * 8;
+      CT *dst = (CT *)a.p.k + slot_head(a, slot, h) * hd;
+      const T *src = &rows[t][d];
+      if constexpr (C8) *reinterpret_cast<u32x2 *>(dst + page_k_offset<CT>(slot % ps, d, hd)) = *reinterpret_cast<const u32x2 *>(&bytes[t][d]);
+      else {
+        *reinterpret_cast<u32x4 *>(dst + page_k_offset<CT>(slot % ps, d, hd)) = *reinterpret_cast<const u32x4 *>(src);
+        if constexpr (sizeof(CT) == 4)
+          *reinterpret_cast<u32x4 *>(dst + page_k_offset<CT>(slot % ps, d + 4, hd)) = *reinterpret_cast<const u32x4 *>(src + 4);
+      }
     }
+    return;
   }
-  // values: eight positions of a dimension do
+  // eight positions of a value's dimension do
   auto value = [&](int t, int d) -> CT {
-    if constexpr (sizeof(CT) == 1) return {(uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(to_f32(rows[1][t][d]) * un[1][t], 0.0f, 0, false)};
-    else return rows[1][t][d];
+    if constexpr (C8) return {bytes[t][d]};
+    else return rows[t][d];
   };
-  if (g.run) {
-    const int s0 = g.slot[0], lead = s0 % 8, groups = (lead + m + 7) / 8;
-    // a thread takes two neighbouring dimensions
-    for (int i = tid; i < groups * hd / 2; i += 256) {
-      const int q = i / (hd / 2), d = i % (hd / 2) * 2, first = q * 8 - lead;
-      const int from = max(first, 0), to = min(first + 8, m), slot = s0 + from;
-      CT *dst = (CT *)a.p.v + slot_head(a, slot, h) * hd;
-      const int pos = slot % ps;
-      if (to - from < 8) {
-        for (int t = from; t < to; ++t)
+  // a thread takes two neighbouring dimensions of a chunk
+  const int work = g.chunks * hd / 2;
+  for (int i0 = tid & ~63; i0 < work; i0 += 256) {
+    const int i = i0 + (tid & 63), d = i % (hd / 2) * 2;
+    const Chunk c = chunk_at(g, i / (hd / 2));
+    if (i < work && c.slot >= 0) {
+      CT *dst = (CT *)a.p.v + slot_head(a, c.slot, h) * hd;
+      const int pos = c.slot % ps, first = c.first;
+      if (c.last - first < 8) {
+        for (int t = first; t < c.last; ++t)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) dst[page_v_offset<CT>(pos + t - from, d + x, hd)] = value(t, d + x);
+          for (int x = 0; x < 2; ++x) dst[page_v_offset<CT>(pos + t - first, d + x, hd)] = value(t, d + x);
         continue;
       }
-      T v[2][8];
+      struct alignas(2 * sizeof(T)) Two { T x[2]; };
+      if constexpr (C8) {
+        unsigned w[8];                                     // a position's two bytes
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        struct alignas(2 * sizeof(T)) Two { T x[2]; };
-        const Two w = *reinterpret_cast<const Two *>(&rows[1][first + e][d]);
-        v[0][e] = w.x[0];
-        v[1][e] = w.x[1];
-      }
+        for (int e = 0; e < 8; ++e) w[e] = *reinterpret_cast<const uint16_t *>(&bytes[first + e][d]);
+        u32x2 y[2];
+        turn_bytes(w, y);
+        put_values(dst, pos, d, hd, y);
+      } else if constexpr (sizeof(CT) == 2) {
+        T v[2][8];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        CT *to8 = dst + page_v_offset<CT>(pos, d + x, hd);
-        if constexpr (sizeof(CT) == 1) {
-          float y[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = to_f32(v[x][e]) * un[1][first + e];
-          *reinterpret_cast<u32x2 *>(to8) = u32x2{four(y, 0), four(y, 4)};
-        } else if constexpr (sizeof(CT) == 2) *reinterpret_cast<u32x4 *>(to8) = __builtin_bit_cast(u32x4, v[x]);
-        else {
-          *reinterpret_cast<f32x4 *>(to8) = f32x4{v[x][0], v[x][1], v[x][2], v[x][3]};
-          *reinterpret_cast<f32x4 *>(dst + page_v_offset<CT>(pos + 4, d + x, hd)) = f32x4{v[x][4], v[x][5], v[x][6], v[x][7]};
+        for (int e = 0; e < 8; ++e) {
+          const Two w = *reinterpret_cast<const Two *>(&rows[first + e][d]);
+          v[0][e] = w.x[0];
+          v[1][e] = w.x[1];
         }
-      }
+        u32x4 y[2];
+        __builtin_memcpy(y, v, sizeof y);
+        put_values(dst, pos, d, hd, y);
+      } else
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+#pragma unroll
+          for (int e = 0; e < 8; e += 4)
+            *reinterpret_cast<f32x4 *>(dst + page_v_offset<CT>(pos + e, d + x, hd)) =
+                f32x4{rows[first + e][d + x], rows[first + e + 1][d + x], rows[first + e + 2][d + x], rows[first + e + 3][d + x]};
+        }
     }
-  } else
-    for (int i = tid; i < m * hd; i += 256) {
-      const int t = i / hd, d = i % hd, slot = g.slot[t];
-      if (slot >= 0) ((CT *)a.p.v + slot_head(a, slot, h) * hd)[page_v_offset<CT>(slot % ps, d, hd)] = value(t, d);
-    }
+  }
+}
+
+// Two 8-bit elements, of the word's upper half if UPPER, times a power of two; exact in both types.
+template <bool UPPER>
+__device__ __forceinline__ void two_wide(unsigned w, float scale, bf16_t *to) {
+  *reinterpret_cast<bf16x2 *>(to) = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, UPPER);
+}
+template <bool UPPER>
+__device__ __forceinline__ void two_wide(unsigned w, float scale, float *to) {
+  to[0] = __builtin_amdgcn_cvt_f32_fp8(w, UPPER ? 2 : 0) * scale;
+  to[1] = __builtin_amdgcn_cvt_f32_fp8(w, UPPER ? 3 : 1) * scale;
 }
 
 template <typename T, typename CT>
 __global__ __launch_bounds__(256) void kv_read_group_kernel(const CacheArgs a, int vec) {
   constexpr int VE = Vec16<T>::n, ROW = 128 + kRowPad / (int)sizeof(T);
-  __shared__ __align__(16) T rows[2][kGroup][ROW];
-  __shared__ float sc[2][kGroup];
-  __shared__ GroupSlots g;
-  const int tid = threadIdx.x, h = blockIdx.y, t0 = blockIdx.x * kGroup, m = min(kGroup, a.n_tokens - t0), hd = a.p.hd, ps = a.p.page_size;
-  load_slots(a, g, t0, m);
-  __syncthreads();
-  if constexpr (sizeof(CT) == 1) {
-    if (tid < 2 * kGroup) {
-      const int kv = tid / kGroup, t = tid % kGroup, slot = g.slot[t];
-      sc[kv][t] = slot >= 0 ? exp_scale((kv ? a.p.v_exp : a.p.k_exp)[slot_head(a, slot, h) + slot % ps]) : 0.0f;
-    }
-    __syncthreads();
-  }
-  auto wide = [&](CT x, int kv, int t) -> T {
-    if constexpr (sizeof(CT) == 1) return from_f32<T>(fp8_to_f32(x.bits) * sc[kv][t]);
+  __shared__ __align__(16) T rows[kGroup][ROW];
+  const int tid = threadIdx.x, h = blockIdx.y, hd = a.p.hd, ps = a.p.page_size;
+  int t0, m;
+  if (!group_tokens(a, t0, m)) return;
+  const bool values = blockIdx.z;
+  T *out = values ? (T *)a.v_out : (T *)a.k_out;
+  if (!out) return;
+  const int64_t stride = values ? a.v_token : a.k_token;
+  out += t0 * stride + h * (values ? a.v_head : a.k_head);
+  const GroupSlots g(a, t0, m);
+  const uint8_t *exps = values ? a.p.v_exp : a.p.k_exp;
+  auto wide = [&](CT x, unsigned e) -> T {                 // e: its exponent
+    if constexpr (sizeof(CT) == 1) return from_f32<T>(fp8_to_f32(x.bits) * exp_scale(e));
     else return x;
   };
-  if (a.k_out)
+  auto exponent = [&](int slot) -> unsigned {
+    if constexpr (sizeof(CT) == 1) return exps[slot_head(a, slot, h) + slot % ps];
+    else return 0;
+  };
+  if (!values) {
+    const int slot = g.slot, t = tid % kGroup;             // (of every turn)
+    const unsigned ex = slot >= 0 ? exponent(slot) : 0;
+#pragma unroll 2
     for (int i = tid; i < kGroup * (hd / 8); i += 256) {
-      const int t = i % kGroup, d = i / kGroup * 8, slot = g.slot[t];
+      const int d = i / kGroup * 8;
       CT x[8] = {};
       if (slot >= 0) {
         const CT *src = (const CT *)a.p.k + slot_head(a, slot, h) * hd;
@@ -437,59 +558,88 @@ __global__ __launch_bounds__(256) void kv_read_group_kernel(const CacheArgs a, i
           if constexpr (sizeof(CT) == 4) *reinterpret_cast<u32x4 *>(x + 4) = *reinterpret_cast<const u32x4 *>(src + page_k_offset<CT>(slot % ps, d + 4, hd));
         }
       }
+      if constexpr (sizeof(CT) == 1) {
+        const float s = exp_scale(ex);
+        const u32x2 w = *reinterpret_cast<const u32x2 *>(x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) rows[0][t][d + e] = wide(x[e], 0, t);
+        for (int e = 0; e < 8; e += 4) {
+          two_wide<false>(w[e / 4], s, &rows[t][d + e]);
+          two_wide<true>(w[e / 4], s, &rows[t][d + e + 2]);
+        }
+      } else
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rows[t][d + e] = x[e];
     }
-  if (a.v_out) {
-    if (g.run) {
-      const int s0 = g.slot[0], lead = s0 % 8, groups = (lead + m + 7) / 8;
-      for (int i = tid; i < groups * hd; i += 256) {
-        const int q = i / hd, d = i % hd, first = q * 8 - lead;
-        const int from = max(first, 0), to = min(first + 8, m), slot = s0 + from;
-        const CT *src = (const CT *)a.p.v + slot_head(a, slot, h) * hd;
-        if (to - from == 8) {
-          CT x[8];
-          if constexpr (sizeof(CT) == 1) *reinterpret_cast<u32x2 *>(x) = *reinterpret_cast<const u32x2 *>(src + page_v_offset<CT>(slot % ps, d, hd));
-          else {
-            *reinterpret_cast<u32x4 *>(x) = *reinterpret_cast<const u32x4 *>(src + page_v_offset<CT>(slot % ps, d, hd));
-            if constexpr (sizeof(CT) == 4) *reinterpret_cast<u32x4 *>(x + 4) = *reinterpret_cast<const u32x4 *>(src + page_v_offset<CT>(slot % ps + 4, d, hd));
-          }
+  } else {
+    const int work = g.chunks * hd / 2;
+    for (int i0 = tid & ~63; i0 < work; i0 += 256) {
+      const int i = i0 + (tid & 63), d = i % (hd / 2) * 2;
+      const Chunk c = chunk_at(g, i / (hd / 2));
+      if (i >= work) continue;
+      const int first = c.first, pos = c.slot < 0 ? 0 : c.slot % ps;
+      const CT *src = (const CT *)a.p.v + (c.slot < 0 ? 0 : slot_head(a, c.slot, h)) * hd;
+      struct alignas(2 * sizeof(T)) Two { T x[2]; };
+      if (c.last - first < 8) {
+        for (int t = first; t < c.last; ++t) {
+          const unsigned ex = c.slot < 0 ? 0 : exponent(c.slot + t - first);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) rows[1][first + e][d] = wide(x[e], 1, first + e);
-        } else
-          for (int t = from; t < to; ++t) rows[1][t][d] = wide(src[page_v_offset<CT>(slot % ps + t - from, d, hd)], 1, t);
+          for (int x = 0; x < 2; ++x) rows[t][d + x] = wide(c.slot < 0 ? CT{} : src[page_v_offset<CT>(pos + t - first, d + x, hd)], ex);
+        }
+        continue;
       }
-    } else
-      for (int i = tid; i < m * hd; i += 256) {
-        const int t = i / hd, d = i % hd, slot = g.slot[t];
-        CT x{};
-        if (slot >= 0) x = ((const CT *)a.p.v + slot_head(a, slot, h) * hd)[page_v_offset<CT>(slot % ps, d, hd)];
-        rows[1][t][d] = wide(x, 1, t);
-      }
+      if constexpr (sizeof(CT) == 1) {
+        u32x2 y[2];
+        get_values(src, pos, d, hd, y);
+        const u32x2 ex = *reinterpret_cast<const u32x2 *>(exps + slot_head(a, c.slot, h) + pos);
+        unsigned w[4];
+        turn_bytes(y, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float s = exp_scale(ex[e >> 2] >> (e & 3) * 8 & 0xff);
+          Two &to = *reinterpret_cast<Two *>(&rows[first + e][d]);
+          if (e & 1) two_wide<true>(w[e / 2], s, to.x); else two_wide<false>(w[e / 2], s, to.x);
+        }
+      } else if constexpr (sizeof(CT) == 2) {
+        u32x4 y[2];
+        get_values(src, pos, d, hd, y);
+        T x[2][8];
+        __builtin_memcpy(x, y, sizeof x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) *reinterpret_cast<Two *>(&rows[first + e][d]) = Two{{x[0][e], x[1][e]}};
+      } else
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int e = 0; e < 8; e += 4) {
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(src + page_v_offset<CT>(pos + e, d + k, hd));
+#pragma unroll
+            for (int n = 0; n < 4; ++n) rows[first + e + n][d + k] = x[n];
+          }
+    }
   }
   __syncthreads();
   const int per = hd / VE;
-  for (int i = tid; i < 2 * m * per; i += 256) {
-    const int kv = i >= m * per, j = kv ? i - m * per : i, t = j / per, e = j % per * VE;
-    T *dst = kv ? (T *)a.v_out : (T *)a.k_out;
-    if (!dst) continue;
-    dst += (kv ? (t0 + t) * a.v_token + h * a.v_head : (t0 + t) * a.k_token + h * a.k_head) + e;
-    if (vec) *reinterpret_cast<u32x4 *>(dst) = *reinterpret_cast<const u32x4 *>(&rows[kv][t][e]);
+  for (int i = tid; i < m * per; i += 256) {
+    const int t = i / per, e = i % per * VE;
+    T *dst = out + t * stride + e;
+    if (vec) *reinterpret_cast<u32x4 *>(dst) = *reinterpret_cast<const u32x4 *>(&rows[t][e]);
     else
 #pragma unroll
-      for (int x = 0; x < VE; ++x) dst[x] = rows[kv][t][e + x];
+      for (int x = 0; x < VE; ++x) dst[x] = rows[t][e + x];
   }
 }
 
-// Calls of few rows have a wave for each (token, head), whose chain of loads is the shorter one: 256 rows of 128 written to a 16-bit
-// cache 3.4 us against 5.2, 7800 to an 8-bit one 8.5 against 7.5.
-constexpr int kFewRows = 4096;
+// Calls of few rows have a wave for each (token, head), whose chain of loads is the shorter one (8 heads of 128, 16 bits, us, by waves
+// and by groups: 1 token written 2.5 and 3.5, 64 tokens 3.4 and 3.6, 256 tokens 3.9 and 3.6, 512 tokens 5.2 and 4.1).
+constexpr int kFewRows = 2048;
 static bool few_rows(const CacheArgs &a) { return (int64_t)a.n_tokens * a.p.Hkv <= kFewRows; }
 template <typename T>
 static bool rows_of_vectors(const CacheArgs &a, const void *k, const void *v) {
   constexpr int VE = Vec16<T>::n;
   return (!k || aligned16(k)) && (!v || aligned16(v)) && a.k_token % VE == 0 && a.k_head % VE == 0 && a.v_token % VE == 0 && a.v_head % VE == 0;
 }
+
+static dim3 groups(const CacheArgs &a) { return dim3((unsigned)(((int64_t)a.n_tokens + 7 + kGroup - 1) / kGroup), a.p.Hkv, 2); }
 
 // dtype: of the tokens; cache: of the pages
 template <template <typename, typename> class Launch>
@@ -502,14 +652,14 @@ static void by_types(int dtype, int cache, const CacheArgs &a, hipStream_t s) {
 template <typename T, typename CT> struct WriteLaunch {
   static void go(const CacheArgs &a, hipStream_t s) {
     if (!few_rows(a))
-      hipLaunchKernelGGL((kv_write_group_kernel<T, CT>), dim3((a.n_tokens + kGroup - 1) / kGroup, a.p.Hkv), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k, a.v));
+      hipLaunchKernelGGL((kv_write_group_kernel<T, CT>), groups(a), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k, a.v));
     else hipLaunchKernelGGL((kv_write_kernel<T, CT>), dim3((a.n_tokens * a.p.Hkv + 3) / 4), dim3(256), 0, s, a);
   }
 };
 template <typename T, typename CT> struct ReadLaunch {
   static void go(const CacheArgs &a, hipStream_t s) {
     if (!few_rows(a))
-      hipLaunchKernelGGL((kv_read_group_kernel<T, CT>), dim3((a.n_tokens + kGroup - 1) / kGroup, a.p.Hkv), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k_out, a.v_out));
+      hipLaunchKernelGGL((kv_read_group_kernel<T, CT>), groups(a), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k_out, a.v_out));
     else hipLaunchKernelGGL((kv_read_kernel<T, CT>), dim3((a.n_tokens * a.p.Hkv + 3) / 4), dim3(256), 0, s, a);
   }
 };

@@ -193,6 +193,34 @@ def test_cache_holds_what_was_written(dtype, cache, hd, Hkv, page, n, order):
         assert torch.equal(bytes_before[0], kv.k_bytes) and torch.equal(bytes_before[1], kv.v_bytes)
 
 
+@pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("bf16", "bf16"), ("f32", "fp8"), ("bf16", "fp8")])
+@pytest.mark.parametrize("hd,Hkv", [(32, 5), (64, 3), (128, 2)])
+@pytest.mark.parametrize("tree,start", [(61, 0), (13, 5), (8, 8), (9, 7), (3, 30), (40, 1)])
+def test_cache_of_many_sequences_runs(dtype, cache, hd, Hkv, tree, start):
+    """Runs of slots that begin and end inside the groups that move together, with places left out, as one call and row by row."""
+    B, page = 20 + 1200 // tree, 64
+    rng = np.random.default_rng(tree)
+    slots = np.concatenate([(2 * page * b + start + 3 * (b % 5) + np.arange(tree)) for b in rng.permutation(B)])
+    slots[rng.permutation(len(slots))[:5]] = -1
+    n, pool = len(slots), 2 * B + 2
+    x = randn(n, 2 * Hkv * hd, seed=tree, dtype=dtype)
+    k, v = x[:, :Hkv * hd].view(n, Hkv, hd), x[:, Hkv * hd:].view(n, Hkv, hd)
+    whole, parts = (ngg.KVPages(pool, page, Hkv, hd, cache) for _ in range(2))
+    whole.write(k, v, ints(slots))
+    for at in range(0, n, 200):
+        parts.write(k[at:at + 200], v[at:at + 200], ints(slots[at:at + 200]))
+    assert torch.equal(whole.k_bytes, parts.k_bytes) and torch.equal(whole.v_bytes, parts.v_bytes)
+    if cache == "fp8":
+        assert torch.equal(whole.k_exps, parts.k_exps) and torch.equal(whole.v_exps, parts.v_exps)
+    got = whole.read(ints(slots), DT[dtype])
+    there = torch.from_numpy(slots >= 0).cuda()
+    for g, t in zip(got, (k, v)):
+        want = eight_bits(t).to(DT[dtype]) if cache == "fp8" else t
+        assert torch.equal(g[there], want[there]) and (g[~there] == 0).all()
+    some = whole.read(ints(slots[:100]), DT[dtype])
+    assert torch.equal(some[0], got[0][:100]) and torch.equal(some[1], got[1][:100])
+
+
 def test_eight_bit_corners():
     """Heads of zeros, the largest value exactly and just above, the smallest exponents, numbers that are not finite."""
     hd = 32
