@@ -47,17 +47,33 @@ __device__ __forceinline__ Sums join(Sums a, Sums b) {
   return {m, a.s + b.s, a.t + b.t};
 }
 
+// A wave's maximum and sum, on every lane: inside rows of 16 lanes by data-parallel moves, the four rows by scalars
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float lane_value(float x, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); }
+constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kHalfMirror = 0x141, kMirror = 0x140;
+__device__ __forceinline__ float wave_max(float x) {
+  x = fmaxf(x, moved<kXor1>(x));
+  x = fmaxf(x, moved<kXor2>(x));
+  x = fmaxf(x, moved<kHalfMirror>(x));
+  x = fmaxf(x, moved<kMirror>(x));
+  return fmaxf(fmaxf(lane_value(x, 0), lane_value(x, 16)), fmaxf(lane_value(x, 32), lane_value(x, 48)));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  x += moved<kXor1>(x);
+  x += moved<kXor2>(x);
+  x += moved<kHalfMirror>(x);
+  x += moved<kMirror>(x);
+  return (lane_value(x, 0) + lane_value(x, 16)) + (lane_value(x, 32) + lane_value(x, 48));
+}
+
 // The sums of a wave, on every lane
 __device__ __forceinline__ Sums wave_sums(Sums a) {
-  float m = a.m;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-  move_to(a, m);
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    a.s += __shfl_xor(a.s, o);
-    a.t += __shfl_xor(a.t, o);
-  }
+  move_to(a, wave_max(a.m));
+  a.s = wave_sum(a.s);
+  a.t = wave_sum(a.t);
   return a;
 }
 
@@ -146,7 +162,7 @@ __device__ __forceinline__ Sums odd_row(const ScoreArgs &a, const T *x, Sums *pa
     m = fmaxf(m, y);
     nan |= y != y;
   }
-  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+  m = wave_max(m);
   __syncthreads();
   if (tid % 64 == 0) part[tid / 64].m = m;
   __syncthreads();
@@ -158,7 +174,8 @@ __device__ __forceinline__ Sums odd_row(const ScoreArgs &a, const T *x, Sums *pa
       s += p;                                              // NaN from plus infinity less itself
       if (p > 0.0f) t += p * d;
     }
-  for (int o = 1; o < 64; o <<= 1) { s += __shfl_xor(s, o); t += __shfl_xor(t, o); }
+  s = wave_sum(s);
+  t = wave_sum(t);
   if (tid % 64 == 0) { part[tid / 64].s = s; part[tid / 64].t = t; }
   __syncthreads();
   return {m, part[0].s + part[1].s + part[2].s + part[3].s, part[0].t + part[1].t + part[2].t + part[3].t};
@@ -209,6 +226,17 @@ __device__ void top_with_nan(const ScoreArgs &a, const RowResult &o, const T *x,
     prev = b;
     if (lane == 0) put_top(a, o, r, i, b, to_f32(x[key_place(b)]));
   }
+}
+
+// Element i of a lane's own, by bits: a choice between elements would be made into an index, and the elements kept in memory for it
+template <int N>
+__device__ __forceinline__ float element(const float (&y)[N], int i) {
+  const unsigned odd = 0u - (i & 1);
+  float x[N / 2];
+#pragma unroll
+  for (int j = 0; j < N / 2; ++j) x[j] = __uint_as_float((__float_as_uint(y[2 * j + 1]) & odd) | (__float_as_uint(y[2 * j]) & ~odd));
+  if constexpr (N == 2) return x[0];
+  else return element(x, i >> 1);
 }
 
 // One workgroup per (row, slice).  TOP: with a list of the likeliest.
@@ -284,9 +312,9 @@ __global__ __launch_bounds__(256, 5) void logprobs_kernel(const ScoreArgs a, int
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int at = ((b * NV + i) * 64 + lane) * VE - off;
-        if (!(at >= 0 && at + VE <= a.V))
+        if (__ballot(at < a.V && (at < 0 || at + VE > a.V)) == 0) continue;
 #pragma unroll
-          for (int e = 0; e < VE; ++e) y[i * VE + e] = at + e >= 0 && at + e < a.V ? to_f32(x[at + e]) : -__builtin_inff();
+        for (int e = 0; e < VE; ++e) y[i * VE + e] = at + e >= 0 && at + e < a.V ? to_f32(x[at + e]) : -__builtin_inff();
       }
     if (b + 4 < b1) fetch(b + 4);
     if constexpr (TOP) {                                   // another wave may have raised the bar
@@ -297,14 +325,9 @@ __global__ __launch_bounds__(256, 5) void logprobs_kernel(const ScoreArgs a, int
       o = uniform(o);
       bar = o > bar ? o : bar;
     }
-    float most[NV], top;
+    float top = y[0];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      most[i] = y[i * VE];
-#pragma unroll
-      for (int e = 1; e < VE; ++e) most[i] = fmaxf(most[i], y[i * VE + e]);
-      top = i ? fmaxf(top, most[i]) : most[0];
-    }
+    for (int e = 1; e < K; ++e) top = fmaxf(top, y[e]);
     // the reference follows the largest value so far at a distance: sums of up to 2^16 more lose nothing
     if (__ballot(top * c - q.m > 16.0f) != 0 && top * c > q.m) move_to(q, ceilf(top * c));
     const float s0 = q.s, t0 = q.t;
@@ -329,42 +352,69 @@ __global__ __launch_bounds__(256, 5) void logprobs_kernel(const ScoreArgs a, int
     if constexpr (TOP) {
       const float tau = key_value((unsigned)(bar >> 32));
       if (__ballot(!(top < tau)) != 0) {
-        int room = cnt;
+        if constexpr (sizeof(T) == 4) {
+          // every lane's candidates as bits, of which all lanes put their lowest into the list at a time: one piece of code for the 16
+          // elements, which a short slice fetches sooner than a copy for each (97 rows of 128256, top 20: 17.5 us against 19.5)
+          unsigned bits = 0;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) room += VE * __builtin_popcountll(__ballot(!(most[i] < tau)));
-        if (room <= kList) {
-          // few vectors hold candidates: they fit whatever there are
-#pragma unroll
-          for (int i = 0; i < NV; ++i) {
-            if (__ballot(!(most[i] < tau)) == 0) continue;
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-              const float z = y[i * VE + e];
-              if (__ballot(!(z < tau)) == 0) continue;
-              const int v = ((b * NV + i) * 64 + lane) * VE - off + e;
-              const key_t64 k = place_key(z, v);
-              const uint64_t m = __ballot(k > bar && v >= 0 && v < a.V);
-              if (m >> lane & 1) list[cnt + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = k;
-              cnt += __builtin_popcountll(m);
-            }
+          for (int e = K - 1; e >= 0; --e) bits = bits << 1 | (y[e] < tau ? 0u : 1u);   // (powers of two would each hold a register)
+          for (;;) {
+            const bool more = __ballot(bits != 0) != 0;
+            if (more ? cnt + 64 > kList : cnt >= raise_at) raise();
+            if (!more) break;
+            const int e = bits ? __builtin_ctz(bits) : 0, v = ((b * NV + e / VE) * 64 + lane) * VE - off + e % VE;
+            const key_t64 k = place_key(element(y, e), v);
+            const uint64_t m = __ballot(bits != 0 && k > bar && v >= 0 && v < a.V);
+            if (m >> lane & 1) list[cnt + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = k;
+            cnt += __builtin_popcountll(m);
+            bits &= bits - 1;
           }
         } else {
-          for (int i = 0; i < NV; ++i)
+          // (the 32 of a lane would not leave that way registers enough)
+          float most[NV];
 #pragma unroll
-            for (int e = 0; e < VE; ++e) {
-              float z = y[e];                              // (i is not unrolled: K copies of this would not fit the instruction cache)
+          for (int i = 0; i < NV; ++i) {
+            most[i] = y[i * VE];
 #pragma unroll
-              for (int j = 1; j < NV; ++j) z = i == j ? y[j * VE + e] : z;
-              const int v = ((b * NV + i) * 64 + lane) * VE - off + e;
-              const key_t64 k = place_key(z, v);
-              const uint64_t m = __ballot(k > bar && v >= 0 && v < a.V);
-              if (m == 0) continue;
-              if (m >> lane & 1) list[cnt + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = k;
-              cnt += __builtin_popcountll(m);
-              if (cnt + 64 > kList) raise();
+            for (int e = 1; e < VE; ++e) most[i] = fmaxf(most[i], y[i * VE + e]);
+          }
+          int room = cnt;
+#pragma unroll
+          for (int i = 0; i < NV; ++i) room += VE * __builtin_popcountll(__ballot(!(most[i] < tau)));
+          if (room <= kList) {
+            // few vectors hold candidates: they fit whatever there are
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+              if (__ballot(!(most[i] < tau)) == 0) continue;
+#pragma unroll
+              for (int e = 0; e < VE; ++e) {
+                const float z = y[i * VE + e];
+                if (__ballot(!(z < tau)) == 0) continue;
+                const int v = ((b * NV + i) * 64 + lane) * VE - off + e;
+                const key_t64 k = place_key(z, v);
+                const uint64_t m = __ballot(k > bar && v >= 0 && v < a.V);
+                if (m >> lane & 1) list[cnt + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = k;
+                cnt += __builtin_popcountll(m);
+              }
             }
+          } else {
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+              for (int e = 0; e < VE; ++e) {
+                float z = y[e];                              // (i is not unrolled: K copies of this would not fit the instruction cache)
+#pragma unroll
+                for (int j = 1; j < NV; ++j) z = i == j ? y[j * VE + e] : z;
+                const int v = ((b * NV + i) * 64 + lane) * VE - off + e;
+                const key_t64 k = place_key(z, v);
+                const uint64_t m = __ballot(k > bar && v >= 0 && v < a.V);
+                if (m == 0) continue;
+                if (m >> lane & 1) list[cnt + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = k;
+                cnt += __builtin_popcountll(m);
+                if (cnt + 64 > kList) raise();
+              }
+          }
+          if (cnt >= raise_at) raise();
         }
-        if (cnt >= raise_at) raise();
       }
     }
   }
