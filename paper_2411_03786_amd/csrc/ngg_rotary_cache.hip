@@ -535,10 +535,6 @@ __global__ __launch_bounds__(256) void kv_read_group_kernel(const CacheArgs a, i
   out += t0 * stride + h * (values ? a.v_head : a.k_head);
   const GroupSlots g(a, t0, m);
   const uint8_t *exps = values ? a.p.v_exp : a.p.k_exp;
-  auto wide = [&](CT x, unsigned e) -> T {                 // e: its exponent
-    if constexpr (sizeof(CT) == 1) return from_f32<T>(fp8_to_f32(x.bits) * exp_scale(e));
-    else return x;
-  };
   auto exponent = [&](int slot) -> unsigned {
     if constexpr (sizeof(CT) == 1) return exps[slot_head(a, slot, h) + slot % ps];
     else return 0;
@@ -576,17 +572,15 @@ __global__ __launch_bounds__(256) void kv_read_group_kernel(const CacheArgs a, i
       const int i = i0 + (tid & 63), d = i % (hd / 2) * 2;
       const Chunk c = chunk_at(g, i / (hd / 2));
       if (i >= work) continue;
-      const int first = c.first, pos = c.slot < 0 ? 0 : c.slot % ps;
-      const CT *src = (const CT *)a.p.v + (c.slot < 0 ? 0 : slot_head(a, c.slot, h)) * hd;
       struct alignas(2 * sizeof(T)) Two { T x[2]; };
-      if (c.last - first < 8) {
-        for (int t = first; t < c.last; ++t) {
-          const unsigned ex = c.slot < 0 ? 0 : exponent(c.slot + t - first);
-#pragma unroll
-          for (int x = 0; x < 2; ++x) rows[t][d + x] = wide(c.slot < 0 ? CT{} : src[page_v_offset<CT>(pos + t - first, d + x, hd)], ex);
-        }
+      if (c.slot < 0) {                                    // one token
+        *reinterpret_cast<Two *>(&rows[c.first][d]) = Two{};
         continue;
       }
+      // all eight positions are fetched, whichever of them are the chunk's: element e is of token t + e
+      const CT *src = (const CT *)a.p.v + slot_head(a, c.slot, h) * hd;
+      const int pos = c.slot % ps / 8 * 8, t = c.first - c.slot % 8;
+      auto wanted = [&](int e) { return t + e >= c.first && t + e < c.last; };
       if constexpr (sizeof(CT) == 1) {
         u32x2 y[2];
         get_values(src, pos, d, hd, y);
@@ -596,8 +590,9 @@ __global__ __launch_bounds__(256) void kv_read_group_kernel(const CacheArgs a, i
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float s = exp_scale(ex[e >> 2] >> (e & 3) * 8 & 0xff);
-          Two &to = *reinterpret_cast<Two *>(&rows[first + e][d]);
+          Two to;
           if (e & 1) two_wide<true>(w[e / 2], s, to.x); else two_wide<false>(w[e / 2], s, to.x);
+          if (wanted(e)) *reinterpret_cast<Two *>(&rows[t + e][d]) = to;
         }
       } else if constexpr (sizeof(CT) == 2) {
         u32x4 y[2];
@@ -605,7 +600,8 @@ __global__ __launch_bounds__(256) void kv_read_group_kernel(const CacheArgs a, i
         T x[2][8];
         __builtin_memcpy(x, y, sizeof x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) *reinterpret_cast<Two *>(&rows[first + e][d]) = Two{{x[0][e], x[1][e]}};
+        for (int e = 0; e < 8; ++e)
+          if (wanted(e)) *reinterpret_cast<Two *>(&rows[t + e][d]) = Two{{x[0][e], x[1][e]}};
       } else
 #pragma unroll
         for (int k = 0; k < 2; ++k)
@@ -613,7 +609,8 @@ __global__ __launch_bounds__(256) void kv_read_group_kernel(const CacheArgs a, i
           for (int e = 0; e < 8; e += 4) {
             const f32x4 x = *reinterpret_cast<const f32x4 *>(src + page_v_offset<CT>(pos + e, d + k, hd));
 #pragma unroll
-            for (int n = 0; n < 4; ++n) rows[first + e + n][d + k] = x[n];
+            for (int n = 0; n < 4; ++n)
+              if (wanted(e + n)) rows[t + e + n][d + k] = x[n];
           }
     }
   }
