@@ -807,17 +807,24 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
   write_row4<T>(a, b, t, hk * a.G + rr % a.G, dim, o, mm, ll);
 }
 
-// Rows of a tile, and with them the kernel: 16 and 32 rows are tree_stream_kernel's, 128 tree_block_kernel's (16-bit operands).  Short
-// lists take the smaller tiles, whose workgroups start and end quicker, though every tile reads the keys again (from the L2); the
-// rule goes by the positions of all (sequence, key head) together.  Measured with 32 heads of 128 (us; tiles of 16, 32, 128 rows):
-//   51 rows, 32 x 2048 positions 23, 25, 28; 32 x 8000: 41, 39, 42; 32 x 24000: 123, 100, 93
-//   128 rows, 64 x 500: 18, 28, 32; 64 x 2048: 37, 41, 44; 64 x 8000: 104, 100, 81
-//   244 rows, 64 x 500: 30, 25, 41; 64 x 2048: 64, 51, 58; 64 x 8000: 193, 151, 118
-static int tile_rows(int dtype, int rows, int64_t positions) {
+// Rows of a tile, and with them the kernel: 16 and 32 rows are tree_stream_kernel's, 128 tree_block_kernel's (16-bit operands).  Every
+// tile reads the keys again (from the L2), but small tiles are more workgroups, of more waves to a SIMD, that start and end quicker.
+// The rule goes by the scores of a call, positions of all (sequence, key head) times rows.  Measured at 16 bits (us; tiles of 16, 32
+// and 128 rows; lists, rows, positions, head_dim):
+//   24, 160, 1000, 64: 12, 16, 23 (3.8 M scores)       32, 51, 3850, 128: 29, 29, 32 (6.3 M)       32, 51, 12000, 128: 53, 46, 52 (20 M)
+//   96, 60, 3850, 128: 56, 48, 53 (22 M)               64, 472, 1000, 128: 60, 53, 56 (30 M)       24, 160, 12000, 64: 60, 50, 49 (46 M)
+//   128, 120, 3850, 128: 115, 83, 80 (59 M)            69, 356, 3850, 64: 138, 101, 69 (95 M)      64, 472, 3850, 128: 193, 149, 115 (116 M)
+// and in fp32 (16 and 32 rows): 96, 26, 4000, 128: 103, 118 (10 M); 64, 472, 400, 128: 117, 127 (13 M); 24, 244, 4000, 64: 88, 84 (24 M);
+// 64, 472, 4000, 128: 733, 713 (121 M).
+static int tile_rows(int dtype, int hd, int rows, int64_t lists, int64_t positions) {
   if (rows <= 16) return 16;
-  if (dtype == NGG_F32) return 32;
-  if (positions < 160 * 1024) return rows <= 128 ? 16 : 32;
-  return rows <= 32 || positions < 400 * 1024 ? 32 : 128;
+  const int64_t scores = lists * positions * rows;
+  if (dtype == NGG_F32) return scores < 16 << 20 ? 16 : 32;
+  if (scores >= 40 << 20) return rows <= 32 ? 32 : 128;
+  // (heads of 128 leave 16-row tiles three waves to a SIMD: from three workgroups to a compute unit on, larger tiles take fewer turns;
+  // 128 lists, 120 rows, 200 positions 17 and 15 us, 1000 positions 36 and 29; heads of 64 rather lose: 69, 356, 1000: 36 and 39)
+  if (scores >= 16 << 20 || (hd == 128 && lists * ((rows + 15) / 16) >= 768)) return 32;
+  return 16;
 }
 static int step_keys(int rows) { return rows <= 32 ? 128 : 64; }
 
@@ -828,7 +835,7 @@ static bool whole_lists(int64_t steps, int64_t workgroups) { return steps <= 8 |
 TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, int64_t max_positions) {
   TreePlan p;
   const int64_t positions = max_positions * B * Hkv;
-  p.rows = tile_rows(dtype, T * G, positions);
+  p.rows = tile_rows(dtype, hd, T * G, (int64_t)B * Hkv, max_positions);
   p.Z = (T * G + p.rows - 1) / p.rows;
   const int64_t steps = (max_positions + step_keys(p.rows) - 1) / step_keys(p.rows);
   p.whole = p.rows <= 32 && whole_lists(steps, (int64_t)B * Hkv * p.Z);

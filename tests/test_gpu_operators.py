@@ -374,7 +374,7 @@ class Case:
             self.kv.v_exps.fill_(255)
         self.table = ints(rng.permutation(pool)[:B * per].reshape(B, per))
         if wide:                                                        # a page list long enough for the kernels of long contexts
-            more = -(-(1 << 19) // (page * B * Hkv))
+            more = -(-max(1 << 19, (42 << 20) // (T * (H // Hkv))) // (page * B * Hkv))
             self.table = torch.cat([self.table, torch.full((B, more), -1, dtype=torch.int32, device="cuda")], 1)
         self.ks, self.vs = [], []
         for b in range(B):
