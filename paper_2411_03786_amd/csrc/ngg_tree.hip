@@ -4,9 +4,12 @@
 // is fetched once for all of them.  softmax(s) V is taken in one pass with a running maximum m and sum l: a tile of 32 keys turns
 // (m, l, O) into (m', l e^(m-m') + sum e^(s-m'), O e^(m-m') + e^(s-m') V), and the same rule joins parts of a list.
 //
-// The work of a call is one list: of every (sequence, key head) its steps of 32 NW keys, behind each other.  `ranges`
-// workgroups (per row tile) take equal shares of it, whatever the lengths of the sequences; a share that ends inside a (sequence,
-// head) leaves a partial result, at most one at either end, and tree_merge_kernel joins those.  The lengths are read on the device.
+// The work of a call is one list: of every (sequence, key head) its steps of 128 (tree_block_kernel: 64) keys, behind each other.
+// `ranges` workgroups (per row tile) take equal shares of it, whatever the lengths of the sequences; a share that ends inside a
+// (sequence, head) leaves a partial result, at most one at either end, and tree_merge_kernel joins those.  Short lists go whole to a
+// workgroup each instead.  The lengths are read on the device.
+//
+// Up to some 200 rows to a key head the keys and values are what a call costs (HBM), above that the products are.
 #include "ngg_operators.h"
 #include "ngg_epilogues.h"
 
@@ -223,7 +226,10 @@ __device__ __forceinline__ void write_row4(const TreeArgs &a, int b, int t, int 
 }
 
 // One workgroup: one row tile (16 QF rows) over its share of the list.  The waves take the tiles of 32 keys of a (sequence, head) in
-// turn, each straight from memory, and are joined through LDS at its end.
+// turn, each straight from memory in the order that the 16x16x32 products want (a tile is one read of 64 lanes times 16 bytes after the
+// other), and are joined through LDS at its end.  Nothing waits for another wave before that, so that few rows stream at the rate of
+// the memory: 32 single tokens of 8 key heads of 128 over up to 8191 positions (619 MB at 16 bits) 103 us, 6.0 TB/s.  The scores come out
+// transposed (keys by rows), so that a lane holds eight neighbouring keys of one row, its operand of the second product.
 // NT: keys that nobody reads again stay out of the caches.
 template <typename T, typename CT, int HD, int QF, bool NT>
 __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
@@ -427,6 +433,11 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
 
 // Row tiles of more than 32 rows on 16-bit operands: the waves of a workgroup own 32 rows each and share the keys, two tiles (64 keys)
 // per step, through LDS, where 8-bit tiles arrive widened (keys with their powers of two; those of the values go to the probabilities).
+// The next step's tiles are on their way meanwhile (16 bits: straight to LDS).  Bound by the issue of products, exponentials and LDS
+// reads together: eight trees of 64 tokens, 32 heads of 128, over 32000 positions each at 8 bits 393 us, 683 TFLOP/s, one over 390000
+// positions 733 (a library product of 16 bits 1230); ragged trees leave waves without rows: eight of up to 61 tokens over up to 32000
+// positions 248 us, 500 TFLOP/s.  64 rows a wave, eight waves, two tiles in turn, the softmax of one behind the products of the other
+// and raised wave priorities did not pay.
 // 32x32x16 products: row 8 j + 4 h + i of a key tile is key 16 (j % 2) + 8 h + 4 (j / 2) + i, so lane (row, h) ends up with keys
 // 16 u + 8 h .. + 7 of every 16, its operand of the second product.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -761,8 +772,9 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
   }
 }
 
-// Joins the parts of every (sequence, head) that more than one workgroup worked on, in their order.  A thread takes four elements of a
-// row, a workgroup 256 of those.
+// Joins the parts of every (sequence, head) that more than one workgroup worked on, in their order: m = max m_i, sums and outputs times
+// 2^(m_i - m).  A thread takes four elements of a row, a workgroup 256 of those.  Bound by its chain of loads: 4 us with 32 heads of 51
+// rows, 10 with 64 of 244.
 template <typename T, int HD, int ROWS, int KS>
 __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
   __shared__ int pre[NGG_TREE_MAX + 1];
