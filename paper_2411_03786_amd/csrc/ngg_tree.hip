@@ -435,8 +435,8 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
 // per step, through LDS, where 8-bit tiles arrive widened (keys with their powers of two; those of the values go to the probabilities).
 // The next step's tiles are on their way meanwhile (16 bits: straight to LDS).  Bound by the issue of products, exponentials and LDS
 // reads together: eight trees of 64 tokens, 32 heads of 128, over 32000 positions each at 8 bits 393 us, 683 TFLOP/s, one over 390000
-// positions 733 (a library product of 16 bits 1230); ragged trees leave waves without rows: eight of up to 61 tokens over up to 32000
-// positions 248 us, 500 TFLOP/s.  64 rows a wave, eight waves, two tiles in turn, the softmax of one behind the products of the other
+// positions 733 (a library product of 16 bits 1230); ragged trees leave waves without rows: eight of 38 to 61 tokens over
+// 13531 to 32000 positions 250 us, 550 TFLOP/s.  64 rows a wave, eight waves, two tiles in turn, the softmax of one behind the products of the other
 // and raised wave priorities did not pay.
 // 32x32x16 products: row 8 j + 4 h + i of a key tile is key 16 (j % 2) + 8 h + 4 (j / 2) + i, so lane (row, h) ends up with keys
 // 16 u + 8 h .. + 7 of every 16, its operand of the second product.
