@@ -842,7 +842,10 @@ static int step_keys(int rows) { return rows <= 32 ? 128 : 64; }
 
 // Short lists go whole to a workgroup each: no parts, no merge.  Measured (us, whole and shared): 32 heads, 51 rows, 800 positions
 // 13.5 and 17.9, 1300 positions 17.5 and 20.0, 1900 positions 22.8 and 18.8; 256 heads of one row, 1900 positions 41.5 and 46.9.
-static bool whole_lists(int64_t steps, int64_t workgroups) { return steps <= 8 || (steps <= 12 && workgroups >= 128) || (steps <= 16 && workgroups >= 256); }
+// (2^23 workgroups: what a launch can hold of them.)
+static bool whole_lists(int64_t steps, int64_t workgroups) {
+  return workgroups <= 1 << 23 && (steps <= 8 || (steps <= 12 && workgroups >= 128) || (steps <= 16 && workgroups >= 256));
+}
 
 TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, int64_t max_positions) {
   TreePlan p;
