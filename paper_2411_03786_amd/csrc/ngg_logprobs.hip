@@ -50,12 +50,7 @@ __device__ __forceinline__ Sums join(Sums a, Sums b) {
 }
 
 // A wave's maximum and sum, on every lane: inside rows of 16 lanes by data-parallel moves, the four rows by scalars
-template <int CTRL>
-__device__ __forceinline__ float moved(float x) {
-  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true));
-}
 __device__ __forceinline__ float lane_value(float x, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); }
-constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kHalfMirror = 0x141, kMirror = 0x140;
 __device__ __forceinline__ float wave_max(float x) {
   x = fmaxf(x, moved<kXor1>(x));
   x = fmaxf(x, moved<kXor2>(x));

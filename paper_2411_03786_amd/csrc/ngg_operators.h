@@ -48,6 +48,13 @@ template <typename CT> __device__ __forceinline__ size_t page_v_offset(int pos, 
   else return v_offset(pos, dim, hd, sizeof(CT));
 }
 
+// The value of another lane of the row of 16: lane ^ 1, lane ^ 2, 7 - lane of eight, 15 - lane.  Four such steps join a row.
+constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kHalfMirror = 0x141, kMirror = 0x140;
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+
 // a head's power of two from its stored exponent (1 .. 254)
 __device__ __forceinline__ float exp_scale(unsigned e) { return __uint_as_float(e << 23); }
 __device__ __forceinline__ float fp8_to_f32(unsigned bits) { return __builtin_amdgcn_cvt_f32_fp8(bits, 0); }

@@ -260,7 +260,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(const CacheArgs a) {
 // Runs of tokens.  One workgroup per (32 tokens, head, keys or values): the rows pass through LDS, so that they are read and written
 // whole, and eight positions of a value's dimension lie in one store where the tokens' slots follow each other (a prompt, a tree);
 // others go element by element.  HBM bound: 16000 tokens of 8 heads of 128 are written in 22 us and read in 21 at 16 bits (6 TB/s,
-// reading and writing), in 27 and 21 at 8 bits (3.7 and 4.7 TB/s; there the conversion is what is left).
+// reading and writing), in 26 and 21 at 8 bits (3.8 and 4.7 TB/s; there the conversion is what is left).
 constexpr int kGroup = 32, kRowPad = 16;                   // tokens of a workgroup; bytes behind a row in LDS (banks)
 
 // A workgroup's tokens t0 .. t0 + m - 1 (none: false).  Groups begin where eights of positions do if all slots follow each other, so
@@ -434,7 +434,11 @@ __global__ __launch_bounds__(256) void kv_write_group_kernel(const CacheArgs a, 
 #pragma unroll
         for (int e = 0; e < VE; ++e) top = fmaxf(top, fabsf(x[e]) < __builtin_inff() ? fabsf(x[e]) : 0.0f);
       }
-      for (int o = 1; o < per; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+      top = fmaxf(top, moved<kXor1>(top));                 // 4 to 32 threads hold a row
+      top = fmaxf(top, moved<kXor2>(top));
+      if (per > 4) top = fmaxf(top, moved<kHalfMirror>(top));
+      if (per > 8) top = fmaxf(top, moved<kMirror>(top));
+      if (per > 16) top = fmaxf(top, __shfl_xor(top, 16));
       const unsigned exp = fp8_exponent(top);
       const float un = exp_unscale(exp);
       if (i % per == 0) ex[i / per] = (uint8_t)exp;
