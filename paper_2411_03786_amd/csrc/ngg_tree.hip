@@ -840,11 +840,15 @@ static int tile_rows(int dtype, int hd, int rows, int64_t lists, int64_t positio
 }
 static int step_keys(int rows) { return rows <= 32 ? 128 : 64; }
 
-// Short lists go whole to a workgroup each: no parts, no merge.  Measured (us, whole and shared): 32 heads, 51 rows, 800 positions
-// 13.5 and 17.9, 1300 positions 17.5 and 20.0, 1900 positions 22.8 and 18.8; 256 heads of one row, 1900 positions 41.5 and 46.9.
+// Short lists go whole to a workgroup each: no parts, no merge; the longer, the more workgroups there have to be, since few leave the
+// chip idle, and the shorter the longer a step takes.  Measured with heads of 128 (us, whole and shared; workgroups, steps):
+//   16 bits: 8 to 48, 6: 12.2, 12.5; 8: 14.1, 12.6.  128, 8: 14.4, 15.4; 12: 18.2, 16.6.  256, 16: 24.2, 29.1; 512, 16: 84, 88
+//   fp32: 8 to 48, 2: 12, 15; 4: 18, 16; 8: 31, 17.  128, 6: 25.9, 25.5; 8: 33, 27.  256, 16: 57, 65; 512, 16: 160, 162
 // (2^23 workgroups: what a launch can hold of them.)
-static bool whole_lists(int64_t steps, int64_t workgroups) {
-  return workgroups <= 1 << 23 && (steps <= 8 || (steps <= 12 && workgroups >= 128) || (steps <= 16 && workgroups >= 256));
+static bool whole_lists(int dtype, int64_t steps, int64_t workgroups) {
+  const bool wide = dtype == NGG_F32;
+  const int most = workgroups >= 256 ? 16 : workgroups >= 128 ? (wide ? 6 : 9) : wide ? 3 : 6;
+  return steps <= most && workgroups <= 1 << 23;
 }
 
 TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, int64_t max_positions) {
@@ -853,7 +857,7 @@ TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, i
   p.rows = tile_rows(dtype, hd, T * G, (int64_t)B * Hkv, max_positions);
   p.Z = (T * G + p.rows - 1) / p.rows;
   const int64_t steps = (max_positions + step_keys(p.rows) - 1) / step_keys(p.rows);
-  p.whole = p.rows <= 32 && whole_lists(steps, (int64_t)B * Hkv * p.Z);
+  p.whole = p.rows <= 32 && whole_lists(dtype, steps, (int64_t)B * Hkv * p.Z);
   // A single tile of 16 rows reads the keys once.  Past what the last cache holds, non-temporal loads: 32 single tokens over 16000 positions 332 us
   // instead of 372; below, a list that is read again soon is better kept (1900 positions 46.9, non-temporal 49.7).
   const int64_t bytes = 2 * positions * hd * (cache == NGG_F32 ? 4 : cache == NGG_BF16 ? 2 : 1);
