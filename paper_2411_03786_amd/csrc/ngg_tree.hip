@@ -92,9 +92,12 @@ __device__ __forceinline__ void step_totals(const TreeArgs &a, int *pre) {
   __syncthreads();
 }
 
-// Steps of a share of the list: as many shares as workgroups were launched for, but of 256 keys at least
+// Steps of a share of the list: as many shares as workgroups were launched for, but of 256 keys at least where there are many (us with
+// one step of 128 keys and with two, 16 bits: 88 steps in all 12.4, 14.4; 240 steps 11.4, 12.1; 384 steps 15.9, 13.4; 504 steps 21.1, 18.2)
 template <int KS>
-__device__ __forceinline__ int share_steps(const TreeArgs &a, int total) { return max((int)((unsigned)(total + a.ranges - 1) / (unsigned)a.ranges), 256 / KS); }
+__device__ __forceinline__ int share_steps(const TreeArgs &a, int total) {
+  return max((int)((unsigned)(total + a.ranges - 1) / (unsigned)a.ranges), KS == 128 && total < 256 ? 1 : 256 / KS);
+}
 
 // A workgroup's place and share of the list, one (sequence, head) after the other.  Whole numbers of 32 bits (the host sees to that):
 // what runs once costs a launch its instruction fetches.
@@ -842,12 +845,14 @@ static int step_keys(int rows) { return rows <= 32 ? 128 : 64; }
 
 // Short lists go whole to a workgroup each: no parts, no merge; the longer, the more workgroups there have to be, since few leave the
 // chip idle, and the shorter the longer a step takes.  Measured with heads of 128 (us, whole and shared; workgroups, steps):
-//   16 bits: 8 to 48, 6: 12.2, 12.5; 8: 14.1, 12.6.  128, 8: 14.4, 15.4; 12: 18.2, 16.6.  256, 16: 24.2, 29.1; 512, 16: 84, 88
-//   fp32: 8 to 48, 2: 12, 15; 4: 18, 16; 8: 31, 17.  128, 6: 25.9, 25.5; 8: 33, 27.  256, 16: 57, 65; 512, 16: 160, 162
+//   16 bits: 8 to 48, 4: 10.4, 11.2-11.8; 6: 12.2, 11.3-12.0; 8: 14.1, 11.2-12.9.  128, 8: 14.4, 15.4; 12: 18.2, 16.6.
+//     256, 16: 24.2, 29.1; 512, 16: 84, 88
+//   fp32: 8 to 48, 2: 12.5, 12.2-13.3; 3: 15.6, 12.6-13.3; 8: 32, 12.3-17.8.  128, 6: 25.9, 25.5; 8: 33, 27.  256, 16: 57, 65;
+//     512, 16: 160, 162
 // (2^23 workgroups: what a launch can hold of them.)
 static bool whole_lists(int dtype, int64_t steps, int64_t workgroups) {
   const bool wide = dtype == NGG_F32;
-  const int most = workgroups >= 256 ? 16 : workgroups >= 128 ? (wide ? 6 : 9) : wide ? 3 : 6;
+  const int most = workgroups >= 256 ? 16 : workgroups >= 128 ? (wide ? 6 : 9) : wide ? 2 : 5;
   return steps <= most && workgroups <= 1 << 23;
 }
 
@@ -863,7 +868,7 @@ TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, i
   const int64_t bytes = 2 * positions * hd * (cache == NGG_F32 ? 4 : cache == NGG_BF16 ? 2 : 1);
   p.stream = p.rows == 16 && p.Z == 1 && bytes > (int64_t)400 << 20;
   const int64_t want = (512 + p.Z - 1) / p.Z, r = p.whole ? (int64_t)B * Hkv : std::max<int64_t>(1, std::min(want, steps * B * Hkv));
-  p.ranges = (int)(p.whole ? r : r >= 8 ? r / 8 * 8 : r);
+  p.ranges = (int)(p.whole || r < 8 ? r : r < want ? (r + 7) / 8 * 8 : r / 8 * 8);   // eights: one for each die; up, if a step each is to be had
   const size_t rows = p.whole ? 0 : (size_t)p.ranges * p.Z * 2 * p.rows;
   p.o_bytes = rows * hd * 4;
   p.ml_bytes = rows * 8;
