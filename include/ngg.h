@@ -423,7 +423,9 @@ ngg_status ngg_tree_mask(const int32_t *parents, int32_t n, uint64_t *mask, int3
  * sees nothing, and a token behind the sequence's own tree_lens[b], gets zeros and an lse of minus infinity.
  * Bits of positions, lengths and pages out of range: negative lengths count as 0, tree_lens is cut to
  * `tree`, positions beyond the page list and those on a page outside the pool are not seen.  What lies behind the last
- * position, or is masked, has no influence, NaN and infinities included. */
+ * position, or is masked, has no influence, NaN and infinities included.
+ * The lengths are read on the device; the launch is planned for max_pages * page_size positions.  A page list no wider than the longest
+ * sequence at hand (its first columns, by max_pages and pages_batch) serves short sequences best. */
 typedef struct {
   const void *q;
   void *out;

@@ -119,7 +119,8 @@ def tree_mask(parents):
 
 def tree_attention(q, kv, pages, context_lens, mask=None, tree_lens=None, scale=None, out=None, want_lse=False, workspace=None, stream=None):
     """ngg_tree_attention: q [batch, tree, heads, head_dim] over kv (KVPages) through pages (int32 [batch, max_pages]) behind
-    context_lens cached positions (int32 [batch]).  mask: int64 [tree, words] for all or [batch, tree, words], None for a chain; tree_lens: int32
+    context_lens cached positions (int32 [batch]); the launch is planned for all of pages, of which its first columns do where no
+    sequence is longer.  mask: int64 [tree, words] for all or [batch, tree, words], None for a chain; tree_lens: int32
     [batch] or None; scale: 1 / sqrt(head_dim) by default.  workspace: a uint8 tensor kept by the caller, or None to take one per
     call.  Returns out, or (out, lse) with lse float32 [batch, tree, heads]."""
     if stream is not None:

@@ -81,6 +81,7 @@ class TreeDecoder:
         # a sequence's pages lie scattered over the pool, as they do after some serving
         self.pages = torch.randperm(batch * per, generator=torch.Generator().manual_seed(seed)).view(batch, per).int().cuda()
         self.lens = torch.zeros(batch, dtype=torch.int32, device="cuda")          # cached positions
+        self.cached = [0] * batch                                                 # the same on the host
 
     @staticmethod
     def norm(x):
@@ -100,13 +101,17 @@ class TreeDecoder:
         place = self.lens[:, None] + torch.arange(T, dtype=torch.int32, device="cuda")
         if tree_lens is not None:
             place = torch.where(torch.arange(T, device="cuda") < tree_lens[:, None], place, -1)
+        longest = max(self.cached) + T
+        if longest > self.pages.shape[1] * self.page:
+            raise ValueError(f"{longest} positions in pages for {self.pages.shape[1] * self.page}")
+        pages = self.pages[:, :-(-longest // self.page)]                # the call is planned for these
         slots, pos = self.slots(place), (self.lens[:, None] + depth).int().flatten()
         x = self.embed[tokens.flatten().long()]
         for w, kv in zip(self.layers, self.kv):
             q, k, v = (self.norm(x).to(self.dtype) @ w["qkv"]).view(B * T, H + 2 * Hkv, hd).split((H, Hkv, Hkv), 1)
             ngg.rotary(self.rope, pos, q, out=q)
             kv.write(k, v, slots, rope=self.rope, positions=pos)
-            a = ngg.tree_attention(q.unflatten(0, (B, T)), kv, self.pages, self.lens, mask=mask, tree_lens=tree_lens)
+            a = ngg.tree_attention(q.unflatten(0, (B, T)), kv, pages, self.lens, mask=mask, tree_lens=tree_lens)
             x = x + a.reshape(B * T, H * hd) @ w["proj"]
             y = self.norm(x).to(self.dtype)
             x = x + (torch.nn.functional.silu(y @ w["gate"]) * (y @ w["up"])) @ w["down"]
@@ -118,6 +123,7 @@ class TreeDecoder:
             part = prompts[:, at:min(at + piece, prompts.shape[1] - 1)]
             self.forward(part, torch.arange(part.shape[1], device="cuda"))
             self.lens += part.shape[1]
+            self.cached = [n + part.shape[1] for n in self.cached]
 
     def keep(self, paths):
         """Keeps of every sequence's tree the nodes of its path (root first, rising): they move behind the context."""
@@ -129,6 +135,7 @@ class TreeDecoder:
         for kv in self.kv:
             kv.write(*kv.read(src), to)
         self.lens += there.sum(1, dtype=torch.int32)
+        self.cached = [c + len(p) for c, p in zip(self.cached, paths)]
 
     def step(self, last, rows):
         """One verify step: last tokens, draft rows of every sequence -> (new tokens, their log probabilities) per sequence."""
@@ -170,6 +177,7 @@ class TreeDecoder:
         """n_new greedy tokens behind each prompt (lists of equal length).  draft(sequence index, tokens) -> rows.  Returns the
         sequences' new tokens, their log probabilities, and the steps taken."""
         self.lens.zero_()
+        self.cached = [0] * self.batch
         self.prefill(torch.tensor(prompts, dtype=torch.int32, device="cuda"))
         seqs, logps, steps = [list(p) for p in prompts], [[] for _ in prompts], 0
         while min(map(len, logps)) < n_new:

@@ -87,6 +87,14 @@ def test_the_command(monkeypatch, capsys):
     assert steps[0] == 70 and steps[1] < 35 and lines[2] == "3 of 3 sequences alike"
 
 
+def test_a_tree_beyond_the_pages_is_refused():
+    dec = tv.TreeDecoder(2, 1, 2, 1, 32, 100, 64, cache="f32", page=32, d_ffn=64)
+    dec.prefill(torch.zeros(2, 61, dtype=torch.int32, device="cuda"))
+    assert len(dec.step([1, 2], [[[3, 4, 5]], []])) == 2                 # 60 cached, trees of up to four
+    with pytest.raises(ValueError):
+        dec.step([1, 2], [[[3, 4, 5, 6]], []])
+
+
 def test_draft_trees_share_their_beginnings():
     tokens, parents, children = tv.draft_tree(9, [[1, 2, 3], [1, 2, 4], [5], [1]])
     assert tokens == [9, 1, 2, 3, 4, 5] and parents == [-1, 0, 1, 2, 2, 0]
