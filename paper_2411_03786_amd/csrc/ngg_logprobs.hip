@@ -49,15 +49,7 @@ __device__ __forceinline__ Sums join(Sums a, Sums b) {
   return {m, a.s + b.s, a.t + b.t};
 }
 
-// A wave's maximum and sum, on every lane: inside rows of 16 lanes by data-parallel moves, the four rows by scalars
-__device__ __forceinline__ float lane_value(float x, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); }
-__device__ __forceinline__ float wave_max(float x) {
-  x = fmaxf(x, moved<kXor1>(x));
-  x = fmaxf(x, moved<kXor2>(x));
-  x = fmaxf(x, moved<kHalfMirror>(x));
-  x = fmaxf(x, moved<kMirror>(x));
-  return fmaxf(fmaxf(lane_value(x, 0), lane_value(x, 16)), fmaxf(lane_value(x, 32), lane_value(x, 48)));
-}
+// A wave's sum, on every lane, as wave_max does it
 __device__ __forceinline__ float wave_sum(float x) {
   x += moved<kXor1>(x);
   x += moved<kXor2>(x);
@@ -464,7 +456,6 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(const ScoreArgs a, i
   __shared__ Sums part[4];
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const T *x = (const T *)a.x + (int64_t)r * a.row_stride;
-  const float c = a.scale * kLog2e;
   const key_t64 *wl = (const key_t64 *)((const char *)a.ws + ((size_t)a.N * slices * sizeof(Sums) + 15) / 16 * 16) + (size_t)r * slices * a.top;
   Sums q = no_sums();
   if (lane < slices) q = ((const Sums *)a.ws)[(size_t)r * slices + lane];

@@ -55,6 +55,16 @@ __device__ __forceinline__ float moved(float x) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true));
 }
 
+__device__ __forceinline__ float lane_value(float x, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); }
+// A wave's maximum, on every lane: inside rows of 16 lanes by data-parallel moves, the four rows by scalars
+__device__ __forceinline__ float wave_max(float x) {
+  x = fmaxf(x, moved<kXor1>(x));
+  x = fmaxf(x, moved<kXor2>(x));
+  x = fmaxf(x, moved<kHalfMirror>(x));
+  x = fmaxf(x, moved<kMirror>(x));
+  return fmaxf(fmaxf(lane_value(x, 0), lane_value(x, 16)), fmaxf(lane_value(x, 32), lane_value(x, 48)));
+}
+
 // a head's power of two from its stored exponent (1 .. 254)
 __device__ __forceinline__ float exp_scale(unsigned e) { return __uint_as_float(e << 23); }
 __device__ __forceinline__ float fp8_to_f32(unsigned bits) { return __builtin_amdgcn_cvt_f32_fp8(bits, 0); }

@@ -169,12 +169,6 @@ void launch_rotary(int dtype, const RotaryArgs &a, hipStream_t s) {
   else launch_rotary_type<bf16_t>(a, s);
 }
 
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
-  return x;
-}
-
 // Element d of a token's key, rotated and rounded to its own type as rotary_kernel leaves it.
 template <typename T>
 __device__ __forceinline__ float rotated(const CacheArgs &a, const T *row, int t, int d) {

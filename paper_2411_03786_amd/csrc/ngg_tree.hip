@@ -236,7 +236,7 @@ __device__ __forceinline__ void write_row4(const TreeArgs &a, int b, int t, int 
 // NT: keys that nobody reads again stay out of the caches.
 template <typename T, typename CT, int HD, int QF, bool NT>
 __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
-  constexpr int NW = 4, DS = HD / 32, DF = HD / 16, TILE = 32 * HD, ROWS = 16 * QF, KS = 32 * NW;
+  constexpr int NW = 4, DS = HD / 32, DF = HD / 16, ROWS = 16 * QF, KS = 32 * NW;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   float *lo = reinterpret_cast<float *>(smem);             // [NW][QF][DF][64][4]
   float *lml = lo + NW * QF * DF * 256;                    // [NW][QF][16][2]
