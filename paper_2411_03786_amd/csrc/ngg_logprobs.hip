@@ -30,12 +30,13 @@ __device__ __forceinline__ float key_value(unsigned k) { return __uint_as_float(
 __device__ __forceinline__ key_t64 place_key(float x, int v) { return (key_t64)order_key(x) << 32 | (unsigned)~v; }
 __device__ __forceinline__ int key_place(key_t64 k) { return (int)~(unsigned)k; }
 
-// Sums in the base-2 domain against a reference m: s = sum 2^d, t = sum 2^d d with d = x c - m, c = scale log2(e).  m is a whole number
-// wherever that is exact (up to 2^24), so that d is rounded once and a change of reference costs nothing.  A row that leaves s = 0
-// (nothing above -1e38), NaN or m >= 1e38 is summed again by odd_row.
+// Sums in the base-2 domain against a reference m: s = sum 2^d, t = sum 2^d d with d = x c - m, c = scale log2(e).  m is a whole number,
+// so that d is rounded once and a change of reference costs nothing; that holds to 2^24 either way.  Beyond, x c and m are whole steps of
+// an fp32 number apart and 2^d is anything, infinity included: a row with a reference above 2^24, or that leaves s = 0 (nothing near
+// -2^24 or above, where references begin) or NaN, is summed again by odd_row.
 struct Sums { float m, s, t; };
-constexpr float kHuge = 1e38f;
-__device__ __forceinline__ Sums no_sums() { return {-kHuge, 0.0f, 0.0f}; }
+constexpr float kFar = 16777216.0f;
+__device__ __forceinline__ Sums no_sums() { return {-kFar, 0.0f, 0.0f}; }
 __device__ __forceinline__ void move_to(Sums &a, float m) {
   const float d = a.m - m, f = __builtin_amdgcn_exp2f(d);
   a.t = f > 0.0f ? f * (a.t + a.s * d) : 0.0f;
@@ -140,14 +141,15 @@ __device__ __forceinline__ unsigned first_bar(const unsigned (&k)[4], int n) {
   return t;
 }
 
-// A row whose sums the fast way cannot hold, by the definition: m = max x, then the sums against it.  256 threads.
+// A row whose sums the fast way cannot hold, by the definition: the largest logit, then the sums of differences from it, which are
+// taken before they are scaled: exact near 0 however large the logits are (and halved, so that none overflows).  256 threads.
 template <typename T>
 __device__ __forceinline__ Sums odd_row(const ScoreArgs &a, const T *x, Sums *part) {
   const int tid = threadIdx.x;
   float m = -__builtin_inff();
   bool nan = false;
   for (int v = tid; v < a.V; v += 256) {
-    const float y = to_f32(x[v]) * a.scale;
+    const float y = to_f32(x[v]);
     m = fmaxf(m, y);
     nan |= y != y;
   }
@@ -159,7 +161,7 @@ __device__ __forceinline__ Sums odd_row(const ScoreArgs &a, const T *x, Sums *pa
   float s = nan ? __builtin_nanf("") : 0.0f, t = 0.0f;
   if (m > -__builtin_inff())
     for (int v = tid; v < a.V; v += 256) {
-      const float d = (to_f32(x[v]) * a.scale - m) * kLog2e, p = __builtin_amdgcn_exp2f(d);
+      const float d = (0.5f * to_f32(x[v]) - 0.5f * m) * a.scale * (2.0f * kLog2e), p = __builtin_amdgcn_exp2f(d);
       s += p;                                              // NaN from plus infinity less itself
       if (p > 0.0f) t += p * d;
     }
@@ -167,7 +169,7 @@ __device__ __forceinline__ Sums odd_row(const ScoreArgs &a, const T *x, Sums *pa
   t = wave_sum(t);
   if (tid % 64 == 0) { part[tid / 64].s = s; part[tid / 64].t = t; }
   __syncthreads();
-  return {m, part[0].s + part[1].s + part[2].s + part[3].s, part[0].t + part[1].t + part[2].t + part[3].t};
+  return {m * a.scale, part[0].s + part[1].s + part[2].s + part[3].s, part[0].t + part[1].t + part[2].t + part[3].t};
 }
 
 // Results of a row from its sums.  256 threads.
@@ -175,7 +177,7 @@ struct RowResult { float lse; bool bad; };
 template <typename T>
 __device__ __forceinline__ RowResult finish_row(const ScoreArgs &a, int r, Sums q, const T *x, Sums *part) {
   RowResult o;
-  const bool odd = !(q.s > 0.0f && q.m < kHuge);           // (the same for every thread)
+  const bool odd = !(q.s > 0.0f && q.m <= kFar);            // (the same for every thread)
   if (odd) q = odd_row(a, x, part);
   o.bad = q.s != q.s;
   const float l2 = __builtin_log2f(q.s);
@@ -187,6 +189,7 @@ __device__ __forceinline__ RowResult finish_row(const ScoreArgs &a, int r, Sums 
   return o;
 }
 __device__ __forceinline__ float logp(const ScoreArgs &a, const RowResult &o, float x) {
+#pragma clang fp contract(off)                             // (the product is rounded as the one in lse is)
   const float y = x * a.scale;
   return y == -__builtin_inff() && !o.bad ? y : y - o.lse;
 }

@@ -1,0 +1,41 @@
+"""Corners of the operators of a batched tree verification on the GPU.  Needs an MI355X."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2411_03786_amd as ngg
+from test_gpu_operators import DT, check_scores, ints, randn, score64
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,scale,size", [(300, 5e8, 20.0), (33000, 5e8, 20.0), (33000, 1e7, 300.0), (5000, 1.0, 3e9), (5000, 1.0, 1e30), (33000, 0.5, 1e38), (700, 1e30, 1.0)])
+def test_token_logprobs_of_large_scores(dtype, V, scale, size):
+    """Finite rows have finite sums whatever their size.  x * scale is off by 2^-24 of itself, a difference of two and a sum of up to V terms by a
+    few of those."""
+    x = randn(9, V, seed=V)
+    x = (x / x.abs().amax() * size).to(DT[dtype])
+    targets, top = np.array([[0, V - 1, V // 2]] * 9), min(V, 7)
+    got = ngg.token_logprobs(x, ints(targets), top_n=top, scale=scale)
+    lp, ent, lse, ids, tlp = score64(x, targets, top, scale)
+    big = np.abs(lse) + 4
+    assert torch.isfinite(got.lse).all() and (np.abs(got.lse.double().cpu().numpy() - lse) <= 2.0 ** -22 * big).all()
+    assert torch.isfinite(got.entropy).all() and (np.abs(got.entropy.double().cpu().numpy() - ent) <= (V / 64 + 64) * 2.0 ** -22).all()
+    assert (got.top_ids.cpu().numpy() == ids).all() and (got.top_logprobs[:, 0] > -1.0).all()
+    for g, w in ((got.logprobs, lp), (got.top_logprobs, tlp)):
+        assert (np.abs(g.double().cpu().numpy() - w) <= 2.0 ** -22 * (np.abs(w) + big[:, None])).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("low", [-1e7, -1e9, -1e12, -1e30])
+def test_token_logprobs_of_rows_with_low_parts(dtype, low):
+    """Ruled-out tokens at a low number instead of minus infinity, in runs longer than what a wave takes at a time, and rows of nothing else."""
+    x = randn(6, 40003, seed=3)
+    x[0, :20000] = low
+    x[1, 20000:] = low
+    x[2, 5000:39000] = low
+    x[3] = low
+    x[4] += low
+    x[5, ::2] = low
+    check_scores(x.to(DT[dtype]), [[0, 39999, 20000]] * 6, 5, 1.0)
