@@ -454,7 +454,9 @@ ngg_status ngg_tree_attention(const ngg_kv_pages *pages, const ngg_tree_args *ar
  * Ruled-out tokens (logits of minus infinity) have no share in the sums.  A target below 0 gives 0 (no token), one
  * beyond the vocabulary NaN.  A row whose logits are all minus infinity has an lse and log probabilities of minus infinity and entropy 0; a row
  * with NaN or plus infinity has NaN in lse, entropy and log probabilities.  Outputs are [n_rows][..] contiguous; lse, entropy and, without
- * targets or top_n, the others may be NULL.  Sums are held in 32 bits.  0 <= top_n <= min(64, vocab), 0 <= n_targets <= 64, vocab <= 2^30. */
+ * targets or top_n, the others may be NULL.  Sums are held in 32 bits.  No log probability is above 0 and no entropy below: a
+ * log probability is the difference from the row's largest logit less the logarithm of a sum near 1, not one of two large numbers.
+ *  0 <= top_n <= min(64, vocab), 0 <= n_targets <= 64, vocab <= 2^30. */
 typedef struct {
   const void *logits;          /* [n_rows][vocab] */
   int64_t row_stride;

@@ -32,11 +32,11 @@ __device__ __forceinline__ int key_place(key_t64 k) { return (int)~(unsigned)k; 
 
 // Sums in the base-2 domain against a reference m: s = sum 2^d, t = sum 2^d d with d = x c - m, c = scale log2(e).  m is a whole number,
 // so that d is rounded once and a change of reference costs nothing; that holds to 2^24 either way.  Beyond, x c and m are whole steps of
-// an fp32 number apart and 2^d is anything, infinity included: a row with a reference above 2^24, or that leaves s = 0 (nothing near
-// -2^24 or above, where references begin) or NaN, is summed again by odd_row.
-struct Sums { float m, s, t; };
+// an fp32 number apart and 2^d is anything, infinity included: a row with a reference above 2^24, or that leaves s near 0 (nothing at
+// -2^24 or above, where references begin) or NaN, is summed again by odd_row.  best: the largest x itself.
+struct Sums { float m, s, t, best; };
 constexpr float kFar = 16777216.0f;
-__device__ __forceinline__ Sums no_sums() { return {-kFar, 0.0f, 0.0f}; }
+__device__ __forceinline__ Sums no_sums() { return {-kFar, 0.0f, 0.0f, -__builtin_inff()}; }
 __device__ __forceinline__ void move_to(Sums &a, float m) {
   const float d = a.m - m, f = __builtin_amdgcn_exp2f(d);
   a.t = f > 0.0f ? f * (a.t + a.s * d) : 0.0f;
@@ -47,7 +47,7 @@ __device__ __forceinline__ Sums join(Sums a, Sums b) {
   const float m = fmaxf(a.m, b.m);
   move_to(a, m);
   move_to(b, m);
-  return {m, a.s + b.s, a.t + b.t};
+  return {m, a.s + b.s, a.t + b.t, fmaxf(a.best, b.best)};
 }
 
 // A wave's sum, on every lane, as wave_max does it
@@ -64,6 +64,7 @@ __device__ __forceinline__ Sums wave_sums(Sums a) {
   move_to(a, wave_max(a.m));
   a.s = wave_sum(a.s);
   a.t = wave_sum(a.t);
+  a.best = wave_max(a.best);
   return a;
 }
 
@@ -169,29 +170,37 @@ __device__ __forceinline__ Sums odd_row(const ScoreArgs &a, const T *x, Sums *pa
   t = wave_sum(t);
   if (tid % 64 == 0) { part[tid / 64].s = s; part[tid / 64].t = t; }
   __syncthreads();
-  return {m * a.scale, part[0].s + part[1].s + part[2].s + part[3].s, part[0].t + part[1].t + part[2].t + part[3].t};
+  return {0.0f, part[0].s + part[1].s + part[2].s + part[3].s, part[0].t + part[1].t + part[2].t + part[3].t, m};
 }
 
-// Results of a row from its sums.  256 threads.
-struct RowResult { float lse; bool bad; };
+// Results of a row from its sums.  256 threads.  The sums are brought to the largest logit itself first: s is 1 and more then, t 0 and less
+// (as they come, the roundings of 2^d may leave them beyond by a few 2^-24), and a log probability is a difference from that logit less
+// log s.  What is left of two large numbers would be off by their last bits, and a sure token's probability above 1.
+struct RowResult { float lse, best, log_s; bool bad; };
 template <typename T>
 __device__ __forceinline__ RowResult finish_row(const ScoreArgs &a, int r, Sums q, const T *x, Sums *part) {
   RowResult o;
-  const bool odd = !(q.s > 0.0f && q.m <= kFar);            // (the same for every thread)
-  if (odd) q = odd_row(a, x, part);
+  if (!(q.s >= 0.25f && q.m <= kFar)) q = odd_row(a, x, part);   // (the same for every thread)
+  else {
+    const float d = __builtin_fmaf(q.best, a.scale * kLog2e, -q.m), f = __builtin_amdgcn_exp2f(-d);
+    q.t = f * (q.t - q.s * d);
+    q.s *= f;
+  }
+  o.best = q.best;
   o.bad = q.s != q.s;
-  const float l2 = __builtin_log2f(q.s);
-  o.lse = o.bad ? __builtin_nanf("") : !(q.s > 0.0f) ? -__builtin_inff() : odd ? q.m + kLn2 * l2 : kLn2 * (q.m + l2);
+  const bool none = q.best == -__builtin_inff();
+  const float s = fmaxf(q.s, 1.0f), t = fminf(q.t, 0.0f), l2 = __builtin_log2f(s);
+  o.log_s = kLn2 * l2;
+  o.lse = o.bad ? __builtin_nanf("") : none ? -__builtin_inff() : __builtin_fmaf(q.best, a.scale, o.log_s);
   if (threadIdx.x == 0) {
     if (a.lse) a.lse[r] = o.lse;
-    if (a.entropy) a.entropy[r] = o.bad ? o.lse : q.s > 0.0f ? kLn2 * (l2 - q.t / q.s) : 0.0f;
+    if (a.entropy) a.entropy[r] = o.bad ? o.lse : none ? 0.0f : kLn2 * (l2 - t / s);
   }
   return o;
 }
 __device__ __forceinline__ float logp(const ScoreArgs &a, const RowResult &o, float x) {
-#pragma clang fp contract(off)                             // (the product is rounded as the one in lse is)
-  const float y = x * a.scale;
-  return y == -__builtin_inff() && !o.bad ? y : y - o.lse;
+  if (o.bad) return o.lse;
+  return x == -__builtin_inff() ? x : 2.0f * ((0.5f * x - 0.5f * o.best) * a.scale) - o.log_s;   // (halved: no difference overflows)
 }
 template <typename T>
 __device__ __forceinline__ void score_targets(const ScoreArgs &a, const RowResult &o, const T *x, int r) {
@@ -320,8 +329,9 @@ __global__ __launch_bounds__(256, 5) void logprobs_kernel(const ScoreArgs a, int
     float top = y[0];
 #pragma unroll
     for (int e = 1; e < K; ++e) top = fmaxf(top, y[e]);
-    // the reference follows the largest value so far at a distance: sums of up to 2^16 more lose nothing
-    if (__ballot(top * c - q.m > 16.0f) != 0 && top * c > q.m) move_to(q, ceilf(top * c));
+    // the reference follows the largest value so far at a distance of a factor of two: 2^d of the largest is rounded as a number near 1 is
+    q.best = fmaxf(q.best, top);
+    if (__ballot(top * c - q.m > 1.0f) != 0 && top * c > q.m) move_to(q, ceilf(top * c));
     const float s0 = q.s, t0 = q.t;
     if (plain) {
 #pragma unroll

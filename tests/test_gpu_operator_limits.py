@@ -39,3 +39,28 @@ def test_token_logprobs_of_rows_with_low_parts(dtype, low):
     x[4] += low
     x[5, ::2] = low
     check_scores(x.to(DT[dtype]), [[0, 39999, 20000]] * 6, 5, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [2000, 32000, 40003])
+@pytest.mark.parametrize("scale", [0.7, 1.0, 1.25, 3e4, 1e6, 1e8])
+def test_token_logprobs_of_peaked_rows(dtype, V, scale):
+    """One token far ahead.  What is left near 0 is off by the roundings of a sum near 1 and of its logarithm, 16 at most, however large the
+    logits are; a probability is never above 1, an entropy never below 0."""
+    n = 60
+    x = randn(n, V, seed=V)
+    rng = np.random.default_rng(V)
+    best = rng.integers(0, V, n)
+    x[torch.arange(n), torch.from_numpy(best).cuda()] = torch.from_numpy(rng.uniform(20.0, 70.0, n)).float().cuda()
+    x = x.to(DT[dtype])
+    targets = np.stack([best, rng.integers(0, V, n)], 1)
+    got = ngg.token_logprobs(x, ints(targets), top_n=3, scale=scale)
+    lp, ent, lse, ids, tlp = score64(x, targets, 3, scale)
+    assert (got.top_ids.cpu().numpy() == ids).all()
+    for g, w in ((got.logprobs, lp), (got.top_logprobs, tlp)):
+        assert (g <= 0).all()
+        assert (np.abs(g.double().cpu().numpy() - w) <= 16 * 2.0 ** -24 + 2.0 ** -22 * np.abs(w)).all()
+    assert (got.entropy >= 0).all()
+    # the same roundings, of sums whose terms are up to 1 as well
+    assert (np.abs(got.entropy.double().cpu().numpy() - ent) <= 32 * 2.0 ** -24).all()
+    assert (np.abs(got.lse.double().cpu().numpy() - lse) <= 2.0 ** -22 * np.abs(lse)).all()
