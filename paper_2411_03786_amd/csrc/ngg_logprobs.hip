@@ -517,11 +517,28 @@ size_t score_workspace(int dtype, int N, int V, int m, int top) {
   return s == 1 ? 0 : ((size_t)N * s * sizeof(Sums) + 15) / 16 * 16 + (size_t)N * s * top * sizeof(key_t64);
 }
 
+// (a launch counts its threads in 32 bits: 2^23 workgroups at a time, and rows that many have one slice each)
+constexpr int kLaunchRows = 1 << 23;
+
 template <typename T>
-static void launch(const ScoreArgs &a, int slices, hipStream_t s) {
+static void launch_rows(const ScoreArgs &a, int slices, hipStream_t s) {
   if (a.top) hipLaunchKernelGGL((logprobs_kernel<T, true>), dim3(a.N * slices), dim3(256), 0, s, a, slices);
   else hipLaunchKernelGGL((logprobs_kernel<T, false>), dim3(a.N * slices), dim3(256), 0, s, a, slices);
   if (slices > 1) hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3(a.N), dim3(256), 0, s, a, slices);
+}
+
+template <typename T>
+static void launch(const ScoreArgs &all, int slices, hipStream_t s) {
+  for (int64_t at = 0; at < all.N; at += kLaunchRows) {
+    ScoreArgs a = all;
+    a.N = (int)std::min<int64_t>(all.N - at, kLaunchRows);
+    a.x = (const T *)all.x + at * all.row_stride;
+    if (a.targets) { a.targets += at * a.m; a.logprobs += at * a.m; }
+    if (a.lse) a.lse += at;
+    if (a.entropy) a.entropy += at;
+    if (a.top) { a.top_ids += at * a.top; a.top_logprobs += at * a.top; }
+    launch_rows<T>(a, slices, s);
+  }
 }
 
 void launch_token_logprobs(int dtype, const ScoreArgs &a, hipStream_t s) {

@@ -64,3 +64,14 @@ def test_token_logprobs_of_peaked_rows(dtype, V, scale):
     # the same roundings, of sums whose terms are up to 1 as well
     assert (np.abs(got.entropy.double().cpu().numpy() - ent) <= 32 * 2.0 ** -24).all()
     assert (np.abs(got.lse.double().cpu().numpy() - lse) <= 2.0 ** -22 * np.abs(lse)).all()
+
+
+def test_token_logprobs_of_more_rows_than_a_launch_has_workgroups():
+    n, V = (1 << 24) + 5, 3
+    x = torch.randn(n, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    t = torch.randint(0, V, (n,), device="cuda", dtype=torch.int32, generator=torch.Generator(device="cuda").manual_seed(2))
+    got = ngg.token_logprobs(x, t, top_n=2)
+    want = x.log_softmax(-1)
+    # a handful of fp32 operations on values of a few units, on either side
+    assert (got.logprobs - want.gather(1, t.long()[:, None])[:, 0]).abs().max() < 16 * 2.0 ** -22
+    assert torch.equal(got.top_ids[:, 0].long(), x.argmax(-1)) and (got.lse - x.logsumexp(-1)).abs().max() < 16 * 2.0 ** -22
