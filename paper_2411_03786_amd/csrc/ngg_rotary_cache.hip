@@ -649,18 +649,39 @@ static void by_types(int dtype, int cache, const CacheArgs &a, hipStream_t s) {
   else if (cache == NGG_BF16) Launch<bf16_t, bf16_t>::go(a, s);
   else Launch<bf16_t, fp8_t>::go(a, s);
 }
+// Groups of 2^28 tokens at a time: a launch counts its threads in 32 bits
+constexpr int kLaunchTokens = 1 << 28;
+template <typename T, typename Launch>
+static void in_parts(const CacheArgs &all, Launch launch) {
+  for (int64_t at = 0; at < all.n_tokens; at += kLaunchTokens) {
+    CacheArgs a = all;
+    const int64_t left = all.n_tokens - at;
+    a.n_tokens = (int)(left < kLaunchTokens ? left : kLaunchTokens);
+    a.slots += at;
+    if (a.positions) a.positions += at;
+    if (a.k) a.k = (const T *)a.k + at * a.k_token;
+    if (a.v) a.v = (const T *)a.v + at * a.v_token;
+    if (a.k_out) a.k_out = (T *)a.k_out + at * a.k_token;
+    if (a.v_out) a.v_out = (T *)a.v_out + at * a.v_token;
+    launch(a);
+  }
+}
 template <typename T, typename CT> struct WriteLaunch {
-  static void go(const CacheArgs &a, hipStream_t s) {
-    if (!few_rows(a))
-      hipLaunchKernelGGL((kv_write_group_kernel<T, CT>), groups(a), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k, a.v));
-    else hipLaunchKernelGGL((kv_write_kernel<T, CT>), dim3((a.n_tokens * a.p.Hkv + 3) / 4), dim3(256), 0, s, a);
+  static void go(const CacheArgs &all, hipStream_t s) {
+    if (!few_rows(all))
+      in_parts<T>(all, [s](const CacheArgs &a) {
+        hipLaunchKernelGGL((kv_write_group_kernel<T, CT>), groups(a), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k, a.v));
+      });
+    else hipLaunchKernelGGL((kv_write_kernel<T, CT>), dim3((all.n_tokens * all.p.Hkv + 3) / 4), dim3(256), 0, s, all);
   }
 };
 template <typename T, typename CT> struct ReadLaunch {
-  static void go(const CacheArgs &a, hipStream_t s) {
-    if (!few_rows(a))
-      hipLaunchKernelGGL((kv_read_group_kernel<T, CT>), groups(a), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k_out, a.v_out));
-    else hipLaunchKernelGGL((kv_read_kernel<T, CT>), dim3((a.n_tokens * a.p.Hkv + 3) / 4), dim3(256), 0, s, a);
+  static void go(const CacheArgs &all, hipStream_t s) {
+    if (!few_rows(all))
+      in_parts<T>(all, [s](const CacheArgs &a) {
+        hipLaunchKernelGGL((kv_read_group_kernel<T, CT>), groups(a), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k_out, a.v_out));
+      });
+    else hipLaunchKernelGGL((kv_read_kernel<T, CT>), dim3((all.n_tokens * all.p.Hkv + 3) / 4), dim3(256), 0, s, all);
   }
 };
 void launch_kv_write(int dtype, int cache, const CacheArgs &a, hipStream_t s) { by_types<WriteLaunch>(dtype, cache, a, s); }

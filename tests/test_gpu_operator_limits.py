@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2411_03786_amd as ngg
-from test_gpu_operators import DT, check_scores, ints, randn, score64
+from test_gpu_operators import DT, check_scores, eight_bits, ints, randn, score64
 
 pytestmark = pytest.mark.gpu
 
@@ -75,3 +75,18 @@ def test_token_logprobs_of_more_rows_than_a_launch_has_workgroups():
     # a handful of fp32 operations on values of a few units, on either side
     assert (got.logprobs - want.gather(1, t.long()[:, None])[:, 0]).abs().max() < 16 * 2.0 ** -22
     assert torch.equal(got.top_ids[:, 0].long(), x.argmax(-1)) and (got.lse - x.logsumexp(-1)).abs().max() < 16 * 2.0 ** -22
+
+
+def test_cache_of_more_tokens_than_a_launch_has_workgroups():
+    """2^29 tokens and some, one row for all but a few of them, and read back from the places around the parts."""
+    n, hd = (1 << 29) + 70, 32
+    kv = ngg.KVPages((n + 63) // 64, 64, 1, hd, "fp8")
+    rows = (torch.arange(2 * hd, device="cuda", dtype=torch.float32) / 64 - 0.5).to(torch.bfloat16).view(2, 1, 1, hd)
+    k, v = (r.expand(n, 1, hd) for r in rows)
+    kv.write(k, v, torch.arange(n, dtype=torch.int32, device="cuda"))
+    at = ints([0, 1 << 20, (1 << 28) - 1, 1 << 28, (1 << 28) + 33, (1 << 29) - 1, 1 << 29, n - 1])
+    for got, row in zip(kv.read(at), rows):
+        assert torch.equal(got, eight_bits(row).to(torch.bfloat16).expand(8, 1, hd))
+    got = kv.read(torch.arange(n, dtype=torch.int32, device="cuda").fill_(5))       # all of them from one place
+    for g, row in zip(got, rows):
+        assert torch.equal(g[-3:], eight_bits(row).to(torch.bfloat16).expand(3, 1, hd)) and torch.equal(g[(1 << 28) - 2:(1 << 28) + 2], g[:4])
