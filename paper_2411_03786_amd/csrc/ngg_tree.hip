@@ -328,7 +328,7 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
         if constexpr (sizeof(CT) == 1)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (pos0 + g4 * 8 + e >= n_keys) vs[e] = 1.0f;
+            if (pos0 + g4 * 8 + e >= n_keys || !(vs[e] < __builtin_inff())) vs[e] = 1.0f;   // (a place that nobody wrote, 0 times it must be 0)
         poison = __ballot(poison) != 0;
       }
 #pragma unroll
@@ -550,7 +550,8 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a
             *reinterpret_cast<bf16x8 *>(vt + 2 * blk * 512 + slot * 8) = f0.v;
             *reinterpret_cast<bf16x8 *>(vt + (2 * blk + 1) * 512 + slot * 8) = f1.v;
           }
-          if (tid / 32 == k) vsl[buf * KS + tid] = (t + k) * 32 + tid % 32 < (there[k] ? n_keys : 0) ? exp_scale(vex) : 1.0f;
+          // (an exponent of ones is of a place that nobody wrote: 0 times it must be 0 where its key is masked)
+          if (tid / 32 == k) vsl[buf * KS + tid] = vex < 255 && (t + k) * 32 + tid % 32 < (there[k] ? n_keys : 0) ? exp_scale(vex) : 1.0f;
         }
       } else __builtin_amdgcn_s_waitcnt(0x0F70);           // vmcnt(0): this wave's transfers to LDS have landed
     };

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2411_03786_amd as ngg
-from test_gpu_operators import DT, check_scores, eight_bits, ints, randn, score64
+from test_gpu_operators import DT, Case, check_scores, eight_bits, ints, randn, score64
 
 pytestmark = pytest.mark.gpu
 
@@ -90,3 +90,24 @@ def test_cache_of_more_tokens_than_a_launch_has_workgroups():
     got = kv.read(torch.arange(n, dtype=torch.int32, device="cuda").fill_(5))       # all of them from one place
     for g, row in zip(got, rows):
         assert torch.equal(g[-3:], eight_bits(row).to(torch.bfloat16).expand(3, 1, hd)) and torch.equal(g[(1 << 28) - 2:(1 << 28) + 2], g[:4])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("wide", [False, True])
+def test_tree_attention_of_a_slot_that_nobody_wrote(dtype, wide):
+    """A tree position inside the sequence that no row sees: whatever its bytes and exponents hold, the rows are as they were."""
+    T, ctx, j = 21, 50, 12
+    c = Case([ctx], [T], T, 4, 2, 64, dtype, "fp8", seed=11, wide=wide)
+    see, words = c.masks(seed=11)
+    see[:, :, j] = False
+    words &= ~(1 << j)
+    clean, clean_lse = c.check(words, see)
+    slot = c.table[0, (ctx + j) // 32] * 32 + (ctx + j) % 32
+    x = torch.full((1, 2, 64), float("nan"), dtype=DT[dtype], device="cuda")
+    c.kv.write(x, x, slot[None].int())
+    page, at = int(slot) // 32, int(slot) % 32
+    for e in (255, 254, 0):
+        for exps in (c.kv.k_exps, c.kv.v_exps):
+            exps.view(c.kv.n_pages, 2, 32)[page, :, at] = e
+        out, lse = ngg.tree_attention(c.q, c.kv, c.table, ints([ctx]), mask=words, want_lse=True)
+        assert torch.equal(out, clean) and torch.equal(lse, clean_lse)
