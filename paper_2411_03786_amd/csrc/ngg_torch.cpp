@@ -85,11 +85,12 @@ py::object rotary(uintptr_t rope_at, const Tensor &table, const Tensor &position
 
 const ngg_kv_pages *pages_of(uintptr_t at) { return (const ngg_kv_pages *)at; }
 
-void kv_write(uintptr_t pages_at, const Tensor &bytes, const Tensor &k, const Tensor &v, const Tensor &slots, uintptr_t rope_at, const Maybe &positions) {
+void kv_write(uintptr_t pages_at, const Tensor &bytes, const Tensor &k, const Tensor &v, const Tensor &slots, uintptr_t rope_at, const Maybe &table,
+              const Maybe &positions) {
   const ngg_kv_pages *p = pages_of(pages_at);
   if (slots.dim() != 1) throw py::type_error("slots must be a contiguous int32 tensor of one dimension");
   const int64_t n = slots.size(0);
-  on_gpu(bytes, {&k, &v, &slots, ptr(positions)});
+  on_gpu(bytes, {&k, &v, &slots, ptr(table), ptr(positions)});
   ints(slots, "slots", n);
   for (const Tensor *t : {&k, &v}) {
     if (t->dim() != 3 || t->size(0) != n || t->size(1) != p->n_kv_heads || t->size(2) != p->head_dim)
@@ -99,7 +100,7 @@ void kv_write(uintptr_t pages_at, const Tensor &bytes, const Tensor &k, const Te
   const int dt = dtype_of(k, "k");
   if (v.scalar_type() != k.scalar_type()) throw py::type_error("k and v must have one dtype");
   if (rope_at) {
-    if (!positions) throw py::value_error("rope needs positions");
+    if (!table || !positions) throw py::value_error("rope needs positions");
     ints(*positions, "positions", n);
   }
   const int64_t stride[4] = {k.stride(0), k.stride(1), v.stride(0), v.stride(1)};

@@ -94,11 +94,11 @@ class KVPages:
     def write(self, k, v, slots, rope=None, positions=None, stream=None):
         """ngg_kv_write: k and v [tokens, kv heads, head_dim], any strides with contiguous heads, to slots (int32 [tokens]); with a
         Rope the keys are rotated to positions (int32 [tokens]) on the way."""
-        at = rope._at if rope is not None else 0
+        at, table = (rope._at, rope.cos) if rope is not None else (0, None)
         if stream is not None:
-            tables = (rope.cos, rope.sin) if rope is not None else ()
-            return _on(stream, _binding.kv_write, self._at, self.k_bytes, k, v, slots, at, positions, keep=self._memory() + tables)
-        _binding.kv_write(self._at, self.k_bytes, k, v, slots, at, positions)
+            sin = (rope.sin,) if rope is not None else ()
+            return _on(stream, _binding.kv_write, self._at, self.k_bytes, k, v, slots, at, table, positions, keep=self._memory() + sin)
+        _binding.kv_write(self._at, self.k_bytes, k, v, slots, at, table, positions)
 
     def read(self, slots, dtype=None, stream=None):
         """ngg_kv_read: the keys and values of slots (int32 [tokens]), [tokens, kv heads, head_dim] each, in dtype (default: the

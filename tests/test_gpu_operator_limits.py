@@ -111,3 +111,17 @@ def test_tree_attention_of_a_slot_that_nobody_wrote(dtype, wide):
             exps.view(c.kv.n_pages, 2, 32)[page, :, at] = e
         out, lse = ngg.tree_attention(c.q, c.kv, c.table, ints([ctx]), mask=words, want_lse=True)
         assert torch.equal(out, clean) and torch.equal(lse, clean_lse)
+
+
+def test_a_table_in_host_memory_is_refused():
+    rope, x, pos = ngg.Rope(32, 16, device="cpu"), randn(3, 2, 32, dtype="bf16"), ints([0, 1, 2])
+    kv = ngg.KVPages(1, 32, 2, 32, "bf16")
+    side = torch.cuda.Stream()
+    for stream in (None, side):
+        with pytest.raises(ValueError):
+            kv.write(x, x, pos, rope=rope, positions=pos, stream=stream)
+        with pytest.raises(ValueError):
+            ngg.rotary(rope, pos, x, stream=stream)
+    with pytest.raises(ValueError):
+        kv.write(x, x, pos, rope=ngg.Rope(32, 16))                     # no positions
+    assert not kv.k_bytes.any()
