@@ -153,7 +153,7 @@ ngg_status ngg_rotary(const ngg_rope *rope, const int32_t *positions, int32_t n_
     if (!r) continue;
     if (r->n_heads < 1 || r->n_heads > 65535) return fail_global(NGG_EINVAL, "ngg_rotary: %d heads", r->n_heads);
     if (n_tokens > 0 && (!r->in || !r->out)) return fail_global(NGG_EINVAL, "ngg_rotary: null rows");
-    if (r->in == r->out && (r->in_token != r->out_token || r->in_head != r->out_head))
+    if (n_tokens > 0 && r->in == r->out && (r->in_token != r->out_token || r->in_head != r->out_head))
       return fail_global(NGG_EINVAL, "ngg_rotary: in place needs equal strides");
     k.rows[i] = {r->in, r->out, r->in_token, r->in_head, r->out_token, r->out_head, r->n_heads};
   }

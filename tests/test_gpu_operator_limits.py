@@ -125,3 +125,14 @@ def test_a_table_in_host_memory_is_refused():
     with pytest.raises(ValueError):
         kv.write(x, x, pos, rope=ngg.Rope(32, 16))                     # no positions
     assert not kv.k_bytes.any()
+
+
+def test_rotary_of_an_empty_projection():
+    """No tokens, and rows that are slices of something wider."""
+    H, Hkv, hd = 4, 2, 64
+    q, k, _ = torch.empty(0, H + 2 * Hkv, hd, dtype=torch.bfloat16, device="cuda").split((H, Hkv, Hkv), 1)
+    assert q.stride(0) != H * hd
+    rope = ngg.Rope(hd, 16)
+    a, b = ngg.rotary(rope, ints([]), q, k)
+    assert a.shape == (0, H, hd) and b.shape == (0, Hkv, hd)
+    assert ngg.rotary(rope, ints([]), q, out=q).shape == (0, H, hd)
