@@ -40,6 +40,13 @@ void on_gpu(const Tensor &first, std::initializer_list<const Tensor *> others) {
 }
 const Tensor *ptr(const Maybe &m) { return m ? &*m : nullptr; }
 
+// No gradient is recorded (a rotation's is the inverse call): a call that autograd would take part in is refused, not cut out of the graph
+void no_grad(std::initializer_list<const Tensor *> all) {
+  if (!at::GradMode::is_enabled()) return;
+  for (const Tensor *t : all)
+    if (t && t->requires_grad()) throw std::runtime_error("ngg records no gradients: detach the tensors, or call it under torch.no_grad()");
+}
+
 void inner(const Tensor &t, const char *what) {
   if (t.stride(-1) != 1 && t.size(-1) != 1) throw py::value_error(std::string("the last dimension of ") + what + " must be contiguous");
 }
@@ -60,12 +67,17 @@ Tensor checked_output(const Maybe &out, const Tensor &like, const char *what) {
   inner(*out, what);
   return *out;
 }
+// autograd sees that a tensor it may hold was written
+void written(const Maybe &out) {
+  if (out && !out->is_inference()) out->unsafeGetTensorImpl()->bump_version();
+}
 
 py::object rotary(uintptr_t rope_at, const Tensor &table, const Tensor &positions, const Tensor &q, const Maybe &k, bool inverse, const Maybe &out, const Maybe &k_out) {
   if (q.dim() != 3) throw py::value_error("q must be [tokens, heads, head_dim]");
   const int64_t n = q.size(0), hd = q.size(2);
   const int dt = dtype_of(q, "q");
   on_gpu(q, {ptr(k), &positions, &table, ptr(out), ptr(k_out)});
+  no_grad({&q, ptr(k), ptr(out), ptr(k_out)});
   ints(positions, "positions", n);
   if (k && (k->dim() != 3 || k->size(0) != n || k->size(2) != hd || k->scalar_type() != q.scalar_type()))
     throw py::value_error("q and k must agree in tokens, head_dim and dtype");
@@ -79,6 +91,8 @@ py::object rotary(uintptr_t rope_at, const Tensor &table, const Tensor &position
     rows[i] = {x.data_ptr(), o[i].data_ptr(), x.stride(0), x.stride(1), o[i].stride(0), o[i].stride(1), narrow(x.size(1), "heads")};
   }
   check(ngg_rotary((const ngg_rope *)rope_at, (const int32_t *)positions.data_ptr(), narrow(n, "tokens"), narrow(hd, "head_dim"), dt, &rows[0], k ? &rows[1] : nullptr, inverse, stream()));
+  written(out);
+  if (k) written(k_out);
   if (k) return py::make_tuple(o[0], o[1]);
   return py::cast(o[0]);
 }
@@ -91,6 +105,7 @@ void kv_write(uintptr_t pages_at, const Tensor &bytes, const Tensor &k, const Te
   if (slots.dim() != 1) throw py::type_error("slots must be a contiguous int32 tensor of one dimension");
   const int64_t n = slots.size(0);
   on_gpu(bytes, {&k, &v, &slots, ptr(table), ptr(positions)});
+  no_grad({&k, &v});
   ints(slots, "slots", n);
   for (const Tensor *t : {&k, &v}) {
     if (t->dim() != 3 || t->size(0) != n || t->size(1) != p->n_kv_heads || t->size(2) != p->head_dim)
@@ -129,6 +144,7 @@ py::object tree_attention(uintptr_t pages_at, const Tensor &bytes, const Tensor 
   const int64_t B = q.size(0), T = q.size(1), H = q.size(2), hd = q.size(3);
   const int dt = dtype_of(q, "q");
   on_gpu(bytes, {&q, &pages, &context_lens, ptr(mask), ptr(tree_lens), ptr(out), ptr(workspace)});
+  no_grad({&q, ptr(out)});
   if (hd != p->head_dim) throw py::value_error("q has heads of " + std::to_string(hd) + ", the cache of " + std::to_string(p->head_dim));
   inner(q, "q");
   if (pages.scalar_type() != at::kInt || pages.dim() != 2 || pages.size(0) != B) throw py::type_error("pages must be an int32 tensor [batch, max_pages]");
@@ -166,6 +182,7 @@ py::object tree_attention(uintptr_t pages_at, const Tensor &bytes, const Tensor 
     ws = *workspace;
   } else if (need) ws = at::empty({need}, q.options().dtype(at::kByte));
   check(ngg_tree_attention(p, &a, ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.numel() : 0, stream()));
+  written(out);
   if (want_lse) return py::make_tuple(o, lse);
   return py::cast(o);
 }
@@ -175,6 +192,7 @@ py::tuple token_logprobs(const Tensor &logits, const Maybe &targets, int64_t top
   const int64_t n = logits.size(0);
   const int dt = dtype_of(logits, "logits");
   on_gpu(logits, {ptr(targets)});
+  no_grad({&logits});
   inner(logits, "logits");
   int64_t m = 0;
   if (targets) {

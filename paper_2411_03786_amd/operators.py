@@ -2,7 +2,8 @@
 probabilities (ngg.h states what each computes; csrc/ngg_torch.cpp checks the tensors and makes the calls).
 
 Outputs and workspaces come from torch's allocator on the stream that the call runs on: the current one, or `stream`, which
-then has to have been made to wait for whatever wrote the inputs.  Nothing is synchronised.
+then has to have been made to wait for whatever wrote the inputs.  Nothing is synchronised.  No gradients are recorded: a call on
+tensors that require them raises, unless gradients are off (`rotary` with inverse=True is the gradient of `rotary`).
 """
 from __future__ import annotations
 

@@ -136,3 +136,37 @@ def test_rotary_of_an_empty_projection():
     a, b = ngg.rotary(rope, ints([]), q, k)
     assert a.shape == (0, H, hd) and b.shape == (0, Hkv, hd)
     assert ngg.rotary(rope, ints([]), q, out=q).shape == (0, H, hd)
+
+
+def operator_calls():
+    """The operators' calls on a tensor of queries (keys, values) and on logits, each by its name."""
+    rope, kv = ngg.Rope(64, 32), ngg.KVPages(2, 32, 4, 64, "bf16")
+    one, at = ints([[0, 1]]), ints(range(6))
+    return dict(rotary=lambda x: ngg.rotary(rope, at, x), rotary_k=lambda x: ngg.rotary(rope, at, x.detach(), x), keys=lambda x: kv.write(x, x.detach(), at),
+                values=lambda x: kv.write(x.detach(), x, at), attention=lambda x: ngg.tree_attention(x[None], kv, one, ints([0])),
+                logprobs=lambda x: ngg.token_logprobs(x.flatten(1), top_n=2), rotary_out=lambda x: ngg.rotary(rope, at, x.detach(), out=x),
+                attention_out=lambda x: ngg.tree_attention(x.detach()[None], kv, one, ints([0]), out=x[None]))
+
+
+@pytest.mark.parametrize("name", ["rotary", "rotary_k", "keys", "values", "attention", "logprobs", "rotary_out", "attention_out"])
+def test_tensors_that_require_gradients_are_refused(name):
+    call, x = operator_calls()[name], randn(6, 4, 64, dtype="bf16")
+    call(x)
+    x.requires_grad_(True)
+    with pytest.raises(RuntimeError, match="gradient"):
+        call(x)
+    with torch.no_grad():
+        call(x)
+    with torch.inference_mode():
+        call(x.clone())
+
+
+def test_outputs_written_in_place_raise_their_version():
+    rope, at, x = ngg.Rope(64, 32), ints(range(6)), randn(6, 4, 64, dtype="bf16")
+    before = x._version
+    ngg.rotary(rope, at, x, out=x)
+    assert x._version > before
+    y = torch.empty(1, 6, 4, 64, dtype=torch.bfloat16, device="cuda")
+    before = y._version
+    ngg.tree_attention(x[None], ngg.KVPages(2, 32, 4, 64, "bf16"), ints([[0, 1]]), ints([0]), out=y)
+    assert y._version > before
