@@ -5,7 +5,9 @@
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 
+#include <algorithm>
 #include <cmath>
+#include <vector>
 
 #include "ngg.h"
 
@@ -65,6 +67,16 @@ Tensor checked_output(const Maybe &out, const Tensor &like, const char *what) {
   if (out->sizes() != like.sizes() || out->scalar_type() != like.scalar_type())
     throw py::value_error(std::string(what) + " must have its input's shape and dtype");
   inner(*out, what);
+  // its elements lie apart: dimensions by rising stride, each beyond what the ones before reach
+  std::vector<std::pair<int64_t, int64_t>> dims;
+  for (int64_t d = 0; d < out->dim(); ++d)
+    if (out->size(d) > 1) dims.emplace_back(out->stride(d), out->size(d));
+  std::sort(dims.begin(), dims.end());
+  int64_t reach = 0;
+  for (const auto &[stride, size] : dims) {
+    if (stride <= reach && out->numel() > 0) throw py::value_error(std::string("elements of ") + what + " share memory");
+    reach += stride * (size - 1);
+  }
   return *out;
 }
 // autograd sees that a tensor it may hold was written

@@ -170,3 +170,20 @@ def test_outputs_written_in_place_raise_their_version():
     before = y._version
     ngg.tree_attention(x[None], ngg.KVPages(2, 32, 4, 64, "bf16"), ints([[0, 1]]), ints([0]), out=y)
     assert y._version > before
+
+
+def test_outputs_whose_elements_share_memory_are_refused():
+    rope, at, x = ngg.Rope(64, 32), ints(range(6)), randn(6, 4, 64, dtype="bf16")
+    kv = ngg.KVPages(2, 32, 4, 64, "bf16")
+    flat = torch.zeros(6 * 4 * 64, dtype=torch.bfloat16, device="cuda")
+    for out in (flat[:4 * 64].view(1, 4, 64).expand(6, -1, -1), flat[:6 * 64].view(6, 1, 64).expand(-1, 4, -1), flat.as_strided((6, 4, 64), (128, 64, 1)),
+                flat.as_strided((6, 4, 64), (256, 63, 1))):
+        with pytest.raises(ValueError):
+            ngg.rotary(rope, at, x, out=out)
+        with pytest.raises(ValueError):
+            ngg.rotary(rope, at, x, x, k_out=out)
+        with pytest.raises(ValueError):
+            ngg.tree_attention(x[None], kv, ints([[0, 1]]), ints([0]), out=out[None])
+    assert not flat.any()
+    for out in (torch.empty(4, 6, 64, dtype=torch.bfloat16, device="cuda").transpose(0, 1), torch.empty(6, 4, 70, dtype=torch.bfloat16, device="cuda")[..., 3:67]):
+        assert torch.equal(ngg.rotary(rope, at, x, out=out), ngg.rotary(rope, at, x))
