@@ -75,8 +75,8 @@ class TreeDecoder:
             self.unembed = (self.embed[before].T.float() * d ** -0.5).to(self.dtype)
         self.layers = [dict(qkv=weight(d, (heads + 2 * kv_heads) * head_dim), proj=weight(d, d), gate=weight(d, d_ffn), up=weight(d, d_ffn),
                             down=weight(d_ffn, d)) for _ in range(layers)]
-        self.rope = ngg.Rope(head_dim, max_tokens)
         per = -(-max_tokens // page)
+        self.rope = ngg.Rope(head_dim, per * page)                                # whatever the pages hold
         self.kv = [ngg.KVPages(batch * per, page, kv_heads, head_dim, cache) for _ in range(layers)]
         # a sequence's pages lie scattered over the pool, as they do after some serving
         self.pages = torch.randperm(batch * per, generator=torch.Generator().manual_seed(seed)).view(batch, per).int().cuda()

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2411_03786_amd as ngg
+from paper_2411_03786_amd import tree_verify as tv
 from test_gpu_operators import DT, Case, check_scores, eight_bits, ints, randn, score64
 
 pytestmark = pytest.mark.gpu
@@ -187,3 +188,9 @@ def test_outputs_whose_elements_share_memory_are_refused():
     assert not flat.any()
     for out in (torch.empty(4, 6, 64, dtype=torch.bfloat16, device="cuda").transpose(0, 1), torch.empty(6, 4, 70, dtype=torch.bfloat16, device="cuda")[..., 3:67]):
         assert torch.equal(ngg.rotary(rope, at, x, out=out), ngg.rotary(rope, at, x))
+
+
+def test_decoder_tables_reach_as_far_as_its_pages():
+    prompts = np.random.default_rng(1).integers(0, 100, (2, 20)).tolist()
+    runs = [tv.TreeDecoder(2, 1, 2, 1, 32, 100, n, cache="f32", page=32, d_ffn=64, seed=4).decode(prompts, 40, lambda b, s: []) for n in (40, 64)]
+    assert np.isfinite(runs[0][1]).all() and runs[0] == runs[1]
