@@ -418,8 +418,9 @@ ngg_status ngg_tree_mask(const int32_t *parents, int32_t n, uint64_t *mask, int3
  * context_lens[b] + j whatever its depth.  Position p lies in slot pages[b][p / page_size] * page_size + p % page_size.  Token t
  * sees every position of the context and the tree's tokens j <= t whose bit is set in row t of the mask (NULL: all j <= t).
  *   out[b][t][h] = sum_p softmax_p(scale * q[b][t][h] . k[p][h'])  v[p][h'],   h' = h / (n_heads / n_kv_heads)
- * with scores, sums and outputs held in 32 bits; for NGG_BF16 the probabilities become bf16 for the product
- * with the values.  lse[b][t][h], if not NULL, is the logarithm of the sum of exp(scale * q . k).  A token that
+ * with scores, sums and outputs held in 32 bits; for NGG_BF16 the probabilities have 16 bits in the product with the
+ * values, and 8 (bf16) in calls of 40 * 2^20 scores and more (batch * n_heads * tree * max_pages * page_size) with over 32 rows (tree * n_heads /
+ * n_kv_heads). lse[b][t][h], if not NULL, is the logarithm of the sum of exp(scale * q . k).  A token that
  * sees nothing, and a token behind the sequence's own tree_lens[b], gets zeros and an lse of minus infinity.
  * Bits of positions, lengths and pages out of range: negative lengths count as 0, tree_lens is cut to
  * `tree`, positions beyond the page list and those on a page outside the pool are not seen.  What lies behind the last

@@ -232,7 +232,9 @@ __device__ __forceinline__ void write_row4(const TreeArgs &a, int b, int t, int 
 // turn, each straight from memory in the order that the 16x16x32 products want (a tile is one read of 64 lanes times 16 bytes after the
 // other), and are joined through LDS at its end.  Nothing waits for another wave before that, so that few rows stream at the rate of
 // the memory: 32 single tokens of 8 key heads of 128 over up to 8191 positions (619 MB at 16 bits) 103 us, 6.0 TB/s.  The scores come out
-// transposed (keys by rows), so that a lane holds eight neighbouring keys of one row, its operand of the second product.
+// transposed (keys by rows), so that a lane holds eight neighbouring keys of one row, its operand of the second product.  At 16 bits
+// that operand is two: a probability rounded to bf16 (8 bits), and the remainder, rounded.  Beside the memory's time the second one is hidden:
+// the 32 single tokens 105 us with and without it, 32 lists of 51 rows over 2047 positions 23.2 and 22.8, tiles of 32 rows up to 0.8 us more.
 // NT: keys that nobody reads again stay out of the caches.
 template <typename T, typename CT, int HD, int QF, bool NT>
 __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
@@ -368,6 +370,16 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
         pack_frag(P, p);
 #pragma unroll
         for (int d = 0; d < DF; ++d) mma(O[f][d], V[d], P);
+        if constexpr (sizeof(T) == 2) {
+          // what the rounding left out has a product of its own: the probabilities count with 16 bits, not with 8
+          float rest[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) rest[e] = p[e] - (float)P.v[e];
+          Frag<T> R;
+          pack_frag(R, rest);
+#pragma unroll
+          for (int d = 0; d < DF; ++d) mma(O[f][d], V[d], R);
+        }
         if (poison) {
           // values that are not finite were left out, because 0 times them must stay 0 where their key is masked: they go to the
           // rows that see them alone
@@ -439,7 +451,9 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
 // The next step's tiles are on their way meanwhile (16 bits: straight to LDS).  Bound by the issue of products, exponentials and LDS
 // reads together: eight trees of 64 tokens, 32 heads of 128, over 32000 positions each at 8 bits 393 us, 683 TFLOP/s, one over 390000
 // positions 733 (a library product of 16 bits 1230); ragged trees leave waves without rows: eight of 38 to 61 tokens over
-// 13531 to 32000 positions 250 us, 550 TFLOP/s.  64 rows a wave, eight waves, two tiles in turn, the softmax of one behind the products of the other
+// 13531 to 32000 positions 250 us, 550 TFLOP/s.  The probabilities of the second product are rounded to bf16: with a product of the
+// remainders too, as tree_stream_kernel has it, these calls take 21 to 26 % longer (the full trees 343 and 431 us, the ragged ones 211 and
+// 255), for an error of the outputs that is a fifth smaller; what a call loses is 2^-9 of each key's share, in no direction.  64 rows a wave, eight waves, two tiles in turn, the softmax of one behind the products of the other
 // and raised wave priorities did not pay.
 // 32x32x16 products: row 8 j + 4 h + i of a key tile is key 16 (j % 2) + 8 h + 4 (j / 2) + i, so lane (row, h) ends up with keys
 // 16 u + 8 h .. + 7 of every 16, its operand of the second product.

@@ -5,7 +5,7 @@ import torch
 
 import paper_2411_03786_amd as ngg
 from paper_2411_03786_amd import tree_verify as tv
-from test_gpu_operators import DT, Case, check_scores, eight_bits, ints, randn, score64
+from test_gpu_operators import DT, Case, attention64, check_scores, eight_bits, ints, randn, score64
 
 pytestmark = pytest.mark.gpu
 
@@ -194,3 +194,16 @@ def test_decoder_tables_reach_as_far_as_its_pages():
     prompts = np.random.default_rng(1).integers(0, 100, (2, 20)).tolist()
     runs = [tv.TreeDecoder(2, 1, 2, 1, 32, 100, n, cache="f32", page=32, d_ffn=64, seed=4).decode(prompts, 40, lambda b, s: []) for n in (40, 64)]
     assert np.isfinite(runs[0][1]).all() and runs[0] == runs[1]
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+@pytest.mark.parametrize("H,Hkv,hd,T,ctx", [(8, 2, 64, 1, 300), (8, 2, 128, 5, 900), (4, 1, 128, 30, 400), (16, 4, 32, 13, 2000)])
+def test_tree_attention_keeps_16_bits_of_a_probability(cache, H, Hkv, hd, T, ctx):
+    """Values of either sign leave little of a row's sum, so that what its terms lose is seen beside the rounding of the output: 2^-16 of
+    a term's share, not the 2^-9 of a probability in bf16, besides what fp32 sums may be off by (test_gpu_operators)."""
+    c = Case([ctx, ctx // 2], [T, T], T, H, Hkv, hd, "bf16", cache, seed=5)
+    see, words = c.masks(seed=5)
+    out = ngg.tree_attention(c.q, c.kv, c.table, ints(c.ctx), mask=words)
+    want, _, mag, qk = attention64(c.q, c.ks, c.vs, c.ctx, c.trees, see, c.scale)
+    e = (2 * (hd + 8) * 2.0 ** -24 * qk + 2.0 ** -15)[..., None]
+    assert ((out.double() - want).abs() <= mag * (e + 2.0 ** -16) + want.abs() * 2.0 ** -8).all()
