@@ -629,10 +629,19 @@ __global__ __launch_bounds__(256) void kv_read_group_kernel(const CacheArgs a, i
   }
 }
 
-// Calls of few rows have a wave for each (token, head), whose chain of loads is the shorter one (8 heads of 128, 16 bits, us, by waves
-// and by groups: 1 token written 2.5 and 3.5, 64 tokens 3.4 and 3.6, 256 tokens 3.9 and 3.6, 512 tokens 5.2 and 4.1).
-constexpr int kFewRows = 2048;
-static bool few_rows(const CacheArgs &a) { return (int64_t)a.n_tokens * a.p.Hkv <= kFewRows; }
+// Calls of few rows (tokens times heads) have a wave for each, whose chain of loads is the shorter one.  Us a call in a graph, by waves and
+// by groups of 8 heads of 128 (with 32 heads of 128, and heads of 64 and 32, the crossing lies up to twice as high), rows:
+//                       1024        1536        2048        3072        4096        8192
+//   written, 16 bits    3.1, 3.3    3.4, 3.3    3.6, 3.4    4.2, 3.4    4.8, 3.6    7.0, 4.1
+//            fp32       3.6, 3.8    4.0, 3.9    4.4, 4.0    5.4, 4.1    5.8, 4.4   10.0, 5.7
+//            to 8 bits  3.2, 3.9    3.4, 4.0    3.5, 4.0    4.0, 4.0    4.4, 4.2    6.6, 4.8
+//   rotated, 16 bits    3.6, 5.4    3.8, 5.4    4.0, 5.4    4.7, 5.5    5.5, 5.6    8.1, 6.3
+//            to 8 bits  3.6, 6.3    3.8, 6.3    3.9, 6.4    4.4, 6.4    5.1, 6.5    7.9, 7.0
+//   read, 16 bits       2.8, 3.3    3.0, 3.3    3.1, 3.4    3.4, 3.4    3.9, 3.6    5.5, 4.2
+//         from 8 bits   3.0, 3.3    3.2, 3.4    3.2, 3.4    3.7, 3.5    4.1, 3.7    5.8, 4.4
+static bool few_rows(const CacheArgs &a, int most) { return (int64_t)a.n_tokens * a.p.Hkv <= most; }
+static int few_written(const CacheArgs &a, bool to8) { return a.cos ? 4096 : to8 ? 3072 : 1536; }
+constexpr int kFewRead = 3072;
 template <typename T>
 static bool rows_of_vectors(const CacheArgs &a, const void *k, const void *v) {
   constexpr int VE = Vec16<T>::n;
@@ -668,7 +677,7 @@ static void in_parts(const CacheArgs &all, Launch launch) {
 }
 template <typename T, typename CT> struct WriteLaunch {
   static void go(const CacheArgs &all, hipStream_t s) {
-    if (!few_rows(all))
+    if (!few_rows(all, few_written(all, sizeof(CT) == 1)))
       in_parts<T>(all, [s](const CacheArgs &a) {
         hipLaunchKernelGGL((kv_write_group_kernel<T, CT>), groups(a), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k, a.v));
       });
@@ -677,7 +686,7 @@ template <typename T, typename CT> struct WriteLaunch {
 };
 template <typename T, typename CT> struct ReadLaunch {
   static void go(const CacheArgs &all, hipStream_t s) {
-    if (!few_rows(all))
+    if (!few_rows(all, kFewRead))
       in_parts<T>(all, [s](const CacheArgs &a) {
         hipLaunchKernelGGL((kv_read_group_kernel<T, CT>), groups(a), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k_out, a.v_out));
       });

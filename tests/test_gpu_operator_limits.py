@@ -207,3 +207,26 @@ def test_tree_attention_keeps_16_bits_of_a_probability(cache, H, Hkv, hd, T, ctx
     want, _, mag, qk = attention64(c.q, c.ks, c.vs, c.ctx, c.trees, see, c.scale)
     e = (2 * (hd + 8) * 2.0 ** -24 * qk + 2.0 ** -15)[..., None]
     assert ((out.double() - want).abs() <= mag * (e + 2.0 ** -16) + want.abs() * 2.0 ** -8).all()
+
+
+@pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("bf16", "bf16"), ("f32", "fp8"), ("bf16", "fp8")])
+@pytest.mark.parametrize("rows", [1536, 3072, 4096])
+def test_cache_by_rows_and_by_groups_alike(dtype, cache, rows):
+    """Calls on either side of the sizes from which rows move in groups, in runs of 13 slots that begin anywhere: one call as two halves."""
+    Hkv, hd = 4, 128
+    for n in (rows // Hkv, rows // Hkv + 1):
+        slots = 5 + np.arange(n) // 13 * 17 + np.arange(n) % 13
+        pool = int(slots[-1]) // 64 + 1
+        x = randn(n, 2 * Hkv, hd, seed=rows, dtype=dtype)
+        rope, pos = ngg.Rope(hd, 300), ints(np.arange(n) % 300)
+        for turn in (dict(), dict(rope=rope)):
+            a, b = (ngg.KVPages(pool, 64, Hkv, hd, cache) for _ in range(2))
+            for kv, parts in ((a, [(0, n)]), (b, [(0, n // 2), (n // 2, n)])):
+                for i, j in parts:
+                    kv.write(x[i:j, :Hkv], x[i:j, Hkv:], ints(slots[i:j]), **(dict(turn, positions=pos[i:j]) if turn else {}))
+            assert torch.equal(a.k_bytes, b.k_bytes) and torch.equal(a.v_bytes, b.v_bytes)
+            if cache == "fp8":
+                assert torch.equal(a.k_exps, b.k_exps) and torch.equal(a.v_exps, b.v_exps)
+            whole, half = a.read(ints(slots), DT[dtype]), a.read(ints(slots[:n // 2]), DT[dtype])
+            assert all(torch.equal(w[:n // 2], h) for w, h in zip(whole, half))
+            assert torch.equal(whole[1], eight_bits(x[:, Hkv:]).to(DT[dtype]) if cache == "fp8" else x[:, Hkv:])
