@@ -511,8 +511,7 @@ int row_slices(int dtype, int N, int V) {
 
 }  // namespace
 
-size_t score_workspace(int dtype, int N, int V, int m, int top) {
-  (void)m;
+size_t score_workspace(int dtype, int N, int V, int top) {
   const int s = N > 0 ? row_slices(dtype, N, V) : 1;
   return s == 1 ? 0 : ((size_t)N * s * sizeof(Sums) + 15) / 16 * 16 + (size_t)N * s * top * sizeof(key_t64);
 }

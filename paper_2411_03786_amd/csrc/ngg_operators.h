@@ -140,7 +140,7 @@ struct ScoreArgs {
   int32_t *top_ids;
   void *ws;
 };
-size_t score_workspace(int dtype, int N, int V, int m, int top);
+size_t score_workspace(int dtype, int N, int V, int top);
 void launch_token_logprobs(int dtype, const ScoreArgs &a, hipStream_t s);
 
 }  // namespace ngg

@@ -267,7 +267,7 @@ ngg_status ngg_token_logprobs_workspace(const ngg_score_args *args, int64_t *byt
   const ngg_status st = check_score("ngg_token_logprobs_workspace", args, false);
   if (st != NGG_OK) return st;
   if (!bytes) return fail_global(NGG_EINVAL, "ngg_token_logprobs_workspace: null bytes");
-  *bytes = (int64_t)score_workspace(args->dtype, args->n_rows, args->vocab, args->n_targets, args->top_n);
+  *bytes = (int64_t)score_workspace(args->dtype, args->n_rows, args->vocab, args->top_n);
   return NGG_OK;
 }
 
@@ -275,7 +275,7 @@ ngg_status ngg_token_logprobs(const ngg_score_args *args, void *workspace, int64
   const ngg_status st = check_score("ngg_token_logprobs", args, true);
   if (st != NGG_OK) return st;
   if (args->n_rows == 0) return NGG_OK;
-  const size_t need = score_workspace(args->dtype, args->n_rows, args->vocab, args->n_targets, args->top_n);
+  const size_t need = score_workspace(args->dtype, args->n_rows, args->vocab, args->top_n);
   if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < (int64_t)need))
     return fail_global(NGG_EINVAL, "ngg_token_logprobs: needs %lld bytes of 16-byte aligned workspace", (long long)need);
   ScoreArgs a{args->logits, args->row_stride, args->n_rows, args->vocab, args->n_targets, args->top_n, args->scale, args->targets,

@@ -459,10 +459,10 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
 // 16 u + 8 h .. + 7 of every 16, its operand of the second product.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-template <typename CT, int HD, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void tree_block_kernel(const TreeArgs a) {
+template <typename CT, int HD>
+__global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
   typedef bf16_t T;
-  constexpr int DS = HD / 32, KQ = HD / 16, DB = HD / 32, TILE = 32 * HD, KT = 2, KS = 32 * KT, ROWS = 32 * NW, NT = 64 * NW;
+  constexpr int NW = 4, DS = HD / 32, KQ = HD / 16, DB = HD / 32, TILE = 32 * HD, KT = 2, KS = 32 * KT, ROWS = 32 * NW, NT = 64 * NW;
   constexpr bool C8 = sizeof(CT) == 1;
   constexpr int PIECES = TILE / 16, PPT = (PIECES + NT - 1) / NT;   // (8 bits) 16-byte pieces of a tile, of a thread
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -908,22 +908,20 @@ static void launch_stream(const TreeArgs &a, hipStream_t s) {
   hipLaunchKernelGGL((tree_stream_kernel<T, CT, HD, QF, NT>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
   merge<T, HD, 16 * QF, 128>(a, s);
 }
-template <typename CT, int HD, int NW>
+template <typename CT, int HD>
 static void launch_block(const TreeArgs &a, hipStream_t s) {
   constexpr size_t lds = (size_t)8 * 32 * HD * 2 + 2 * 64 * 4 + 2 * 4;
-  static const bool once = (allow_lds(&tree_block_kernel<CT, HD, NW>, lds + (NGG_TREE_MAX + 1) * 4), true);
+  static const bool once = (allow_lds(&tree_block_kernel<CT, HD>, lds + (NGG_TREE_MAX + 1) * 4), true);
   (void)once;
-  hipLaunchKernelGGL((tree_block_kernel<CT, HD, NW>), dim3(a.ranges * a.Z), dim3(64 * NW), lds + (a.B + 1) * 4, s, a);
-  merge<bf16_t, HD, 32 * NW, 64>(a, s);
+  hipLaunchKernelGGL((tree_block_kernel<CT, HD>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
+  merge<bf16_t, HD, 128, 64>(a, s);
 }
 template <typename T, typename CT, int HD>
 static void by_rows(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
   if (p.rows == 16 && p.stream) launch_stream<T, CT, HD, 1, true>(a, s);
   else if (p.rows == 16) launch_stream<T, CT, HD, 1, false>(a, s);
   else if (p.rows == 32) launch_stream<T, CT, HD, 2, false>(a, s);
-  else if constexpr (sizeof(T) == 2) {
-    launch_block<CT, HD, 4>(a, s);
-  }
+  else if constexpr (sizeof(T) == 2) launch_block<CT, HD>(a, s);
 }
 template <typename T, typename CT>
 static void by_head(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
