@@ -93,9 +93,9 @@ class TreeDecoder:
         at = torch.gather(self.pages, 1, (places.clamp(min=0) // self.page).long()) * self.page + places.clamp(min=0) % self.page
         return torch.where(places < 0, -1, at).int().flatten()
 
-    def forward(self, tokens, depth, mask=None, tree_lens=None):
-        """Logits [batch * tree, vocab] of the trees' tokens [batch, tree] behind the cached positions; their keys and values are
-        left at the positions behind those, in the trees' order."""
+    def forward(self, tokens, depth, mask=None, tree_lens=None, logits=True):
+        """Logits [batch * tree, vocab] of the trees' tokens [batch, tree] behind the cached positions, or None without `logits`; their
+        keys and values are left at the positions behind those, in the trees' order."""
         B, T = tokens.shape
         H, Hkv, hd = self.heads, self.kv_heads, self.hd
         place = self.lens[:, None] + torch.arange(T, dtype=torch.int32, device="cuda")
@@ -115,13 +115,13 @@ class TreeDecoder:
             x = x + a.reshape(B * T, H * hd) @ w["proj"]
             y = self.norm(x).to(self.dtype)
             x = x + (torch.nn.functional.silu(y @ w["gate"]) * (y @ w["up"])) @ w["down"]
-        return (self.norm(x).to(self.dtype) @ self.unembed).float()
+        return self.norm(x).to(self.dtype) @ self.unembed if logits else None
 
     def prefill(self, prompts, piece=512):
         """Caches all tokens of the prompts [batch, n] but the last."""
         for at in range(0, prompts.shape[1] - 1, piece):
             part = prompts[:, at:min(at + piece, prompts.shape[1] - 1)]
-            self.forward(part, torch.arange(part.shape[1], device="cuda"))
+            self.forward(part, torch.arange(part.shape[1], device="cuda"), logits=False)
             self.lens += part.shape[1]
             self.cached = [n + part.shape[1] for n in self.cached]
 
