@@ -230,3 +230,22 @@ def test_cache_by_rows_and_by_groups_alike(dtype, cache, rows):
             whole, half = a.read(ints(slots), DT[dtype]), a.read(ints(slots[:n // 2]), DT[dtype])
             assert all(torch.equal(w[:n // 2], h) for w, h in zip(whole, half))
             assert torch.equal(whole[1], eight_bits(x[:, Hkv:]).to(DT[dtype]) if cache == "fp8" else x[:, Hkv:])
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+def test_trees_of_16_bit_models_accept_what_single_tokens_wrote(cache):
+    """The single tokens' run as drafts of eight: every step takes nine tokens until the runs part, and they part only where two tokens are
+    as likely but for 16-bit sums.  Those are off by 2^-9 a dozen times on the way to logits of up to 4 (an 8-bit cache by some of its
+    2^-4 steps where such a sum turns one): some hundredths, and 1 / 8 at most; a wrong mask, depth or kept path changes them by whole units."""
+    prompt, n = 130, 48
+    dec = tv.TreeDecoder(4, 2, 8, 2, 64, 1000, 400, cache=cache, page=64, d_ffn=512, seed=5)
+    prompts = np.random.default_rng(2).integers(0, 1000, (4, prompt)).tolist()
+    plain, lp, _ = dec.decode(prompts, n, lambda b, s: [])
+    follow = lambda b, s: [plain[b][len(s) - prompt:len(s) - prompt + 8]] if s[prompt:] == plain[b][:len(s) - prompt] else []
+    got, got_lp, steps = dec.decode(prompts, n, follow)
+    most = 0
+    for b in range(4):
+        same = next((i for i in range(n) if got[b][i] != plain[b][i]), n)
+        assert np.abs(np.array(got_lp[b][:same + 1]) - np.array(lp[b][:same + 1])).max() < 0.125
+        most = max(most, -(-same // 9) + n - same)
+    assert steps <= most + 1
