@@ -453,7 +453,9 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
 // positions 733 (a library product of 16 bits 1230); ragged trees leave waves without rows: eight of 38 to 61 tokens over
 // 13531 to 32000 positions 250 us, 550 TFLOP/s.  The probabilities of the second product are rounded to bf16: with a product of the
 // remainders too, as tree_stream_kernel has it, these calls take 21 to 26 % longer (the full trees 343 and 431 us, the ragged ones 211 and
-// 255), for an error of the outputs that is a fifth smaller; what a call loses is 2^-9 of each key's share, in no direction.  64 rows a wave, eight waves, two tiles in turn, the softmax of one behind the products of the other
+// 255), for an error of the outputs that is a fifth to a quarter smaller; what a call loses is 2^-9 of each key's share, in no direction.  fp16 for 8-bit
+// caches, whose elements it holds, would keep 11 bits where the heads' powers of two are not far apart, but steps of both kinds in
+// one loop spill 130 registers (533 us).  64 rows a wave, eight waves, two tiles in turn, the softmax of one behind the products of the other
 // and raised wave priorities did not pay.
 // 32x32x16 products: row 8 j + 4 h + i of a key tile is key 16 (j % 2) + 8 h + 4 (j / 2) + i, so lane (row, h) ends up with keys
 // 16 u + 8 h .. + 7 of every 16, its operand of the second product.
@@ -839,20 +841,21 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
 
 // Rows of a tile, and with them the kernel: 16 and 32 rows are tree_stream_kernel's, 128 tree_block_kernel's (16-bit operands).  Every
 // tile reads the keys again (from the L2), but small tiles are more workgroups, of more waves to a SIMD, that start and end quicker.
-// The rule goes by the scores of a call, positions of all (sequence, key head) times rows.  Measured at 16 bits (us; tiles of 16, 32
-// and 128 rows; lists, rows, positions, head_dim):
-//   24, 160, 1000, 64: 12, 16, 23 (3.8 M scores)       32, 51, 3850, 128: 29, 29, 32 (6.3 M)       32, 51, 12000, 128: 53, 46, 52 (20 M)
-//   96, 60, 3850, 128: 56, 48, 53 (22 M)               64, 472, 1000, 128: 60, 53, 56 (30 M)       24, 160, 12000, 64: 60, 50, 49 (46 M)
-//   128, 120, 3850, 128: 115, 83, 80 (59 M)            69, 356, 3850, 64: 138, 101, 69 (95 M)      64, 472, 3850, 128: 193, 149, 115 (116 M)
-// and in fp32 (16 and 32 rows): 96, 26, 4000, 128: 103, 118 (10 M); 64, 472, 400, 128: 117, 127 (13 M); 24, 244, 4000, 64: 88, 84 (24 M);
-// 64, 472, 4000, 128: 733, 713 (121 M).
+// The rule goes by the scores of a call, positions of all (sequence, key head) times rows.  Measured at 16 bits (us a call in a graph;
+// tiles of 16, 32 and 128 rows; lists, rows, positions, head_dim):
+//   24, 160, 1000, 64: 11, 15, 17 (4 M scores)         32, 51, 3850, 128: 27, 29, 31 (6 M)         32, 51, 12000, 128: 53, 48, 49 (19 M)
+//   96, 60, 3850, 128: 52, 47, 49 (21 M)               64, 472, 1000, 128: 56, 51, 48 (29 M)       24, 160, 12000, 64: 57, 52, 47 (44 M)
+//   128, 120, 3850, 128: 108, 83, 77 (56 M)            69, 356, 3850, 64: 140, 104, 63 (90 M)      64, 472, 3850, 128: 185, 149, 99 (111 M)
+// (from 25 to 40 M tiles of 128 rows would gain some 5 %, but have 8 bits of a probability where the others have 16)
+// and in fp32 (16 and 32 rows): 96, 26, 4000, 128: 98, 109 (10 M); 64, 472, 400, 128: 90, 103 (12 M); 24, 244, 4000, 64: 76, 72 (22 M);
+// 64, 472, 4000, 128: 689, 682 (115 M).
 static int tile_rows(int dtype, int hd, int rows, int64_t lists, int64_t positions) {
   if (rows <= 16) return 16;
   const int64_t scores = lists * positions * rows;
   if (dtype == NGG_F32) return scores < 16 << 20 ? 16 : 32;
   if (scores >= 40 << 20) return rows <= 32 ? 32 : 128;
   // (heads of 128 leave 16-row tiles three waves to a SIMD: from three workgroups to a compute unit on, larger tiles take fewer turns;
-  // 128 lists, 120 rows, 200 positions 17 and 15 us, 1000 positions 36 and 29; heads of 64 rather lose: 69, 356, 1000: 36 and 39)
+  // 128 lists, 120 rows, 200 positions 15 and 14 us, 1000 positions 33 and 28; heads of 64 rather lose: 69, 356, 1000: 33 and 39)
   if (scores >= 16 << 20 || (hd == 128 && lists * ((rows + 15) / 16) >= 768)) return 32;
   return 16;
 }
