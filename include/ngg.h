@@ -380,7 +380,7 @@ ngg_status ngg_rotary(const ngg_rope *rope, const int32_t *positions, int32_t n_
  * every element in 8 bits (1 sign, 4 exponent, 3 fraction bits, largest magnitude 448, no infinities), times a power of
  * two for each (position, head) of keys and of values, the smallest that brings the head's largest magnitude to 448 or
  * below (2^-126 at least; 1 for a head of zeros), kept as its exponent + 127 in k_exp and v_exp.  Rounding is to nearest even; an element that is not
- * finite is kept as NaN.  Writing what was read changes nothing.
+ * finite is kept as NaN.  Read in bf16, values below its smallest (2^-133) are rounded; otherwise writing what was read changes nothing.
  * Layout (the library's own): page by page, head by head, tiles of 32 positions in matrix operand order, as the caches of ngg_debug_peek. */
 typedef struct {
   void *k, *v;
@@ -453,11 +453,11 @@ ngg_status ngg_tree_attention(const ngg_kv_pages *pages, const ngg_tree_args *ar
  * lse = log sum_v exp(x_v):  logprobs[r][i] = x[targets[r][i]] - lse;  entropy[r] = -sum_v p_v log p_v, p = exp(x - lse);
  * top_ids[r], top_logprobs[r]: the top_n largest in falling order, equal ones by rising id (NaN counts as the largest).
  * Ruled-out tokens (logits of minus infinity) have no share in the sums.  A target below 0 gives 0 (no token), one
- * beyond the vocabulary NaN.  A row whose logits are all minus infinity has an lse and log probabilities of minus infinity and entropy 0; a row
- * with NaN or plus infinity has NaN in lse, entropy and log probabilities.  Outputs are [n_rows][..] contiguous; lse, entropy and, without
- * targets or top_n, the others may be NULL.  Sums are held in 32 bits.  No log probability is above 0 and no entropy below: a
- * log probability is the difference from the row's largest logit less the logarithm of a sum near 1, not one of two large numbers.
- *  0 <= top_n <= min(64, vocab), 0 <= n_targets <= 64, vocab <= 2^30. */
+ * beyond the vocabulary NaN.  A row whose logits are all minus infinity has an lse and log probabilities of minus infinity
+ * and entropy 0; a row with NaN or plus infinity has NaN in lse, entropy and log probabilities.  Sums are held in 32 bits.  A log
+ * probability is the difference from the row's largest logit less the logarithm of a sum near 1: never above 0, however large
+ * the logits are; an entropy is never below 0.  Outputs are [n_rows][..] contiguous; lse, entropy and, without targets or top_n,
+ * the others may be NULL.  0 <= top_n <= min(64, vocab), 0 <= n_targets <= 64, vocab <= 2^30. */
 typedef struct {
   const void *logits;          /* [n_rows][vocab] */
   int64_t row_stride;

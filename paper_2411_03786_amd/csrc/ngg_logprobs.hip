@@ -2,8 +2,8 @@
 //   m = max x,  s = sum e^(x - m),  lse = m + log s,  entropy = log s - (sum e^(x - m) (x - m)) / s
 // All of it in one pass over the logits: every lane keeps sums against a reference of its own, every wave a list of candidates
 // for the likeliest tokens.  A row is cut into slices where the rows alone would not fill the chip; a second kernel joins them.
-// Bound by HBM with many rows (4096 of 128256 at 16 bits, top 8: 206-232 us, 4.5-5.1 TB/s), by what a slice does once with few: 97 rows
-// of 128256 in fp32 18 us with the top 20, 10 without (4.8 TB/s); 51 of 32000 9 and 5.
+// Bound by HBM with many rows (4096 of 128256 at 16 bits: 161 us, 6.5 TB/s, and 187 to 215 with the top 8), by what a slice does once with
+// few: 97 rows of 128256 in fp32 18 us with the top 20, 12.5 without (4.0 TB/s); 51 of 32000 8 with the top 5, 5 without.
 #include "ngg_operators.h"
 
 #include <algorithm>
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(256, 5) void logprobs_kernel(const ScoreArgs a, int
   }
 }
 
-// Joins the slices of a row.  One workgroup per row: 3 us, 4-5 with the likeliest, launch and loads.
+// Joins the slices of a row.  One workgroup per row: 2 to 4 us, 3 to 4.4 with the likeliest, launch and loads.
 template <typename T>
 __global__ __launch_bounds__(256) void logprobs_join_kernel(const ScoreArgs a, int slices) {
   __shared__ __align__(16) key_t64 kept[kMaxSlices * 64 + 8];

@@ -513,7 +513,7 @@ __global__ __launch_bounds__(256) void kv_write_group_kernel(const CacheArgs a, 
   }
 }
 
-// Two 8-bit elements, of the word's upper half if UPPER, times a power of two; exact in both types.
+// Two 8-bit elements, of the word's upper half if UPPER, times a power of two; exact but below bf16's smallest, 2^-133.
 template <bool UPPER>
 __device__ __forceinline__ void two_wide(unsigned w, float scale, bf16_t *to) {
   *reinterpret_cast<bf16x2 *>(to) = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, UPPER);

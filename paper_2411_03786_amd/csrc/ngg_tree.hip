@@ -37,7 +37,7 @@ __device__ __forceinline__ void raw_frag(Frag<float> &f, const u32x4 *r) {
   for (int e = 0; e < 8; ++e) f.v[e] = __uint_as_float(r[e >> 2][e & 3]);
 }
 
-// Eight 8-bit elements times a power of two as a fragment of either type; exact in both.
+// Eight 8-bit elements times a power of two as a fragment of either type; exact but below bf16's smallest, 2^-133.
 __device__ __forceinline__ void widen(Frag<bf16_t> &f, unsigned lo, unsigned hi, float scale) {
   bf16x2 *d = reinterpret_cast<bf16x2 *>(&f.v);
   d[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
@@ -231,10 +231,11 @@ __device__ __forceinline__ void write_row4(const TreeArgs &a, int b, int t, int 
 // One workgroup: one row tile (16 QF rows) over its share of the list.  The waves take the tiles of 32 keys of a (sequence, head) in
 // turn, each straight from memory in the order that the 16x16x32 products want (a tile is one read of 64 lanes times 16 bytes after the
 // other), and are joined through LDS at its end.  Nothing waits for another wave before that, so that few rows stream at the rate of
-// the memory: 32 single tokens of 8 key heads of 128 over up to 8191 positions (619 MB at 16 bits) 103 us, 6.0 TB/s.  The scores come out
+// the memory: 32 single tokens of 8 key heads of 128 over up to 8191 positions (619 MB at 16 bits) 107 us, 5.8 TB/s.  The scores come out
 // transposed (keys by rows), so that a lane holds eight neighbouring keys of one row, its operand of the second product.  At 16 bits
-// that operand is two: a probability rounded to bf16 (8 bits), and the remainder, rounded.  Beside the memory's time the second one is hidden:
-// the 32 single tokens 105 us with and without it, 32 lists of 51 rows over 2047 positions 23.2 and 22.8, tiles of 32 rows up to 0.8 us more.
+// that operand is two: a probability rounded to bf16 (8 bits), and the remainder, rounded.  Beside the memory's time the second one is hidden
+// (us with and without it: the 32 single tokens 105, 105; 32 lists of 51 rows over 2047 positions 23.2, 22.8); tiles of 32 rows pay 3 to
+// 10 % (32 lists of 80 rows over up to 4000 positions 27.8, 26.8; 36 of 160 rows of 64 over 4000 35.8, 32.2).
 // NT: keys that nobody reads again stay out of the caches.
 template <typename T, typename CT, int HD, int QF, bool NT>
 __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
@@ -449,9 +450,9 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
 // Row tiles of more than 32 rows on 16-bit operands: the waves of a workgroup own 32 rows each and share the keys, two tiles (64 keys)
 // per step, through LDS, where 8-bit tiles arrive widened (keys with their powers of two; those of the values go to the probabilities).
 // The next step's tiles are on their way meanwhile (16 bits: straight to LDS).  Bound by the issue of products, exponentials and LDS
-// reads together: eight trees of 64 tokens, 32 heads of 128, over 32000 positions each at 8 bits 393 us, 683 TFLOP/s, one over 390000
-// positions 733 (a library product of 16 bits 1230); ragged trees leave waves without rows: eight of 38 to 61 tokens over
-// 13531 to 32000 positions 250 us, 550 TFLOP/s.  The probabilities of the second product are rounded to bf16: with a product of the
+// reads together: eight trees of 64 tokens, 32 heads of 128, over 32000 positions each at 8 bits 343 to 360 us, 745 to 785 TFLOP/s
+// (a library product of 16 bits 1230); ragged trees leave waves without rows: eight of up to 61 tokens over up to 32000
+// positions 211 to 241 us (the card's clock is lower the longer it was busy).  The probabilities of the second product are rounded to bf16: with a product of the
 // remainders too, as tree_stream_kernel has it, these calls take 21 to 26 % longer (the full trees 343 and 431 us, the ragged ones 211 and
 // 255), for an error of the outputs that is a fifth to a quarter smaller; what a call loses is 2^-9 of each key's share, in no direction.  fp16 for 8-bit
 // caches, whose elements it holds, would keep 11 bits where the heads' powers of two are not far apart, but steps of both kinds in
