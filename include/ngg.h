@@ -33,7 +33,7 @@ typedef enum {
   NGG_ENOMEM = -5     /* device or host allocation failed */
 } ngg_status;
 
-typedef enum { NGG_F32 = 0, NGG_BF16 = 1, NGG_FP8 = 2 /* cached keys and values of ngg_kv_pages only */ } ngg_dtype;
+typedef enum { NGG_F32 = 0, NGG_BF16 = 1, NGG_FP8 = 2, NGG_FP4 = 4 /* the last two: cached keys and values of ngg_kv_pages only */ } ngg_dtype;
 
 /* Decoder shape.  The base model M of Section 4.1 is a pre-norm decoder with
  * RMSNorm, rotary multi-head attention (rotate-half pairing: element i pairs
@@ -374,17 +374,23 @@ typedef struct {
 ngg_status ngg_rotary(const ngg_rope *rope, const int32_t *positions, int32_t n_tokens, int32_t head_dim, int32_t dtype,
                       const ngg_rotary_rows *a, const ngg_rotary_rows *b, int32_t inverse, void *hip_stream);
 
+#define NGG_TREE_MAX 1024 /* sequences of a call, tokens of a tree */
+
 /* A pool of pages of page_size positions each (a multiple of 32), shared by any number of sequences.  The caller owns the
  * memory: k and v of the bytes that ngg_kv_bytes returns, 16-byte aligned, with no value that has to be set before
- * the first write.  Slot s is position s % page_size of page s / page_size.  dtype NGG_F32, NGG_BF16, or NGG_FP8:
- * every element in 8 bits (1 sign, 4 exponent, 3 fraction bits, largest magnitude 448, no infinities), times a power of
+ * the first write.  Slot s is position s % page_size of page s / page_size.  dtype NGG_F32, NGG_BF16, or packed, NGG_FP8 or NGG_FP4.
+ * NGG_FP8: every element in 8 bits (1 sign, 4 exponent, 3 fraction bits, largest magnitude 448, no infinities), times a power of
  * two for each (position, head) of keys and of values, the smallest that brings the head's largest magnitude to 448 or
  * below (2^-126 at least; 1 for a head of zeros), kept as its exponent + 127 in k_exp and v_exp.  Rounding is to nearest even; an element that is not
  * finite is kept as NaN.  Read in bf16, values below its smallest (2^-133) are rounded; otherwise writing what was read changes nothing.
+ * NGG_FP4: every element in 4 bits (a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6), times a power of two for each 32 dimensions of a
+ * (position, head), the smallest that brings the largest of their magnitudes to 6 or below (2^-126 at least; 1 for zeros), kept as its
+ * exponent + 127.  Rounding is to nearest even.  Where one of the 32 is not finite, all of them read as NaN; magnitudes that round to 2^128
+ * read as infinity; writing what was read changes no value.
  * Layout (the library's own): page by page, head by head, tiles of 32 positions in matrix operand order, as the caches of ngg_debug_peek. */
 typedef struct {
   void *k, *v;
-  uint8_t *k_exp, *v_exp; /* NGG_FP8: [n_pages][n_kv_heads][page_size]; otherwise NULL */
+  uint8_t *k_exp, *v_exp; /* NGG_FP8: [n_pages][n_kv_heads][page_size]; NGG_FP4: head_dim / 32 for each of those; otherwise NULL */
   int32_t n_pages, page_size, n_kv_heads;
   int32_t head_dim;       /* 32, 64 or 128 */
   int32_t dtype;
@@ -393,7 +399,7 @@ typedef struct {
 /* Bytes of k (and of v), and of k_exp (and of v_exp; 0 without).  Host only; reads the sizes alone. */
 ngg_status ngg_kv_bytes(const ngg_kv_pages *pages, int64_t *values, int64_t *exponents);
 
-/* Writes keys and values [n_tokens][n_kv_heads][head_dim] of `dtype` (the pool's own, or any into NGG_FP8) to the slots
+/* Writes keys and values [n_tokens][n_kv_heads][head_dim] of `dtype` (the pool's own, or any into a packed one) to the slots
  * [n_tokens], which are distinct; a token whose slot is negative or beyond the pool is not written.  rope
  * not NULL: keys are rotated to `positions` on the way and rounded to `dtype` as ngg_rotary does (rotary_dim <= head_dim).  stride:
  * HOST, of k's token and head and of v's token and head. */
@@ -402,15 +408,56 @@ ngg_status ngg_kv_write(const ngg_kv_pages *pages, const void *k, const void *v,
                         void *hip_stream);
 
 /* Reads slots [n_tokens] back into k and v, [n_tokens][n_kv_heads][head_dim] of `dtype` (the pool's own, or any from
- * NGG_FP8); either may be NULL.  A slot outside the pool reads as zeros.  stride as in ngg_kv_write. */
+ * a packed one); either may be NULL.  A slot outside the pool reads as zeros.  stride as in ngg_kv_write. */
 ngg_status ngg_kv_read(const ngg_kv_pages *pages, const int32_t *slots, int32_t n_tokens, int32_t dtype, void *k, void *v,
                        const int64_t *stride, void *hip_stream);
+
+/* Between steps.  The pool consists of `layers` equal parts (n_pages / layers pages each: the layers of a model that share their page
+ * lists; 1: one part), and a call does the same in each: slots and pages count from the beginning of a part, and a layer's own
+ * ngg_kv_pages for the calls above has the addresses of its part.  Bits are moved as they are.
+ *
+ * ngg_kv_move: of every list [n_lists][n] (lists src_list and dst_list apart) slot src[i] moves to slot dst[i], the keys and values of all
+ * heads; all of a list's sources are read before the first is written, in whatever order they lie, and of equal destinations the last
+ * counts.  The destinations of a list are in no other one.  An entry whose source or destination is outside the part is passed over.
+ * n <= NGG_TREE_MAX.  (After a verified tree: its accepted nodes, to behind the context.)
+ * ngg_kv_copy: page src[i] to page dst[i]; of it the first positions[i] (rounded up to 32s; NULL: all).  No destination is a source, or there twice.
+ * An entry whose source or destination is outside the part is passed over. */
+ngg_status ngg_kv_move(const ngg_kv_pages *pages, int32_t layers, const int32_t *src, const int32_t *dst, int64_t src_list,
+                       int64_t dst_list, int32_t n_lists, int32_t n, void *hip_stream);
+ngg_status ngg_kv_copy(const ngg_kv_pages *pages, int32_t layers, const int32_t *src, const int32_t *dst, const int32_t *positions,
+                       int32_t n, void *hip_stream);
+
+/* Which pages hold which sequence, on the device: row s of `pages` lists the pages of sequence s from the left, -1 behind them; lens[s]
+ * positions are cached; refs[p] rows list page p, 0: it is free.  pages and lens are what ngg_tree_attention takes.  A table begins with
+ * -1 in all of pages and 0 in lens and refs; the caller counts lens up as positions are cached, and down through ngg_pages_release alone.
+ *
+ * ngg_pages_fork: sequence targets[i] gives its pages back and shares the ones that hold the cached positions of sequence sources[i].
+ * An entry outside the sequences, one whose target is a source of the call, and of equal targets all but the first are passed over.
+ * n <= NGG_TREE_MAX.
+ * ngg_pages_reserve: every sequence with new_tokens[s] > 0 gets pages for that many positions behind its cached ones, and a page of its own in the
+ * place of the one that holds its last positions, if that is not full and other rows list it too: its contents have to be copied,
+ * positions[s] of page src[s] to page dst[s] (-1, -1 and 0: nothing to copy; the three are arguments of ngg_kv_copy).  Of sequences that
+ * all go on in one page that no other row lists, the last keeps it.  Pages are the lowest that are free before the call, by sequence and
+ * place.  missing[0]: 0, or how many pages (of the pool, or of max_pages) the call lacks; nothing changes then.
+ * ngg_pages_release: sequence s is cut to keep[s] positions if it has more (NULL: none is cut), and the pages behind those that hold its
+ * positions become free, or others' alone; a negative keep[s] leaves the sequence as it is. */
+typedef struct {
+  int32_t *pages;                                 /* [n_seqs][max_pages] */
+  int64_t pages_seq;
+  int32_t *lens, *refs;                           /* [n_seqs], [n_pages] */
+  int32_t n_seqs, max_pages, n_pages, page_size;  /* n_seqs 1 .. NGG_TREE_MAX; max_pages * page_size <= 2^30; the pool's, of a layer */
+} ngg_page_table;
+
+ngg_status ngg_pages_fork(const ngg_page_table *table, const int32_t *sources, const int32_t *targets, int32_t n, void *hip_stream);
+ngg_status ngg_pages_reserve_workspace(const ngg_page_table *table, int64_t *bytes); /* Host only */
+ngg_status ngg_pages_reserve(const ngg_page_table *table, const int32_t *new_tokens, int32_t *src, int32_t *dst, int32_t *positions,
+                             int32_t *missing, void *workspace, int64_t workspace_bytes, void *hip_stream);
+ngg_status ngg_pages_release(const ngg_page_table *table, const int32_t *keep, void *hip_stream);
 
 /* The mask and depths of a tree of n tokens.  parents: HOST [n], parents[j] < j, -1 for a token that follows the context
  * directly.  mask: HOST [n][(n + 63) / 64], bit j % 64 of word j / 64 of row t set where j is t or one of its
  * ancestors.  depth: HOST [n] or NULL, the number of ancestors (the token's position is the context's length plus
  * it).  Host only; n <= NGG_TREE_MAX. */
-#define NGG_TREE_MAX 1024
 ngg_status ngg_tree_mask(const int32_t *parents, int32_t n, uint64_t *mask, int32_t *depth);
 
 /* Attention of a tree of tokens (a chain, a single new token: tree = 1) of every sequence over its cached positions.
@@ -439,7 +486,7 @@ typedef struct {
   int64_t mask_batch, mask_token;          /* mask_batch 0: one mask for all */
   int32_t max_pages, batch, tree, n_heads; /* batch 1 .. NGG_TREE_MAX, tree 1 .. NGG_TREE_MAX; n_heads <= 1024;
                                               max_pages * page_size <= 2^30, (that / 64 + 1) * batch * n_kv_heads <= 2^30 */
-  int32_t dtype;                           /* of q and out; the pool's own, or any with NGG_FP8 */
+  int32_t dtype;                           /* of q and out; the pool's own, or any with a packed one */
   float scale;                             /* > 0 */
 } ngg_tree_args;
 

@@ -17,7 +17,7 @@ LIB_PATH = os.path.join(_HERE, "csrc", "libngg.so")
 BINDING_PATH = os.path.join(_HERE, "csrc", "ngg_torch.so")
 
 NGG_OK, NGG_EINVAL, NGG_ECAPACITY, NGG_ESTATE, NGG_EHIP, NGG_ENOMEM = 0, -1, -2, -3, -4, -5
-NGG_F32, NGG_BF16, NGG_FP8 = 0, 1, 2
+NGG_F32, NGG_BF16, NGG_FP8, NGG_FP4 = 0, 1, 2, 4
 PROF_CLASSES = ("gemm_qkv", "gemm_o", "gemm_gateup", "gemm_down", "gemm_unembed", "attention", "norm", "drafts",
                 "accept_commit", "other")
 
@@ -25,7 +25,8 @@ EXPORTS = ("ngg_create", "ngg_destroy", "ngg_prefill", "ngg_build_drafts", "ngg_
            "ngg_greedy_decode", "ngg_get_tokens", "ngg_last_error", "ngg_profile_enable", "ngg_profile_reset",
            "ngg_profile_read", "ngg_debug_peek", "ngg_bigram_table_build", "ngg_bigram_source", "ngg_profile_bracket_overhead", "ngg_unigram_build", "ngg_decode_more", "ngg_profile_sample",
            "ngg_context_drafts_static", "ngg_allocation", "ngg_profile_read_bandwidth", "ngg_step_graphs", "ngg_debug_plan", "ngg_debug_tiles",
-           "ngg_debug_gemm_kernel", "ngg_rope_table", "ngg_rotary", "ngg_kv_bytes", "ngg_kv_write", "ngg_kv_read", "ngg_tree_mask",
+           "ngg_debug_gemm_kernel", "ngg_rope_table", "ngg_rotary", "ngg_kv_bytes", "ngg_kv_write", "ngg_kv_read", "ngg_kv_move", "ngg_kv_copy",
+           "ngg_pages_fork", "ngg_pages_reserve_workspace", "ngg_pages_reserve", "ngg_pages_release", "ngg_tree_mask",
            "ngg_tree_attention_workspace", "ngg_tree_attention", "ngg_token_logprobs_workspace", "ngg_token_logprobs")
 NGG_STATIC_MAX_TOKENS = 32768
 
@@ -80,6 +81,11 @@ class ngg_rotary_rows(C.Structure):
 class ngg_kv_pages(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_exp", "v_exp")] + \
                [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")]
+
+
+class ngg_page_table(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("pages_seq", C.c_int64), ("lens", C.c_void_p), ("refs", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("n_seqs", "max_pages", "n_pages", "page_size")]
 
 
 class ngg_tree_args(C.Structure):
@@ -143,6 +149,12 @@ def load_library():
     lib.ngg_kv_bytes.argtypes = [ref(ngg_kv_pages), ref(C.c_int64), ref(C.c_int64)]
     lib.ngg_kv_write.argtypes = [ref(ngg_kv_pages), vp, vp, C.c_int32, vp, vp, C.c_int32, ref(ngg_rope), vp, vp]
     lib.ngg_kv_read.argtypes = [ref(ngg_kv_pages), vp, C.c_int32, C.c_int32, vp, vp, vp, vp]
+    lib.ngg_kv_move.argtypes = [ref(ngg_kv_pages), C.c_int32, vp, vp, C.c_int64, C.c_int64, C.c_int32, C.c_int32, vp]
+    lib.ngg_kv_copy.argtypes = [ref(ngg_kv_pages), C.c_int32, vp, vp, vp, C.c_int32, vp]
+    lib.ngg_pages_fork.argtypes = [ref(ngg_page_table), vp, vp, C.c_int32, vp]
+    lib.ngg_pages_reserve_workspace.argtypes = [ref(ngg_page_table), ref(C.c_int64)]
+    lib.ngg_pages_reserve.argtypes = [ref(ngg_page_table), vp, vp, vp, vp, vp, vp, C.c_int64, vp]
+    lib.ngg_pages_release.argtypes = [ref(ngg_page_table), vp, vp]
     lib.ngg_tree_mask.argtypes = [vp, C.c_int32, vp, vp]
     lib.ngg_tree_attention_workspace.argtypes = [ref(ngg_kv_pages), ref(ngg_tree_args), ref(C.c_int64)]
     lib.ngg_tree_attention.argtypes = [ref(ngg_kv_pages), ref(ngg_tree_args), vp, C.c_int64, vp]
@@ -422,11 +434,11 @@ def context_drafts_static(tokens, w, k_ctx_max, q_min, q_max, rows, n_rows, stre
         raise NggError(st, lib.ngg_last_error(None).decode())
 
 
-_OPERATORS = ("KVPages", "Rope", "TokenLogprobs", "rotary", "token_logprobs", "tree_attention", "tree_mask")
+_OPERATORS = ("KVPages", "PageCopies", "PageTable", "Rope", "TokenLogprobs", "rotary", "token_logprobs", "tree_attention", "tree_mask")
 
 
 def __getattr__(name):
-    """The operators of a batched tree verification (operators.py), which import torch, on their first use."""
+    """The operators of a batched tree verification and of a cache's pages (operators.py), which import torch, on their first use."""
     if name not in _OPERATORS:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
     from . import operators

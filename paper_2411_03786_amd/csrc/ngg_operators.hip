@@ -1,5 +1,5 @@
-// C entry points of the operators of a batched tree verification (declared in ngg.h): argument checks, launches, and the two that
-// run on the host, the rotary table and the tree's mask.
+// C entry points of the operators of a batched tree verification and of a cache's pages (declared in ngg.h): argument checks, launches,
+// and the two that run on the host, the rotary table and the tree's mask.
 #include "ngg_operators.h"
 
 #include <cmath>
@@ -16,6 +16,7 @@ namespace {
 
 bool element_type(int dtype) { return dtype == NGG_F32 || dtype == NGG_BF16; }
 size_t element_size(int dtype) { return dtype == NGG_F32 ? 4 : dtype == NGG_BF16 ? 2 : 1; }
+bool packed(int dtype) { return dtype == NGG_FP8 || dtype == NGG_FP4; }
 bool aligned(const void *p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
 ngg_status check_rope(const char *what, const ngg_rope *r, int32_t head_dim) {
@@ -28,8 +29,8 @@ ngg_status check_rope(const char *what, const ngg_rope *r, int32_t head_dim) {
 
 ngg_status check_pages(const char *what, const ngg_kv_pages *p, bool pointers) {
   if (!p) return fail_global(NGG_EINVAL, "%s: null pages", what);
-  if (p->dtype != NGG_F32 && p->dtype != NGG_BF16 && p->dtype != NGG_FP8)
-    return fail_global(NGG_EINVAL, "%s: the pages' dtype must be NGG_F32, NGG_BF16 or NGG_FP8", what);
+  if (p->dtype != NGG_F32 && p->dtype != NGG_BF16 && !packed(p->dtype))
+    return fail_global(NGG_EINVAL, "%s: the pages' dtype must be NGG_F32, NGG_BF16, NGG_FP8 or NGG_FP4", what);
   if (p->head_dim != 32 && p->head_dim != 64 && p->head_dim != 128)
     return fail_global(NGG_EINVAL, "%s: head_dim %d must be 32, 64 or 128", what, p->head_dim);
   if (p->n_pages < 1 || p->n_kv_heads < 1 || p->n_kv_heads > 65535)
@@ -40,8 +41,8 @@ ngg_status check_pages(const char *what, const ngg_kv_pages *p, bool pointers) {
   if (!pointers) return NGG_OK;
   if (!p->k || !p->v) return fail_global(NGG_EINVAL, "%s: null page memory", what);
   if (!aligned(p->k, 16) || !aligned(p->v, 16)) return fail_global(NGG_EINVAL, "%s: page memory must be 16-byte aligned", what);
-  if (p->dtype == NGG_FP8) {
-    if (!p->k_exp || !p->v_exp) return fail_global(NGG_EINVAL, "%s: NGG_FP8 pages need k_exp and v_exp", what);
+  if (packed(p->dtype)) {
+    if (!p->k_exp || !p->v_exp) return fail_global(NGG_EINVAL, "%s: NGG_FP8 and NGG_FP4 pages need k_exp and v_exp", what);
     if (!aligned(p->k_exp, 16) || !aligned(p->v_exp, 16)) return fail_global(NGG_EINVAL, "%s: k_exp and v_exp must be 16-byte aligned", what);
   }
   return NGG_OK;
@@ -51,7 +52,7 @@ PagesView view(const ngg_kv_pages *p) { return {p->k, p->v, p->k_exp, p->v_exp, 
 
 ngg_status check_tokens(const char *what, const ngg_kv_pages *p, int32_t dtype, const int32_t *slots, int32_t n, const int64_t *stride) {
   if (!element_type(dtype)) return fail_global(NGG_EINVAL, "%s: dtype must be NGG_F32 or NGG_BF16", what);
-  if (p->dtype != NGG_FP8 && p->dtype != dtype) return fail_global(NGG_EINVAL, "%s: pages of dtype %d and tokens of dtype %d", what, p->dtype, dtype);
+  if (!packed(p->dtype) && p->dtype != dtype) return fail_global(NGG_EINVAL, "%s: pages of dtype %d and tokens of dtype %d", what, p->dtype, dtype);
   if (n < 0) return fail_global(NGG_EINVAL, "%s: n_tokens %d", what, n);
   if (!stride) return fail_global(NGG_EINVAL, "%s: null stride", what);
   if (n > 0 && !slots) return fail_global(NGG_EINVAL, "%s: null slots", what);
@@ -63,7 +64,7 @@ ngg_status check_tree(const char *what, const ngg_kv_pages *p, const ngg_tree_ar
   if (st != NGG_OK) return st;
   if (!a) return fail_global(NGG_EINVAL, "%s: null arguments", what);
   if (!element_type(a->dtype)) return fail_global(NGG_EINVAL, "%s: dtype must be NGG_F32 or NGG_BF16", what);
-  if (p->dtype != NGG_FP8 && p->dtype != a->dtype) return fail_global(NGG_EINVAL, "%s: pages of dtype %d and queries of dtype %d", what, p->dtype, a->dtype);
+  if (!packed(p->dtype) && p->dtype != a->dtype) return fail_global(NGG_EINVAL, "%s: pages of dtype %d and queries of dtype %d", what, p->dtype, a->dtype);
   if (a->batch < 1 || a->batch > NGG_TREE_MAX || a->tree < 1 || a->tree > NGG_TREE_MAX)
     return fail_global(NGG_EINVAL, "%s: batch %d and tree %d must be 1 .. %d", what, a->batch, a->tree, NGG_TREE_MAX);
   if (a->n_heads < 1 || a->n_heads % p->n_kv_heads || a->n_heads > 1024)
@@ -92,6 +93,27 @@ ngg_status check_score(const char *what, const ngg_score_args *a, bool pointers)
   if (a->top_n && (!a->top_ids || !a->top_logprobs)) return fail_global(NGG_EINVAL, "%s: top_n without top_ids or top_logprobs", what);
   return NGG_OK;
 }
+
+// a pool of `layers` equal parts
+ngg_status check_layers(const char *what, const ngg_kv_pages *p, int32_t layers) {
+  const ngg_status st = check_pages(what, p, true);
+  if (st != NGG_OK) return st;
+  if (layers < 1 || layers > 65535 || p->n_pages % layers) return fail_global(NGG_EINVAL, "%s: %d pages in %d layers", what, p->n_pages, layers);
+  return NGG_OK;
+}
+
+ngg_status check_table(const char *what, const ngg_page_table *t) {
+  if (!t) return fail_global(NGG_EINVAL, "%s: null table", what);
+  if (!t->pages || !t->lens || !t->refs) return fail_global(NGG_EINVAL, "%s: null pointer in the table", what);
+  if (t->n_seqs < 1 || t->n_seqs > NGG_TREE_MAX) return fail_global(NGG_EINVAL, "%s: %d sequences (1 .. %d)", what, t->n_seqs, NGG_TREE_MAX);
+  if (t->page_size < 32 || t->page_size % 32) return fail_global(NGG_EINVAL, "%s: page_size %d must be a multiple of 32", what, t->page_size);
+  if (t->max_pages < 1 || (int64_t)t->max_pages * t->page_size > (1 << 30))
+    return fail_global(NGG_EINVAL, "%s: %d pages of %d positions per sequence", what, t->max_pages, t->page_size);
+  if (t->n_pages < 1 || (int64_t)t->n_pages * t->page_size > INT32_MAX)
+    return fail_global(NGG_EINVAL, "%s: %d pages of %d positions", what, t->n_pages, t->page_size);
+  return NGG_OK;
+}
+TableArgs table_of(const ngg_page_table *t) { return {t->pages, t->pages_seq, t->lens, t->refs, t->n_seqs, t->max_pages, t->n_pages, t->page_size}; }
 
 TreePlan plan_of(const ngg_kv_pages *p, const ngg_tree_args *a) {
   return tree_plan(a->dtype, p->dtype, p->head_dim, a->batch, a->tree, p->n_kv_heads, a->n_heads / p->n_kv_heads, (int64_t)a->max_pages * p->page_size);
@@ -167,8 +189,9 @@ ngg_status ngg_kv_bytes(const ngg_kv_pages *pages, int64_t *values, int64_t *exp
   const ngg_status st = check_pages("ngg_kv_bytes", pages, false);
   if (st != NGG_OK) return st;
   const int64_t heads = (int64_t)pages->n_pages * pages->page_size * pages->n_kv_heads;
-  if (values) *values = heads * pages->head_dim * (int64_t)element_size(pages->dtype);
-  if (exponents) *exponents = pages->dtype == NGG_FP8 ? heads : 0;
+  const bool four = pages->dtype == NGG_FP4;
+  if (values) *values = four ? heads * (pages->head_dim / 2) : heads * pages->head_dim * (int64_t)element_size(pages->dtype);
+  if (exponents) *exponents = four ? heads * (pages->head_dim / kGroup4) : pages->dtype == NGG_FP8 ? heads : 0;
   return NGG_OK;
 }
 
@@ -206,6 +229,70 @@ ngg_status ngg_kv_read(const ngg_kv_pages *pages, const int32_t *slots, int32_t 
   a.slots = slots; a.n_tokens = n_tokens;
   launch_kv_read(dtype, pages->dtype, a, (hipStream_t)hip_stream);
   NGG_LAUNCHED("ngg_kv_read");
+  return NGG_OK;
+}
+
+ngg_status ngg_kv_move(const ngg_kv_pages *pages, int32_t layers, const int32_t *src, const int32_t *dst, int64_t src_list, int64_t dst_list,
+                       int32_t n_lists, int32_t n, void *hip_stream) {
+  const ngg_status st = check_layers("ngg_kv_move", pages, layers);
+  if (st != NGG_OK) return st;
+  if (n_lists < 0 || n < 0 || n > NGG_TREE_MAX) return fail_global(NGG_EINVAL, "ngg_kv_move: %d lists of %d positions (up to %d)", n_lists, n, NGG_TREE_MAX);
+  if (n_lists == 0 || n == 0) return NGG_OK;
+  if (!src || !dst) return fail_global(NGG_EINVAL, "ngg_kv_move: null pointer");
+  const MoveArgs a{view(pages), layers, pages->n_pages / layers, src, dst, nullptr, n_lists, n, src_list, dst_list};
+  launch_kv_move(pages->dtype, a, (hipStream_t)hip_stream);
+  NGG_LAUNCHED("ngg_kv_move");
+  return NGG_OK;
+}
+
+ngg_status ngg_kv_copy(const ngg_kv_pages *pages, int32_t layers, const int32_t *src, const int32_t *dst, const int32_t *positions, int32_t n,
+                       void *hip_stream) {
+  const ngg_status st = check_layers("ngg_kv_copy", pages, layers);
+  if (st != NGG_OK) return st;
+  if (n < 0) return fail_global(NGG_EINVAL, "ngg_kv_copy: %d pages", n);
+  if (n == 0) return NGG_OK;
+  if (!src || !dst) return fail_global(NGG_EINVAL, "ngg_kv_copy: null pointer");
+  const MoveArgs a{view(pages), layers, pages->n_pages / layers, src, dst, positions, 1, n, 0, 0};
+  launch_kv_copy(pages->dtype, a, (hipStream_t)hip_stream);
+  NGG_LAUNCHED("ngg_kv_copy");
+  return NGG_OK;
+}
+
+ngg_status ngg_pages_fork(const ngg_page_table *table, const int32_t *sources, const int32_t *targets, int32_t n, void *hip_stream) {
+  const ngg_status st = check_table("ngg_pages_fork", table);
+  if (st != NGG_OK) return st;
+  if (n < 0 || n > NGG_TREE_MAX) return fail_global(NGG_EINVAL, "ngg_pages_fork: %d forks (up to %d)", n, NGG_TREE_MAX);
+  if (n == 0) return NGG_OK;
+  if (!sources || !targets) return fail_global(NGG_EINVAL, "ngg_pages_fork: null pointer");
+  launch_pages_fork(table_of(table), sources, targets, n, (hipStream_t)hip_stream);
+  NGG_LAUNCHED("ngg_pages_fork");
+  return NGG_OK;
+}
+
+ngg_status ngg_pages_reserve_workspace(const ngg_page_table *table, int64_t *bytes) {
+  if (!table || table->n_pages < 1) return fail_global(NGG_EINVAL, "ngg_pages_reserve_workspace: no pages");
+  if (!bytes) return fail_global(NGG_EINVAL, "ngg_pages_reserve_workspace: null bytes");
+  *bytes = (int64_t)table->n_pages * 4;
+  return NGG_OK;
+}
+
+ngg_status ngg_pages_reserve(const ngg_page_table *table, const int32_t *new_tokens, int32_t *src, int32_t *dst, int32_t *positions, int32_t *missing,
+                             void *workspace, int64_t workspace_bytes, void *hip_stream) {
+  const ngg_status st = check_table("ngg_pages_reserve", table);
+  if (st != NGG_OK) return st;
+  if (!new_tokens || !src || !dst || !positions || !missing) return fail_global(NGG_EINVAL, "ngg_pages_reserve: null pointer");
+  if (!workspace || !aligned(workspace, 16) || workspace_bytes < (int64_t)table->n_pages * 4)
+    return fail_global(NGG_EINVAL, "ngg_pages_reserve: needs %lld bytes of 16-byte aligned workspace", (long long)table->n_pages * 4);
+  launch_pages_reserve(table_of(table), new_tokens, {src, dst, positions, missing}, (int32_t *)workspace, (hipStream_t)hip_stream);
+  NGG_LAUNCHED("ngg_pages_reserve");
+  return NGG_OK;
+}
+
+ngg_status ngg_pages_release(const ngg_page_table *table, const int32_t *keep, void *hip_stream) {
+  const ngg_status st = check_table("ngg_pages_release", table);
+  if (st != NGG_OK) return st;
+  launch_pages_release(table_of(table), keep, (hipStream_t)hip_stream);
+  NGG_LAUNCHED("ngg_pages_release");
   return NGG_OK;
 }
 

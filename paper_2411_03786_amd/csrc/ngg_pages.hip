@@ -1,0 +1,322 @@
+// What happens to the pages of a cache between steps: positions that move (the accepted path of a tree), pages that are copied, and the
+// lists, lengths and reference counts of sequences that share pages.  Bits are moved as they are; bound by memory or by a launch.
+#include "ngg_operators.h"
+
+#include <algorithm>
+
+namespace ngg {
+
+// The bytes of a cached position of one head in its (page, head), by units that no other position has a part in: KU of keys, VU of
+// values, and EU exponents of either.
+template <int CACHE, int HD> struct Units;
+template <int HD> struct Units<NGG_F32, HD> {
+  static constexpr int KU = HD / 4, KB = 16, VU = HD, VB = 4, EU = 0, value_bits = 32;
+  static __device__ __forceinline__ size_t k(int pos, int u) { return k_offset(pos, u * 4, HD, 4) * 4; }
+  static __device__ __forceinline__ size_t v(int pos, int u) { return v_offset(pos, u, HD, 4) * 4; }
+  static __device__ __forceinline__ size_t ke(int, int) { return 0; }
+  static __device__ __forceinline__ size_t ve(int, int) { return 0; }
+};
+template <int HD> struct Units<NGG_BF16, HD> {
+  static constexpr int KU = HD / 8, KB = 16, VU = HD, VB = 2, EU = 0, value_bits = 16;
+  static __device__ __forceinline__ size_t k(int pos, int u) { return k_offset(pos, u * 8, HD, 2) * 2; }
+  static __device__ __forceinline__ size_t v(int pos, int u) { return v_offset(pos, u, HD, 2) * 2; }
+  static __device__ __forceinline__ size_t ke(int, int) { return 0; }
+  static __device__ __forceinline__ size_t ve(int, int) { return 0; }
+};
+template <int HD> struct Units<NGG_FP8, HD> {
+  static constexpr int KU = HD / 8, KB = 8, VU = HD, VB = 1, EU = 1, value_bits = 8;
+  static __device__ __forceinline__ size_t k(int pos, int u) { return k_offset8(pos, u * 8, HD); }
+  static __device__ __forceinline__ size_t v(int pos, int u) { return v_offset8(pos, u, HD); }
+  static __device__ __forceinline__ size_t ke(int pos, int) { return pos; }
+  static __device__ __forceinline__ size_t ve(int pos, int) { return pos; }
+};
+template <int HD> struct Units<NGG_FP4, HD> {
+  static constexpr int KU = 4, KB = HD / 8, VU = HD / 2, VB = 1, EU = HD / 32, value_bits = 4;
+  static __device__ __forceinline__ size_t k(int pos, int u) { return k_offset4(pos, u * (HD / 4), HD); }
+  static __device__ __forceinline__ size_t v(int pos, int u) { return v_offset4(pos, u / 16 * 32 + u % 16, HD); }
+  static __device__ __forceinline__ size_t ke(int pos, int u) { return k_exp_offset4(pos, u * 32, HD); }
+  static __device__ __forceinline__ size_t ve(int pos, int u) { return v_exp_offset4(pos, u * 32, HD); }
+};
+
+template <int BYTES> struct Unit;
+template <> struct Unit<1> { typedef uint8_t T; };
+template <> struct Unit<2> { typedef uint16_t T; };
+template <> struct Unit<4> { typedef uint32_t T; };
+template <> struct Unit<8> { typedef u32x2 T; };
+template <> struct Unit<16> { typedef u32x4 T; };
+
+// Moves one unit of every entry of a list: all are read before the first is written.  at(pos): the unit's byte offset in its (page,
+// head).  Up to 16 entries wait in registers, more in LDS.
+struct Entry { int64_t from, to; int from_pos, to_pos; };  // first position of the (page, head 0); -1: none
+constexpr int kInRegisters = 16;
+template <int BYTES, typename At>
+__device__ __forceinline__ void move_unit(uint8_t *base, const Entry *list, int n, int64_t head, int position_bytes, At at, uint8_t *wait) {
+  typedef typename Unit<BYTES>::T U;
+  auto place = [&](int64_t first, int pos) { return reinterpret_cast<U *>(base + (first + head) * position_bytes + at(pos)); };
+  if (n <= kInRegisters) {
+    U x[kInRegisters];
+#pragma unroll
+    for (int i = 0; i < kInRegisters; ++i)
+      if (i < n && list[i].from >= 0) x[i] = *place(list[i].from, list[i].from_pos);
+#pragma unroll
+    for (int i = 0; i < kInRegisters; ++i)
+      if (i < n && list[i].from >= 0) *place(list[i].to, list[i].to_pos) = x[i];
+    return;
+  }
+  U *mine = reinterpret_cast<U *>(wait) + threadIdx.x;     // (a thread's own column)
+  for (int i = 0; i < n; ++i)
+    if (list[i].from >= 0) mine[i * blockDim.x] = *place(list[i].from, list[i].from_pos);
+  for (int i = 0; i < n; ++i)
+    if (list[i].from >= 0) *place(list[i].to, list[i].to_pos) = mine[i * blockDim.x];
+}
+
+// One thread per unit of a (layer, list, head); a thread reads and writes bytes that no other one touches.
+template <int CACHE, int HD>
+__global__ __launch_bounds__(256) void kv_move_kernel(const MoveArgs a, int lists_first) {
+  typedef Units<CACHE, HD> U;
+  constexpr int ALL = U::KU + U::VU + 2 * U::EU;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  Entry *list = reinterpret_cast<Entry *>(smem);
+  uint8_t *wait = smem + (a.n + a.n % 2) * sizeof(Entry);
+  const int layer = blockIdx.z, b = lists_first + blockIdx.y, ps = a.p.page_size, Hkv = a.p.Hkv;
+  const int positions = a.layer_pages * ps;                // of a layer
+  for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
+    const int from = a.src[b * a.src_list + i], to = a.dst[b * a.dst_list + i];
+    Entry e = {-1, -1, 0, 0};
+    if (from >= 0 && from < positions && to >= 0 && to < positions) {
+      e.from = (int64_t)(layer * a.layer_pages + from / ps) * Hkv * ps;
+      e.to = (int64_t)(layer * a.layer_pages + to / ps) * Hkv * ps;
+      e.from_pos = from % ps;
+      e.to_pos = to % ps;
+    }
+    list[i] = e;
+  }
+  __syncthreads();
+  const int unit = blockIdx.x * blockDim.x + threadIdx.x;
+  if (unit >= Hkv * ALL) return;
+  const int64_t head = (int64_t)(unit / ALL) * ps;
+  const int u = unit % ALL;
+  if (u < U::KU) move_unit<U::KB>((uint8_t *)a.p.k, list, a.n, head, HD * U::value_bits / 8, [&](int pos) { return U::k(pos, u); }, wait);
+  else if (u < U::KU + U::VU) move_unit<U::VB>((uint8_t *)a.p.v, list, a.n, head, HD * U::value_bits / 8, [&](int pos) { return U::v(pos, u - U::KU); }, wait);
+  else if (u < U::KU + U::VU + U::EU) move_unit<1>(a.p.k_exp, list, a.n, head, U::EU, [&](int pos) { return U::ke(pos, u - U::KU - U::VU); }, wait);
+  else move_unit<1>(a.p.v_exp, list, a.n, head, U::EU, [&](int pos) { return U::ve(pos, u - U::KU - U::VU - U::EU); }, wait);
+}
+
+// Copies pages, of each the tiles of 32 positions that hold its first positions[i] (all without): one workgroup per (layer, page, head).
+__global__ __launch_bounds__(256) void kv_copy_kernel(const MoveArgs a, int first, int tile_bytes, int exp_bytes) {
+  const int layer = blockIdx.z, i = first + blockIdx.y, h = blockIdx.x, ps = a.p.page_size;
+  const int from = a.src[i], to = a.dst[i];
+  if (from < 0 || from >= a.layer_pages || to < 0 || to >= a.layer_pages) return;
+  const int n = a.positions ? min(max(a.positions[i], 0), ps) : ps, tiles = (n + 31) / 32;
+  const int64_t tile0 = ((int64_t)(layer * a.layer_pages + from) * a.p.Hkv + h) * (ps / 32), tile1 = ((int64_t)(layer * a.layer_pages + to) * a.p.Hkv + h) * (ps / 32);
+  auto copy = [&](void *base, int bytes) {
+    const u32x4 *s = reinterpret_cast<const u32x4 *>((const uint8_t *)base + tile0 * bytes);
+    u32x4 *d = reinterpret_cast<u32x4 *>((uint8_t *)base + tile1 * bytes);
+    for (int j = threadIdx.x; j < tiles * bytes / 16; j += 256) d[j] = s[j];
+  };
+  copy(a.p.k, tile_bytes);
+  copy(a.p.v, tile_bytes);
+  if (exp_bytes) {
+    copy(a.p.k_exp, exp_bytes);
+    copy(a.p.v_exp, exp_bytes);
+  }
+}
+
+template <int CACHE, int HD>
+static void launch_move(const MoveArgs &a, hipStream_t s) {
+  typedef Units<CACHE, HD> U;
+  const int units = a.p.Hkv * (U::KU + U::VU + 2 * U::EU);
+  // what waits in LDS: as many threads as 64 KB have room for
+  const int list = (a.n + a.n % 2) * (int)sizeof(Entry), threads = a.n <= kInRegisters ? 256 : a.n <= 64 ? 64 : a.n <= 128 ? 32 : a.n <= 256 ? 16 : a.n <= 512 ? 8 : 4;
+  const size_t lds = list + (a.n <= kInRegisters ? 0 : (size_t)threads * a.n * 16);
+  allow_lds(&kv_move_kernel<CACHE, HD>, lds);
+  for (int at = 0; at < a.lists; at += 65535)
+    hipLaunchKernelGGL((kv_move_kernel<CACHE, HD>), dim3((units + threads - 1) / threads, std::min(a.lists - at, 65535), a.layers), dim3(threads), lds, s, a, at);
+}
+template <int CACHE>
+static void move_head(const MoveArgs &a, hipStream_t s) {
+  if (a.p.hd == 32) launch_move<CACHE, 32>(a, s);
+  else if (a.p.hd == 64) launch_move<CACHE, 64>(a, s);
+  else launch_move<CACHE, 128>(a, s);
+}
+void launch_kv_move(int cache, const MoveArgs &a, hipStream_t s) {
+  if (cache == NGG_F32) move_head<NGG_F32>(a, s);
+  else if (cache == NGG_BF16) move_head<NGG_BF16>(a, s);
+  else if (cache == NGG_FP8) move_head<NGG_FP8>(a, s);
+  else move_head<NGG_FP4>(a, s);
+}
+void launch_kv_copy(int cache, const MoveArgs &a, hipStream_t s) {
+  const int bits = cache == NGG_F32 ? 32 : cache == NGG_BF16 ? 16 : cache == NGG_FP8 ? 8 : 4;
+  const int exps = cache == NGG_FP8 ? 32 : cache == NGG_FP4 ? a.p.hd : 0;
+  for (int at = 0; at < a.n; at += 65535)
+    hipLaunchKernelGGL(kv_copy_kernel, dim3(a.p.Hkv, std::min(a.n - at, 65535), a.layers), dim3(256), 0, s, a, at, 4 * a.p.hd * bits, exps);
+}
+
+// ---- page lists -------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ bool is_page(const TableArgs &a, int p) { return p >= 0 && p < a.n_pages; }
+__device__ __forceinline__ void drop(const TableArgs &a, int p) {
+  if (is_page(a, p)) atomicSub(a.refs + p, 1);
+}
+
+// One workgroup per fork: target's pages are given back, source's are shared.  The sums of the counts do not hang on their order.
+__global__ __launch_bounds__(256) void pages_fork_kernel(const TableArgs a, const int32_t *sources, const int32_t *targets, int n) {
+  const int i = blockIdx.x, from = sources[i], to = targets[i];
+  if (from < 0 || from >= a.n_seqs || to < 0 || to >= a.n_seqs) return;
+  // a sequence that is a source of the call stays as it is, and of equal targets the first counts
+  bool taken = false;
+  for (int k = threadIdx.x; k < n; k += 256) taken |= sources[k] == to || (k < i && targets[k] == to);
+  if (__syncthreads_or(taken)) return;
+  const int len = max(a.lens[from], 0), held = (int)(((int64_t)len + a.page_size - 1) / a.page_size);
+  for (int j = threadIdx.x; j < a.max_pages; j += 256) {
+    int32_t *at = a.pages + to * a.pages_seq + j;
+    const int p = j < held ? a.pages[from * a.pages_seq + j] : -1;
+    drop(a, *at);
+    if (is_page(a, p)) atomicAdd(a.refs + p, 1);
+    *at = is_page(a, p) ? p : -1;
+  }
+  if (threadIdx.x == 0) a.lens[to] = len;
+}
+
+__global__ __launch_bounds__(256) void pages_release_kernel(const TableArgs a, const int32_t *keep) {
+  const int s = blockIdx.x, k = keep ? keep[s] : INT32_MAX;
+  if (k < 0) return;
+  const int len = min(max(a.lens[s], 0), k), held = (int)(((int64_t)len + a.page_size - 1) / a.page_size);
+  for (int j = held + threadIdx.x; j < a.max_pages; j += 256) {
+    int32_t *at = a.pages + s * a.pages_seq + j;
+    drop(a, *at);
+    *at = -1;
+  }
+  __syncthreads();                                         // (every thread has read the length)
+  if (threadIdx.x == 0) a.lens[s] = len;
+}
+
+// The exclusive sum of a workgroup's numbers, and their total
+__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t *part, int64_t &total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  int64_t inc = x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t up = __shfl_up(inc, o);
+    if (lane >= o) inc += up;
+  }
+  if (lane == 63) part[wave] = inc;
+  __syncthreads();
+  int64_t before = 0;
+  total = 0;
+  for (int v = 0; v < waves; ++v) {
+    if (v < wave) before += part[v];
+    total += part[v];
+  }
+  __syncthreads();
+  return before + inc - x;
+}
+
+// One workgroup.  The entries that the new tokens reach, of one sequence behind the other, are counted through; the pages they need are
+// the lowest free ones in that order.  Nothing changes where there are too few.
+__global__ __launch_bounds__(1024) void pages_reserve_kernel(const TableArgs a, const int32_t *new_tokens, const ReserveOut out, int32_t *free_list) {
+  __shared__ int64_t pre[NGG_TREE_MAX + 1];                // entries before a sequence's
+  __shared__ int first[NGG_TREE_MAX];                      // its first entry's place
+  __shared__ int shared_page[NGG_TREE_MAX];                // the page that it would write to, while others hold it; -1
+  __shared__ int64_t part[16];
+  const int s = threadIdx.x, ps = a.page_size;
+  int64_t n = 0, beyond = 0, total, too_long;
+  int mine = -1, rest = 0, refs = 0;
+  if (s < a.n_seqs) {
+    const int64_t len = max(a.lens[s], 0), want = max(new_tokens[s], 0);
+    const int64_t j0 = len / ps, end = want ? (len + want + ps - 1) / ps : j0;
+    beyond = max(end - a.max_pages, (int64_t)0);
+    n = max(min(end, (int64_t)a.max_pages) - j0, (int64_t)0);
+    first[s] = (int)j0;
+    rest = (int)(len % ps);
+    if (n && rest) {
+      mine = a.pages[s * a.pages_seq + j0];
+      if (!is_page(a, mine)) mine = -1;
+      else refs = a.refs[mine];
+    }
+    shared_page[s] = mine;
+  }
+  const int64_t at = block_sum(n, part, total);
+  (void)block_sum(beyond, part, too_long);
+  if (s < a.n_seqs) pre[s] = at;
+  if (s == 0) pre[a.n_seqs] = total;
+  __syncthreads();
+  // of the sequences that go on in a page that nobody else holds, the last keeps it
+  bool copies = mine >= 0 && refs > 1;
+  if (copies) {
+    int users = 0, last = 0;
+    for (int k = 0; k < a.n_seqs; ++k)
+      if (shared_page[k] == mine) { ++users; last = k; }
+    copies = !(users == refs && last == s);
+  }
+  __syncthreads();
+  if (s < a.n_seqs && !copies) shared_page[s] = -1;
+  __syncthreads();
+  // entry f of all: its sequence and place, and whether it needs a page
+  auto needs = [&](int64_t f, int &q, int &j) {
+    int lo = 0, hi = a.n_seqs;                             // pre[lo] <= f < pre[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (pre[mid] <= f) lo = mid;
+      else hi = mid;
+    }
+    q = lo;
+    j = first[lo] + (int)(f - pre[lo]);
+    return (f == pre[lo] && shared_page[lo] >= 0) || a.pages[q * a.pages_seq + j] < 0;
+  };
+  int64_t need = 0;
+  for (int64_t f0 = 0; f0 < total; f0 += 1024) {
+    const int64_t f = f0 + threadIdx.x;
+    int q, j;
+    need += __syncthreads_count(f < total && needs(f, q, j));
+  }
+  int64_t found = 0;
+  for (int64_t p0 = 0; p0 < a.n_pages && found < need; p0 += 1024) {
+    const int64_t p = p0 + threadIdx.x;
+    const bool free = p < a.n_pages && a.refs[p] == 0;
+    int64_t more;
+    const int64_t rank = found + block_sum(free, part, more);
+    if (free && rank < need) free_list[rank] = (int)p;
+    found += more;
+  }
+  __syncthreads();
+  const int64_t missing = max(need - found, (int64_t)0) + too_long;
+  if (s == 0) *out.missing = (int)min(missing, (int64_t)INT32_MAX);
+  if (s < a.n_seqs) {
+    out.src[s] = out.dst[s] = -1;
+    out.positions[s] = 0;
+  }
+  if (missing) return;
+  __syncthreads();
+  int64_t rank0 = 0;
+  for (int64_t f0 = 0; f0 < total; f0 += 1024) {
+    const int64_t f = f0 + threadIdx.x;
+    int q = 0, j = 0;
+    const bool take = f < total && needs(f, q, j);
+    int64_t more;
+    const int64_t rank = rank0 + block_sum(take, part, more);
+    rank0 += more;
+    if (!take) continue;
+    const int page = free_list[rank];
+    if (f == pre[q] && shared_page[q] >= 0) {
+      out.src[q] = shared_page[q];
+      out.dst[q] = page;
+      out.positions[q] = max(a.lens[q], 0) % ps;
+      atomicSub(a.refs + shared_page[q], 1);
+    }
+    a.pages[q * a.pages_seq + j] = page;
+    a.refs[page] = 1;
+  }
+}
+
+void launch_pages_fork(const TableArgs &a, const int32_t *sources, const int32_t *targets, int n, hipStream_t s) {
+  hipLaunchKernelGGL(pages_fork_kernel, dim3(n), dim3(256), 0, s, a, sources, targets, n);
+}
+void launch_pages_reserve(const TableArgs &a, const int32_t *new_tokens, const ReserveOut &out, int32_t *free_list, hipStream_t s) {
+  hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(1024), 0, s, a, new_tokens, out, free_list);
+}
+void launch_pages_release(const TableArgs &a, const int32_t *keep, hipStream_t s) {
+  hipLaunchKernelGGL(pages_release_kernel, dim3(a.n_seqs), dim3(256), 0, s, a, keep);
+}
+
+}  // namespace ngg

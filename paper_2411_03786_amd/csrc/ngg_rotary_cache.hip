@@ -6,10 +6,6 @@
 
 namespace ngg {
 
-// Either element of a pair turned by the angle of (c, s); o: the other one, s: negative for the first.  The order of operations is
-// written out, so that every kernel rounds alike.
-__device__ __forceinline__ float turned(float x, float o, float c, float s) { return __builtin_fmaf(x, c, __fmul_rn(o, s)); }
-
 // Any sizes, strides and alignment: one thread per pair of elements of a head, or per element behind the rotated ones.
 template <typename T>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
@@ -167,20 +163,6 @@ static void launch_rotary_type(const RotaryArgs &a, hipStream_t s) {
 void launch_rotary(int dtype, const RotaryArgs &a, hipStream_t s) {
   if (dtype == NGG_F32) launch_rotary_type<float>(a, s);
   else launch_rotary_type<bf16_t>(a, s);
-}
-
-// Element d of a token's key, rotated and rounded to its own type as rotary_kernel leaves it.
-template <typename T>
-__device__ __forceinline__ float rotated(const CacheArgs &a, const T *row, int t, int d) {
-  const float x = to_f32(row[d]);
-  if (!a.cos || d >= a.rd) return x;
-  const int half = a.rd / 2, pos = a.positions[t];
-  const bool second = a.interleaved ? (d & 1) != 0 : d >= half;
-  const int pair = a.interleaved ? d >> 1 : (second ? d - half : d);
-  const float o = to_f32(row[a.interleaved ? d ^ 1 : (second ? d - half : d + half)]);
-  const bool ok = pos >= 0 && pos < a.n_positions;
-  const float c = ok ? a.cos[(int64_t)pos * half + pair] : __builtin_nanf(""), s = ok ? a.sin[(int64_t)pos * half + pair] : 0.0f;
-  return to_f32(from_f32<T>(turned(x, o, c, second ? s : -s)));
 }
 
 // One wave per (token, head), two elements a lane: calls of few rows, whose time is the chain slot -> row -> exponent -> store (32 tokens
@@ -693,7 +675,13 @@ template <typename T, typename CT> struct ReadLaunch {
     else hipLaunchKernelGGL((kv_read_kernel<T, CT>), dim3((all.n_tokens * all.p.Hkv + 3) / 4), dim3(256), 0, s, all);
   }
 };
-void launch_kv_write(int dtype, int cache, const CacheArgs &a, hipStream_t s) { by_types<WriteLaunch>(dtype, cache, a, s); }
-void launch_kv_read(int dtype, int cache, const CacheArgs &a, hipStream_t s) { by_types<ReadLaunch>(dtype, cache, a, s); }
+void launch_kv_write(int dtype, int cache, const CacheArgs &a, hipStream_t s) {
+  if (cache == NGG_FP4) launch_kv4_write(dtype, a, s);
+  else by_types<WriteLaunch>(dtype, cache, a, s);
+}
+void launch_kv_read(int dtype, int cache, const CacheArgs &a, hipStream_t s) {
+  if (cache == NGG_FP4) launch_kv4_read(dtype, a, s);
+  else by_types<ReadLaunch>(dtype, cache, a, s);
+}
 
 }  // namespace ngg

@@ -149,6 +149,75 @@ py::tuple kv_read(uintptr_t pages_at, const Tensor &bytes, const Tensor &slots, 
   return py::make_tuple(k, v);
 }
 
+// src and dst of a move: int32 [lists, n], or [n]
+void kv_move(uintptr_t pages_at, const Tensor &bytes, int64_t layers, const Tensor &src, const Tensor &dst) {
+  for (const Tensor *t : {&src, &dst}) {
+    if (t->scalar_type() != at::kInt || t->dim() < 1 || t->dim() > 2 || t->sizes() != src.sizes())
+      throw py::type_error("src and dst must be int32 tensors of one shape, [lists, positions] or [positions]");
+    inner(*t, "src and dst");
+  }
+  on_gpu(bytes, {&src, &dst});
+  const bool many = src.dim() == 2;
+  check(ngg_kv_move(pages_of(pages_at), narrow(layers, "layers"), (const int32_t *)src.data_ptr(), (const int32_t *)dst.data_ptr(), many ? src.stride(0) : 0,
+                    many ? dst.stride(0) : 0, many ? narrow(src.size(0), "lists") : 1, narrow(src.size(-1), "positions"), stream()));
+}
+
+void kv_copy(uintptr_t pages_at, const Tensor &bytes, int64_t layers, const Tensor &src, const Tensor &dst, const Maybe &positions) {
+  if (src.dim() != 1) throw py::type_error("src must be a contiguous int32 tensor of one dimension");
+  const int64_t n = src.size(0);
+  on_gpu(bytes, {&src, &dst, ptr(positions)});
+  ints(src, "src", n);
+  ints(dst, "dst", n);
+  if (positions) ints(*positions, "positions", n);
+  check(ngg_kv_copy(pages_of(pages_at), narrow(layers, "layers"), (const int32_t *)src.data_ptr(), (const int32_t *)dst.data_ptr(),
+                    positions ? (const int32_t *)positions->data_ptr() : nullptr, narrow(n, "pages"), stream()));
+}
+
+// A table's tensors
+ngg_page_table table_of(const Tensor &pages, const Tensor &lens, const Tensor &refs, int64_t page_size) {
+  if (pages.scalar_type() != at::kInt || pages.dim() != 2) throw py::type_error("pages must be an int32 tensor [sequences, max_pages]");
+  on_gpu(pages, {&lens, &refs});
+  inner(pages, "pages");
+  ints(lens, "lens", pages.size(0));
+  if (refs.dim() != 1) throw py::type_error("refs must be a contiguous int32 tensor of one dimension");
+  ints(refs, "refs", refs.size(0));
+  return {(int32_t *)pages.data_ptr(), pages.stride(0), (int32_t *)lens.data_ptr(), (int32_t *)refs.data_ptr(), narrow(pages.size(0), "sequences"),
+          narrow(pages.size(1), "max_pages"), narrow(refs.size(0), "pages"), narrow(page_size, "page_size")};
+}
+
+void pages_fork(const Tensor &pages, const Tensor &lens, const Tensor &refs, int64_t page_size, const Tensor &sources, const Tensor &targets) {
+  const ngg_page_table t = table_of(pages, lens, refs, page_size);
+  if (sources.dim() != 1) throw py::type_error("sources must be a contiguous int32 tensor of one dimension");
+  const int64_t n = sources.size(0);
+  on_gpu(pages, {&sources, &targets});
+  ints(sources, "sources", n);
+  ints(targets, "targets", n);
+  check(ngg_pages_fork(&t, (const int32_t *)sources.data_ptr(), (const int32_t *)targets.data_ptr(), narrow(n, "forks"), stream()));
+}
+
+py::tuple pages_reserve(const Tensor &pages, const Tensor &lens, const Tensor &refs, int64_t page_size, const Tensor &new_tokens) {
+  const ngg_page_table t = table_of(pages, lens, refs, page_size);
+  const int64_t n = pages.size(0);
+  on_gpu(pages, {&new_tokens});
+  ints(new_tokens, "new_tokens", n);
+  int64_t need = 0;
+  check(ngg_pages_reserve_workspace(&t, &need));
+  // one allocation for the numbers: src, dst, positions, missing
+  const Tensor out = at::empty({3 * n + 1}, pages.options()), ws = at::empty({need}, pages.options().dtype(at::kByte));
+  int32_t *at = (int32_t *)out.data_ptr();
+  check(ngg_pages_reserve(&t, (const int32_t *)new_tokens.data_ptr(), at, at + n, at + 2 * n, at + 3 * n, ws.data_ptr(), need, stream()));
+  return py::make_tuple(out.narrow(0, 0, n), out.narrow(0, n, n), out.narrow(0, 2 * n, n), out.narrow(0, 3 * n, 1));
+}
+
+void pages_release(const Tensor &pages, const Tensor &lens, const Tensor &refs, int64_t page_size, const Maybe &keep) {
+  const ngg_page_table t = table_of(pages, lens, refs, page_size);
+  if (keep) {
+    on_gpu(pages, {ptr(keep)});
+    ints(*keep, "keep", pages.size(0));
+  }
+  check(ngg_pages_release(&t, keep ? (const int32_t *)keep->data_ptr() : nullptr, stream()));
+}
+
 py::object tree_attention(uintptr_t pages_at, const Tensor &bytes, const Tensor &q, const Tensor &pages, const Tensor &context_lens, const Maybe &mask,
                           const Maybe &tree_lens, std::optional<double> scale, const Maybe &out, bool want_lse, const Maybe &workspace) {
   const ngg_kv_pages *p = pages_of(pages_at);
@@ -252,6 +321,11 @@ PYBIND11_MODULE(ngg_torch, mod) {
     if (!THPDtype_Check(dtype.ptr())) throw py::type_error("dtype must be a torch.dtype");
     return kv_read(pages, bytes, slots, reinterpret_cast<THPDtype *>(dtype.ptr())->scalar_type);
   });
+  mod.def("kv_move", &kv_move);
+  mod.def("kv_copy", &kv_copy);
+  mod.def("pages_fork", &pages_fork);
+  mod.def("pages_reserve", &pages_reserve);
+  mod.def("pages_release", &pages_release);
   mod.def("tree_attention", &tree_attention);
   mod.def("token_logprobs", &token_logprobs);
 }

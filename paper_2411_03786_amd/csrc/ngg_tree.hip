@@ -10,25 +10,12 @@
 // workgroup each instead.  The lengths are read on the device.
 //
 // Up to some 200 rows to a key head the keys and values are what a call costs (HBM), above that the products are.
-#include "ngg_operators.h"
+#include "ngg_tree.h"
 #include "ngg_epilogues.h"
 
 #include <algorithm>
 
 namespace ngg {
-
-constexpr float kLn2 = 0.6931471805599453f;
-
-template <> __device__ __forceinline__ Frag<bf16_t> zero_frag<bf16_t>() {
-  Frag<bf16_t> f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) f.v[e] = (bf16_t)0.0f;
-  return f;
-}
-__device__ __forceinline__ void pack_frag(Frag<bf16_t> &f, const float *p) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) f.v[e] = (bf16_t)p[e];
-}
 
 // A fragment from the 16-byte parts of a tile as they lie in memory.
 __device__ __forceinline__ void raw_frag(Frag<bf16_t> &f, const u32x4 *r) { f.v = __builtin_bit_cast(bf16x8, r[0]); }
@@ -52,143 +39,6 @@ __device__ __forceinline__ void widen(Frag<float> &f, unsigned lo, unsigned hi, 
   f.v[6] = __builtin_amdgcn_cvt_f32_fp8(hi, 2) * scale; f.v[7] = __builtin_amdgcn_cvt_f32_fp8(hi, 3) * scale;
 }
 
-// The sequence's cached and tree tokens, cut to what the page list can hold.
-struct SeqLens { int ctx, tree; };
-__device__ __forceinline__ SeqLens seq_lens(const TreeArgs &a, int b) {
-  const int cap = a.max_pages * a.p.page_size;
-  SeqLens s;
-  s.ctx = min(max(a.context_lens[b], 0), cap);
-  s.tree = a.tree_lens ? min(max(a.tree_lens[b], 0), a.T) : a.T;
-  return s;
-}
-__device__ __forceinline__ int seq_keys(const TreeArgs &a, const SeqLens &s) {
-  return s.tree ? min(s.ctx + s.tree, a.max_pages * a.p.page_size) : 0;
-}
-
-// Steps of KS keys of a sequence (of one head): one at least, so that someone writes its rows
-template <int KS>
-__device__ __forceinline__ int seq_steps(const TreeArgs &a, int b) { return max(1, (seq_keys(a, seq_lens(a, b)) + KS - 1) / KS); }
-
-// Running totals of those: pre[b] steps lie before sequence b, pre[B] in all.  The first wave's work.
-template <int KS>
-__device__ __forceinline__ void step_totals(const TreeArgs &a, int *pre) {
-  const int tid = threadIdx.x;
-  if (tid < 64) {
-    int carry = 0;
-#pragma unroll 1
-    for (int first = 0; first < a.B; first += 64) {
-      const int b = first + tid, n = b < a.B ? seq_steps<KS>(a, b) : 0;
-      int inc = n;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int up = __shfl_up(inc, o);
-        if (tid >= o) inc += up;
-      }
-      if (b < a.B) pre[b] = carry + inc - n;
-      carry += __builtin_amdgcn_readlane(inc, 63);
-    }
-    if (tid == 0) pre[a.B] = carry;
-  }
-  __syncthreads();
-}
-
-// Steps of a share of the list: as many shares as workgroups were launched for, but of 256 keys at least where there are many (us with
-// one step of 128 keys and with two, 16 bits: 88 steps in all 12.4, 14.4; 240 steps 11.4, 12.1; 384 steps 15.9, 13.4; 504 steps 21.1, 18.2)
-template <int KS>
-__device__ __forceinline__ int share_steps(const TreeArgs &a, int total) {
-  return max((int)((unsigned)(total + a.ranges - 1) / (unsigned)a.ranges), KS == 128 && total < 256 ? 1 : 256 / KS);
-}
-
-// A workgroup's place and share of the list, one (sequence, head) after the other.  Whole numbers of 32 bits (the host sees to that):
-// what runs once costs a launch its instruction fetches.
-template <int KS>
-struct Work {
-  const TreeArgs &a;
-  int *pre;
-  int z, range, u, u_end;
-  // of the part at hand: steps s_begin .. s_end - 1 of `steps`
-  int b, hk, s_begin, s_end, steps;
-
-  __device__ __forceinline__ Work(const TreeArgs &args, int *totals) : a(args), pre(totals), b(0) {
-    // the row tiles of a share run next to each other on one die: its keys come from memory once
-    if (a.Z == 1) {
-      z = 0;
-      range = blockIdx.x;
-    } else {
-      const bool dealt = a.ranges % 8 == 0;
-      const int slot = dealt ? blockIdx.x / 8 : blockIdx.x;
-      range = slot / a.Z;
-      z = slot - range * a.Z;
-      if (dealt) range = range * 8 + blockIdx.x % 8;
-    }
-    if (a.whole) {                                         // a (sequence, head) for each
-      u = range;
-      u_end = range + 1;
-      return;
-    }
-    step_totals<KS>(a, pre);
-    const int total = before(a.B) * a.p.Hkv, per = share_steps<KS>(a, total);
-    u = range * per;
-    u_end = min(u + per, total);
-  }
-  // (uniform: what comes from LDS does not look it, and would keep every address in vector registers)
-  __device__ __forceinline__ int before(int i) const { return __builtin_amdgcn_readfirstlane(pre[i]); }
-  __device__ __forceinline__ bool next() {
-    if (u >= u_end) return false;
-    if (a.whole) {
-      b = u / a.p.Hkv;
-      hk = u - b * a.p.Hkv;
-      s_begin = 0;
-      steps = s_end = seq_steps<KS>(a, b);
-      ++u;
-      return true;
-    }
-    int p0 = before(b), p1 = before(b + 1);
-    while (p1 * a.p.Hkv <= u) {
-      ++b;
-      p0 = p1;
-      p1 = before(b + 1);
-    }
-    steps = p1 - p0;
-    const int in_b = u - p0 * a.p.Hkv;
-    hk = in_b / steps;
-    s_begin = in_b - hk * steps;
-    s_end = min(steps, s_begin + (u_end - u));
-    u += s_end - s_begin;
-    return true;
-  }
-  __device__ __forceinline__ bool is_whole() const { return s_begin == 0 && s_end == steps; }
-  // where a part goes: one that begins inside a (sequence, head) is the first of its share, one that ends inside it the last
-  __device__ __forceinline__ size_t part() const { return ((size_t)range * a.Z + z) * 2 + (s_begin == 0 ? 1 : 0); }
-};
-
-// Two words of a token's row of the mask, from the one that holds tree position at (or the first): enough for the 64 positions from
-// there.  Without a mask every bit is set.
-struct MaskWindow { uint64_t lo, hi; };
-__device__ __forceinline__ MaskWindow mask_window(const TreeArgs &a, int b, int tok, int at) {
-  MaskWindow w = {~0ull, ~0ull};
-  if (!a.mask) return w;
-  const int words = (a.T + 63) / 64, i = max(at, 0) >> 6;
-  const uint64_t *row = a.mask + b * a.mask_batch + min(tok, a.T - 1) * a.mask_token;
-  w.lo = row[min(i, words - 1)];
-  w.hi = row[min(i + 1, words - 1)];                       // (words that are not there are of positions behind every token)
-  return w;
-}
-// Eight bits, bit e set if token t sees tree position at + e (negative: the context).  w: the window from tree position from;
-// tree_keys: how many tree positions there are
-__device__ __forceinline__ unsigned visible8(const MaskWindow &w, int from, int t, int at, int tree_keys) {
-  unsigned v = 0xff;
-  if (at + 7 >= 0) {
-    const int sh = max(at, 0) - (max(from, 0) & ~63);      // 0 .. 127
-    uint64_t x = sh >= 64 ? w.hi >> (sh & 63) : w.lo >> sh;
-    if (sh > 0 && sh < 64) x |= w.hi << (64 - sh);
-    v = (unsigned)(x & 0xff);
-    if (at < 0) v = ((v << -at) | ((1u << -at) - 1)) & 0xff;
-  }
-  const int n = min(t + 1, tree_keys) - at;                // positions at .. at + n - 1 are there and not behind t
-  return n >= 8 ? v : n <= 0 ? 0u : v & ((1u << n) - 1);
-}
-
 // Takes zeros in the place of values of positions that are not there (pos + e >= n) and of those that are not finite; true if there
 // were any of the latter.
 template <typename T>
@@ -202,30 +52,6 @@ __device__ __forceinline__ bool only_there(Frag<T> &f, int pos, int n) {
     bad |= b;
   }
   return bad;
-}
-
-// Elements of a query row, 16-byte aligned.
-__device__ __forceinline__ Frag<bf16_t> load_frag_row(const bf16_t *p) {
-  Frag<bf16_t> f;
-  f.v = *reinterpret_cast<const bf16x8 *>(p);
-  return f;
-}
-__device__ __forceinline__ Frag<float> load_frag_row(const float *p) { return load_frag(p); }
-
-__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? -__builtin_inff() : kLn2 * (m + __builtin_log2f(l)); }
-template <typename T>
-__device__ __forceinline__ void put4(T *out, const f32x4 &o, int vec) {
-  if (vec) store4(out, o[0], o[1], o[2], o[3]);
-  else
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = from_f32<T>(o[i]);
-}
-// Four elements of an output row from their sum o with its running maximum (base 2) and sum; a row that saw nothing is zero.
-template <typename T>
-__device__ __forceinline__ void write_row4(const TreeArgs &a, int b, int t, int h, int dim, const f32x4 &o, float m, float l) {
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  put4((T *)a.out + b * a.out_batch + t * a.out_token + h * a.out_head + dim, f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv}, a.out_vec);
-  if (dim == 0 && a.lse) a.lse[((int64_t)b * a.T + t) * a.H + h] = log_sum(m, l);
 }
 
 // One workgroup: one row tile (16 QF rows) over its share of the list.  The waves take the tiles of 32 keys of a (sequence, head) in
@@ -407,42 +233,7 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
       }
     }
 
-    // the waves' shares, joined in their order
-#pragma unroll
-    for (int f = 0; f < QF; ++f) {
-      const float lsum = rows_sum(l[f]);
-#pragma unroll
-      for (int d = 0; d < DF; ++d) *reinterpret_cast<f32x4 *>(lo + (((wave * QF + f) * DF + d) * 64 + lane) * 4) = O[f][d];
-      if (g4 == 0) { lml[((wave * QF + f) * 16 + c) * 2] = m[f]; lml[((wave * QF + f) * 16 + c) * 2 + 1] = lsum; }
-    }
-    __syncthreads();
-    const bool whole = w.is_whole();
-    const size_t part = w.part();
-    for (int i = tid; i < QF * DF * 64; i += 256) {
-      const int f = i / (DF * 64), d = i / 64 % DF, ln = i & 63, cc = ln & 15;
-      float mm = -__builtin_inff(), ll = 0.0f;
-      f32x4 o{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int v = 0; v < NW; ++v) mm = fmaxf(mm, lml[((v * QF + f) * 16 + cc) * 2]);
-      const float ref = mm == -__builtin_inff() ? 0.0f : mm;
-#pragma unroll
-      for (int v = 0; v < NW; ++v) {
-        const float x = __builtin_amdgcn_exp2f(lml[((v * QF + f) * 16 + cc) * 2] - ref);
-        ll += x * lml[((v * QF + f) * 16 + cc) * 2 + 1];
-        const f32x4 y = *reinterpret_cast<const f32x4 *>(lo + (((v * QF + f) * DF + d) * 64 + ln) * 4);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] += x * y[k];
-      }
-      const int r = f * 16 + cc, rr = z * ROWS + r, t = rr / a.G, dim = d * 16 + (ln >> 4) * 4;
-      if (t >= a.T) continue;
-      if (t >= len.tree) { o = f32x4{0.f, 0.f, 0.f, 0.f}; ll = 0.0f; mm = -__builtin_inff(); }   // not a token of this sequence
-      if (!whole) {
-        *reinterpret_cast<f32x4 *>(a.part_o + (part * ROWS + r) * HD + dim) = o;
-        if (dim == 0) { a.part_ml[(part * ROWS + r) * 2] = mm; a.part_ml[(part * ROWS + r) * 2 + 1] = ll; }
-        continue;
-      }
-      write_row4<T>(a, b, t, hk * a.G + rr % a.G, dim, o, mm, ll);
-    }
+    join_waves<T, HD, QF, NW>(a, w, len, m, l, O, lo, lml);
     __syncthreads();
   }
 }
@@ -879,12 +670,13 @@ TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, i
   TreePlan p;
   const int64_t positions = max_positions * B * Hkv;
   p.rows = tile_rows(dtype, hd, T * G, (int64_t)B * Hkv, max_positions);
+  if (cache == NGG_FP4) p.rows = std::min(p.rows, 32);
   p.Z = (T * G + p.rows - 1) / p.rows;
   const int64_t steps = (max_positions + step_keys(p.rows) - 1) / step_keys(p.rows);
   p.whole = p.rows <= 32 && whole_lists(dtype, steps, (int64_t)B * Hkv * p.Z);
   // A single tile of 16 rows reads the keys once.  Past what the last cache holds, non-temporal loads: 32 single tokens over 16000 positions 332 us
   // instead of 372; below, a list that is read again soon is better kept (1900 positions 46.9, non-temporal 49.7).
-  const int64_t bytes = 2 * positions * hd * (cache == NGG_F32 ? 4 : cache == NGG_BF16 ? 2 : 1);
+  const int64_t bytes = cache == NGG_FP4 ? positions * (hd + hd / kGroup4 * 2) : 2 * positions * hd * (cache == NGG_F32 ? 4 : cache == NGG_BF16 ? 2 : 1);
   p.stream = p.rows == 16 && p.Z == 1 && bytes > (int64_t)400 << 20;
   const int64_t want = (512 + p.Z - 1) / p.Z, r = p.whole ? (int64_t)B * Hkv : std::max<int64_t>(1, std::min(want, steps * B * Hkv));
   p.ranges = (int)(p.whole || r < 8 ? r : r < want ? (r + 7) / 8 * 8 : r / 8 * 8);   // eights: one for each die; up, if a step each is to be had
@@ -894,10 +686,6 @@ TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, i
   return p;
 }
 
-template <typename K>
-static void allow_lds(K kernel, size_t bytes) {
-  if (bytes > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-}
 template <typename T, int HD, int ROWS, int KS>
 static void merge(const TreeArgs &a, hipStream_t s) {
   if (a.whole) return;
@@ -934,8 +722,26 @@ static void by_head(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
   else by_rows<T, CT, 128>(a, p, s);
 }
 
+template <typename T, int HD>
+static void merge_rows(int rows, const TreeArgs &a, hipStream_t s) {
+  if (rows == 16) merge<T, HD, 16, 128>(a, s);
+  else if (rows == 32) merge<T, HD, 32, 128>(a, s);
+  else if constexpr (sizeof(T) == 2) merge<T, HD, 128, 64>(a, s);
+}
+template <typename T>
+static void merge_head(int rows, const TreeArgs &a, hipStream_t s) {
+  if (a.p.hd == 32) merge_rows<T, 32>(rows, a, s);
+  else if (a.p.hd == 64) merge_rows<T, 64>(rows, a, s);
+  else merge_rows<T, 128>(rows, a, s);
+}
+void launch_tree_merge(int dtype, int rows, const TreeArgs &a, hipStream_t s) {
+  if (dtype == NGG_F32) merge_head<float>(rows, a, s);
+  else merge_head<bf16_t>(rows, a, s);
+}
+
 void launch_tree_attention(int dtype, int cache, const TreeArgs &a, const TreePlan &p, hipStream_t s) {
-  if (dtype == NGG_F32 && cache == NGG_F32) by_head<float, float>(a, p, s);
+  if (cache == NGG_FP4) launch_tree_attention4(dtype, a, p, s);
+  else if (dtype == NGG_F32 && cache == NGG_F32) by_head<float, float>(a, p, s);
   else if (dtype == NGG_F32) by_head<float, fp8_t>(a, p, s);
   else if (cache == NGG_BF16) by_head<bf16_t, bf16_t>(a, p, s);
   else by_head<bf16_t, fp8_t>(a, p, s);

@@ -1,5 +1,5 @@
-"""The operators of a batched tree verification: rotary positions, a paged cache of 16 or 8 bits, tree attention and log
-probabilities (ngg.h states what each computes; csrc/ngg_torch.cpp checks the tensors and makes the calls).
+"""The operators of a batched tree verification: rotary positions, a paged cache of 16, 8 or 4 bits, its pages between steps, tree
+attention and log probabilities (ngg.h states what each computes; csrc/ngg_torch.cpp checks the tensors and makes the calls).
 
 Outputs and workspaces come from torch's allocator on the stream that the call runs on: the current one, or `stream`, which
 then has to have been made to wait for whatever wrote the inputs.  Nothing is synchronised.  No gradients are recorded: a call on
@@ -13,14 +13,15 @@ import ctypes as C
 import numpy as np
 import torch
 
-from . import NGG_BF16, NGG_F32, NGG_FP8, NGG_OK, NggError, load_binding, load_library
+from . import NGG_BF16, NGG_F32, NGG_FP4, NGG_FP8, NGG_OK, NggError, load_binding, load_library
 from . import ngg_kv_pages, ngg_rope, ngg_rope_scaling
 
 _binding = load_binding()
 _KINDS = {"linear": 1, "base": 2, "bands": 3, "ramp": 4}
-_CACHES = {"f32": NGG_F32, "bf16": NGG_BF16, "fp8": NGG_FP8}
+_CACHES = {"f32": NGG_F32, "bf16": NGG_BF16, "fp8": NGG_FP8, "fp4": NGG_FP4}
 
 TokenLogprobs = collections.namedtuple("TokenLogprobs", "logprobs entropy lse top_ids top_logprobs")
+PageCopies = collections.namedtuple("PageCopies", "src dst positions missing")
 
 
 def _check(st):
@@ -68,26 +69,50 @@ def rotary(rope, positions, q, k=None, inverse=False, out=None, k_out=None, stre
 
 
 class KVPages:
-    """A pool of pages of keys and values (ngg_kv_pages) in memory of its own.  cache: "f32", "bf16", or "fp8" for 8 bits an
-    element with a power of two for every position and head."""
+    """A pool of pages of keys and values (ngg_kv_pages) in memory of its own.  cache: "f32", "bf16", "fp8" for 8 bits an element with
+    a power of two for every position and head, or "fp4" for 4 bits with a power of two for every 32 of a head's dimensions.  layers:
+    that many pools of n_pages side by side, for the layers of a model that share their page lists; `layer(i)` is one of them,
+    `move` and `copy` work on all at once, and `write`, `read` and `tree_attention` take the whole as one pool of layers * n_pages."""
 
-    def __init__(self, n_pages, page_size, n_kv_heads, head_dim, cache="bf16", device="cuda"):
+    def __init__(self, n_pages, page_size, n_kv_heads, head_dim, cache="bf16", device="cuda", layers=1):
         if cache not in _CACHES:
             raise ValueError(f"unknown cache type {cache!r}")
-        self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, self.cache = n_pages, page_size, n_kv_heads, head_dim, cache
-        self._c = ngg_kv_pages(None, None, None, None, n_pages, page_size, n_kv_heads, head_dim, _CACHES[cache])
+        if layers < 1:
+            raise ValueError(f"{layers} layers")
+        self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, self.cache = layers * n_pages, page_size, n_kv_heads, head_dim, cache
+        self.layers = layers
+        self._c = ngg_kv_pages(None, None, None, None, layers * n_pages, page_size, n_kv_heads, head_dim, _CACHES[cache])
         values, exps = C.c_int64(0), C.c_int64(0)
         _check(load_library().ngg_kv_bytes(self._c, values, exps))
         if not torch.cuda.is_available():
             raise RuntimeError("ngg needs a GPU: there is no CPU fallback")
         self.k_bytes, self.v_bytes = (torch.zeros(values.value, dtype=torch.uint8, device=device) for _ in range(2))
-        self._c.k, self._c.v = self.k_bytes.data_ptr(), self.v_bytes.data_ptr()
         self.k_exps = self.v_exps = None
         if exps.value:
             self.k_exps, self.v_exps = (torch.full((exps.value,), 127, dtype=torch.uint8, device=device) for _ in range(2))
+        self._own = torch.float32 if cache == "f32" else torch.bfloat16
+        self._point()
+
+    def _point(self):
+        self._c.k, self._c.v = self.k_bytes.data_ptr(), self.v_bytes.data_ptr()
+        if self.k_exps is not None:
             self._c.k_exp, self._c.v_exp = self.k_exps.data_ptr(), self.v_exps.data_ptr()
         self._at = C.addressof(self._c)
-        self._own = torch.float32 if cache == "f32" else torch.bfloat16
+
+    def layer(self, i):
+        """The pool of layer i, in the same memory."""
+        if not 0 <= i < self.layers:
+            raise IndexError(f"layer {i} of {self.layers}")
+        part = object.__new__(KVPages)
+        part.__dict__.update(self.__dict__, layers=1, n_pages=self.n_pages // self.layers)
+        for name in ("k_bytes", "v_bytes", "k_exps", "v_exps"):
+            whole = getattr(self, name)
+            if whole is not None:
+                n = whole.numel() // self.layers
+                setattr(part, name, whole[i * n:(i + 1) * n])
+        part._c = ngg_kv_pages(None, None, None, None, part.n_pages, self.page_size, self.n_kv_heads, self.head_dim, _CACHES[self.cache])
+        part._point()
+        return part
 
     def _memory(self):
         return (self.k_bytes, self.v_bytes, self.k_exps, self.v_exps)
@@ -107,6 +132,54 @@ class KVPages:
         if stream is not None:
             return _on(stream, _binding.kv_read, self._at, self.k_bytes, slots, dtype or self._own, keep=self._memory())
         return _binding.kv_read(self._at, self.k_bytes, slots, dtype or self._own)
+
+
+    def move(self, src, dst, stream=None):
+        """ngg_kv_move: in every layer the slots src to the slots dst (int32 [lists, n] or [n], of a layer; -1: none), each list read before
+        it is written."""
+        if stream is not None:
+            return _on(stream, _binding.kv_move, self._at, self.k_bytes, self.layers, src, dst, keep=self._memory())
+        _binding.kv_move(self._at, self.k_bytes, self.layers, src, dst)
+
+    def copy(self, src, dst, positions=None, stream=None):
+        """ngg_kv_copy: in every layer pages src to pages dst (int32 [n], of a layer; -1: none), of each the first positions (int32 [n]; None:
+        all)."""
+        if stream is not None:
+            return _on(stream, _binding.kv_copy, self._at, self.k_bytes, self.layers, src, dst, positions, keep=self._memory())
+        _binding.kv_copy(self._at, self.k_bytes, self.layers, src, dst, positions)
+
+
+class PageTable:
+    """Which pages of a pool hold which sequence (ngg_page_table), on the device: pages (int32 [sequences, max_pages], -1: none), lens
+    (int32 [sequences], the cached positions, which the caller counts up) and refs (int32 [n_pages], the rows that list a page).  One
+    table serves all layers of a KVPages."""
+
+    def __init__(self, n_seqs, max_pages, n_pages, page_size, device="cuda"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("ngg needs a GPU: there is no CPU fallback")
+        self.page_size = page_size
+        self.pages = torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device)
+        self.lens, self.refs = (torch.zeros(n, dtype=torch.int32, device=device) for n in (n_seqs, n_pages))
+
+    def _call(self, stream, call, *args):
+        if stream is not None:
+            return _on(stream, call, self.pages, self.lens, self.refs, self.page_size, *args)
+        return call(self.pages, self.lens, self.refs, self.page_size, *args)
+
+    def fork(self, sources, targets, stream=None):
+        """ngg_pages_fork: sequences targets share the pages of sequences sources (int32 [n] each)."""
+        self._call(stream, _binding.pages_fork, sources, targets)
+
+    def reserve(self, new_tokens, stream=None):
+        """ngg_pages_reserve: pages for new_tokens (int32 [sequences]) behind the cached ones.  Returns PageCopies of src, dst and positions
+        (int32 [sequences], what KVPages.copy has to copy before anything is written) and missing (int32 [1]; unless 0, nothing
+        was given out)."""
+        return PageCopies(*self._call(stream, _binding.pages_reserve, new_tokens))
+
+    def release(self, keep=None, stream=None):
+        """ngg_pages_release: cuts the sequences to keep positions (int32 [sequences], negative: untouched; None: as long as they are) and
+        gives back the pages behind them."""
+        self._call(stream, _binding.pages_release, keep)
 
 
 def tree_mask(parents):
