@@ -2,7 +2,7 @@
 //   (x, y) of pair i at position p -> (x c - y s, y c + x s), c = cos(p w_i), s = sin(p w_i) from the table; the inverse turns by -s
 //   8 bits: x -> nearest e4m3 of x 2^-e, with the smallest e for which the head's largest magnitude stays within 448
 // Every element is read and written once: large calls are bound by HBM, small ones by their launch and chain of loads.
-#include "ngg_operators.h"
+#include "ngg_cache.h"
 
 namespace ngg {
 
@@ -31,34 +31,6 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
     out[e1] = from_f32<T>(turned(y, x, c, s));
   }
 }
-
-template <typename T> struct Vec16;                       // 16 bytes of elements
-template <> struct Vec16<float> {
-  static constexpr int n = 4;
-  static __device__ __forceinline__ void get(const u32x4 &v, float *x) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(v[e]);
-  }
-  static __device__ __forceinline__ u32x4 put(const float *x) {
-    u32x4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(x[e]);
-    return v;
-  }
-};
-template <> struct Vec16<bf16_t> {
-  static constexpr int n = 8;
-  static __device__ __forceinline__ void get(const u32x4 &v, float *x) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16);
-  }
-  static __device__ __forceinline__ u32x4 put(const float *x) {
-    u32x4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2){x[2 * e], x[2 * e + 1]}, bf16x2));
-    return v;
-  }
-};
 
 // The same where rows and their parts are made of whole 16-byte vectors.  HBM bound: 16384 tokens of 40 heads of 128 at 16 bits take
 // 66 us, 5.1 TB/s of reading and writing (a copy of 4 GiB reaches 4.9).  A thread keeps its part of a token's angles for all the heads
@@ -129,8 +101,6 @@ __global__ __launch_bounds__(256) void rotary_rows_kernel(const RotaryArgs a, in
     }
   }
 }
-
-static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
 template <typename T>
 static void launch_rotary_type(const RotaryArgs &a, hipStream_t s) {
@@ -237,53 +207,6 @@ __global__ __launch_bounds__(256) void kv_read_kernel(const CacheArgs a) {
 // whole, and eight positions of a value's dimension lie in one store where the tokens' slots follow each other (a prompt, a tree);
 // others go element by element.  HBM bound: 16000 tokens of 8 heads of 128 are written in 22 us and read in 21 at 16 bits (6 TB/s,
 // reading and writing), in 26 and 21 at 8 bits (3.8 and 4.7 TB/s; there the conversion is what is left).
-constexpr int kGroup = 32, kRowPad = 16;                   // tokens of a workgroup; bytes behind a row in LDS (banks)
-
-// A workgroup's tokens t0 .. t0 + m - 1 (none: false).  Groups begin where eights of positions do if all slots follow each other, so
-// that no chunk (below) lies in two of them: 16000 tokens of 8 heads from position 37, 16 bits, are written in 22 us, from groups
-// that begin at token 0 in 30.
-__device__ __forceinline__ bool group_tokens(const CacheArgs &a, int &t0, int &m) {
-  const int64_t begin = (int64_t)blockIdx.x * kGroup - (a.slots[0] & 7);
-  t0 = (int)max(begin, (int64_t)0);
-  m = (int)(min(begin + kGroup, (int64_t)a.n_tokens) - t0);
-  return m > 0;
-}
-
-// The slots of a workgroup's tokens, in every wave by itself, and their chunks: tokens whose slots follow each other inside eight
-// positions, which lie in one place of a value's dimension.
-struct GroupSlots {
-  int slot;                                                // of token lane % 32; -1: not there
-  int chunk;                                               // of chunk lane % 32: its first token
-  int chunks;
-  __device__ __forceinline__ GroupSlots(const CacheArgs &a, int t0, int m) {
-    const int lane = threadIdx.x & 63, t = lane % kGroup;
-    slot = -1;
-    if (t < m) {
-      slot = a.slots[t0 + t];
-      if (slot < 0 || slot / a.p.page_size >= a.p.n_pages) slot = -1;
-    }
-    const int before = __shfl_up(slot, 1);
-    const bool leads = lane < m && (t == 0 || slot < 0 || slot % 8 == 0 || before < 0 || slot != before + 1);
-    const unsigned mask = (unsigned)__ballot(leads);
-    chunks = __builtin_popcount(mask);
-    // (every other lane sends to one that nobody reads)
-    chunk = __builtin_amdgcn_ds_permute((leads ? __builtin_popcount(mask & ((1u << t) - 1)) : 63) * 4, t);
-    chunk = lane < chunks ? chunk : m;
-  }
-};
-// Chunk q's tokens first .. last - 1 and the slot of the first; all lanes take part.
-struct Chunk { int first, last, slot; };
-__device__ __forceinline__ Chunk chunk_at(const GroupSlots &g, int q) {
-  Chunk c;
-  c.first = __shfl(g.chunk, min(q, 62));
-  c.last = __shfl(g.chunk, min(q + 1, 62));
-  c.slot = __shfl(g.slot, c.first);
-  return c;
-}
-__device__ __forceinline__ size_t slot_head(const CacheArgs &a, int slot, int h) {   // first position of the slot's (page, head)
-  return ((size_t)(slot / a.p.page_size) * a.p.Hkv + h) * a.p.page_size;
-}
-
 // Eight positions of value dimensions d and d + 1 (y[0], y[1]) to and from the cache, d even, by the lanes of a group of 16 that hold
 // dimensions 32 i + 2 (lane % 16) at the same positions: they trade one of the two, so that the lanes of a load or store follow each
 // other in memory.  tile: position 0 of the page and head.
@@ -326,15 +249,7 @@ __device__ __forceinline__ void get_values(const fp8_t *tile, int pos, int d, in
   y[1] = upper ? v : got;
 }
 
-// Two bytes each of eight positions to eight bytes of each of two dimensions, and back.
-__device__ __forceinline__ void turn_bytes(const unsigned (&w)[8], u32x2 (&y)[2]) {
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const unsigned u = __builtin_amdgcn_perm(w[4 * k + 1], w[4 * k], 0x05010400), v = __builtin_amdgcn_perm(w[4 * k + 3], w[4 * k + 2], 0x05010400);
-    y[0][k] = __builtin_amdgcn_perm(v, u, 0x05040100);
-    y[1][k] = __builtin_amdgcn_perm(v, u, 0x07060302);
-  }
-}
+// ... and back
 __device__ __forceinline__ void turn_bytes(const u32x2 (&y)[2], unsigned (&w)[4]) {   // positions 2 i and 2 i + 1 in a word
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -624,14 +539,6 @@ __global__ __launch_bounds__(256) void kv_read_group_kernel(const CacheArgs a, i
 static bool few_rows(const CacheArgs &a, int most) { return (int64_t)a.n_tokens * a.p.Hkv <= most; }
 static int few_written(const CacheArgs &a, bool to8) { return a.cos ? 4096 : to8 ? 3072 : 1536; }
 constexpr int kFewRead = 3072;
-template <typename T>
-static bool rows_of_vectors(const CacheArgs &a, const void *k, const void *v) {
-  constexpr int VE = Vec16<T>::n;
-  return (!k || aligned16(k)) && (!v || aligned16(v)) && a.k_token % VE == 0 && a.k_head % VE == 0 && a.v_token % VE == 0 && a.v_head % VE == 0;
-}
-
-static dim3 groups(const CacheArgs &a) { return dim3((unsigned)(((int64_t)a.n_tokens + 7 + kGroup - 1) / kGroup), a.p.Hkv, 2); }
-
 // dtype: of the tokens; cache: of the pages
 template <template <typename, typename> class Launch>
 static void by_types(int dtype, int cache, const CacheArgs &a, hipStream_t s) {
@@ -639,23 +546,6 @@ static void by_types(int dtype, int cache, const CacheArgs &a, hipStream_t s) {
   else if (dtype == NGG_F32) Launch<float, fp8_t>::go(a, s);
   else if (cache == NGG_BF16) Launch<bf16_t, bf16_t>::go(a, s);
   else Launch<bf16_t, fp8_t>::go(a, s);
-}
-// Groups of 2^28 tokens at a time: a launch counts its threads in 32 bits
-constexpr int kLaunchTokens = 1 << 28;
-template <typename T, typename Launch>
-static void in_parts(const CacheArgs &all, Launch launch) {
-  for (int64_t at = 0; at < all.n_tokens; at += kLaunchTokens) {
-    CacheArgs a = all;
-    const int64_t left = all.n_tokens - at;
-    a.n_tokens = (int)(left < kLaunchTokens ? left : kLaunchTokens);
-    a.slots += at;
-    if (a.positions) a.positions += at;
-    if (a.k) a.k = (const T *)a.k + at * a.k_token;
-    if (a.v) a.v = (const T *)a.v + at * a.v_token;
-    if (a.k_out) a.k_out = (T *)a.k_out + at * a.k_token;
-    if (a.v_out) a.v_out = (T *)a.v_out + at * a.v_token;
-    launch(a);
-  }
 }
 template <typename T, typename CT> struct WriteLaunch {
   static void go(const CacheArgs &all, hipStream_t s) {
