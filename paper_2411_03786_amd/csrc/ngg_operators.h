@@ -214,6 +214,7 @@ struct TreePlan { int rows, ranges, Z; bool whole, stream; size_t o_bytes, ml_by
 TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, int64_t max_positions);
 void launch_tree_attention(int dtype, int cache, const TreeArgs &a, const TreePlan &p, hipStream_t s);
 void launch_tree_attention4(int dtype, const TreeArgs &a, const TreePlan &p, hipStream_t s);
+void launch_tree_block4(const TreeArgs &a, hipStream_t s);                  // (rows of 128)
 void launch_tree_merge(int dtype, int rows, const TreeArgs &a, hipStream_t s);   // (nothing where lists go whole)
 
 struct ScoreArgs {

@@ -19,6 +19,35 @@ __device__ __forceinline__ void pack_frag(Frag<bf16_t> &f, const float *p) {
   for (int e = 0; e < 8; ++e) f.v[e] = (bf16_t)p[e];
 }
 
+// Eight 4-bit elements times a power of two
+__device__ __forceinline__ bf16x8 widen4(unsigned w, float scale) {
+  u32x4 x;
+  x[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+  x[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+  x[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+  x[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+  return __builtin_bit_cast(bf16x8, x);
+}
+// Eight positions of a byte of values with their exponents: dimensions c (lo) and c + 16 (hi) of the group, times their powers of two
+__device__ __forceinline__ void widen4_values(const u32x2 &v, const u32x2 &e, bf16x8 &lo, bf16x8 &hi) {
+  unsigned two[8];
+#define NGG_TWO(i) two[i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[i >> 2], exp_scale(e[i >> 2] >> (i & 3) * 8 & 0xff), i & 3))
+  NGG_TWO(0); NGG_TWO(1); NGG_TWO(2); NGG_TWO(3); NGG_TWO(4); NGG_TWO(5); NGG_TWO(6); NGG_TWO(7);
+#undef NGG_TWO
+  u32x4 x, y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[i] = __builtin_amdgcn_perm(two[2 * i + 1], two[2 * i], 0x05040100);
+    y[i] = __builtin_amdgcn_perm(two[2 * i + 1], two[2 * i], 0x07060302);
+  }
+  lo = __builtin_bit_cast(bf16x8, x);
+  hi = __builtin_bit_cast(bf16x8, y);
+}
+__device__ __forceinline__ float fp4_value(unsigned byte, int upper, unsigned e) {
+  const auto two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(byte, exp_scale(e), 0);
+  return upper ? two[1] : two[0];
+}
+
 // The sequence's cached and tree tokens, cut to what the page list can hold.
 struct SeqLens { int ctx, tree; };
 __device__ __forceinline__ SeqLens seq_lens(const TreeArgs &a, int b) {

@@ -14,6 +14,7 @@
 #include "ngg_epilogues.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ngg {
 
@@ -257,8 +258,9 @@ template <typename CT, int HD>
 __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
   typedef bf16_t T;
   constexpr int NW = 4, DS = HD / 32, KQ = HD / 16, DB = HD / 32, TILE = 32 * HD, KT = 2, KS = 32 * KT, ROWS = 32 * NW, NT = 64 * NW;
-  constexpr bool C8 = sizeof(CT) == 1;
+  constexpr bool C4 = std::is_same_v<CT, fp4x2_t>, C8 = sizeof(CT) == 1 && !C4, REGS = C4 || C8;   // REGS: by way of registers
   constexpr int PIECES = TILE / 16, PPT = (PIECES + NT - 1) / NT;   // (8 bits) 16-byte pieces of a tile, of a thread
+  constexpr int PIECES4 = KT * HD, V0 = PIECES4 < NT ? PIECES4 : 0; // (4 bits) pieces of a step's keys, and the thread that has the first of its values
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   T *kl = reinterpret_cast<T *>(smem);                     // [2][KT][TILE]
   T *vl = kl + 2 * KT * TILE;                              // [2][KT][TILE]
@@ -294,10 +296,12 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
         if (at_off == a.p.page_size) { at_off = 0; ++at_page; }
       }
     };
-    // 16-bit tiles go straight to LDS, 1 KB per wave and instruction; 8-bit ones by way of registers
+    // 16-bit tiles go straight to LDS, 1 KB per wave and instruction; 8-bit and 4-bit ones by way of registers
     u32x4 kst[C8 ? KT : 1][C8 ? PPT : 1], vst[C8 ? KT : 1][C8 ? PPT : 1];
     u32x2 kex[C8 ? KT : 1][C8 ? PPT : 1];
     unsigned vex = 0;
+    u32x4 k4, v4, ve4;                                     // (4 bits) a piece of keys and one of values, at most
+    unsigned ke4 = 0;
     bool there[KT];                                        // (uniform) the tile's page is one of the pool's
     const int tok = (z * ROWS + wave * 32 + r32) / a.G;
     const bool live = tok < len.tree;
@@ -313,10 +317,30 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
         const int page = __builtin_amdgcn_readfirstlane(pg[k]);
         there[k] = page >= 0 && page < a.p.n_pages;
         head[k] = there[k] ? ((size_t)page * Hkv + hk) * a.p.page_size + pg_off[k] : 0;
-        kp[k] = (const uint8_t *)a.p.k + head[k] * HD * sizeof(CT);
-        vp[k] = (const uint8_t *)a.p.v + head[k] * HD * sizeof(CT);
+        kp[k] = (const uint8_t *)a.p.k + (C4 ? head[k] * (HD / 2) : head[k] * HD * sizeof(CT));
+        vp[k] = (const uint8_t *)a.p.v + (C4 ? head[k] * (HD / 2) : head[k] * HD * sizeof(CT));
       }
-      if constexpr (C8) {
+      if constexpr (C4) {
+        const int x = tid / HD, pc = tid % HD;             // (a tile is HD pieces)
+        if (x < KT) {
+          k4 = reinterpret_cast<const u32x4 *>(x == 0 ? kp[0] : kp[1])[pc];
+          const uint8_t *e = a.p.k_exp + (x == 0 ? head[0] : head[1]) * DS;
+          if constexpr (HD == 128) ke4 = e[pc % 64 * 2 + pc / 64];
+          else if constexpr (HD == 64) ke4 = *reinterpret_cast<const uint16_t *>(e + (pc / 32 * 16 + pc % 16) * 2);
+          else ke4 = *reinterpret_cast<const unsigned *>(e + pc % 8 * 4);
+        }
+        if (tid >= V0 && tid < V0 + PIECES4) {
+          const int xv = (tid - V0) / HD, pv = (tid - V0) % HD;
+          v4 = reinterpret_cast<const u32x4 *>(xv == 0 ? vp[0] : vp[1])[pv];
+          const uint8_t *e = a.p.v_exp + (xv == 0 ? head[0] : head[1]) * DS;
+          if constexpr (HD == 128) ve4 = *reinterpret_cast<const u32x4 *>(e + pv % 64 / 16 * 32 + pv / 64 * 16);
+          else if constexpr (HD == 64) ve4 = *reinterpret_cast<const u32x4 *>(e + pv / 16 * 16);
+          else {
+            const u32x2 y = *reinterpret_cast<const u32x2 *>(e + pv / 8 * 8);
+            ve4 = u32x4{y[0], y[1], y[0], y[1]};
+          }
+        }
+      } else if constexpr (C8) {
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
 #pragma unroll
@@ -341,7 +365,32 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
       look_up();
     };
     auto stage_store = [&](int t, int buf) {
-      if constexpr (C8) {
+      if constexpr (C4) {
+        const int x = tid / HD, pc = tid % HD;
+        if (x < KT) {
+          T *kt = kl + (buf * KT + x) * TILE;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            // word i: eight dimensions from dim of row (half, ln % 16)
+            const int ln = HD == 128 ? pc % 64 : HD == 64 ? pc : pc * 2 + i / 2, half = HD == 128 ? pc / 64 : HD == 64 ? i / 2 : i % 2;
+            const int dim = ln / 16 * (HD / 4) + (HD == 128 ? i * 8 : HD == 64 ? i % 2 * 8 : 0);
+            const float scale = exp_scale(ke4 >> (HD == 128 ? 0 : HD == 64 ? half * 8 : i * 8) & 0xff);
+            *reinterpret_cast<bf16x8 *>(kt + (half * DS + dim / 32) * 512 + (dim % 32 / 8 * 16 + ln % 16) * 8) = widen4(k4[i], scale);
+          }
+        }
+        if (tid >= V0 && tid < V0 + PIECES4) {
+          const int xv = (tid - V0) / HD, pv = (tid - V0) % HD;
+          T *vt = vl + (buf * KT + xv) * TILE;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int ln = HD == 32 ? pv * 2 + i : pv % 64, group = HD == 32 ? 0 : pv / 64 * 2 + i;
+            bf16x8 lo, hi;
+            widen4_values(u32x2{v4[2 * i], v4[2 * i + 1]}, u32x2{ve4[2 * i], ve4[2 * i + 1]}, lo, hi);
+            *reinterpret_cast<bf16x8 *>(vt + 2 * group * 512 + ln * 8) = lo;
+            *reinterpret_cast<bf16x8 *>(vt + (2 * group + 1) * 512 + ln * 8) = hi;
+          }
+        }
+      } else if constexpr (C8) {
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
           T *kt = kl + (buf * KT + k) * TILE, *vt = vl + (buf * KT + k) * TILE;
@@ -390,7 +439,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
       for (int k = 0; k < KT; ++k) here[k] = there[k];
       see = see_next;
     };
-    if constexpr (!C8) {                                   // both buffers are empty: the second step's tiles may come at once
+    if constexpr (!REGS) {                                 // both buffers are empty: the second step's tiles may come at once
       arrive();
       stage_load(1);
     }
@@ -480,7 +529,8 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
         if (!all && odd[k]) {                              // (uniform)
           // values that are not finite were left out, because 0 times them must stay 0 where their key is masked
           const int page = a.pages[b * a.pages_batch + pos0 / a.p.page_size];
-          const CT *vg = (const CT *)a.p.v + (((size_t)page * Hkv + hk) * a.p.page_size + pos0 % a.p.page_size) * HD;
+          const size_t place = ((size_t)page * Hkv + hk) * a.p.page_size + pos0 % a.p.page_size;
+          const CT *vg = (const CT *)a.p.v + (C4 ? place * (HD / 2) : place * HD);
           for (int j = 0; j < 32 && pos0 + j < n_keys; ++j) {
             unsigned pair = 0, vj = 0;                     // the probability of key j is half of a register of lane (row, j / 8 % 2)
 #pragma unroll
@@ -499,10 +549,11 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
             for (int d = 0; d < DB; ++d)
 #pragma unroll
               for (int r = 0; r < 16; ++r) {
-                const CT x = vg[page_v_offset<CT>(j, d * 32 + 8 * (r >> 2) + 4 * hh + (r & 3), HD)];
+                const int dim = d * 32 + 8 * (r >> 2) + 4 * hh + (r & 3);
                 float v;
-                if constexpr (C8) v = fp8_to_f32(x.bits);
-                else v = to_f32(x);
+                if constexpr (C4) v = fp4_value(vg[v_offset4(j, dim, HD)].bits, dim >> 4 & 1, (a.p.v_exp + place * DS)[v_exp_offset4(j, dim, HD)]);
+                else if constexpr (C8) v = fp8_to_f32(vg[page_v_offset<CT>(j, dim, HD)].bits);
+                else v = to_f32(vg[page_v_offset<CT>(j, dim, HD)]);
                 if ((vj >> (j & 7) & 1) && !(fabsf(v) < __builtin_inff())) O[d][r] += pj * v;
                 if ((r & 3) == 3) asm volatile("" ::: "memory");         // few loads at a time: this path must not cost the other registers
               }
@@ -516,9 +567,9 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
     int buf = 0;
     for (int t = t_begin; t < t_end; t += KT) {            // barriers are uniform
       stage_store(t, buf);
-      if (C8 || t > t_begin) arrive();
+      if (REGS || t > t_begin) arrive();
       __syncthreads();
-      if (C8 || t > t_begin) stage_load(buf ^ 1);
+      if (REGS || t > t_begin) stage_load(buf ^ 1);
       const bool all = (t + KT) * 32 <= len.ctx && here[0] && here[1];
       if (!all) {
         // a step at the end of the list: values that are not there become zeros, and those that are not finite
@@ -544,7 +595,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
       buf ^= 1;
     }
     // (the last transfers, of no step's tiles, have landed before LDS is used again)
-    if constexpr (!C8) __builtin_amdgcn_s_waitcnt(0x0F70);
+    if constexpr (!REGS) __builtin_amdgcn_s_waitcnt(0x0F70);
 
     const bool whole = w.is_whole();
     float lsum = l + other_half(l);
@@ -670,7 +721,6 @@ TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, i
   TreePlan p;
   const int64_t positions = max_positions * B * Hkv;
   p.rows = tile_rows(dtype, hd, T * G, (int64_t)B * Hkv, max_positions);
-  if (cache == NGG_FP4) p.rows = std::min(p.rows, 32);
   p.Z = (T * G + p.rows - 1) / p.rows;
   const int64_t steps = (max_positions + step_keys(p.rows) - 1) / step_keys(p.rows);
   p.whole = p.rows <= 32 && whole_lists(dtype, steps, (int64_t)B * Hkv * p.Z);
@@ -707,6 +757,11 @@ static void launch_block(const TreeArgs &a, hipStream_t s) {
   (void)once;
   hipLaunchKernelGGL((tree_block_kernel<CT, HD>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
   merge<bf16_t, HD, 128, 64>(a, s);
+}
+void launch_tree_block4(const TreeArgs &a, hipStream_t s) {
+  if (a.p.hd == 32) launch_block<fp4x2_t, 32>(a, s);
+  else if (a.p.hd == 64) launch_block<fp4x2_t, 64>(a, s);
+  else launch_block<fp4x2_t, 128>(a, s);
 }
 template <typename T, typename CT, int HD>
 static void by_rows(const TreeArgs &a, const TreePlan &p, hipStream_t s) {

@@ -47,16 +47,6 @@ template <typename T, int HD> struct Query4 {
     }
   }
 };
-// Eight 4-bit elements times a power of two
-__device__ __forceinline__ bf16x8 widen4(unsigned w, float scale) {
-  u32x4 x;
-  x[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
-  x[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
-  x[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
-  x[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
-  return __builtin_bit_cast(bf16x8, x);
-}
-
 // A lane's part of a tile of 32 keys and values as it lies in memory.
 template <int HD> struct Tile4 {
   static constexpr int NG = HD / 32;
@@ -65,11 +55,6 @@ template <int HD> struct Tile4 {
   unsigned ke;                                             // either half's
   bool there;                                              // (uniform) the page is one of the pool's
 };
-
-__device__ __forceinline__ float fp4_value(unsigned byte, int upper, unsigned e) {
-  const auto two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(byte, exp_scale(e), 0);
-  return upper ? two[1] : two[0];
-}
 
 // One workgroup: one row tile (16 QF rows) over its share of the list, as tree_stream_kernel: the waves take the tiles of 32 keys in
 // turn and are joined through LDS.  The next tile is on its way while one is computed.
@@ -229,19 +214,8 @@ __global__ __launch_bounds__(256) void tree4_stream_kernel(const TreeArgs a) {
       }
 #pragma unroll
       for (int j = 0; j < NG; ++j) {
-        unsigned pair[8];                                  // dimensions c and c + 16 of the group at a position
-#define NGG_PAIR(e) pair[e] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.v[j][e >> 2], exp_scale(t.ve[j][e >> 2] >> (e & 3) * 8 & 0xff), e & 3))
-        NGG_PAIR(0); NGG_PAIR(1); NGG_PAIR(2); NGG_PAIR(3); NGG_PAIR(4); NGG_PAIR(5); NGG_PAIR(6); NGG_PAIR(7);
-#undef NGG_PAIR
         Frag<bf16_t> V[2];
-        u32x4 x, y;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[i] = __builtin_amdgcn_perm(pair[2 * i + 1], pair[2 * i], 0x05040100);
-          y[i] = __builtin_amdgcn_perm(pair[2 * i + 1], pair[2 * i], 0x07060302);
-        }
-        V[0].v = __builtin_bit_cast(bf16x8, x);
-        V[1].v = __builtin_bit_cast(bf16x8, y);
+        widen4_values(t.v[j], t.ve[j], V[0].v, V[1].v);
 #pragma unroll
         for (int f = 0; f < QF; ++f)
 #pragma unroll
@@ -306,7 +280,7 @@ template <typename T, int HD>
 static void by_rows(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
   if (p.rows == 16 && p.stream) launch_stream<T, HD, 1, true>(a, s);
   else if (p.rows == 16) launch_stream<T, HD, 1, false>(a, s);
-  else launch_stream<T, HD, 2, false>(a, s);
+  else if (p.rows == 32) launch_stream<T, HD, 2, false>(a, s);
 }
 template <typename T>
 static void by_head(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
@@ -315,6 +289,7 @@ static void by_head(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
   else by_rows<T, 128>(a, p, s);
 }
 void launch_tree_attention4(int dtype, const TreeArgs &a, const TreePlan &p, hipStream_t s) {
+  if (p.rows == 128) return launch_tree_block4(a, s);
   if (dtype == NGG_F32) by_head<float>(a, p, s);
   else by_head<bf16_t>(a, p, s);
   launch_tree_merge(dtype, p.rows, a, s);
