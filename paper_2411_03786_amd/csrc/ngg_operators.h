@@ -209,12 +209,13 @@ struct TreeArgs {
   float *part_o, *part_ml;    // workspace (tree_plan)
   int ranges, Z;              // workgroups along the list of key steps, row tiles
   int whole;                  // a workgroup for every (sequence, head) instead: no parts, no merge
+  int pieces, piece_steps;    // 0, or so many workgroups for every (sequence, head), with so many steps each: parts, but no common list
 };
-struct TreePlan { int rows, ranges, Z; bool whole, stream; size_t o_bytes, ml_bytes; };
+struct TreePlan { int rows, ranges, Z, pieces, piece_steps; bool whole, stream; size_t o_bytes, ml_bytes; };
 TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, int64_t max_positions);
 void launch_tree_attention(int dtype, int cache, const TreeArgs &a, const TreePlan &p, hipStream_t s);
 void launch_tree_attention4(int dtype, const TreeArgs &a, const TreePlan &p, hipStream_t s);
-void launch_tree_block4(const TreeArgs &a, hipStream_t s);                  // (rows of 128)
+void launch_tree_block4(int rows, const TreeArgs &a, hipStream_t s);        // (64 or 128 rows)
 void launch_tree_merge(int dtype, int rows, const TreeArgs &a, hipStream_t s);   // (nothing where lists go whole)
 
 struct ScoreArgs {

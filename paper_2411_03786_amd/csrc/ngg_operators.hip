@@ -344,7 +344,7 @@ ngg_status ngg_tree_attention(const ngg_kv_pages *pages, const ngg_tree_args *ar
   a.out_vec = aligned(args->out, 4 * es) && args->out_batch % 4 == 0 && args->out_token % 4 == 0 && args->out_head % 4 == 0;
   a.part_o = (float *)workspace;
   a.part_ml = (float *)((char *)workspace + p.o_bytes);
-  a.ranges = p.ranges; a.Z = p.Z; a.whole = p.whole;
+  a.ranges = p.ranges; a.Z = p.Z; a.whole = p.whole; a.pieces = p.pieces; a.piece_steps = p.piece_steps;
   launch_tree_attention(args->dtype, pages->dtype, a, p, (hipStream_t)hip_stream);
   NGG_LAUNCHED("ngg_tree_attention");
   return NGG_OK;

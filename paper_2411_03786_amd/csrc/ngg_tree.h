@@ -19,6 +19,9 @@ __device__ __forceinline__ void pack_frag(Frag<bf16_t> &f, const float *p) {
   for (int e = 0; e < 8; ++e) f.v[e] = (bf16_t)p[e];
 }
 
+// A power of two for the conversions from 4 bits, from byte I of w, its exponent: they read the exponent of the number alone, so that what
+// else the shift brings does not matter.
+template <int I> __device__ __forceinline__ float scale4(unsigned w) { return __uint_as_float(I == 0 ? w << 23 : I == 1 ? w << 15 : I == 2 ? w << 7 : w >> 1); }
 // Eight 4-bit elements times a power of two
 __device__ __forceinline__ bf16x8 widen4(unsigned w, float scale) {
   u32x4 x;
@@ -31,7 +34,7 @@ __device__ __forceinline__ bf16x8 widen4(unsigned w, float scale) {
 // Eight positions of a byte of values with their exponents: dimensions c (lo) and c + 16 (hi) of the group, times their powers of two
 __device__ __forceinline__ void widen4_values(const u32x2 &v, const u32x2 &e, bf16x8 &lo, bf16x8 &hi) {
   unsigned two[8];
-#define NGG_TWO(i) two[i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[i >> 2], exp_scale(e[i >> 2] >> (i & 3) * 8 & 0xff), i & 3))
+#define NGG_TWO(i) two[i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[i >> 2], scale4<(i & 3)>(e[i >> 2]), i & 3))
   NGG_TWO(0); NGG_TWO(1); NGG_TWO(2); NGG_TWO(3); NGG_TWO(4); NGG_TWO(5); NGG_TWO(6); NGG_TWO(7);
 #undef NGG_TWO
   u32x4 x, y;
@@ -97,7 +100,8 @@ __device__ __forceinline__ int share_steps(const TreeArgs &a, int total) {
 
 // A workgroup's place and share of the list, one (sequence, head) after the other.  Whole numbers of 32 bits (the host sees to that):
 // what runs once costs a launch its instruction fetches.
-template <int KS>
+// PIECES: the call may be one of a.pieces.
+template <int KS, bool PIECES = false>
 struct Work {
   const TreeArgs &a;
   int *pre;
@@ -117,7 +121,7 @@ struct Work {
       z = slot - range * a.Z;
       if (dealt) range = range * 8 + blockIdx.x % 8;
     }
-    if (a.whole) {                                         // a (sequence, head) for each
+    if (a.whole || (PIECES && a.pieces)) {                 // a (sequence, head) for each, or a piece of one
       u = range;
       u_end = range + 1;
       return;
@@ -139,12 +143,24 @@ struct Work {
       ++u;
       return true;
     }
-    int p0 = before(b), p1 = before(b + 1);
-    while (p1 * a.p.Hkv <= u) {
-      ++b;
-      p0 = p1;
-      p1 = before(b + 1);
+    if (PIECES && a.pieces) {
+      const int list = u / a.pieces;
+      b = list / a.p.Hkv;
+      hk = list - b * a.p.Hkv;
+      steps = seq_steps<KS>(a, b);
+      s_begin = (u - list * a.pieces) * a.piece_steps;
+      s_end = min(steps, s_begin + a.piece_steps);
+      ++u;
+      return s_begin < steps;
     }
+    if constexpr (!PIECES) {
+      while (before(b + 1) * a.p.Hkv <= u) ++b;
+    } else while (true) {                                  // 64 sequences are looked at at once (at the price of four registers)
+      const int i = b + 1 + (int)(threadIdx.x & 63), n = (int)__builtin_popcountll(__ballot(i <= a.B && pre[min(i, a.B)] * a.p.Hkv <= u));
+      b += n;
+      if (n < 64) break;
+    }
+    const int p0 = before(b), p1 = before(b + 1);
     steps = p1 - p0;
     const int in_b = u - p0 * a.p.Hkv;
     hk = in_b / steps;
@@ -155,7 +171,7 @@ struct Work {
   }
   __device__ __forceinline__ bool is_whole() const { return s_begin == 0 && s_end == steps; }
   // where a part goes: one that begins inside a (sequence, head) is the first of its share, one that ends inside it the last
-  __device__ __forceinline__ size_t part() const { return ((size_t)range * a.Z + z) * 2 + (s_begin == 0 ? 1 : 0); }
+  __device__ __forceinline__ size_t part() const { return PIECES && a.pieces ? (size_t)range * a.Z + z : ((size_t)range * a.Z + z) * 2 + (s_begin == 0 ? 1 : 0); }
 };
 
 // Two words of a token's row of the mask, from the one that holds tree position at (or the first): enough for the 64 positions from
@@ -213,16 +229,15 @@ __device__ __forceinline__ void write_row4(const TreeArgs &a, int b, int t, int 
 // their order through LDS and written: the rows of a whole (sequence, head), or a partial result.  lo: [NW][QF][DF][64][4], lml:
 // [NW][QF][16][2].
 template <typename T, int HD, int QF, int NW, typename W>
-__device__ __forceinline__ void join_waves(const TreeArgs &a, const W &w, const SeqLens &len, const float (&m)[QF], const float (&l)[QF],
-                                           const f32x4 (&O)[QF][HD / 16], float *lo, float *lml) {
+__device__ __forceinline__ void join_waves(const TreeArgs &a, const W &w, int b, int hk, int z, const SeqLens &len, int tid, int lane, int wave, int c, int g4,
+                                           const float (&m)[QF], const float (&l)[QF], const f32x4 (&O)[QF][HD / 16], float *lo, float *lml) {
   constexpr int DF = HD / 16, ROWS = 16 * QF;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15;
 #pragma unroll
   for (int f = 0; f < QF; ++f) {
     const float lsum = rows_sum(l[f]);
 #pragma unroll
     for (int d = 0; d < DF; ++d) *reinterpret_cast<f32x4 *>(lo + (((wave * QF + f) * DF + d) * 64 + lane) * 4) = O[f][d];
-    if (lane < 16) { lml[((wave * QF + f) * 16 + c) * 2] = m[f]; lml[((wave * QF + f) * 16 + c) * 2 + 1] = lsum; }
+    if (g4 == 0) { lml[((wave * QF + f) * 16 + c) * 2] = m[f]; lml[((wave * QF + f) * 16 + c) * 2 + 1] = lsum; }
   }
   __syncthreads();
   const bool whole = w.is_whole();
@@ -242,7 +257,7 @@ __device__ __forceinline__ void join_waves(const TreeArgs &a, const W &w, const 
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[k] += x * y[k];
     }
-    const int r = f * 16 + cc, rr = w.z * ROWS + r, t = rr / a.G, dim = d * 16 + (ln >> 4) * 4;
+    const int r = f * 16 + cc, rr = z * ROWS + r, t = rr / a.G, dim = d * 16 + (ln >> 4) * 4;
     if (t >= a.T) continue;
     if (t >= len.tree) { o = f32x4{0.f, 0.f, 0.f, 0.f}; ll = 0.0f; mm = -__builtin_inff(); }   // not a token of this sequence
     if (!whole) {
@@ -250,7 +265,7 @@ __device__ __forceinline__ void join_waves(const TreeArgs &a, const W &w, const 
       if (dim == 0) { a.part_ml[(part * ROWS + r) * 2] = mm; a.part_ml[(part * ROWS + r) * 2 + 1] = ll; }
       continue;
     }
-    write_row4<T>(a, w.b, t, w.hk * a.G + rr % a.G, dim, o, mm, ll);
+    write_row4<T>(a, b, t, hk * a.G + rr % a.G, dim, o, mm, ll);
   }
 }
 

@@ -234,7 +234,7 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
       }
     }
 
-    join_waves<T, HD, QF, NW>(a, w, len, m, l, O, lo, lml);
+    join_waves<T, HD, QF, NW>(a, w, b, hk, z, len, tid, lane, wave, c, g4, m, l, O, lo, lml);
     __syncthreads();
   }
 }
@@ -254,10 +254,11 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
 // 16 u + 8 h .. + 7 of every 16, its operand of the second product.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-template <typename CT, int HD>
+template <typename CT, int HD, int RG>
 __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
   typedef bf16_t T;
-  constexpr int NW = 4, DS = HD / 32, KQ = HD / 16, DB = HD / 32, TILE = 32 * HD, KT = 2, KS = 32 * KT, ROWS = 32 * NW, NT = 64 * NW;
+  constexpr int NW = 4, DS = HD / 32, KQ = HD / 16, DB = HD / 32, TILE = 32 * HD, KT = 2, KS = 32 * KT, ROWS = 32 * RG, NT = 64 * NW;
+  constexpr bool SPLIT = RG == 2;                          // two waves for the same rows, each a tile of every step
   constexpr bool C4 = std::is_same_v<CT, fp4x2_t>, C8 = sizeof(CT) == 1 && !C4, REGS = C4 || C8;   // REGS: by way of registers
   constexpr int PIECES = TILE / 16, PPT = (PIECES + NT - 1) / NT;   // (8 bits) 16-byte pieces of a tile, of a thread
   constexpr int PIECES4 = KT * HD, V0 = PIECES4 < NT ? PIECES4 : 0; // (4 bits) pieces of a step's keys, and the thread that has the first of its values
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
   int *odd = reinterpret_cast<int *>(vsl + 2 * KS);        // [KT] a tile of this step holds values that are not finite
   int *pre = odd + KT;                                     // [B + 1]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int r32 = lane & 31, h = lane >> 5;
+  const int r32 = lane & 31, h = lane >> 5, rg = SPLIT ? wave & 1 : wave, ks = SPLIT ? wave >> 1 : 0;
   const int Hkv = a.p.Hkv;
   const int loff = (h * 16 + (r32 & 15)) * 8, koff = (r32 >> 4) * DS * 512 + loff, voff = (r32 >> 4) * 512 + loff;
   Work<KS> w(a, pre);
@@ -280,7 +281,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
       const int t_last = min(len.tree, (r0 + rows - 1) / a.G + 1) - 1;
       return (t_last + 1) * a.G > r0 ? min(n_keys, len.ctx + t_last + 1) : 0;
     };
-    const int group_keys = seen(z * ROWS, ROWS), wave_keys = seen(z * ROWS + wave * 32, 32);
+    const int group_keys = seen(z * ROWS, ROWS), wave_keys = seen(z * ROWS + rg * 32, 32);
     const int t_begin = w.s_begin * KT, t_end = min(w.s_end * KT, (group_keys + 31) / 32);
 
     // Tiles are taken in order; the pages of a step are looked up a step before its keys are asked for.
@@ -303,7 +304,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
     u32x4 k4, v4, ve4;                                     // (4 bits) a piece of keys and one of values, at most
     unsigned ke4 = 0;
     bool there[KT];                                        // (uniform) the tile's page is one of the pool's
-    const int tok = (z * ROWS + wave * 32 + r32) / a.G;
+    const int tok = (z * ROWS + rg * 32 + r32) / a.G;
     const bool live = tok < len.tree;
     MaskWindow see_next;                                   // ... and what the rows see of a step that holds tree tokens
     int at_step = t_begin;
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
     stage_load(0);
     bf16x8 Q[KQ];
     {
-      const int row = z * ROWS + wave * 32 + r32;
+      const int row = z * ROWS + rg * 32 + r32;
       const T *q = (const T *)a.q + b * a.q_batch + (live ? tok : 0) * a.q_token + (int64_t)(hk * a.G + row % a.G) * a.q_head;
 #pragma unroll
       for (int d = 0; d < KQ; ++d) Q[d] = zero_frag<T>().v;
@@ -455,7 +456,9 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
     auto compute = [&](bool all, int t, int buf) {
       if (t * 32 >= wave_keys) return;                     // (uniform per wave)
 #pragma unroll
-      for (int k = 0; k < KT; ++k) {
+      for (int k2 = 0; k2 < (SPLIT ? 1 : KT); ++k2) {
+        const int k = SPLIT ? ks : k2;
+        const bool is_here = SPLIT ? (ks ? here[1] : here[0]) : here[k2];
         const T *kt = kl + (buf * KT + k) * TILE + koff, *vt = vl + (buf * KT + k) * TILE + voff;
         const int pos0 = (t + k) * 32;
         // (left to itself the compiler fetches one fragment, waits, and multiplies: the fences keep the fetches together and ahead)
@@ -477,7 +480,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
         if (!all) {
 #pragma unroll
           for (int u = 0; u < 2; ++u)
-            vis[u] = here[k] ? visible8(see, t * 32 - len.ctx, tok, pos0 + 16 * u + 8 * h - len.ctx, n_keys - len.ctx) : 0u;
+            vis[u] = is_here ? visible8(see, t * 32 - len.ctx, tok, pos0 + 16 * u + 8 * h - len.ctx, n_keys - len.ctx) : 0u;
 #pragma unroll
           for (int r = 0; r < 16; ++r)
             if (!(vis[r >> 2 & 1] >> ((r >> 3) * 4 + (r & 3)) & 1)) S[r] = -__builtin_inff();
@@ -597,11 +600,39 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
     // (the last transfers, of no step's tiles, have landed before LDS is used again)
     if constexpr (!REGS) __builtin_amdgcn_s_waitcnt(0x0F70);
 
+    if constexpr (SPLIT) {                                 // the second wave's share goes to the first by way of LDS
+      f32x4 *lo = reinterpret_cast<f32x4 *>(smem) + rg * DB * 256 + lane;
+      f32x2 *lml = reinterpret_cast<f32x2 *>(reinterpret_cast<f32x4 *>(smem) + 2 * DB * 256) + rg * 64 + lane;
+      __syncthreads();
+      if (ks) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) lo[(d * 4 + j) * 64] = f32x4{O[d][4 * j], O[d][4 * j + 1], O[d][4 * j + 2], O[d][4 * j + 3]};
+        *lml = f32x2{m, l};
+      }
+      __syncthreads();
+      if (!ks) {
+        const f32x2 other = *lml;
+        const float top = fmaxf(m, other[0]), ref = top == -__builtin_inff() ? 0.0f : top;
+        const float x = __builtin_amdgcn_exp2f(m - ref), y = __builtin_amdgcn_exp2f(other[0] - ref);
+        m = top;
+        l = l * x + other[1] * y;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const f32x4 o = lo[(d * 4 + j) * 64];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) O[d][4 * j + i] = O[d][4 * j + i] * x + o[i] * y;
+          }
+      }
+    }
     const bool whole = w.is_whole();
     float lsum = l + other_half(l);
-    if (tok < a.T) {
+    if (tok < a.T && !ks) {
       if (!live) lsum = 0.0f;                              // not a token of this sequence
-      const int r = wave * 32 + r32;
+      const int r = rg * 32 + r32;
       if (whole) {
         const int head = hk * a.G + (z * ROWS + r) % a.G;
         const float inv = lsum == 0.0f ? 0.0f : 1.0f / lsum;
@@ -641,10 +672,17 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
 template <typename T, int HD, int ROWS, int KS>
 __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
   __shared__ int pre[NGG_TREE_MAX + 1];
-  step_totals<KS>(a, pre);
   const int z = blockIdx.y, b = blockIdx.x / a.p.Hkv, hk = blockIdx.x % a.p.Hkv;
-  const int per = share_steps<KS>(a, pre[a.B] * a.p.Hkv), steps = pre[b + 1] - pre[b], u0 = pre[b] * a.p.Hkv + hk * steps;
-  const int first = u0 / per, last = (u0 + steps - 1) / per;   // the shares that hold its first and its last step
+  int first, last;                                         // the shares that hold its first and its last step
+  if (a.pieces) {
+    first = blockIdx.x * a.pieces;
+    last = first + (seq_steps<KS>(a, b) - 1) / a.piece_steps;
+  } else {
+    step_totals<KS>(a, pre);
+    const int per = share_steps<KS>(a, pre[a.B] * a.p.Hkv), steps = pre[b + 1] - pre[b], u0 = pre[b] * a.p.Hkv + hk * steps;
+    first = u0 / per;
+    last = (u0 + steps - 1) / per;
+  }
   if (first == last) return;
   const int i = blockIdx.z * 256 + threadIdx.x;
   const int r = i / (HD / 4), dim = i % (HD / 4) * 4, rr = z * ROWS + r, t = rr / a.G;
@@ -658,7 +696,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int x = min(w + j, last);
-      const size_t part = (((size_t)x * a.Z + z) * 2 + (x == first ? 1 : 0)) * ROWS + r;
+      const size_t at = (size_t)x * a.Z + z, part = (a.pieces ? at : at * 2 + (x == first ? 1 : 0)) * ROWS + r;
       ml[j] = *reinterpret_cast<const f32x2 *>(a.part_ml + part * 2);
       v[j] = *reinterpret_cast<const f32x4 *>(a.part_o + part * HD + dim);
     }
@@ -702,6 +740,22 @@ static int tile_rows(int dtype, int hd, int rows, int64_t lists, int64_t positio
   if (scores >= 16 << 20 || (hd == 128 && lists * ((rows + 15) / 16) >= 768)) return 32;
   return 16;
 }
+// The same over 4 bits, where a tile's keys and values are widened again for each: 16 and 32 rows are tree4_stream_kernel's, 64 and
+// 128 tree_block_kernel's.  Measured at 16 bits (us a call in a graph; tiles of 16, 32, 64 and 128 rows; lists, rows, positions, head_dim):
+//   32, 51, 2047, 128: 19, 21, 28, 29 (3 M scores)       16, 244, 2000, 128: 29, 25, 33, 33 (7 M)     48, 51, 2000, 64: 21, 18, 25, 26 (5 M)
+//   24, 132, 4000, 64: 27, 23, 31, 30 (12 M)             32, 512, 1000, 128: 34, 29, 41, 43 (16 M)    16, 244, 8000, 128: 53, 44, 49, 47 (30 M)
+//   64, 244, 4000, 128: 97, 72, 73, 64 (60 M)            9, 480, 12000, 64: 55, 49, 52, 45 (49 M)     144, 80, 4000, 128: 75, 75, 82, 63 (44 M)
+//   256, 36, 8000, 128: 128, 134, 120, 151 (70 M)        192, 64, 8000, 64: 89, 84, 78, 92 (94 M)     1024, 51, 2047, 128: 213, 172, 139, 170 (102 M)
+// and in fp32 (16 and 32 rows; at heads of 128 the latter leaves a SIMD one wave): 64, 244, 4000, 128: 123, 136 (60 M); 24, 132, 4000, 64:
+// 34, 32 (12 M); 128, 100, 2000, 64: 60, 48 (24 M); 32, 40, 9000, 32: 23, 25 (11 M).
+// (What tiles of 64 and 128 rows lose: 8 bits of a probability, where the others have 16.)
+static int tile_rows4(int dtype, int hd, int rows, int64_t lists, int64_t positions) {
+  if (rows <= 16) return 16;
+  const int64_t scores = lists * positions * rows;
+  if (dtype == NGG_F32) return hd == 128 || scores < (hd == 64 ? 8 << 20 : 32 << 20) ? 16 : 32;
+  if (scores >= 40 << 20) return rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  return scores < (hd == 128 ? 6 << 20 : 4 << 20) ? 16 : 32;
+}
 static int step_keys(int rows) { return rows <= 32 ? 128 : 64; }
 
 // Short lists go whole to a workgroup each: no parts, no merge; the longer, the more workgroups there have to be, since few leave the
@@ -720,7 +774,7 @@ static bool whole_lists(int dtype, int64_t steps, int64_t workgroups) {
 TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, int64_t max_positions) {
   TreePlan p;
   const int64_t positions = max_positions * B * Hkv;
-  p.rows = tile_rows(dtype, hd, T * G, (int64_t)B * Hkv, max_positions);
+  p.rows = (cache == NGG_FP4 ? tile_rows4 : tile_rows)(dtype, hd, T * G, (int64_t)B * Hkv, max_positions);
   p.Z = (T * G + p.rows - 1) / p.rows;
   const int64_t steps = (max_positions + step_keys(p.rows) - 1) / step_keys(p.rows);
   p.whole = p.rows <= 32 && whole_lists(dtype, steps, (int64_t)B * Hkv * p.Z);
@@ -728,7 +782,27 @@ TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, i
   // instead of 372; below, a list that is read again soon is better kept (1900 positions 46.9, non-temporal 49.7).
   const int64_t bytes = cache == NGG_FP4 ? positions * (hd + hd / kGroup4 * 2) : 2 * positions * hd * (cache == NGG_F32 ? 4 : cache == NGG_BF16 ? 2 : 1);
   p.stream = p.rows == 16 && p.Z == 1 && bytes > (int64_t)400 << 20;
-  const int64_t want = (512 + p.Z - 1) / p.Z, r = p.whole ? (int64_t)B * Hkv : std::max<int64_t>(1, std::min(want, steps * B * Hkv));
+  p.pieces = p.piece_steps = 0;
+  const int64_t lists = (int64_t)B * Hkv;
+  // Over 4 bits few lists go in pieces: no workgroup has to look for its share or to work on two lists (us, shares and pieces: 32 lists of
+  // 2047 positions, 51 rows 24.4, 19.3; 27 of up to 5001, 28 rows, fp32 21.8, 17.9; 8 of 60000, 4 rows 38.9, 30.0; with two pieces a
+  // list, 256 of up to 8000, 16 rows 47.6, 61.5)
+  if (cache == NGG_FP4 && p.rows <= 32 && !p.whole) {
+    const int64_t least = lists * steps < 256 ? 1 : 2;     // steps of a piece
+    const int64_t n = std::min<int64_t>((steps + least - 1) / least, 512 / (lists * p.Z));
+    if (n >= 4 || n * least >= steps) {
+      p.piece_steps = (int)((steps + n - 1) / n);
+      p.pieces = (int)((steps + p.piece_steps - 1) / p.piece_steps);
+      p.ranges = (int)lists * p.pieces;
+      const size_t rows = (size_t)p.ranges * p.Z * p.rows;
+      p.o_bytes = rows * hd * 4;
+      p.ml_bytes = rows * 8;
+      return p;
+    }
+  }
+  // (768: three workgroups to a compute unit, as many as tree4_stream_kernel's registers allow; with 512 32 single tokens over up to 32000
+  // positions take 123 us instead of 113)
+  const int64_t want = ((cache == NGG_FP4 && p.rows == 16 && dtype != NGG_F32 ? 768 : 512) + p.Z - 1) / p.Z, r = p.whole ? (int64_t)B * Hkv : std::max<int64_t>(1, std::min(want, steps * B * Hkv));
   p.ranges = (int)(p.whole || r < 8 ? r : r < want ? (r + 7) / 8 * 8 : r / 8 * 8);   // eights: one for each die; up, if a step each is to be had
   const size_t rows = p.whole ? 0 : (size_t)p.ranges * p.Z * 2 * p.rows;
   p.o_bytes = rows * hd * 4;
@@ -750,25 +824,30 @@ static void launch_stream(const TreeArgs &a, hipStream_t s) {
   hipLaunchKernelGGL((tree_stream_kernel<T, CT, HD, QF, NT>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
   merge<T, HD, 16 * QF, 128>(a, s);
 }
-template <typename CT, int HD>
+template <typename CT, int HD, int RG>
 static void launch_block(const TreeArgs &a, hipStream_t s) {
   constexpr size_t lds = (size_t)8 * 32 * HD * 2 + 2 * 64 * 4 + 2 * 4;
-  static const bool once = (allow_lds(&tree_block_kernel<CT, HD>, lds + (NGG_TREE_MAX + 1) * 4), true);
+  static const bool once = (allow_lds(&tree_block_kernel<CT, HD, RG>, lds + (NGG_TREE_MAX + 1) * 4), true);
   (void)once;
-  hipLaunchKernelGGL((tree_block_kernel<CT, HD>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
-  merge<bf16_t, HD, 128, 64>(a, s);
+  hipLaunchKernelGGL((tree_block_kernel<CT, HD, RG>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
+  merge<bf16_t, HD, 32 * RG, 64>(a, s);
 }
-void launch_tree_block4(const TreeArgs &a, hipStream_t s) {
-  if (a.p.hd == 32) launch_block<fp4x2_t, 32>(a, s);
-  else if (a.p.hd == 64) launch_block<fp4x2_t, 64>(a, s);
-  else launch_block<fp4x2_t, 128>(a, s);
+template <int HD>
+static void block4(int rows, const TreeArgs &a, hipStream_t s) {
+  if (rows == 64) launch_block<fp4x2_t, HD, 2>(a, s);
+  else launch_block<fp4x2_t, HD, 4>(a, s);
+}
+void launch_tree_block4(int rows, const TreeArgs &a, hipStream_t s) {
+  if (a.p.hd == 32) block4<32>(rows, a, s);
+  else if (a.p.hd == 64) block4<64>(rows, a, s);
+  else block4<128>(rows, a, s);
 }
 template <typename T, typename CT, int HD>
 static void by_rows(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
   if (p.rows == 16 && p.stream) launch_stream<T, CT, HD, 1, true>(a, s);
   else if (p.rows == 16) launch_stream<T, CT, HD, 1, false>(a, s);
   else if (p.rows == 32) launch_stream<T, CT, HD, 2, false>(a, s);
-  else if constexpr (sizeof(T) == 2) launch_block<CT, HD>(a, s);
+  else if constexpr (sizeof(T) == 2) launch_block<CT, HD, 4>(a, s);
 }
 template <typename T, typename CT>
 static void by_head(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
@@ -781,7 +860,6 @@ template <typename T, int HD>
 static void merge_rows(int rows, const TreeArgs &a, hipStream_t s) {
   if (rows == 16) merge<T, HD, 16, 128>(a, s);
   else if (rows == 32) merge<T, HD, 32, 128>(a, s);
-  else if constexpr (sizeof(T) == 2) merge<T, HD, 128, 64>(a, s);
 }
 template <typename T>
 static void merge_head(int rows, const TreeArgs &a, hipStream_t s) {

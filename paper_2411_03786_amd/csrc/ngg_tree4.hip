@@ -6,20 +6,25 @@
 // some 2^-14 below the largest product: scores were off by up to 2^-15 of the sum of |q k|.)
 #include "ngg_tree.h"
 
+#include <type_traits>
+
 namespace ngg {
 
 // x rounded to a sum of N bf16 numbers, each the rounding of what the ones before left
 template <int N>
 __device__ __forceinline__ void bf16_terms(const float (&x)[8], Frag<bf16_t> (&t)[N]) {
+  u32x4 w[N];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float rest = x[e];
+  for (int e = 0; e < 8; e += 2) {
+    f32x2 rest{x[e], x[e + 1]};
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      t[i].v[e] = (bf16_t)rest;
-      rest -= (float)t[i].v[e];
+      w[i][e / 2] = __builtin_bit_cast(unsigned, __builtin_convertvector(rest, bf16x2));
+      rest = f32x2{rest[0] - __uint_as_float(w[i][e / 2] << 16), rest[1] - __uint_as_float(w[i][e / 2] & 0xffff0000u)};
     }
   }
+#pragma unroll
+  for (int i = 0; i < N; ++i) t[i].v = __builtin_bit_cast(bf16x8, w[i]);
 }
 
 // A row of queries as operands, and the scores of a tile of 32 keys under it.  Lane (c, g4) has row c, and dimensions g4 HD / 4
@@ -57,9 +62,9 @@ template <int HD> struct Tile4 {
 };
 
 // One workgroup: one row tile (16 QF rows) over its share of the list, as tree_stream_kernel: the waves take the tiles of 32 keys in
-// turn and are joined through LDS.  The next tile is on its way while one is computed.
+// turn and are joined through LDS.  Two more tiles are on their way while one is computed.
 template <typename T, int HD, int QF, bool NT>
-__global__ __launch_bounds__(256) void tree4_stream_kernel(const TreeArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 && QF == 1 ? 3 : 1) void tree4_stream_kernel(const TreeArgs a) {
   constexpr int NW = 4, NG = HD / 32, DF = HD / 16, ROWS = 16 * QF, KS = 32 * NW, TERMS = sizeof(T) == 2 ? 2 : 3;
   typedef Query4<T, HD> Query;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -68,7 +73,7 @@ __global__ __launch_bounds__(256) void tree4_stream_kernel(const TreeArgs a) {
   int *pre = reinterpret_cast<int *>(lml + NW * QF * 32);  // [B + 1]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, g4 = lane >> 4, Hkv = a.p.Hkv, ps = a.p.page_size;
-  Work<KS> w(a, pre);
+  Work<KS, true> w(a, pre);
   while (w.next()) {
     const int b = w.b, hk = w.hk, z = w.z;
     const SeqLens len = seq_lens(a, b);
@@ -140,12 +145,13 @@ __global__ __launch_bounds__(256) void tree4_stream_kernel(const TreeArgs a) {
       while (at_off >= ps) { at_off -= ps; ++at_page; }
       page = at_tile < t_end ? a.pages[b * a.pages_batch + at_page] : -1;
     };
-    auto compute = [&](Tile4<HD> &t, int tile) {
+    // FULL: every row sees every key of the tile
+    auto compute = [&](auto all, Tile4<HD> &t, int tile) {
+      constexpr bool FULL = decltype(all)::value;
       if (!t.there) return;
       const int pos0 = tile * 32;
-      const bool full = pos0 + 32 <= len.ctx;              // (uniform) every row sees every key
       bool wild = false;
-      if (!full) {
+      if constexpr (!FULL) {
         // what lies behind the last position is anything, and 0 times it must be 0: such powers of two are taken as 1, and so are those
         // of places that may not be finite, which the rows that see them get below
 #pragma unroll
@@ -164,7 +170,8 @@ __global__ __launch_bounds__(256) void tree4_stream_kernel(const TreeArgs a) {
       f32x4 S[QF][2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float scale = exp_scale(t.ke >> (8 * h) & 0xff);
+        __builtin_amdgcn_sched_barrier(0);
+        const float scale = h ? scale4<1>(t.ke) : scale4<0>(t.ke);
 #pragma unroll
         for (int f = 0; f < QF; ++f) S[f][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -180,7 +187,7 @@ __global__ __launch_bounds__(256) void tree4_stream_kernel(const TreeArgs a) {
 #pragma unroll
       for (int f = 0; f < QF; ++f) {
         vis[f] = 0xff;
-        if (!full) {
+        if constexpr (!FULL) {
           const int from = a.T > 64 ? pos0 - len.ctx : 0;
           if (a.T > 64) see[f] = mask_window(a, b, tok[f], from);
           vis[f] = visible8(see[f], from, tok[f], pos0 + g4 * 8 - len.ctx, n_keys - len.ctx);
@@ -188,6 +195,7 @@ __global__ __launch_bounds__(256) void tree4_stream_kernel(const TreeArgs a) {
           for (int e = 0; e < 8; ++e)
             if (!(vis[f] >> e & 1)) S[f][e >> 2][e & 3] = -__builtin_inff();
         }
+        __builtin_amdgcn_sched_barrier(0);
         float mx = S[f][0][0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) mx = fmaxf(mx, S[f][e >> 2][e & 3]);
@@ -214,6 +222,7 @@ __global__ __launch_bounds__(256) void tree4_stream_kernel(const TreeArgs a) {
       }
 #pragma unroll
       for (int j = 0; j < NG; ++j) {
+        __builtin_amdgcn_sched_barrier(0);
         Frag<bf16_t> V[2];
         widen4_values(t.v[j], t.ve[j], V[0].v, V[1].v);
 #pragma unroll
@@ -253,19 +262,26 @@ __global__ __launch_bounds__(256) void tree4_stream_kernel(const TreeArgs a) {
           }
       }
     };
-    Tile4<HD> t0, t1;
+    Tile4<HD> t[2];
     int tile = at_tile;
-    if (tile < t_end) fetch(t0);
-    while (tile < t_end) {
-      if (tile + NW < t_end) fetch(t1);
-      compute(t0, tile);
+    const int full_end = min(t_end, len.ctx / 32);
+    if (tile < t_end) fetch(t[0]);
+    while (true) {
+#define NGG_STEP(i)                                             \
+      if (tile >= full_end) { t[0] = t[i]; break; }             \
+      if (tile + NW < t_end) fetch(t[1 - i]);                   \
+      compute(std::true_type{}, t[i], tile);                    \
       tile += NW;
-      if (tile >= t_end) break;
-      if (tile + NW < t_end) fetch(t0);
-      compute(t1, tile);
-      tile += NW;
+      NGG_STEP(0)
+      NGG_STEP(1)
+#undef NGG_STEP
     }
-    join_waves<T, HD, QF, NW>(a, w, len, m, l, O, lo, lml);
+    for (; tile < t_end; tile += NW) {                     // the last of the context, and the tree's own
+      if (tile + NW < t_end) fetch(t[1]);
+      compute(std::false_type{}, t[0], tile);
+      t[0] = t[1];
+    }
+    join_waves<T, HD, QF, NW>(a, w, b, hk, z, len, tid, lane, wave, c, g4, m, l, O, lo, lml);
     __syncthreads();
   }
 }
@@ -289,7 +305,7 @@ static void by_head(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
   else by_rows<T, 128>(a, p, s);
 }
 void launch_tree_attention4(int dtype, const TreeArgs &a, const TreePlan &p, hipStream_t s) {
-  if (p.rows == 128) return launch_tree_block4(a, s);
+  if (p.rows >= 64) return launch_tree_block4(p.rows, a, s);
   if (dtype == NGG_F32) by_head<float>(a, p, s);
   else by_head<bf16_t>(a, p, s);
   launch_tree_merge(dtype, p.rows, a, s);
