@@ -260,6 +260,20 @@ __global__ __launch_bounds__(256) void kv4_read_group_kernel(const CacheArgs a, 
   const int64_t stride = values ? a.v_token : a.k_token;
   out += t0 * stride + h * (values ? a.v_head : a.k_head);
   const GroupSlots g(a, t0, m);
+  // a thread's parts of the output, eight dimensions of a token each: where they come from, on its way before anything waits
+  constexpr int PARTS = kGroup * 128 / 8 / 256;
+  const int per = hd / 8;
+  unsigned w[PARTS], e[PARTS];
+#pragma unroll
+  for (int j = 0; j < PARTS; ++j) {
+    const int i = tid + 256 * j, t = i / per, d = i % per * 8, slot = __shfl(g.slot, min(t, kGroup - 1));
+    w[j] = 0;
+    e[j] = 127;
+    if (i >= m * per || slot < 0) continue;
+    const size_t first = slot_head(a, slot, h);
+    if (!values) w[j] = *reinterpret_cast<const unsigned *>((const uint8_t *)a.p.k + first * (hd / 2) + k_offset4(slot % ps, d, hd));
+    e[j] = values ? a.p.v_exp[first * ng + v_exp_offset4(slot % ps, d, hd)] : a.p.k_exp[first * ng + k_exp_offset4(slot % ps, d, hd)];
+  }
   if (values) {
     const int pairs = hd == 32 ? 1 : hd / 64, units = 8 * pairs, work = g.chunks * units;
     for (int i0 = tid & ~63; i0 < work; i0 += 256) {
@@ -292,31 +306,22 @@ __global__ __launch_bounds__(256) void kv4_read_group_kernel(const CacheArgs a, 
     }
     __syncthreads();
   }
-  // eight dimensions of a token each
-  const int per = hd / 8;
-  for (int i0 = tid & ~63; i0 < m * per; i0 += 256) {
-    const int i = i0 + (tid & 63), t = i / per, d = i % per * 8;
-    const int slot = __shfl(g.slot, min(t, kGroup - 1));
+#pragma unroll
+  for (int j = 0; j < PARTS; ++j) {
+    const int i = tid + 256 * j, t = i / per, d = i % per * 8;
+    const int slot_there = __shfl(g.slot, min(t, kGroup - 1));
     if (i >= m * per) continue;
-    unsigned w = 0, e = 127;
-    if (slot >= 0) {
-      const size_t first = slot_head(a, slot, h);
-      if (!values) {
-        w = *reinterpret_cast<const unsigned *>((const uint8_t *)a.p.k + first * (hd / 2) + k_offset4(slot % ps, d, hd));
-        e = a.p.k_exp[first * ng + k_exp_offset4(slot % ps, d, hd)];
-      } else {
-        const u32x2 b = *reinterpret_cast<const u32x2 *>(&bytes[t][d / 32 * 16 + d % 16]);
-        const int up = d % 32 / 16 * 4;
-        auto close = [&](unsigned x) {                     // the wanted halves of four bytes
-          x = x >> up & 0x0f0f0f0fu;
-          x = (x | x >> 4) & 0x00ff00ffu;
-          return (x | x >> 8) & 0xffffu;
-        };
-        w = close(b[0]) | close(b[1]) << 16;
-        e = a.p.v_exp[first * ng + v_exp_offset4(slot % ps, d, hd)];
-      }
+    if (values && slot_there >= 0) {
+      const u32x2 b = *reinterpret_cast<const u32x2 *>(&bytes[t][d / 32 * 16 + d % 16]);
+      const int up = d % 32 / 16 * 4;
+      auto close = [&](unsigned x) {                       // the wanted halves of four bytes
+        x = x >> up & 0x0f0f0f0fu;
+        x = (x | x >> 4) & 0x00ff00ffu;
+        return (x | x >> 8) & 0xffffu;
+      };
+      w[j] = close(b[0]) | close(b[1]) << 16;
     }
-    put_eight(out + t * stride + d, w, exp_scale(e), vec);
+    put_eight(out + t * stride + d, w[j], exp_scale(e[j]), vec);
   }
 }
 

@@ -45,61 +45,73 @@ template <> struct Unit<4> { typedef uint32_t T; };
 template <> struct Unit<8> { typedef u32x2 T; };
 template <> struct Unit<16> { typedef u32x4 T; };
 
-// Moves one unit of every entry of a list: all are read before the first is written.  at(pos): the unit's byte offset in its (page,
-// head).  Up to 16 entries wait in registers, more in LDS.
-struct Entry { int64_t from, to; int from_pos, to_pos; };  // first position of the (page, head 0); -1: none
+// What an entry of a list moves from and to, in bytes of keys, values and the exponents of either: the offset of a unit is the
+// position's plus the unit's own.
+struct Entry { int64_t from[4], to[4]; };
 constexpr int kInRegisters = 16;
-template <int BYTES, typename At>
-__device__ __forceinline__ void move_unit(uint8_t *base, const Entry *list, int n, int64_t head, int position_bytes, At at, uint8_t *wait) {
+
+// Moves one unit of every entry: all are read before the first is written.  Up to 16 entries wait in registers, more in LDS.
+template <int BYTES>
+__device__ __forceinline__ void move_unit(uint8_t *mine, const Entry *list, int n, int kind, uint8_t *wait) {
   typedef typename Unit<BYTES>::T U;
-  auto place = [&](int64_t first, int pos) { return reinterpret_cast<U *>(base + (first + head) * position_bytes + at(pos)); };
   if (n <= kInRegisters) {
     U x[kInRegisters];
 #pragma unroll
     for (int i = 0; i < kInRegisters; ++i)
-      if (i < n && list[i].from >= 0) x[i] = *place(list[i].from, list[i].from_pos);
+      if (i < n) x[i] = *reinterpret_cast<const U *>(mine + list[i].from[kind]);
 #pragma unroll
     for (int i = 0; i < kInRegisters; ++i)
-      if (i < n && list[i].from >= 0) *place(list[i].to, list[i].to_pos) = x[i];
+      if (i < n) *reinterpret_cast<U *>(mine + list[i].to[kind]) = x[i];
     return;
   }
-  U *mine = reinterpret_cast<U *>(wait) + threadIdx.x;     // (a thread's own column)
-  for (int i = 0; i < n; ++i)
-    if (list[i].from >= 0) mine[i * blockDim.x] = *place(list[i].from, list[i].from_pos);
-  for (int i = 0; i < n; ++i)
-    if (list[i].from >= 0) *place(list[i].to, list[i].to_pos) = mine[i * blockDim.x];
+  U *column = reinterpret_cast<U *>(wait) + threadIdx.x;   // (a thread's own)
+  for (int i = 0; i < n; ++i) column[i * blockDim.x] = *reinterpret_cast<const U *>(mine + list[i].from[kind]);
+  for (int i = 0; i < n; ++i) *reinterpret_cast<U *>(mine + list[i].to[kind]) = column[i * blockDim.x];
 }
 
-// One thread per unit of a (layer, list, head); a thread reads and writes bytes that no other one touches.
+// One thread per unit of a (layer, list, head); a thread reads and writes bytes that no other one touches.  Bound by two chains of loads
+// and the scattered bytes of values: FIGURES.
 template <int CACHE, int HD>
 __global__ __launch_bounds__(256) void kv_move_kernel(const MoveArgs a, int lists_first) {
   typedef Units<CACHE, HD> U;
-  constexpr int ALL = U::KU + U::VU + 2 * U::EU;
+  constexpr int ALL = U::KU + U::VU + 2 * U::EU, BYTES = HD * U::value_bits / 8;   // BYTES: of a position's keys (or values) of a head
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  __shared__ int count;
   Entry *list = reinterpret_cast<Entry *>(smem);
-  uint8_t *wait = smem + (a.n + a.n % 2) * sizeof(Entry);
   const int layer = blockIdx.z, b = lists_first + blockIdx.y, ps = a.p.page_size, Hkv = a.p.Hkv;
   const int positions = a.layer_pages * ps;                // of a layer
-  for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
-    const int from = a.src[b * a.src_list + i], to = a.dst[b * a.dst_list + i];
-    Entry e = {-1, -1, 0, 0};
-    if (from >= 0 && from < positions && to >= 0 && to < positions) {
-      e.from = (int64_t)(layer * a.layer_pages + from / ps) * Hkv * ps;
-      e.to = (int64_t)(layer * a.layer_pages + to / ps) * Hkv * ps;
-      e.from_pos = from % ps;
-      e.to_pos = to % ps;
+  if (threadIdx.x < 64) {                                  // the entries that there are, in their order (the first wave; blocks of less have one)
+    int n = 0;
+    for (int i0 = 0; i0 < a.n; i0 += min(blockDim.x, 64u)) {
+      const int i = i0 + threadIdx.x;
+      int from = -1, to = -1;
+      if (i < a.n) {
+        from = a.src[b * a.src_list + i];
+        to = a.dst[b * a.dst_list + i];
+      }
+      const bool ok = from >= 0 && from < positions && to >= 0 && to < positions;
+      const uint64_t all = __ballot(ok);
+      if (ok) {
+        Entry &e = list[n + __builtin_popcountll(all & ((1ull << threadIdx.x) - 1))];
+        const int64_t f = (int64_t)(layer * a.layer_pages + from / ps) * Hkv * ps, t = (int64_t)(layer * a.layer_pages + to / ps) * Hkv * ps;
+        const int fp = from % ps, tp = to % ps;
+        e.from[0] = f * BYTES + U::k(fp, 0); e.from[1] = f * BYTES + U::v(fp, 0); e.from[2] = f * U::EU + U::ke(fp, 0); e.from[3] = f * U::EU + U::ve(fp, 0);
+        e.to[0] = t * BYTES + U::k(tp, 0); e.to[1] = t * BYTES + U::v(tp, 0); e.to[2] = t * U::EU + U::ke(tp, 0); e.to[3] = t * U::EU + U::ve(tp, 0);
+      }
+      n += __builtin_popcountll(all);
     }
-    list[i] = e;
+    if (threadIdx.x == 0) count = n;
   }
   __syncthreads();
-  const int unit = blockIdx.x * blockDim.x + threadIdx.x;
-  if (unit >= Hkv * ALL) return;
+  const int n = count, unit = blockIdx.x * blockDim.x + threadIdx.x;
+  if (unit >= Hkv * ALL || n == 0) return;
+  uint8_t *wait = smem + a.n * sizeof(Entry);
   const int64_t head = (int64_t)(unit / ALL) * ps;
-  const int u = unit % ALL;
-  if (u < U::KU) move_unit<U::KB>((uint8_t *)a.p.k, list, a.n, head, HD * U::value_bits / 8, [&](int pos) { return U::k(pos, u); }, wait);
-  else if (u < U::KU + U::VU) move_unit<U::VB>((uint8_t *)a.p.v, list, a.n, head, HD * U::value_bits / 8, [&](int pos) { return U::v(pos, u - U::KU); }, wait);
-  else if (u < U::KU + U::VU + U::EU) move_unit<1>(a.p.k_exp, list, a.n, head, U::EU, [&](int pos) { return U::ke(pos, u - U::KU - U::VU); }, wait);
-  else move_unit<1>(a.p.v_exp, list, a.n, head, U::EU, [&](int pos) { return U::ve(pos, u - U::KU - U::VU - U::EU); }, wait);
+  const int u = unit % ALL, v = u - U::KU, ke = v - U::VU, ve = ke - U::EU;
+  if (u < U::KU) move_unit<U::KB>((uint8_t *)a.p.k + head * BYTES + U::k(0, u), list, n, 0, wait);
+  else if (v < U::VU) move_unit<U::VB>((uint8_t *)a.p.v + head * BYTES + U::v(0, v), list, n, 1, wait);
+  else if (ke < U::EU) move_unit<1>(a.p.k_exp + head * U::EU + U::ke(0, ke), list, n, 2, wait);
+  else move_unit<1>(a.p.v_exp + head * U::EU + U::ve(0, ve), list, n, 3, wait);
 }
 
 // Copies pages, of each the tiles of 32 positions that hold its first positions[i] (all without): one workgroup per (layer, page, head).
@@ -127,7 +139,7 @@ static void launch_move(const MoveArgs &a, hipStream_t s) {
   typedef Units<CACHE, HD> U;
   const int units = a.p.Hkv * (U::KU + U::VU + 2 * U::EU);
   // what waits in LDS: as many threads as 64 KB have room for
-  const int list = (a.n + a.n % 2) * (int)sizeof(Entry), threads = a.n <= kInRegisters ? 256 : a.n <= 64 ? 64 : a.n <= 128 ? 32 : a.n <= 256 ? 16 : a.n <= 512 ? 8 : 4;
+  const int list = a.n * (int)sizeof(Entry), threads = a.n <= kInRegisters ? 256 : a.n <= 64 ? 64 : a.n <= 128 ? 32 : a.n <= 256 ? 16 : a.n <= 512 ? 8 : 4;
   const size_t lds = list + (a.n <= kInRegisters ? 0 : (size_t)threads * a.n * 16);
   allow_lds(&kv_move_kernel<CACHE, HD>, lds);
   for (int at = 0; at < a.lists; at += 65535)
@@ -192,17 +204,18 @@ __global__ __launch_bounds__(256) void pages_release_kernel(const TableArgs a, c
 }
 
 // The exclusive sum of a workgroup's numbers, and their total
-__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t *part, int64_t &total) {
+template <typename N>
+__device__ __forceinline__ N block_sum(N x, N *part, N &total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  int64_t inc = x;
+  N inc = x;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t up = __shfl_up(inc, o);
+    const N up = __shfl_up(inc, o);
     if (lane >= o) inc += up;
   }
   if (lane == 63) part[wave] = inc;
   __syncthreads();
-  int64_t before = 0;
+  N before = 0;
   total = 0;
   for (int v = 0; v < waves; ++v) {
     if (v < wave) before += part[v];
@@ -212,35 +225,41 @@ __device__ __forceinline__ int64_t block_sum(int64_t x, int64_t *part, int64_t &
   return before + inc - x;
 }
 
-// One workgroup.  The entries that the new tokens reach, of one sequence behind the other, are counted through; the pages they need are
-// the lowest free ones in that order.  Nothing changes where there are too few.
+// One workgroup, a thread for a sequence.  The entries that the new tokens reach, of one sequence behind the other, are counted through;
+// the pages they need are the lowest free ones in that order.  Nothing changes where there are too few.  Where no sequence reaches more than
+// kFewEntries, as in a step of a few tokens, its thread looks at them, otherwise all threads do in turn (us, FIGURES).  Bound by its chain of
+// loads: length, entry, count.
+constexpr int kFewEntries = 4, kFreeHere = 2048;           // free pages that LDS has room for
 __global__ __launch_bounds__(1024) void pages_reserve_kernel(const TableArgs a, const int32_t *new_tokens, const ReserveOut out, int32_t *free_list) {
   __shared__ int64_t pre[NGG_TREE_MAX + 1];                // entries before a sequence's
   __shared__ int first[NGG_TREE_MAX];                      // its first entry's place
   __shared__ int shared_page[NGG_TREE_MAX];                // the page that it would write to, while others hold it; -1
-  __shared__ int64_t part[16];
+  __shared__ int64_t part64[16];
+  __shared__ int part[16];
+  __shared__ int free_here[kFreeHere];
   const int s = threadIdx.x, ps = a.page_size;
-  int64_t n = 0, beyond = 0, total, too_long;
-  int mine = -1, rest = 0, refs = 0;
+  int counts[4];                                           // of the first pages of all, four a thread
+#pragma unroll
+  for (int i = 0; i < 4; ++i) counts[i] = 4 * s + i < a.n_pages ? a.refs[4 * s + i] : 1;
+  int64_t n = 0, beyond = 0, total = 0, too_long = 0;
+  int mine = -1, rest = 0, refs = 0, j0 = 0, entry[kFewEntries] = {};
+  int32_t *row = a.pages + s * a.pages_seq;
   if (s < a.n_seqs) {
-    const int64_t len = max(a.lens[s], 0), want = max(new_tokens[s], 0);
-    const int64_t j0 = len / ps, end = want ? (len + want + ps - 1) / ps : j0;
+    const int64_t len = max(a.lens[s], 0), want = max(new_tokens[s], 0), end = want ? (len + want + ps - 1) / ps : len / ps;
     beyond = max(end - a.max_pages, (int64_t)0);
-    n = max(min(end, (int64_t)a.max_pages) - j0, (int64_t)0);
-    first[s] = (int)j0;
+    n = max(min(end, (int64_t)a.max_pages) - len / ps, (int64_t)0);
+    j0 = (int)(len / ps);
     rest = (int)(len % ps);
-    if (n && rest) {
-      mine = a.pages[s * a.pages_seq + j0];
-      if (!is_page(a, mine)) mine = -1;
-      else refs = a.refs[mine];
+#pragma unroll
+    for (int i = 0; i < kFewEntries; ++i) entry[i] = i < n ? row[j0 + i] : 0;
+    if (n && rest && is_page(a, entry[0])) {
+      mine = entry[0];
+      refs = a.refs[mine];
     }
+    first[s] = j0;
     shared_page[s] = mine;
   }
-  const int64_t at = block_sum(n, part, total);
-  (void)block_sum(beyond, part, too_long);
-  if (s < a.n_seqs) pre[s] = at;
-  if (s == 0) pre[a.n_seqs] = total;
-  __syncthreads();
+  const bool few = !__syncthreads_or(n > kFewEntries || beyond > 0);
   // of the sequences that go on in a page that nobody else holds, the last keeps it
   bool copies = mine >= 0 && refs > 1;
   if (copies) {
@@ -251,6 +270,19 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(const TableArgs a, 
   }
   __syncthreads();
   if (s < a.n_seqs && !copies) shared_page[s] = -1;
+  int64_t need = 0, rank = 0;
+  if (few) {
+    int mine_too = copies, all;
+#pragma unroll
+    for (int i = 0; i < kFewEntries; ++i) mine_too += entry[i] < 0;
+    rank = block_sum(mine_too, part, all);
+    need = all;
+  } else {
+    const int64_t at = block_sum(n, part64, total);
+    (void)block_sum(beyond, part64, too_long);
+    if (s < a.n_seqs) pre[s] = at;
+    if (s == 0) pre[a.n_seqs] = total;
+  }
   __syncthreads();
   // entry f of all: its sequence and place, and whether it needs a page
   auto needs = [&](int64_t f, int &q, int &j) {
@@ -264,40 +296,64 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(const TableArgs a, 
     j = first[lo] + (int)(f - pre[lo]);
     return (f == pre[lo] && shared_page[lo] >= 0) || a.pages[q * a.pages_seq + j] < 0;
   };
-  int64_t need = 0;
-  for (int64_t f0 = 0; f0 < total; f0 += 1024) {
-    const int64_t f = f0 + threadIdx.x;
-    int q, j;
-    need += __syncthreads_count(f < total && needs(f, q, j));
-  }
-  int64_t found = 0;
-  for (int64_t p0 = 0; p0 < a.n_pages && found < need; p0 += 1024) {
-    const int64_t p = p0 + threadIdx.x;
-    const bool free = p < a.n_pages && a.refs[p] == 0;
-    int64_t more;
-    const int64_t rank = found + block_sum(free, part, more);
-    if (free && rank < need) free_list[rank] = (int)p;
+  if (!few)
+    for (int64_t f0 = 0; f0 < total; f0 += 1024) {
+      const int64_t f = f0 + s;
+      int q, j;
+      need += __syncthreads_count(f < total && needs(f, q, j));
+    }
+  // the free pages, as many as are needed, in LDS if they fit
+  const bool here = need <= kFreeHere;
+  int found = 0;
+  for (int64_t p0 = 0; p0 < a.n_pages && found < need; p0 += 4096) {
+    if (p0)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) counts[i] = p0 + 4 * s + i < a.n_pages ? a.refs[p0 + 4 * s + i] : 1;
+    int more, at = found + block_sum((counts[0] == 0) + (counts[1] == 0) + (counts[2] == 0) + (counts[3] == 0), part, more);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (counts[i] == 0) {
+        if (at < need) (here ? free_here : free_list)[at] = (int)p0 + 4 * s + i;
+        ++at;
+      }
     found += more;
   }
-  __syncthreads();
   const int64_t missing = max(need - found, (int64_t)0) + too_long;
   if (s == 0) *out.missing = (int)min(missing, (int64_t)INT32_MAX);
-  if (s < a.n_seqs) {
-    out.src[s] = out.dst[s] = -1;
-    out.positions[s] = 0;
-  }
-  if (missing) return;
+  int src = -1, dst = -1, positions = 0;
   __syncthreads();
-  int64_t rank0 = 0;
+  auto take = [&](int64_t rank) {
+    const int page = (here ? free_here : free_list)[rank];
+    a.refs[page] = 1;
+    return page;
+  };
+  if (few && !missing && s < a.n_seqs) {
+    if (copies) {
+      src = mine;
+      positions = rest;
+      row[j0] = dst = take(rank++);
+      atomicSub(a.refs + mine, 1);
+    }
+#pragma unroll
+    for (int i = 0; i < kFewEntries; ++i)
+      if (entry[i] < 0) row[j0 + i] = take(rank++);
+  }
+  if (s < a.n_seqs) {
+    out.src[s] = src;
+    out.dst[s] = dst;
+    out.positions[s] = positions;
+  }
+  if (few || missing) return;
+  __syncthreads();
+  int rank0 = 0;
   for (int64_t f0 = 0; f0 < total; f0 += 1024) {
-    const int64_t f = f0 + threadIdx.x;
-    int q = 0, j = 0;
-    const bool take = f < total && needs(f, q, j);
-    int64_t more;
-    const int64_t rank = rank0 + block_sum(take, part, more);
+    const int64_t f = f0 + s;
+    int q = 0, j = 0, more;
+    const bool wants = f < total && needs(f, q, j);
+    const int r = rank0 + block_sum((int)wants, part, more);
     rank0 += more;
-    if (!take) continue;
-    const int page = free_list[rank];
+    if (!wants) continue;
+    const int page = take(r);
     if (f == pre[q] && shared_page[q] >= 0) {
       out.src[q] = shared_page[q];
       out.dst[q] = page;
@@ -305,7 +361,6 @@ __global__ __launch_bounds__(1024) void pages_reserve_kernel(const TableArgs a, 
       atomicSub(a.refs + shared_page[q], 1);
     }
     a.pages[q * a.pages_seq + j] = page;
-    a.refs[page] = 1;
   }
 }
 
