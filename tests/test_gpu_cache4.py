@@ -101,6 +101,23 @@ def test_cache_of_many_sequences_runs(dtype, hd, Hkv, tree, start):
     assert torch.equal(some[0], got[0][:100]) and torch.equal(some[1], got[1][:100])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hd,Hkv,n,gap", [(32, 301, 470, 0), (32, 301, 470, 3), (64, 150, 300, 0), (128, 33, 900, 0)])
+def test_cache_of_many_heads(dtype, hd, Hkv, n, gap):
+    """More heads than a workgroup takes at once, with an odd number left over; runs, single places and places left out."""
+    rng = np.random.default_rng(n)
+    slots = np.concatenate([5 + np.arange(n // 2), n + 40 + rng.permutation(n)[:n - n // 2]])
+    slots[[3, n - 1]] = -1
+    kv = ngg.KVPages(2 * n // 32 + 3, 32, Hkv, hd, "fp4")
+    x = randn(n, 2 * Hkv * hd + gap, seed=n, dtype=dtype)
+    k, v = x[:, gap:gap + Hkv * hd].view(n, Hkv, hd), x[:, gap + Hkv * hd:].view(n, Hkv, hd)
+    kv.write(k, v, ints(slots))
+    there = torch.from_numpy(slots >= 0).cuda()
+    for out in ("f32", "bf16"):
+        for g, t in zip(kv.read(ints(slots), DT[out]), (k, v)):
+            assert torch.equal(g[there].double(), four_bits(t)[there]) and (g[~there] == 0).all()
+
+
 def test_four_bit_corners():
     """Zeros, the largest value exactly and just above, every tie, the smallest and largest exponents, numbers that are not finite; each
     32 dimensions by themselves."""
@@ -177,13 +194,13 @@ def test_cache_takes_rows_with_strides(dtype, gap, n):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("hd,rd,inter", [(32, 32, False), (64, 32, True), (128, 128, True), (128, 128, False), (128, 34, False), (64, 6, True)])
-@pytest.mark.parametrize("Hkv,n", [(3, 75), (60, 75)])
+@pytest.mark.parametrize("Hkv,n", [(3, 75), (120, 75), (203, 700)])
 def test_cache_rotates_as_rotary_does(dtype, hd, rd, inter, Hkv, n):
     rope, pos = ngg.Rope(rd, 300, interleaved=inter), ints(np.random.default_rng(2).integers(0, 300, n))
     pos[3] = 300                                                        # behind the table: NaN
     x = randn(n, 2 * Hkv * hd + 2, seed=hd, dtype=dtype)
     k, v = x[:, :Hkv * hd].view(n, Hkv, hd), x[:, Hkv * hd:2 * Hkv * hd].view(n, Hkv, hd)
-    a, b = (ngg.KVPages(4, 32, Hkv, hd, "fp4") for _ in range(2))
+    a, b = (ngg.KVPages(23, 32, Hkv, hd, "fp4") for _ in range(2))
     slots = ints(7 + np.arange(n))
     a.write(k, v, slots, rope=rope, positions=pos)
     b.write(ngg.rotary(rope, pos, k), v, slots)
