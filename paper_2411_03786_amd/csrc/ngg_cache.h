@@ -40,8 +40,8 @@ constexpr int kGroup = 32, kRowPad = 16;                   // tokens of a workgr
 // A workgroup's tokens t0 .. t0 + m - 1 (none: false).  Groups begin where eights of positions do if all slots follow each other, so
 // that no chunk (below) lies in two of them: 16000 tokens of 8 heads from position 37, 16 bits, are written in 22 us, from groups
 // that begin at token 0 in 30.
-__device__ __forceinline__ bool group_tokens(const CacheArgs &a, int &t0, int &m) {
-  const int64_t begin = (int64_t)blockIdx.x * kGroup - (a.slots[0] & 7);
+__device__ __forceinline__ bool group_tokens(const CacheArgs &a, int group, int &t0, int &m) {
+  const int64_t begin = (int64_t)group * kGroup - (a.slots[0] & 7);
   t0 = (int)max(begin, (int64_t)0);
   m = (int)(min(begin + kGroup, (int64_t)a.n_tokens) - t0);
   return m > 0;
@@ -103,11 +103,11 @@ inline dim3 groups(const CacheArgs &a) { return dim3((unsigned)(((int64_t)a.n_to
 // Groups of 2^28 tokens at a time: a launch counts its threads in 32 bits
 constexpr int kLaunchTokens = 1 << 28;
 template <typename T, typename Launch>
-void in_parts(const CacheArgs &all, Launch launch) {
-  for (int64_t at = 0; at < all.n_tokens; at += kLaunchTokens) {
+void in_parts(const CacheArgs &all, Launch launch, int64_t most = kLaunchTokens) {
+  for (int64_t at = 0; at < all.n_tokens; at += most) {
     CacheArgs a = all;
     const int64_t left = all.n_tokens - at;
-    a.n_tokens = (int)(left < kLaunchTokens ? left : kLaunchTokens);
+    a.n_tokens = (int)(left < most ? left : most);
     a.slots += at;
     if (a.positions) a.positions += at;
     if (a.k) a.k = (const T *)a.k + at * a.k_token;

@@ -87,10 +87,11 @@ __global__ __launch_bounds__(256) void kv4_write_group_kernel(const CacheArgs a,
   __shared__ __align__(16) T rows[kGroup][ROW];            // (keys that turn)
   __shared__ __align__(16) uint8_t both[2][kGroup][64 + 4];  // values: dimensions c and c + 16 of a group; of every other head
   __shared__ uint8_t both_ex[2][kGroup][4];
-  const int tid = threadIdx.x, h0 = blockIdx.y * heads, h_end = min(h0 + heads, a.p.Hkv), hd = a.p.hd, ps = a.p.page_size, ng = hd / kGroup4;
+  const int tid = threadIdx.x, per_group = (a.p.Hkv + heads - 1) / heads, group = blockIdx.x / per_group;
+  const int in_group = blockIdx.x - group * per_group, h0 = in_group * heads, h_end = min(h0 + heads, a.p.Hkv), hd = a.p.hd, ps = a.p.page_size, ng = hd / kGroup4;
   int t0, m;
-  if (!group_tokens(a, t0, m)) return;
-  const bool values = blockIdx.z, turns = a.cos && !values;
+  if (!group_tokens(a, group, t0, m)) return;
+  const bool values = blockIdx.y, turns = a.cos && !values;
   const int per = hd / VE;
   const int64_t stride = values ? a.v_token : a.k_token;
   u32x4 part[PARTS], next[PARTS];
@@ -262,10 +263,11 @@ __device__ __forceinline__ void put_eight(T *dst, unsigned w, float scale, int v
 template <typename T>
 __global__ __launch_bounds__(256) void kv4_read_group_kernel(const CacheArgs a, int vec, int heads) {
   __shared__ __align__(16) uint8_t both[2][kGroup][64 + 8];  // of every other head
-  const int tid = threadIdx.x, h0 = blockIdx.y * heads, h_end = min(h0 + heads, a.p.Hkv), hd = a.p.hd, ps = a.p.page_size, ng = hd / kGroup4;
+  const int tid = threadIdx.x, per_group = (a.p.Hkv + heads - 1) / heads, group = blockIdx.x / per_group;
+  const int in_group = blockIdx.x - group * per_group, h0 = in_group * heads, h_end = min(h0 + heads, a.p.Hkv), hd = a.p.hd, ps = a.p.page_size, ng = hd / kGroup4;
   int t0, m;
-  if (!group_tokens(a, t0, m)) return;
-  const bool values = blockIdx.z;
+  if (!group_tokens(a, group, t0, m)) return;
+  const bool values = blockIdx.y;
   T *out = values ? (T *)a.v_out : (T *)a.k_out;
   if (!out) return;
   const int64_t stride = values ? a.v_token : a.k_token;
@@ -346,12 +348,18 @@ static dim3 row_blocks(const CacheArgs &a) { return dim3((unsigned)((a.n_tokens 
 // 15.6 and 16.5, 15.5, 15.7, rotated 24.1, 21.5, 24.7; 16384, 8: 33.5, 26.3, 23.7 and 26.2, 22.9, 23.1; 43008, 8: 76, 57, 49 and 58, 47, 44).
 static int heads_of_group(const CacheArgs &a) {
   const int64_t all = (int64_t)groups(a).x * a.p.Hkv * 2;
-  return all >= 8000 ? 4 : all >= 2048 ? 2 : 1;
+  const int most = all >= 8000 ? 4 : all >= 2048 ? 2 : 1;
+  if (most == 1 || a.p.Hkv % most == 0) return most;
+  // (even shares: workgroups go round the dies, and one that always gets the smaller share waits for the others)
+  return a.p.Hkv <= 4 ? a.p.Hkv : a.p.Hkv % 3 == 0 ? 3 : a.p.Hkv % 2 == 0 ? 2 : most;
 }
+// One group of tokens behind the other, with all heads next to each other: they lie in the same pages (1344 pages of 42 positions in all of
+// 32 layers are read in 56 us, head by head in 72).  A launch counts its threads in 32 bits.
 static dim3 head_groups(const CacheArgs &a) {
   const int n = heads_of_group(a);
-  return dim3(groups(a).x, (a.p.Hkv + n - 1) / n, 2);
+  return dim3(groups(a).x * ((a.p.Hkv + n - 1) / n), 2);
 }
+static int64_t launch_tokens(const CacheArgs &a) { return ((1 << 22) / a.p.Hkv - 1) * (int64_t)kGroup; }
 // Calls of few rows (tokens times heads) have 16 lanes for 32 dimensions, whose chain of loads is the shorter one.  Us a call in a graph, so
 // and by groups, of 8 heads of 128, rows:
 //                       512         2048        3072        4096        8192
@@ -367,7 +375,7 @@ static void write_type(const CacheArgs &all, hipStream_t s) {
   else
     in_parts<T>(all, [s](const CacheArgs &a) {
       hipLaunchKernelGGL((kv4_write_group_kernel<T>), head_groups(a), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k, a.v), heads_of_group(a));
-    });
+    }, launch_tokens(all));
 }
 template <typename T>
 static void read_type(const CacheArgs &all, hipStream_t s) {
@@ -375,7 +383,7 @@ static void read_type(const CacheArgs &all, hipStream_t s) {
   else
     in_parts<T>(all, [s](const CacheArgs &a) {
       hipLaunchKernelGGL((kv4_read_group_kernel<T>), head_groups(a), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k_out, a.v_out), heads_of_group(a));
-    });
+    }, launch_tokens(all));
 }
 void launch_kv4_write(int dtype, const CacheArgs &a, hipStream_t s) {
   if (dtype == NGG_F32) write_type<float>(a, s);

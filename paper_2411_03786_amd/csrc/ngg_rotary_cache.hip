@@ -268,7 +268,7 @@ __global__ __launch_bounds__(256) void kv_write_group_kernel(const CacheArgs a, 
   __shared__ uint8_t ex[kGroup];                           // their exponents
   const int tid = threadIdx.x, h = blockIdx.y, hd = a.p.hd, ps = a.p.page_size;
   int t0, m;
-  if (!group_tokens(a, t0, m)) return;
+  if (!group_tokens(a, blockIdx.x, t0, m)) return;
   const bool values = blockIdx.z, turns = a.cos && !values;
   const int per = hd / VE;
   const int64_t stride = values ? a.v_token : a.k_token;
@@ -427,7 +427,7 @@ __global__ __launch_bounds__(256) void kv_read_group_kernel(const CacheArgs a, i
   __shared__ __align__(16) T rows[kGroup][ROW];
   const int tid = threadIdx.x, h = blockIdx.y, hd = a.p.hd, ps = a.p.page_size;
   int t0, m;
-  if (!group_tokens(a, t0, m)) return;
+  if (!group_tokens(a, blockIdx.x, t0, m)) return;
   const bool values = blockIdx.z;
   T *out = values ? (T *)a.v_out : (T *)a.k_out;
   if (!out) return;
