@@ -1,14 +1,15 @@
 """Greedy decoding of several sequences at once whose drafts are verified as trees, on the framework's operators.
 
   python -m paper_2411_03786_amd.tree_verify [--batch 4] [--layers 4] [--heads 32] [--kv-heads 8] [--head-dim 128]
-         [--vocab 32000] [--prompt 512] [--new 64] [--k 6] [--w 8] [--cycle 40] [--cache bf16|fp8|f32]
+         [--vocab 32000] [--prompt 512] [--shared 0] [--new 64] [--k 6] [--w 8] [--cycle 40] [--cache bf16|fp8|fp4|f32]
 
 Every step takes up to k rows of w tokens that followed earlier occurrences of a sequence's last tokens (the paper's context
 N-grams, Section 4.2), merges the rows that begin alike into a tree behind the last token, and runs the trees of all sequences
 through the model in one pass: `rotary` on the queries, `KVPages.write` of keys (rotated on the way) and values, `tree_attention`
 over each sequence's pages, `token_logprobs` for the greedy token of every node and the log probabilities of its children.  The
-path that the greedy tokens follow is kept: its keys and values are read from where the tree left them and written behind the
-context.  Output tokens are those of plain greedy decoding (one token a step), which runs beside it for comparison, where no two
+path that the greedy tokens follow is kept: `KVPages.move` brings its keys and values from where the tree left them to behind the
+context, in all layers at once.  A `PageTable` gives the sequences their pages as they grow; prompts that begin alike can share the pages
+of their beginning (`fork`), of which each sequence gets its own copy (`reserve`, `KVPages.copy`) when it writes to one.  Output tokens are those of plain greedy decoding (one token a step), which runs beside it for comparison, where no two
 tokens are as likely but for the rounding of a 16-bit sum.  The projections are torch matrix products; weights and prompts are synthetic and seeded; one GPU.
 """
 from __future__ import annotations
@@ -77,10 +78,10 @@ class TreeDecoder:
                             down=weight(d_ffn, d)) for _ in range(layers)]
         per = -(-max_tokens // page)
         self.rope = ngg.Rope(head_dim, per * page)                                # whatever the pages hold
-        self.kv = [ngg.KVPages(batch * per, page, kv_heads, head_dim, cache) for _ in range(layers)]
-        # a sequence's pages lie scattered over the pool, as they do after some serving
-        self.pages = torch.randperm(batch * per, generator=torch.Generator().manual_seed(seed)).view(batch, per).int().cuda()
-        self.lens = torch.zeros(batch, dtype=torch.int32, device="cuda")          # cached positions
+        self.pool = ngg.KVPages(batch * per, page, kv_heads, head_dim, cache, layers=layers)
+        self.kv = [self.pool.layer(i) for i in range(layers)]
+        self.table = ngg.PageTable(batch, per, batch * per, page)
+        self.pages, self.lens = self.table.pages, self.table.lens                 # cached positions
         self.cached = [0] * batch                                                 # the same on the host
 
     @staticmethod
@@ -89,41 +90,59 @@ class TreeDecoder:
         return x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-6)
 
     def slots(self, places):
-        """Slots of positions [batch, n]; -1 stays."""
-        at = torch.gather(self.pages, 1, (places.clamp(min=0) // self.page).long()) * self.page + places.clamp(min=0) % self.page
+        """Slots of positions [batch, n] of the first sequences; -1 stays."""
+        at = torch.gather(self.pages[:len(places)], 1, (places.clamp(min=0) // self.page).long()) * self.page + places.clamp(min=0) % self.page
         return torch.where(places < 0, -1, at).int().flatten()
 
     def forward(self, tokens, depth, mask=None, tree_lens=None, logits=True):
-        """Logits [batch * tree, vocab] of the trees' tokens [batch, tree] behind the cached positions, or None without `logits`; their
-        keys and values are left at the positions behind those, in the trees' order."""
+        """Logits [batch * tree, vocab] of the trees' tokens [batch, tree] behind the cached positions of the first sequences, or None
+        without `logits`; their keys and values are left at the positions behind those, in the trees' order."""
         B, T = tokens.shape
         H, Hkv, hd = self.heads, self.kv_heads, self.hd
-        place = self.lens[:, None] + torch.arange(T, dtype=torch.int32, device="cuda")
+        lens = self.lens[:B]
+        place = lens[:, None] + torch.arange(T, dtype=torch.int32, device="cuda")
         if tree_lens is not None:
             place = torch.where(torch.arange(T, device="cuda") < tree_lens[:, None], place, -1)
-        longest = max(self.cached) + T
+        longest = max(self.cached[:B]) + T
         if longest > self.pages.shape[1] * self.page:
             raise ValueError(f"{longest} positions in pages for {self.pages.shape[1] * self.page}")
-        pages = self.pages[:, :-(-longest // self.page)]                # the call is planned for these
-        slots, pos = self.slots(place), (self.lens[:, None] + depth).int().flatten()
+        new = torch.zeros_like(self.lens)
+        new[:B] = T if tree_lens is None else tree_lens
+        shared = self.table.reserve(new)                                # (there are pages for all sequences at their longest)
+        self.pool.copy(shared.src, shared.dst, shared.positions)
+        pages = self.pages[:B, :-(-longest // self.page)]               # the call is planned for these
+        slots, pos = self.slots(place), (lens[:, None] + depth).int().flatten()
         x = self.embed[tokens.flatten().long()]
         for w, kv in zip(self.layers, self.kv):
             q, k, v = (self.norm(x).to(self.dtype) @ w["qkv"]).view(B * T, H + 2 * Hkv, hd).split((H, Hkv, Hkv), 1)
             ngg.rotary(self.rope, pos, q, out=q)
             kv.write(k, v, slots, rope=self.rope, positions=pos)
-            a = ngg.tree_attention(q.unflatten(0, (B, T)), kv, pages, self.lens, mask=mask, tree_lens=tree_lens)
+            a = ngg.tree_attention(q.unflatten(0, (B, T)), kv, pages, lens, mask=mask, tree_lens=tree_lens)
             x = x + a.reshape(B * T, H * hd) @ w["proj"]
             y = self.norm(x).to(self.dtype)
             x = x + (torch.nn.functional.silu(y @ w["gate"]) * (y @ w["up"])) @ w["down"]
         return self.norm(x).to(self.dtype) @ self.unembed if logits else None
 
     def prefill(self, prompts, piece=512):
-        """Caches all tokens of the prompts [batch, n] but the last."""
-        for at in range(0, prompts.shape[1] - 1, piece):
-            part = prompts[:, at:min(at + piece, prompts.shape[1] - 1)]
+        """Caches all tokens of the prompts [batch, n], of the first sequences, but the last."""
+        B, n = prompts.shape
+        for at in range(0, n - 1, piece):
+            part = prompts[:, at:min(at + piece, n - 1)]
             self.forward(part, torch.arange(part.shape[1], device="cuda"), logits=False)
-            self.lens += part.shape[1]
-            self.cached = [n + part.shape[1] for n in self.cached]
+            self.lens[:B] += part.shape[1]
+            self.cached[:B] = [c + part.shape[1] for c in self.cached[:B]]
+
+    def clear(self):
+        """Gives all pages back."""
+        self.table.release(torch.zeros_like(self.lens))
+        self.cached = [0] * self.batch
+
+    def share(self, tokens):
+        """Caches the tokens [n] that all prompts begin with once; the sequences, which hold nothing yet, share their pages."""
+        self.prefill(torch.nn.functional.pad(tokens, (0, 1))[None])
+        others = torch.arange(1, self.batch, dtype=torch.int32, device="cuda")
+        self.table.fork(torch.zeros_like(others), others)
+        self.cached = self.cached[:1] * self.batch
 
     def keep(self, paths):
         """Keeps of every sequence's tree the nodes of its path (root first, rising): they move behind the context."""
@@ -131,9 +150,8 @@ class TreeDecoder:
         src = torch.tensor([p + [-1] * (n - len(p)) for p in paths], dtype=torch.int32, device="cuda")
         there = src >= 0
         to = torch.where(there, self.lens[:, None] + torch.arange(n, dtype=torch.int32, device="cuda"), -1)
-        src, to = self.slots(torch.where(there, self.lens[:, None] + src, -1)), self.slots(to)
-        for kv in self.kv:
-            kv.write(*kv.read(src), to)
+        src, to = (self.slots(x).view(there.shape) for x in (torch.where(there, self.lens[:, None] + src, -1), to))
+        self.pool.move(src, to)
         self.lens += there.sum(1, dtype=torch.int32)
         self.cached = [c + len(p) for c, p in zip(self.cached, paths)]
 
@@ -173,12 +191,18 @@ class TreeDecoder:
         self.keep(paths)
         return out
 
-    def decode(self, prompts, n_new, draft):
-        """n_new greedy tokens behind each prompt (lists of equal length).  draft(sequence index, tokens) -> rows.  Returns the
-        sequences' new tokens, their log probabilities, and the steps taken."""
-        self.lens.zero_()
-        self.cached = [0] * self.batch
-        self.prefill(torch.tensor(prompts, dtype=torch.int32, device="cuda"))
+    def decode(self, prompts, n_new, draft, share=False):
+        """n_new greedy tokens behind each prompt (lists of equal length).  draft(sequence index, tokens) -> rows.  share: what the
+        prompts begin with is cached once.  Returns the sequences' new tokens, their log probabilities, and the steps taken."""
+        self.clear()
+        tokens = torch.tensor(prompts, dtype=torch.int32, device="cuda")
+        alike = 0
+        if share:
+            alike = next((i for i, t in enumerate(zip(*prompts)) if len(set(t)) > 1), len(prompts[0]))
+            alike = min(alike, len(prompts[0]) - 1)
+        if alike:
+            self.share(tokens[0, :alike])
+        self.prefill(tokens[:, alike:])
         seqs, logps, steps = [list(p) for p in prompts], [[] for _ in prompts], 0
         while min(map(len, logps)) < n_new:
             rows = [draft(b, s) if len(logps[b]) < n_new else [] for b, s in enumerate(seqs)]
@@ -192,22 +216,24 @@ class TreeDecoder:
 
 def main():
     ap = argparse.ArgumentParser()
-    for name, value in dict(batch=4, layers=4, heads=32, kv_heads=8, head_dim=128, vocab=32000, prompt=512, new=64, k=6, w=8, cycle=40, seed=0).items():
+    for name, value in dict(batch=4, layers=4, heads=32, kv_heads=8, head_dim=128, vocab=32000, prompt=512, new=64, k=6, w=8, cycle=40, shared=0, seed=0).items():
         ap.add_argument("--" + name.replace("_", "-"), type=int, default=value)
-    ap.add_argument("--cache", default="bf16", choices=("f32", "bf16", "fp8"))
+    ap.add_argument("--cache", default="bf16", choices=("f32", "bf16", "fp8", "fp4"))
     args = ap.parse_args()
     # a finished sequence still takes a token a step until the last one is done
     dec = TreeDecoder(args.batch, args.layers, args.heads, args.kv_heads, args.head_dim, args.vocab,
                       args.prompt + 2 * args.new + args.k * args.w + args.w + 2, args.cache, seed=args.seed, cycle=args.cycle)
     rng = np.random.default_rng(args.seed)
-    prompts = rng.integers(0, args.vocab, (args.batch, args.prompt)).tolist()
+    prompts = rng.integers(0, args.vocab, (args.batch, args.prompt))
+    prompts[:, :args.shared] = prompts[0, :args.shared]
+    prompts = prompts.tolist()
     runs = dict(plain=lambda b, s: [], trees=lambda b, s: context_rows(s, args.k, args.w))
     results = {}
     for name, draft in runs.items():
-        dec.decode(prompts, 4, draft)                                   # warm up
+        dec.decode(prompts, 4, draft, share=args.shared > 0)            # warm up
         torch.cuda.synchronize()
         t0 = time.perf_counter()
-        results[name] = tokens, logps, steps = dec.decode(prompts, args.new, draft)
+        results[name] = tokens, logps, steps = dec.decode(prompts, args.new, draft, share=args.shared > 0)
         torch.cuda.synchronize()
         dt = time.perf_counter() - t0
         print(f"{name}: {args.batch} sequences, {args.new} tokens each, {steps} steps, {dt * 1e3:.1f} ms with the prompts, "
