@@ -418,7 +418,8 @@ ngg_status ngg_kv_read(const ngg_kv_pages *pages, const int32_t *slots, int32_t 
  *
  * ngg_kv_move: of every list [n_lists][n] (lists src_list and dst_list apart) slot src[i] moves to slot dst[i], the keys and values of all
  * heads; all of a list's sources are read before the first is written, in whatever order they lie, and of equal destinations the last
- * counts.  The destinations of a list are in no other one.  An entry whose source or destination is outside the part is passed over.
+ * counts.  No destination of a list is in another one,
+ * as a source or a destination.  An entry whose source or destination is outside the part is passed over.
  * n <= NGG_TREE_MAX.  (After a verified tree: its accepted nodes, to behind the context.)
  * ngg_kv_copy: page src[i] to page dst[i]; of it the first positions[i] (rounded up to 32s; NULL: all).  No destination is a source, or there twice.
  * An entry whose source or destination is outside the part is passed over. */

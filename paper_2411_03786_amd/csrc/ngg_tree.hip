@@ -673,36 +673,39 @@ template <typename T, int HD, int ROWS, int KS>
 __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
   __shared__ int pre[NGG_TREE_MAX + 1];
   const int z = blockIdx.y, b = blockIdx.x / a.p.Hkv, hk = blockIdx.x % a.p.Hkv;
-  int first, last;                                         // the shares that hold its first and its last step
+  int first, last, most;                                   // the shares that hold its first and its last step, and could
   if (a.pieces) {
     first = blockIdx.x * a.pieces;
+    most = first + a.pieces - 1;                           // (the parts are on their way before the length is there)
     last = first + (seq_steps<KS>(a, b) - 1) / a.piece_steps;
   } else {
     step_totals<KS>(a, pre);
     const int per = share_steps<KS>(a, pre[a.B] * a.p.Hkv), steps = pre[b + 1] - pre[b], u0 = pre[b] * a.p.Hkv + hk * steps;
     first = u0 / per;
-    last = (u0 + steps - 1) / per;
+    most = last = (u0 + steps - 1) / per;
+    if (first == last) return;
   }
-  if (first == last) return;
   const int i = blockIdx.z * 256 + threadIdx.x;
   const int r = i / (HD / 4), dim = i % (HD / 4) * 4, rr = z * ROWS + r, t = rr / a.G;
   if (r >= ROWS || t >= a.T) return;
   // (the last part of its first share, the first of the others)
   float mm = -__builtin_inff(), ll = 0.0f;
   f32x4 o{0.f, 0.f, 0.f, 0.f};
-  for (int w = first; w <= last; w += 8) {                 // eight parts on their way at a time
+  int w = first;
+  do {                                                     // eight parts on their way at a time
     f32x2 ml[8];
     f32x4 v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int x = min(w + j, last);
+      const int x = min(w + j, most);
       const size_t at = (size_t)x * a.Z + z, part = (a.pieces ? at : at * 2 + (x == first ? 1 : 0)) * ROWS + r;
       ml[j] = *reinterpret_cast<const f32x2 *>(a.part_ml + part * 2);
       v[j] = *reinterpret_cast<const f32x4 *>(a.part_o + part * HD + dim);
     }
     float mn = mm;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) mn = fmaxf(mn, ml[j][0]);
+    for (int j = 0; j < 8; ++j)
+      if (w + j <= last) mn = fmaxf(mn, ml[j][0]);
     const float ref = mn == -__builtin_inff() ? 0.0f : mn, x = __builtin_amdgcn_exp2f(mm - ref);
     mm = mn;
     ll *= x;
@@ -716,8 +719,9 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[k] += v[j][k] * y;
     }
-  }
-  write_row4<T>(a, b, t, hk * a.G + rr % a.G, dim, o, mm, ll);
+    w += 8;
+  } while (w <= last);
+  if (first != last) write_row4<T>(a, b, t, hk * a.G + rr % a.G, dim, o, mm, ll);
 }
 
 // Rows of a tile, and with them the kernel: 16 and 32 rows are tree_stream_kernel's, 128 tree_block_kernel's (16-bit operands).  Every

@@ -32,21 +32,20 @@ __device__ __forceinline__ void bf16_terms(const float (&x)[8], Frag<bf16_t> (&t
 template <typename T, int HD> struct Query4 {
   static constexpr int DS = HD / 32, N = sizeof(T) == 2 ? 1 : 3;
   Frag<bf16_t> q[DS][N];
-  // row: null for a row that is not there
+  // (the row is read whether or not it is one of the sequence's, which its length says: that is on its way too)
   __device__ __forceinline__ void load(const T *row, int vec, int g4) {
 #pragma unroll
     for (int d = 0; d < DS; ++d) {
       const int at = g4 * (HD / 4) + d * 8;
       if constexpr (N == 1) {
-        if (!row) q[d][0] = zero_frag<bf16_t>();
-        else if (vec) q[d][0] = load_frag_row(row + at);
+        if (vec) q[d][0] = load_frag_row(row + at);
         else
 #pragma unroll
           for (int e = 0; e < 8; ++e) q[d][0].v[e] = row[at + e];
       } else {
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = row ? row[at + e] : 0.0f;
+        for (int e = 0; e < 8; ++e) x[e] = row[at + e];
         bf16_terms<N>(x, q[d]);
       }
     }
@@ -87,9 +86,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && QF == 1 ? 3 : 1) void tree4_
       const int r = z * ROWS + f * 16 + c;
       tok[f] = r / a.G;
       see[f] = mask_window(a, b, tok[f], 0);
-      const bool live = tok[f] < len.tree;
-      const T *q = (const T *)a.q + b * a.q_batch + (live ? tok[f] : 0) * a.q_token + (int64_t)(hk * a.G + r % a.G) * a.q_head;
-      Q[f].load(live ? q : nullptr, a.q_vec, g4);
+      const T *q = (const T *)a.q + b * a.q_batch + min(tok[f], a.T - 1) * a.q_token + (int64_t)(hk * a.G + r % a.G) * a.q_head;
+      Q[f].load(q, a.q_vec, g4);
     }
     const int t_last = min(len.tree, (z * ROWS + ROWS - 1) / a.G + 1) - 1;          // the tile's last token
     const int keys_seen = t_last * a.G + a.G > z * ROWS ? min(n_keys, len.ctx + t_last + 1) : 0;
@@ -104,7 +102,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && QF == 1 ? 3 : 1) void tree4_
     }
 
     int at_page = (w.s_begin * NW + wave) * 32 / ps, at_off = (w.s_begin * NW + wave) * 32 % ps, at_tile = w.s_begin * NW + wave;
-    int page = at_tile < t_end ? a.pages[b * a.pages_batch + at_page] : -1;
+    int page = at_page < a.max_pages ? a.pages[b * a.pages_batch + at_page] : -1;
     // asks for the tile at at_tile, and looks up the page of the wave's next one
     auto fetch = [&](Tile4<HD> &t) {
       const int pg = __builtin_amdgcn_readfirstlane(page);
@@ -143,7 +141,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && QF == 1 ? 3 : 1) void tree4_
       at_tile += NW;
       at_off += KS;
       while (at_off >= ps) { at_off -= ps; ++at_page; }
-      page = at_tile < t_end ? a.pages[b * a.pages_batch + at_page] : -1;
+      page = at_page < a.max_pages ? a.pages[b * a.pages_batch + at_page] : -1;
     };
     // FULL: every row sees every key of the tile
     auto compute = [&](auto all, Tile4<HD> &t, int tile) {

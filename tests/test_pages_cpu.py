@@ -74,6 +74,10 @@ def test_tables_are_checked_by_every_call(lib, over):
     assert lib.ngg_pages_release(t, None, None) == ngg.NGG_EINVAL
 
 
+def test_struct_size_matches_the_header():
+    assert C.sizeof(ngg.ngg_page_table) == 4 * 8 + 4 * 4
+
+
 def test_table_calls_refuse(lib):
     need = C.c_int64(0)
     assert lib.ngg_pages_reserve_workspace(table(), need) == ngg.NGG_OK and need.value >= 12 * 4
