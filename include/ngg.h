@@ -421,7 +421,7 @@ ngg_status ngg_kv_read(const ngg_kv_pages *pages, const int32_t *slots, int32_t 
  * counts.  No destination of a list is in another one,
  * as a source or a destination.  An entry whose source or destination is outside the part is passed over.
  * n <= NGG_TREE_MAX.  (After a verified tree: its accepted nodes, to behind the context.)
- * ngg_kv_copy: page src[i] to page dst[i]; of it the first positions[i] (rounded up to 32s; NULL: all).  No destination is a source, or there twice.
+ * ngg_kv_copy: page src[i] to page dst[i]; of it the first positions[i] (rounded up to 8s; NULL: all).  No destination is a source, or there twice.
  * An entry whose source or destination is outside the part is passed over. */
 ngg_status ngg_kv_move(const ngg_kv_pages *pages, int32_t layers, const int32_t *src, const int32_t *dst, int64_t src_list,
                        int64_t dst_list, int32_t n_lists, int32_t n, void *hip_stream);

@@ -45,105 +45,153 @@ template <> struct Unit<4> { typedef uint32_t T; };
 template <> struct Unit<8> { typedef u32x2 T; };
 template <> struct Unit<16> { typedef u32x4 T; };
 
-// What an entry of a list moves from and to, in bytes of keys, values and the exponents of either: the offset of a unit is the
-// position's plus the unit's own.
-struct Entry { int64_t from[4], to[4]; };
-constexpr int kInRegisters = 16;
-
-// Moves one unit of every entry: all are read before the first is written.  Up to 16 entries wait in registers, more in LDS.
-template <int BYTES>
-__device__ __forceinline__ void move_unit(uint8_t *mine, const Entry *list, int n, int kind, uint8_t *wait) {
-  typedef typename Unit<BYTES>::T U;
-  if (n <= kInRegisters) {
-    U x[kInRegisters];
-#pragma unroll
-    for (int i = 0; i < kInRegisters; ++i)
-      if (i < n) x[i] = *reinterpret_cast<const U *>(mine + list[i].from[kind]);
-#pragma unroll
-    for (int i = 0; i < kInRegisters; ++i)
-      if (i < n) *reinterpret_cast<U *>(mine + list[i].to[kind]) = x[i];
-    return;
+// Kinds of units: keys, values, and the exponents of either; the threads of a wave have one kind, units of all heads.
+template <int CACHE, int HD, int KIND> struct Kind {
+  typedef Units<CACHE, HD> U;
+  static constexpr int N = KIND == 0 ? U::KU : KIND == 1 ? U::VU : U::EU;                        // of a head
+  static constexpr int B = KIND == 0 ? U::KB : KIND == 1 ? U::VB : 1;                            // bytes
+  static constexpr int POS = KIND < 2 ? HD * U::value_bits / 8 : U::EU;                          // bytes of a position
+  static __device__ __forceinline__ size_t at(int pos, int u) {
+    if constexpr (KIND == 0) return U::k(pos, u);
+    else if constexpr (KIND == 1) return U::v(pos, u);
+    else if constexpr (KIND == 2) return U::ke(pos, u);
+    else return U::ve(pos, u);
   }
-  U *column = reinterpret_cast<U *>(wait) + threadIdx.x;   // (a thread's own)
-  for (int i = 0; i < n; ++i) column[i * blockDim.x] = *reinterpret_cast<const U *>(mine + list[i].from[kind]);
-  for (int i = 0; i < n; ++i) *reinterpret_cast<U *>(mine + list[i].to[kind]) = column[i * blockDim.x];
+};
+struct Move { int64_t from, to; bool ok; };                // byte offsets of an entry's places: a unit's are those and its own
+template <typename K>
+__device__ __forceinline__ Move entry(const MoveArgs &a, int layer, int b, int i) {
+  const int ps = a.p.page_size, positions = a.layer_pages * ps;
+  const int from = i < a.n ? a.src[b * a.src_list + i] : -1, to = i < a.n ? a.dst[b * a.dst_list + i] : -1;
+  Move m = {0, 0, from >= 0 && from < positions && to >= 0 && to < positions};
+  if (m.ok) {
+    m.from = (int64_t)(layer * a.layer_pages + from / ps) * a.p.Hkv * ps * K::POS + K::at(from % ps, 0);
+    m.to = (int64_t)(layer * a.layer_pages + to / ps) * a.p.Hkv * ps * K::POS + K::at(to % ps, 0);
+  }
+  return m;
+}
+__device__ __forceinline__ int64_t of_lane(int64_t x, int l) {
+  return (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32 | (unsigned)__builtin_amdgcn_readlane((int)x, l));
 }
 
-// One thread per unit of a (layer, list, head); a thread reads and writes bytes that no other one touches.  Bound by two chains of loads
-// and the scattered bytes of values: FIGURES.
-template <int CACHE, int HD>
+// Up to 16 entries, a lane's each; they wait in the registers of the threads that move their units, so that nothing waits for another wave.
+// Bound by two chains of loads and by the scattered bytes of values: the paths of 16 sequences in 32 layers, 20 MB of whole lines both
+// ways, take FIGURES us.
+constexpr int kInRegisters = 16;
+template <typename K>
+__device__ __forceinline__ void move_few(const MoveArgs &a, void *base, int layer, int b, int unit) {
+  typedef typename Unit<K::B>::T U;
+  const Move m = entry<K>(a, layer, b, threadIdx.x & 63);
+  const uint64_t all = __ballot(m.ok);
+  const int h = unit / K::N, u = unit - h * K::N;
+  if (h >= a.p.Hkv || all == 0) return;
+  uint8_t *mine = (uint8_t *)base + (int64_t)h * a.p.page_size * K::POS + K::at(0, u);
+  U x[kInRegisters];
+  uint64_t left = all;
+#pragma unroll
+  for (int i = 0; i < kInRegisters; ++i) {
+    if (left) x[i] = *reinterpret_cast<const U *>(mine + of_lane(m.from, __builtin_ctzll(left)));
+    left &= left - 1;                                      // (of none: none)
+  }
+  left = all;
+#pragma unroll
+  for (int i = 0; i < kInRegisters; ++i) {
+    if (left) *reinterpret_cast<U *>(mine + of_lane(m.to, __builtin_ctzll(left))) = x[i];
+    left &= left - 1;
+  }
+}
+// More entries wait in LDS, a column for each thread.
+template <typename K>
+__device__ __forceinline__ void move_many(const MoveArgs &a, void *base, int layer, int b, int unit, uint8_t *wait) {
+  typedef typename Unit<K::B>::T U;
+  const int h = unit / K::N, u = unit - h * K::N;
+  const bool mine_too = h < a.p.Hkv;
+  uint8_t *mine = (uint8_t *)base + (int64_t)(mine_too ? h : 0) * a.p.page_size * K::POS + K::at(0, mine_too ? u : 0);
+  U *column = reinterpret_cast<U *>(wait) + threadIdx.x;
+  const int lanes = blockDim.x;                            // (64 at most)
+#pragma unroll
+  for (int turn = 0; turn < 2; ++turn)
+    for (int i0 = 0; i0 < a.n; i0 += lanes) {
+      const Move m = entry<K>(a, layer, b, i0 + threadIdx.x);
+      for (uint64_t left = __ballot(m.ok); left; left &= left - 1) {
+        const int l = __builtin_ctzll(left);
+        const int64_t from = of_lane(m.from, l), to = of_lane(m.to, l);
+        if (!mine_too) continue;
+        if (turn == 0) column[(i0 + l) * lanes] = *reinterpret_cast<const U *>(mine + from);
+        else *reinterpret_cast<U *>(mine + to) = column[(i0 + l) * lanes];
+      }
+    }
+}
+
+// Blocks of a row of the grid: of keys, then values, then exponents
+template <int CACHE, int HD> struct MoveBlocks {
+  typedef Units<CACHE, HD> U;
+  static __host__ __device__ int of(int units, int Hkv, int threads) { return (int)(((int64_t)units * Hkv + threads - 1) / threads); }
+};
+template <int CACHE, int HD, bool FEW>
 __global__ __launch_bounds__(256) void kv_move_kernel(const MoveArgs a, int lists_first) {
   typedef Units<CACHE, HD> U;
-  constexpr int ALL = U::KU + U::VU + 2 * U::EU, BYTES = HD * U::value_bits / 8;   // BYTES: of a position's keys (or values) of a head
+  typedef MoveBlocks<CACHE, HD> N;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  __shared__ int count;
-  Entry *list = reinterpret_cast<Entry *>(smem);
-  const int layer = blockIdx.z, b = lists_first + blockIdx.y, ps = a.p.page_size, Hkv = a.p.Hkv;
-  const int positions = a.layer_pages * ps;                // of a layer
-  if (threadIdx.x < 64) {                                  // the entries that there are, in their order (the first wave; blocks of less have one)
-    int n = 0;
-    for (int i0 = 0; i0 < a.n; i0 += min(blockDim.x, 64u)) {
-      const int i = i0 + threadIdx.x;
-      int from = -1, to = -1;
-      if (i < a.n) {
-        from = a.src[b * a.src_list + i];
-        to = a.dst[b * a.dst_list + i];
-      }
-      const bool ok = from >= 0 && from < positions && to >= 0 && to < positions;
-      const uint64_t all = __ballot(ok);
-      if (ok) {
-        Entry &e = list[n + __builtin_popcountll(all & ((1ull << threadIdx.x) - 1))];
-        const int64_t f = (int64_t)(layer * a.layer_pages + from / ps) * Hkv * ps, t = (int64_t)(layer * a.layer_pages + to / ps) * Hkv * ps;
-        const int fp = from % ps, tp = to % ps;
-        e.from[0] = f * BYTES + U::k(fp, 0); e.from[1] = f * BYTES + U::v(fp, 0); e.from[2] = f * U::EU + U::ke(fp, 0); e.from[3] = f * U::EU + U::ve(fp, 0);
-        e.to[0] = t * BYTES + U::k(tp, 0); e.to[1] = t * BYTES + U::v(tp, 0); e.to[2] = t * U::EU + U::ke(tp, 0); e.to[3] = t * U::EU + U::ve(tp, 0);
-      }
-      n += __builtin_popcountll(all);
-    }
-    if (threadIdx.x == 0) count = n;
+  const int layer = blockIdx.z, b = lists_first + blockIdx.y, threads = blockDim.x, Hkv = a.p.Hkv;
+  int block = blockIdx.x;
+  const int nk = N::of(U::KU, Hkv, threads), nv = N::of(U::VU, Hkv, threads), ne = N::of(U::EU, Hkv, threads);
+  auto move = [&](auto kind, void *base) {
+    const int unit = block * threads + threadIdx.x;
+    if constexpr (FEW) move_few<decltype(kind)>(a, base, layer, b, unit);
+    else move_many<decltype(kind)>(a, base, layer, b, unit, smem);
+  };
+  if (block < nk) return move(Kind<CACHE, HD, 0>{}, a.p.k);
+  block -= nk;
+  if (block < nv) return move(Kind<CACHE, HD, 1>{}, a.p.v);
+  if constexpr (U::EU > 0) {
+    block -= nv;
+    if (block < ne) return move(Kind<CACHE, HD, 2>{}, a.p.k_exp);
+    block -= ne;
+    move(Kind<CACHE, HD, 3>{}, a.p.v_exp);
   }
-  __syncthreads();
-  const int n = count, unit = blockIdx.x * blockDim.x + threadIdx.x;
-  if (unit >= Hkv * ALL || n == 0) return;
-  uint8_t *wait = smem + a.n * sizeof(Entry);
-  const int64_t head = (int64_t)(unit / ALL) * ps;
-  const int u = unit % ALL, v = u - U::KU, ke = v - U::VU, ve = ke - U::EU;
-  if (u < U::KU) move_unit<U::KB>((uint8_t *)a.p.k + head * BYTES + U::k(0, u), list, n, 0, wait);
-  else if (v < U::VU) move_unit<U::VB>((uint8_t *)a.p.v + head * BYTES + U::v(0, v), list, n, 1, wait);
-  else if (ke < U::EU) move_unit<1>(a.p.k_exp + head * U::EU + U::ke(0, ke), list, n, 2, wait);
-  else move_unit<1>(a.p.v_exp + head * U::EU + U::ve(0, ve), list, n, 3, wait);
 }
 
-// Copies pages, of each the tiles of 32 positions that hold its first positions[i] (all without): one workgroup per (layer, page, head).
-__global__ __launch_bounds__(256) void kv_copy_kernel(const MoveArgs a, int first, int tile_bytes, int exp_bytes) {
+// Copies pages, of each the eights of positions that hold its first positions[i] (all without): one workgroup per (layer, page, head).
+// An eight is a quarter of every 16 rows of a tile of keys and of every 64 lanes of one of values, 16 bytes each (4 bits, heads of 32: 8).
+// HBM bound: FIGURES.
+__global__ __launch_bounds__(256) void kv_copy_kernel(const MoveArgs a, int first, int tile_bytes, int exp_bytes, int half) {
   const int layer = blockIdx.z, i = first + blockIdx.y, h = blockIdx.x, ps = a.p.page_size;
   const int from = a.src[i], to = a.dst[i];
   if (from < 0 || from >= a.layer_pages || to < 0 || to >= a.layer_pages) return;
-  const int n = a.positions ? min(max(a.positions[i], 0), ps) : ps, tiles = (n + 31) / 32;
+  const int n = a.positions ? min(max(a.positions[i], 0), ps) : ps, eights = (n + 7) / 8, tiles = (n + 31) / 32;
   const int64_t tile0 = ((int64_t)(layer * a.layer_pages + from) * a.p.Hkv + h) * (ps / 32), tile1 = ((int64_t)(layer * a.layer_pages + to) * a.p.Hkv + h) * (ps / 32);
-  auto copy = [&](void *base, int bytes) {
-    const u32x4 *s = reinterpret_cast<const u32x4 *>((const uint8_t *)base + tile0 * bytes);
-    u32x4 *d = reinterpret_cast<u32x4 *>((uint8_t *)base + tile1 * bytes);
-    for (int j = threadIdx.x; j < tiles * bytes / 16; j += 256) d[j] = s[j];
+  auto copy = [&](void *base, int bytes, auto part, auto eight) {
+    typedef decltype(part) P;
+    const P *s = reinterpret_cast<const P *>((const uint8_t *)base + tile0 * bytes);
+    P *d = reinterpret_cast<P *>((uint8_t *)base + tile1 * bytes);
+    const int per = bytes / (int)sizeof(P);
+    for (int j = threadIdx.x; j < tiles * per; j += 256)
+      if (j / per * 4 + eight(j % per) < eights) d[j] = s[j];
   };
-  copy(a.p.k, tile_bytes);
-  copy(a.p.v, tile_bytes);
+  copy(a.p.k, tile_bytes, u32x4{}, [half](int j) { return (j << half) % 16 / 4; });
+  copy(a.p.v, tile_bytes, u32x4{}, [half](int j) { return (j << half) / 16 % 4; });
   if (exp_bytes) {
-    copy(a.p.k_exp, exp_bytes);
-    copy(a.p.v_exp, exp_bytes);
+    const int groups = exp_bytes / 32;                     // of a position
+    copy(a.p.k_exp, exp_bytes, u32x2{}, [](int j) { return j % 4; });
+    copy(a.p.v_exp, exp_bytes, u32x2{}, [groups](int j) { return j / groups; });
   }
 }
 
 template <int CACHE, int HD>
 static void launch_move(const MoveArgs &a, hipStream_t s) {
   typedef Units<CACHE, HD> U;
-  const int units = a.p.Hkv * (U::KU + U::VU + 2 * U::EU);
+  typedef MoveBlocks<CACHE, HD> N;
   // what waits in LDS: as many threads as 64 KB have room for
-  const int list = a.n * (int)sizeof(Entry), threads = a.n <= kInRegisters ? 256 : a.n <= 64 ? 64 : a.n <= 128 ? 32 : a.n <= 256 ? 16 : a.n <= 512 ? 8 : 4;
-  const size_t lds = list + (a.n <= kInRegisters ? 0 : (size_t)threads * a.n * 16);
-  allow_lds(&kv_move_kernel<CACHE, HD>, lds);
-  for (int at = 0; at < a.lists; at += 65535)
-    hipLaunchKernelGGL((kv_move_kernel<CACHE, HD>), dim3((units + threads - 1) / threads, std::min(a.lists - at, 65535), a.layers), dim3(threads), lds, s, a, at);
+  const bool few = a.n <= kInRegisters;
+  const int threads = few ? 256 : a.n <= 64 ? 64 : a.n <= 128 ? 32 : a.n <= 256 ? 16 : a.n <= 512 ? 8 : 4;
+  const size_t lds = few ? 0 : (size_t)threads * a.n * 16;
+  const int x = N::of(U::KU, a.p.Hkv, threads) + N::of(U::VU, a.p.Hkv, threads) + 2 * N::of(U::EU, a.p.Hkv, threads);
+  for (int at = 0; at < a.lists; at += 65535) {
+    const dim3 grid(x, std::min(a.lists - at, 65535), a.layers);
+    if (few) hipLaunchKernelGGL((kv_move_kernel<CACHE, HD, true>), grid, dim3(threads), 0, s, a, at);
+    else hipLaunchKernelGGL((kv_move_kernel<CACHE, HD, false>), grid, dim3(threads), lds, s, a, at);
+  }
 }
 template <int CACHE>
 static void move_head(const MoveArgs &a, hipStream_t s) {
@@ -161,7 +209,8 @@ void launch_kv_copy(int cache, const MoveArgs &a, hipStream_t s) {
   const int bits = cache == NGG_F32 ? 32 : cache == NGG_BF16 ? 16 : cache == NGG_FP8 ? 8 : 4;
   const int exps = cache == NGG_FP8 ? 32 : cache == NGG_FP4 ? a.p.hd : 0;
   for (int at = 0; at < a.n; at += 65535)
-    hipLaunchKernelGGL(kv_copy_kernel, dim3(a.p.Hkv, std::min(a.n - at, 65535), a.layers), dim3(256), 0, s, a, at, 4 * a.p.hd * bits, exps);
+    hipLaunchKernelGGL(kv_copy_kernel, dim3(a.p.Hkv, std::min(a.n - at, 65535), a.layers), dim3(256), 0, s, a, at, 4 * a.p.hd * bits, exps,
+                       cache == NGG_FP4 && a.p.hd == 32 ? 1 : 0);
 }
 
 // ---- page lists -------------------------------------------------------------------------------------------------------
