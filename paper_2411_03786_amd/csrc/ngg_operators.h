@@ -209,7 +209,7 @@ struct TreeArgs {
   float *part_o, *part_ml;    // workspace (tree_plan)
   int ranges, Z;              // workgroups along the list of key steps, row tiles
   int whole;                  // a workgroup for every (sequence, head) instead: no parts, no merge
-  int pieces, piece_steps;    // 0, or so many workgroups for every (sequence, head), with so many steps each: parts, but no common list
+  int pieces, piece_steps;    // (4 bits) 0, or so many workgroups for every (sequence, head), with so many steps each: parts, but no common list
 };
 struct TreePlan { int rows, ranges, Z, pieces, piece_steps; bool whole, stream; size_t o_bytes, ml_bytes; };
 TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, int64_t max_positions);

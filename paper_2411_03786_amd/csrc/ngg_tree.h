@@ -98,10 +98,20 @@ __device__ __forceinline__ int share_steps(const TreeArgs &a, int total) {
   return max((int)((unsigned)(total + a.ranges - 1) / (unsigned)a.ranges), KS == 128 && total < 256 ? 1 : 256 / KS);
 }
 
+// Waves of tree4_stream_kernel on a SIMD, by its registers: a launch of shares is of as many workgroups as the chip holds
+// (32 single tokens of 8 key heads of 128 over up to 32000 positions with 2, 3 and 4 to a compute unit 123, 113 and 133 us; of 3 of 64 over
+// 16000 43, 40 and 38).
+constexpr int stream4_waves(bool wide, int hd, int row_tiles) {
+  return row_tiles == 2 ? (hd == 32 && !wide ? 3 : hd == 128 && wide ? 1 : 2) : wide ? (hd == 32 ? 4 : hd == 64 ? 3 : 2) : hd == 128 ? 3 : 4;
+}
+
+// How a launch parts its lists: into shares of all (or whole, a.whole); the same, its workgroups looking at 64 sequences at once for theirs
+// (at the price of some registers); into a.pieces of each.
+enum class Parts { kShares, kSharesWide, kPieces };
+
 // A workgroup's place and share of the list, one (sequence, head) after the other.  Whole numbers of 32 bits (the host sees to that):
 // what runs once costs a launch its instruction fetches.
-// PIECES: the call may be one of a.pieces.
-template <int KS, bool PIECES = false>
+template <int KS, Parts PARTS = Parts::kShares>
 struct Work {
   const TreeArgs &a;
   int *pre;
@@ -121,7 +131,7 @@ struct Work {
       z = slot - range * a.Z;
       if (dealt) range = range * 8 + blockIdx.x % 8;
     }
-    if (a.whole || (PIECES && a.pieces)) {                 // a (sequence, head) for each, or a piece of one
+    if (PARTS == Parts::kPieces || a.whole) {              // a (sequence, head) for each, or a piece of one
       u = range;
       u_end = range + 1;
       return;
@@ -135,6 +145,16 @@ struct Work {
   __device__ __forceinline__ int before(int i) const { return __builtin_amdgcn_readfirstlane(pre[i]); }
   __device__ __forceinline__ bool next() {
     if (u >= u_end) return false;
+    if constexpr (PARTS == Parts::kPieces) {
+      const int list = u / a.pieces;
+      b = list / a.p.Hkv;
+      hk = list - b * a.p.Hkv;
+      steps = seq_steps<KS>(a, b);
+      s_begin = (u - list * a.pieces) * a.piece_steps;
+      s_end = steps - s_begin > a.piece_steps ? s_begin + a.piece_steps : steps;
+      ++u;
+      return s_begin < steps;
+    }
     if (a.whole) {
       b = u / a.p.Hkv;
       hk = u - b * a.p.Hkv;
@@ -143,19 +163,9 @@ struct Work {
       ++u;
       return true;
     }
-    if (PIECES && a.pieces) {
-      const int list = u / a.pieces;
-      b = list / a.p.Hkv;
-      hk = list - b * a.p.Hkv;
-      steps = seq_steps<KS>(a, b);
-      s_begin = (u - list * a.pieces) * a.piece_steps;
-      s_end = min(steps, s_begin + a.piece_steps);
-      ++u;
-      return s_begin < steps;
-    }
-    if constexpr (!PIECES) {
+    if constexpr (PARTS == Parts::kShares) {
       while (before(b + 1) * a.p.Hkv <= u) ++b;
-    } else while (true) {                                  // 64 sequences are looked at at once (at the price of four registers)
+    } else while (true) {
       const int i = b + 1 + (int)(threadIdx.x & 63), n = (int)__builtin_popcountll(__ballot(i <= a.B && pre[min(i, a.B)] * a.p.Hkv <= u));
       b += n;
       if (n < 64) break;
@@ -171,7 +181,7 @@ struct Work {
   }
   __device__ __forceinline__ bool is_whole() const { return s_begin == 0 && s_end == steps; }
   // where a part goes: one that begins inside a (sequence, head) is the first of its share, one that ends inside it the last
-  __device__ __forceinline__ size_t part() const { return PIECES && a.pieces ? (size_t)range * a.Z + z : ((size_t)range * a.Z + z) * 2 + (s_begin == 0 ? 1 : 0); }
+  __device__ __forceinline__ size_t part() const { return PARTS == Parts::kPieces ? (size_t)range * a.Z + z : ((size_t)range * a.Z + z) * 2 + (s_begin == 0 ? 1 : 0); }
 };
 
 // Two words of a token's row of the mask, from the one that holds tree position at (or the first): enough for the 64 positions from

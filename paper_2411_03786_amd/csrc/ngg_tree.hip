@@ -786,14 +786,18 @@ TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, i
   // instead of 372; below, a list that is read again soon is better kept (1900 positions 46.9, non-temporal 49.7).
   const int64_t bytes = cache == NGG_FP4 ? positions * (hd + hd / kGroup4 * 2) : 2 * positions * hd * (cache == NGG_F32 ? 4 : cache == NGG_BF16 ? 2 : 1);
   p.stream = p.rows == 16 && p.Z == 1 && bytes > (int64_t)400 << 20;
-  p.pieces = p.piece_steps = 0;
+  p.pieces = cache == NGG_FP4 && p.whole;                  // (whole lists are pieces, too)
+  p.piece_steps = p.pieces ? INT32_MAX : 0;
   const int64_t lists = (int64_t)B * Hkv;
+  const int64_t held = cache == NGG_FP4 && p.rows <= 32 ? 256 * stream4_waves(dtype == NGG_F32, hd, p.rows / 16) : 512;
   // Over 4 bits few lists go in pieces: no workgroup has to look for its share or to work on two lists (us, shares and pieces: 32 lists of
   // 2047 positions, 51 rows 24.4, 19.3; 27 of up to 5001, 28 rows, fp32 21.8, 17.9; 8 of 60000, 4 rows 38.9, 30.0; with two pieces a
   // list, 256 of up to 8000, 16 rows 47.6, 61.5)
   if (cache == NGG_FP4 && p.rows <= 32 && !p.whole) {
-    const int64_t least = lists * steps < 256 ? 1 : 2;     // steps of a piece
-    const int64_t n = std::min<int64_t>((steps + least - 1) / least, 512 / (lists * p.Z));
+    const int64_t least = lists * steps < 256 ? 1 : 2, most = (steps + least - 1) / least;       // steps of a piece, pieces of a list
+    int64_t n = std::min<int64_t>(most, 512 / (lists * p.Z));
+    // (long ones by what the chip holds: 96 lists of 16000 positions, heads of 64, by 512 and 768 workgroups 39.9, 33.8; 8 of 60000 30.0, 35.6)
+    if (n > 0 && steps >= 16 * n) n = std::min<int64_t>(most, held / (lists * p.Z));
     if (n >= 4 || n * least >= steps) {
       p.piece_steps = (int)((steps + n - 1) / n);
       p.pieces = (int)((steps + p.piece_steps - 1) / p.piece_steps);
@@ -804,9 +808,7 @@ TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, i
       return p;
     }
   }
-  // (768: three workgroups to a compute unit, as many as tree4_stream_kernel's registers allow; with 512 32 single tokens over up to 32000
-  // positions take 123 us instead of 113)
-  const int64_t want = ((cache == NGG_FP4 && p.rows == 16 && dtype != NGG_F32 ? 768 : 512) + p.Z - 1) / p.Z, r = p.whole ? (int64_t)B * Hkv : std::max<int64_t>(1, std::min(want, steps * B * Hkv));
+  const int64_t want = (held + p.Z - 1) / p.Z, r = p.whole ? (int64_t)B * Hkv : std::max<int64_t>(1, std::min(want, steps * B * Hkv));
   p.ranges = (int)(p.whole || r < 8 ? r : r < want ? (r + 7) / 8 * 8 : r / 8 * 8);   // eights: one for each die; up, if a step each is to be had
   const size_t rows = p.whole ? 0 : (size_t)p.ranges * p.Z * 2 * p.rows;
   p.o_bytes = rows * hd * 4;

@@ -62,8 +62,8 @@ template <int HD> struct Tile4 {
 
 // One workgroup: one row tile (16 QF rows) over its share of the list, as tree_stream_kernel: the waves take the tiles of 32 keys in
 // turn and are joined through LDS.  Two more tiles are on their way while one is computed.
-template <typename T, int HD, int QF, bool NT>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && QF == 1 ? 3 : 1) void tree4_stream_kernel(const TreeArgs a) {
+template <typename T, int HD, int QF, bool NT, Parts PARTS>
+__global__ __launch_bounds__(256, stream4_waves(sizeof(T) == 4, HD, QF)) void tree4_stream_kernel(const TreeArgs a) {
   constexpr int NW = 4, NG = HD / 32, DF = HD / 16, ROWS = 16 * QF, KS = 32 * NW, TERMS = sizeof(T) == 2 ? 2 : 3;
   typedef Query4<T, HD> Query;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && QF == 1 ? 3 : 1) void tree4_
   int *pre = reinterpret_cast<int *>(lml + NW * QF * 32);  // [B + 1]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, g4 = lane >> 4, Hkv = a.p.Hkv, ps = a.p.page_size;
-  Work<KS, true> w(a, pre);
+  Work<KS, PARTS> w(a, pre);
   while (w.next()) {
     const int b = w.b, hk = w.hk, z = w.z;
     const SeqLens len = seq_lens(a, b);
@@ -284,17 +284,19 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && QF == 1 ? 3 : 1) void tree4_
   }
 }
 
-template <typename T, int HD, int QF, bool NT>
+template <typename T, int HD, int QF, bool NT, Parts PARTS>
 static void launch_stream(const TreeArgs &a, hipStream_t s) {
   constexpr size_t lds = (size_t)4 * QF * (HD / 16 * 256 + 32) * 4;
-  allow_lds(&tree4_stream_kernel<T, HD, QF, NT>, lds + (a.B + 1) * 4);
-  hipLaunchKernelGGL((tree4_stream_kernel<T, HD, QF, NT>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
+  allow_lds(&tree4_stream_kernel<T, HD, QF, NT, PARTS>, lds + (a.B + 1) * 4);
+  hipLaunchKernelGGL((tree4_stream_kernel<T, HD, QF, NT, PARTS>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
 }
 template <typename T, int HD>
 static void by_rows(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
-  if (p.rows == 16 && p.stream) launch_stream<T, HD, 1, true>(a, s);
-  else if (p.rows == 16) launch_stream<T, HD, 1, false>(a, s);
-  else if (p.rows == 32) launch_stream<T, HD, 2, false>(a, s);
+  if (p.rows == 16 && a.pieces) launch_stream<T, HD, 1, false, Parts::kPieces>(a, s);
+  else if (p.rows == 16 && p.stream) launch_stream<T, HD, 1, true, Parts::kSharesWide>(a, s);
+  else if (p.rows == 16) launch_stream<T, HD, 1, false, Parts::kSharesWide>(a, s);
+  else if (a.pieces) launch_stream<T, HD, 2, false, Parts::kPieces>(a, s);
+  else launch_stream<T, HD, 2, false, Parts::kSharesWide>(a, s);
 }
 template <typename T>
 static void by_head(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
