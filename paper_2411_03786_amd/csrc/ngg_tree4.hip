@@ -292,7 +292,8 @@ static void launch_stream(const TreeArgs &a, hipStream_t s) {
 }
 template <typename T, int HD>
 static void by_rows(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
-  if (p.rows == 16 && a.pieces) launch_stream<T, HD, 1, false, Parts::kPieces>(a, s);
+  if (p.rows == 16 && a.pieces && p.stream) launch_stream<T, HD, 1, true, Parts::kPieces>(a, s);
+  else if (p.rows == 16 && a.pieces) launch_stream<T, HD, 1, false, Parts::kPieces>(a, s);
   else if (p.rows == 16 && p.stream) launch_stream<T, HD, 1, true, Parts::kSharesWide>(a, s);
   else if (p.rows == 16) launch_stream<T, HD, 1, false, Parts::kSharesWide>(a, s);
   else if (a.pieces) launch_stream<T, HD, 2, false, Parts::kPieces>(a, s);
