@@ -444,7 +444,7 @@ ngg_status ngg_kv_copy(const ngg_kv_pages *pages, int32_t layers, const int32_t 
  * positions become free, or others' alone; a negative keep[s] leaves the sequence as it is. */
 typedef struct {
   int32_t *pages;                                 /* [n_seqs][max_pages] */
-  int64_t pages_seq;
+  int64_t pages_seq;                              /* max_pages or more (or any, of one sequence) */
   int32_t *lens, *refs;                           /* [n_seqs], [n_pages] */
   int32_t n_seqs, max_pages, n_pages, page_size;  /* n_seqs 1 .. NGG_TREE_MAX; max_pages * page_size <= 2^30; the pool's, of a layer */
 } ngg_page_table;

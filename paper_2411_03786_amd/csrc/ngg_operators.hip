@@ -109,6 +109,8 @@ ngg_status check_table(const char *what, const ngg_page_table *t) {
   if (t->page_size < 32 || t->page_size % 32) return fail_global(NGG_EINVAL, "%s: page_size %d must be a multiple of 32", what, t->page_size);
   if (t->max_pages < 1 || (int64_t)t->max_pages * t->page_size > (1 << 30))
     return fail_global(NGG_EINVAL, "%s: %d pages of %d positions per sequence", what, t->max_pages, t->page_size);
+  if (t->n_seqs > 1 && t->pages_seq < t->max_pages)
+    return fail_global(NGG_EINVAL, "%s: rows of %d pages that lie %lld apart", what, t->max_pages, (long long)t->pages_seq);
   if (t->n_pages < 1 || (int64_t)t->n_pages * t->page_size > INT32_MAX)
     return fail_global(NGG_EINVAL, "%s: %d pages of %d positions", what, t->n_pages, t->page_size);
   return NGG_OK;

@@ -134,6 +134,23 @@ def test_copies(cache, layers, Hkv, hd, page):
             p.kv.copy(*args)
 
 
+def test_more_entries_than_a_launch_has_rows():
+    p = Pool("fp4", 2, 6, 32, 1, 32)
+    n = 65535 + 3
+    src, dst = np.full(n, -1), np.full(n, -1)
+    for i, (a, b) in {0: (3, 40), 65534: (50, 3), 65535: (7, 60), n - 1: (100, 9)}.items():
+        src[i], dst[i] = a, b
+    p.kv.move(ints(src[:, None]), ints(dst[:, None]))
+    p.move(src[src >= 0][:, None], dst[src >= 0][:, None])
+    p.check()
+    src[src >= 0], dst[dst >= 0] = [0, 0, 1, 2], [3, 4, 5, -1]
+    p.kv.copy(ints(src), ints(dst))
+    for x in (p.k, p.v):
+        for a, b in ((0, 3), (0, 4), (1, 5)):
+            x[:, 32 * b:32 * b + 32] = x[:, 32 * a:32 * a + 32]
+    p.check()
+
+
 def test_layers_of_a_pool_are_pools():
     kv = ngg.KVPages(3, 32, 2, 64, "fp8", layers=4)
     x = randn(5, 2, 64, dtype="bf16")
@@ -271,6 +288,22 @@ def test_page_lists_of_a_life(n_seqs, max_pages, n_pages, page, seed):
     assert went
     table.release(ints(np.zeros(n_seqs)))
     assert not table.refs.any() and (table.pages == -1).all() and not table.lens.any()
+
+
+def test_more_pages_than_a_workgroup_keeps():
+    """Thousands of pages in one call, from between others that are taken."""
+    n_seqs, max_pages, n_pages, page = 17, 300, 9000, 32
+    table, lists = ngg.PageTable(n_seqs, max_pages, n_pages, page), Lists(n_seqs, max_pages, n_pages, page)
+    for new in ([page * (i + 1) for i in range(n_seqs)], [page * 220 - 3 * i for i in range(n_seqs)], [1] * n_seqs):
+        r, want = table.reserve(ints(new)), lists.reserve(new)
+        assert [t.tolist() for t in r] == [list(w) for w in want] and want[3] == [0]
+        keep = [page * (i + 1) if i % 2 else 0 for i in range(n_seqs)]
+        table.lens += ints(new)
+        lists.lens = [a + b for a, b in zip(lists.lens, new)]
+        if new[0] == page:
+            table.release(ints(keep))
+            lists.release(keep)
+        lists.check(table)
 
 
 def test_who_keeps_a_shared_page():

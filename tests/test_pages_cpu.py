@@ -66,7 +66,7 @@ def test_moves_and_copies_refuse(lib):
 
 
 @pytest.mark.parametrize("over", [dict(pages=None), dict(lens=None), dict(refs=None), dict(n_seqs=0), dict(n_seqs=1025), dict(max_pages=0),
-                                  dict(max_pages=1 << 25), dict(n_pages=0), dict(n_pages=1 << 26), dict(page_size=0), dict(page_size=48)])
+                                  dict(max_pages=1 << 25), dict(pages_seq=4), dict(pages_seq=0), dict(n_pages=0), dict(n_pages=1 << 26), dict(page_size=0), dict(page_size=48)])
 def test_tables_are_checked_by_every_call(lib, over):
     t = table(**over)
     assert lib.ngg_pages_fork(t, 16, 16, 1, None) == ngg.NGG_EINVAL
