@@ -353,8 +353,8 @@ static int heads_of_group(const CacheArgs &a) {
   // (even shares: workgroups go round the dies, and one that always gets the smaller share waits for the others)
   return a.p.Hkv <= 4 ? a.p.Hkv : a.p.Hkv % 3 == 0 ? 3 : a.p.Hkv % 2 == 0 ? 2 : most;
 }
-// One group of tokens behind the other, with all heads next to each other: they lie in the same pages (1344 pages of 42 positions in all of
-// 32 layers are read in 56 us, head by head in 72).  A launch counts its threads in 32 bits.
+// One group of tokens behind the other, with all heads next to each other: they lie in the same pages (42 positions of each of 1024 pages
+// are read in 56 us, head by head in 72).  A launch counts its threads in 32 bits.
 static dim3 head_groups(const CacheArgs &a) {
   const int n = heads_of_group(a);
   return dim3(groups(a).x * ((a.p.Hkv + n - 1) / n), 2);

@@ -154,7 +154,8 @@ __global__ __launch_bounds__(256) void kv_move_kernel(const MoveArgs a, int list
 
 // Copies pages, of each the eights of positions that hold its first positions[i] (all without): one workgroup per (layer, page, head).
 // An eight is a quarter of every 16 rows of a tile of keys and of every 64 lanes of one of values, 16 bytes each (4 bits, heads of 32: 8).
-// HBM bound: 32 pages of 42 positions in 32 layers of 8 heads of 128, 4 bits, 53 MB each way, 25 us (4.2 TB/s), 18 in a graph.
+// Bound by memory's writes: the last pages of 8 sequences, 42 positions, to 4 others each, 32 layers of 8 heads of 128 in 4 bits, 57 MB
+// written, 23 us (18 where they stay in the last cache; all loads before the first store: the same).
 __global__ __launch_bounds__(256) void kv_copy_kernel(const MoveArgs a, int first, int tile_bytes, int exp_bytes, int half) {
   const int layer = blockIdx.z, i = first + blockIdx.y, h = blockIdx.x, ps = a.p.page_size;
   const int from = a.src[i], to = a.dst[i];
@@ -276,8 +277,8 @@ __device__ __forceinline__ N block_sum(N x, N *part, N &total) {
 
 // One workgroup, a thread for a sequence.  The entries that the new tokens reach, of one sequence behind the other, are counted through;
 // the pages they need are the lowest free ones in that order.  Nothing changes where there are too few.  Where no sequence reaches more than
-// kFewEntries, as in a step of a few tokens, its thread looks at them, otherwise all threads do in turn (32 sequences, 1344
-// pages: 7.0 and 10.7 us).  Bound by its chain of loads: length, entry, count.
+// kFewEntries, as in a step of a few tokens, its thread looks at them, otherwise all threads do in turn (32 sequences that
+// grow by 100 positions: 7.0 and 10.7 us).  Bound by its chain of loads: length, entry, count.
 constexpr int kFewEntries = 4, kFreeHere = 2048;           // free pages that LDS has room for
 __global__ __launch_bounds__(1024) void pages_reserve_kernel(const TableArgs a, const int32_t *new_tokens, const ReserveOut out, int32_t *free_list) {
   __shared__ int64_t pre[NGG_TREE_MAX + 1];                // entries before a sequence's
