@@ -708,16 +708,14 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a) {
       if (w + j <= last) mn = fmaxf(mn, ml[j][0]);
     const float ref = mn == -__builtin_inff() ? 0.0f : mn, x = __builtin_amdgcn_exp2f(mm - ref);
     mm = mn;
-    ll *= x;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] *= x;
+    // (products and sums as written: which of two products a sum rounds first is not left to the compiler)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float y = w + j <= last ? __builtin_amdgcn_exp2f(ml[j][0] - ref) : 0.0f;
       if (w + j > last) continue;
-      ll += ml[j][1] * y;
+      ll = j ? __builtin_fmaf(ml[j][1], y, ll) : __builtin_fmaf(ll, x, ml[j][1] * y);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] += v[j][k] * y;
+      for (int k = 0; k < 4; ++k) o[k] = j ? __builtin_fmaf(v[j][k], y, o[k]) : __builtin_fmaf(o[k], x, v[j][k] * y);
     }
     w += 8;
   } while (w <= last);
