@@ -362,12 +362,12 @@ static dim3 head_groups(const CacheArgs &a) {
 static int64_t launch_tokens(const CacheArgs &a) { return ((1 << 22) / a.p.Hkv - 1) * (int64_t)kGroup; }
 // Calls of few rows (tokens times heads) have 16 lanes for 32 dimensions, whose chain of loads is the shorter one.  Us a call in a graph, so
 // and by groups, of 8 heads of 128, rows:
-//                       512         2048        3072        4096        8192
-//   written, 16 bits    4.6, 5.3    5.0, 5.5    5.5, 5.5    6.0, 5.9    8.6, 6.6
-//            fp32       4.4, 6.4    4.9, 6.5    5.4, 6.6    5.8, 7.3    8.5, 8.8
-//   rotated, 16 bits    4.8, 7.3    5.4, 7.4    5.8, 7.5    6.5, 7.5    9.5, 8.2
-//   read, 16 bits       4.6, 5.3    4.8, 5.4    5.2, 5.5    5.7, 5.7    8.0, 6.3
-//         fp32          4.7, 5.5    4.9, 5.7    5.4, 5.8    5.9, 6.1    8.5, 7.1
+//                       512         2048        4096        8192
+//   written, 16 bits    4.6, 5.3    5.0, 5.5    6.0, 5.9    8.6, 6.6
+//            fp32       4.4, 6.4    4.9, 6.5    5.8, 7.3    8.5, 8.8
+//   rotated, 16 bits    4.8, 7.3    5.4, 7.4    6.5, 7.5    9.5, 8.2
+//   read, 16 bits       4.6, 5.3    4.8, 5.4    5.7, 5.7    8.0, 6.3
+//         fp32          4.7, 5.5    4.9, 5.7    5.9, 6.1    8.5, 7.1
 static bool few_rows4(const CacheArgs &a, int most) { return (int64_t)a.n_tokens * a.p.Hkv <= most; }
 template <typename T>
 static void write_type(const CacheArgs &all, hipStream_t s) {
