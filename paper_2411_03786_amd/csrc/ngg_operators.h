@@ -215,7 +215,7 @@ struct TreePlan { int rows, ranges, Z, pieces, piece_steps; bool whole, stream; 
 TreePlan tree_plan(int dtype, int cache, int hd, int B, int T, int Hkv, int G, int64_t max_positions);
 void launch_tree_attention(int dtype, int cache, const TreeArgs &a, const TreePlan &p, hipStream_t s);
 void launch_tree_attention4(int dtype, const TreeArgs &a, const TreePlan &p, hipStream_t s);
-void launch_tree_block4(int rows, const TreeArgs &a, hipStream_t s);        // (64 or 128 rows)
+void launch_tree_block4(const TreeArgs &a, hipStream_t s);        // (128 rows, heads of 64 or 128)
 void launch_tree_merge(int dtype, int rows, const TreeArgs &a, hipStream_t s);   // (nothing where lists go whole)
 
 struct ScoreArgs {

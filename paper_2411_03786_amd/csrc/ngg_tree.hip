@@ -250,18 +250,18 @@ __global__ __launch_bounds__(256) void tree_stream_kernel(const TreeArgs a) {
 // caches, whose elements it holds, would keep 11 bits where the heads' powers of two are not far apart, but steps of both kinds in
 // one loop spill 130 registers (533 us).  64 rows a wave, eight waves, two tiles in turn, the softmax of one behind the products of the other
 // and raised wave priorities did not pay.
-// At 4 bits keys and values both arrive widened to bf16: the ragged trees 160 us.  Tiles of 64 rows (RG = 2) have two waves for the same rows, each
-// with one tile of every step, joined at the end: 1024 lists of 2047 positions, 51 rows, 139 us instead of 172 by 32 rows.
+// At 4 bits keys and values both arrive widened to bf16, and the remainders have their product: the ragged trees 187 us, without that product 153 for
+// outputs off by 0.0022 of their size instead of 0.0017 (the rounding of the result alone).
 // 32x32x16 products: row 8 j + 4 h + i of a key tile is key 16 (j % 2) + 8 h + 4 (j / 2) + i, so lane (row, h) ends up with keys
 // 16 u + 8 h .. + 7 of every 16, its operand of the second product.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-template <typename CT, int HD, int RG>
+template <typename CT, int HD>
 __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
   typedef bf16_t T;
-  constexpr int NW = 4, DS = HD / 32, KQ = HD / 16, DB = HD / 32, TILE = 32 * HD, KT = 2, KS = 32 * KT, ROWS = 32 * RG, NT = 64 * NW;
-  constexpr bool SPLIT = RG == 2;                          // two waves for the same rows, each a tile of every step
+  constexpr int NW = 4, DS = HD / 32, KQ = HD / 16, DB = HD / 32, TILE = 32 * HD, KT = 2, KS = 32 * KT, ROWS = 32 * NW, NT = 64 * NW;
   constexpr bool C4 = std::is_same_v<CT, fp4x2_t>, C8 = sizeof(CT) == 1 && !C4, REGS = C4 || C8;   // REGS: by way of registers
+  static_assert(!C4 || HD > 32, "heads of 32 stay with tiles of 32 rows");
   constexpr int PIECES = TILE / 16, PPT = (PIECES + NT - 1) / NT;   // (8 bits) 16-byte pieces of a tile, of a thread
   constexpr int PIECES4 = KT * HD, V0 = PIECES4 < NT ? PIECES4 : 0; // (4 bits) pieces of a step's keys, and the thread that has the first of its values
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
   int *odd = reinterpret_cast<int *>(vsl + 2 * KS);        // [KT] a tile of this step holds values that are not finite
   int *pre = odd + KT;                                     // [B + 1]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int r32 = lane & 31, h = lane >> 5, rg = SPLIT ? wave & 1 : wave, ks = SPLIT ? wave >> 1 : 0;
+  const int r32 = lane & 31, h = lane >> 5;
   const int Hkv = a.p.Hkv;
   const int loff = (h * 16 + (r32 & 15)) * 8, koff = (r32 >> 4) * DS * 512 + loff, voff = (r32 >> 4) * 512 + loff;
   Work<KS> w(a, pre);
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
       const int t_last = min(len.tree, (r0 + rows - 1) / a.G + 1) - 1;
       return (t_last + 1) * a.G > r0 ? min(n_keys, len.ctx + t_last + 1) : 0;
     };
-    const int group_keys = seen(z * ROWS, ROWS), wave_keys = seen(z * ROWS + rg * 32, 32);
+    const int group_keys = seen(z * ROWS, ROWS), wave_keys = seen(z * ROWS + wave * 32, 32);
     const int t_begin = w.s_begin * KT, t_end = min(w.s_end * KT, (group_keys + 31) / 32);
 
     // Tiles are taken in order; the pages of a step are looked up a step before its keys are asked for.
@@ -306,7 +306,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
     u32x4 k4, v4, ve4;                                     // (4 bits) a piece of keys and one of values, at most
     unsigned ke4 = 0;
     bool there[KT];                                        // (uniform) the tile's page is one of the pool's
-    const int tok = (z * ROWS + rg * 32 + r32) / a.G;
+    const int tok = (z * ROWS + wave * 32 + r32) / a.G;
     const bool live = tok < len.tree;
     MaskWindow see_next;                                   // ... and what the rows see of a step that holds tree tokens
     int at_step = t_begin;
@@ -329,19 +329,13 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
           k4 = reinterpret_cast<const u32x4 *>(x == 0 ? kp[0] : kp[1])[pc];
           const uint8_t *e = a.p.k_exp + (x == 0 ? head[0] : head[1]) * DS;
           if constexpr (HD == 128) ke4 = e[pc % 64 * 2 + pc / 64];
-          else if constexpr (HD == 64) ke4 = *reinterpret_cast<const uint16_t *>(e + (pc / 32 * 16 + pc % 16) * 2);
-          else ke4 = *reinterpret_cast<const unsigned *>(e + pc % 8 * 4);
+          else ke4 = *reinterpret_cast<const uint16_t *>(e + (pc / 32 * 16 + pc % 16) * 2);
         }
         if (tid >= V0 && tid < V0 + PIECES4) {
           const int xv = (tid - V0) / HD, pv = (tid - V0) % HD;
           v4 = reinterpret_cast<const u32x4 *>(xv == 0 ? vp[0] : vp[1])[pv];
           const uint8_t *e = a.p.v_exp + (xv == 0 ? head[0] : head[1]) * DS;
-          if constexpr (HD == 128) ve4 = *reinterpret_cast<const u32x4 *>(e + pv % 64 / 16 * 32 + pv / 64 * 16);
-          else if constexpr (HD == 64) ve4 = *reinterpret_cast<const u32x4 *>(e + pv / 16 * 16);
-          else {
-            const u32x2 y = *reinterpret_cast<const u32x2 *>(e + pv / 8 * 8);
-            ve4 = u32x4{y[0], y[1], y[0], y[1]};
-          }
+          ve4 = *reinterpret_cast<const u32x4 *>(e + (HD == 128 ? pv % 64 / 16 * 32 + pv / 64 * 16 : pv / 16 * 16));
         }
       } else if constexpr (C8) {
 #pragma unroll
@@ -375,9 +369,8 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             // word i: eight dimensions from dim of row (half, ln % 16)
-            const int ln = HD == 128 ? pc % 64 : HD == 64 ? pc : pc * 2 + i / 2, half = HD == 128 ? pc / 64 : HD == 64 ? i / 2 : i % 2;
-            const int dim = ln / 16 * (HD / 4) + (HD == 128 ? i * 8 : HD == 64 ? i % 2 * 8 : 0);
-            const float scale = exp_scale(ke4 >> (HD == 128 ? 0 : HD == 64 ? half * 8 : i * 8) & 0xff);
+            const int ln = pc % 64, half = HD == 128 ? pc / 64 : i / 2, dim = ln / 16 * (HD / 4) + (HD == 128 ? i : i % 2) * 8;
+            const float scale = exp_scale(ke4 >> (HD == 128 ? 0 : half * 8) & 0xff);
             *reinterpret_cast<bf16x8 *>(kt + (half * DS + dim / 32) * 512 + (dim % 32 / 8 * 16 + ln % 16) * 8) = widen4(k4[i], scale);
           }
         }
@@ -386,7 +379,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
           T *vt = vl + (buf * KT + xv) * TILE;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const int ln = HD == 32 ? pv * 2 + i : pv % 64, group = HD == 32 ? 0 : pv / 64 * 2 + i;
+            const int ln = pv % 64, group = pv / 64 * 2 + i;
             bf16x8 lo, hi;
             widen4_values(u32x2{v4[2 * i], v4[2 * i + 1]}, u32x2{ve4[2 * i], ve4[2 * i + 1]}, lo, hi);
             *reinterpret_cast<bf16x8 *>(vt + 2 * group * 512 + ln * 8) = lo;
@@ -419,7 +412,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
     stage_load(0);
     bf16x8 Q[KQ];
     {
-      const int row = z * ROWS + rg * 32 + r32;
+      const int row = z * ROWS + wave * 32 + r32;
       const T *q = (const T *)a.q + b * a.q_batch + (live ? tok : 0) * a.q_token + (int64_t)(hk * a.G + row % a.G) * a.q_head;
 #pragma unroll
       for (int d = 0; d < KQ; ++d) Q[d] = zero_frag<T>().v;
@@ -458,9 +451,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
     auto compute = [&](bool all, int t, int buf) {
       if (t * 32 >= wave_keys) return;                     // (uniform per wave)
 #pragma unroll
-      for (int k2 = 0; k2 < (SPLIT ? 1 : KT); ++k2) {
-        const int k = SPLIT ? ks : k2;
-        const bool is_here = SPLIT ? (ks ? here[1] : here[0]) : here[k2];
+      for (int k = 0; k < KT; ++k) {
         const T *kt = kl + (buf * KT + k) * TILE + koff, *vt = vl + (buf * KT + k) * TILE + voff;
         const int pos0 = (t + k) * 32;
         // (left to itself the compiler fetches one fragment, waits, and multiplies: the fences keep the fetches together and ahead)
@@ -482,7 +473,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
         if (!all) {
 #pragma unroll
           for (int u = 0; u < 2; ++u)
-            vis[u] = is_here ? visible8(see, t * 32 - len.ctx, tok, pos0 + 16 * u + 8 * h - len.ctx, n_keys - len.ctx) : 0u;
+            vis[u] = here[k] ? visible8(see, t * 32 - len.ctx, tok, pos0 + 16 * u + 8 * h - len.ctx, n_keys - len.ctx) : 0u;
 #pragma unroll
           for (int r = 0; r < 16; ++r)
             if (!(vis[r >> 2 & 1] >> ((r >> 3) * 4 + (r & 3)) & 1)) S[r] = -__builtin_inff();
@@ -504,7 +495,7 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
           m = mnew;
         }
         const float ref = m == -__builtin_inff() ? 0.0f : m;
-        bf16x8 P[2];
+        bf16x8 P[2], R[2];                                 // (4 bits) R: what the rounding of P left out
         float ps[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -524,6 +515,11 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
             const bf16x2 q = __builtin_convertvector(p, bf16x2);
             P[u][e] = q[0];
             P[u][e + 1] = q[1];
+            if constexpr (C4) {
+              const bf16x2 r = __builtin_convertvector((f32x2){p[0] - (float)q[0], p[1] - (float)q[1]}, bf16x2);
+              R[u][e] = r[0];
+              R[u][e + 1] = r[1];
+            }
           }
         }
         l += ps[0] + ps[1];
@@ -531,6 +527,11 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int d = 0; d < DB; ++d) O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[u][d], P[u], O[d], 0, 0, 0);
+        if constexpr (C4)                                  // the probabilities count with 16 bits, not with 8
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[u][d], R[u], O[d], 0, 0, 0);
         if (!all && odd[k]) {                              // (uniform)
           // values that are not finite were left out, because 0 times them must stay 0 where their key is masked
           const int page = a.pages[b * a.pages_batch + pos0 / a.p.page_size];
@@ -602,39 +603,11 @@ __global__ __launch_bounds__(256, 2) void tree_block_kernel(const TreeArgs a) {
     // (the last transfers, of no step's tiles, have landed before LDS is used again)
     if constexpr (!REGS) __builtin_amdgcn_s_waitcnt(0x0F70);
 
-    if constexpr (SPLIT) {                                 // the second wave's share goes to the first by way of LDS
-      f32x4 *lo = reinterpret_cast<f32x4 *>(smem) + rg * DB * 256 + lane;
-      f32x2 *lml = reinterpret_cast<f32x2 *>(reinterpret_cast<f32x4 *>(smem) + 2 * DB * 256) + rg * 64 + lane;
-      __syncthreads();
-      if (ks) {
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) lo[(d * 4 + j) * 64] = f32x4{O[d][4 * j], O[d][4 * j + 1], O[d][4 * j + 2], O[d][4 * j + 3]};
-        *lml = f32x2{m, l};
-      }
-      __syncthreads();
-      if (!ks) {
-        const f32x2 other = *lml;
-        const float top = fmaxf(m, other[0]), ref = top == -__builtin_inff() ? 0.0f : top;
-        const float x = __builtin_amdgcn_exp2f(m - ref), y = __builtin_amdgcn_exp2f(other[0] - ref);
-        m = top;
-        l = l * x + other[1] * y;
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const f32x4 o = lo[(d * 4 + j) * 64];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) O[d][4 * j + i] = O[d][4 * j + i] * x + o[i] * y;
-          }
-      }
-    }
     const bool whole = w.is_whole();
     float lsum = l + other_half(l);
-    if (tok < a.T && !ks) {
+    if (tok < a.T) {
       if (!live) lsum = 0.0f;                              // not a token of this sequence
-      const int r = rg * 32 + r32;
+      const int r = wave * 32 + r32;
       if (whole) {
         const int head = hk * a.G + (z * ROWS + r) % a.G;
         const float inv = lsum == 0.0f ? 0.0f : 1.0f / lsum;
@@ -744,20 +717,25 @@ static int tile_rows(int dtype, int hd, int rows, int64_t lists, int64_t positio
   if (scores >= 16 << 20 || (hd == 128 && lists * ((rows + 15) / 16) >= 768)) return 32;
   return 16;
 }
-// The same over 4 bits, where a tile's keys and values are widened again for each: 16 and 32 rows are tree4_stream_kernel's, 64 and
-// 128 tree_block_kernel's.  Measured at 16 bits (us a call in a graph; tiles of 16, 32, 64 and 128 rows; lists, rows, positions, head_dim):
-//   32, 51, 2047, 128: 19, 21, 28, 29 (3 M scores)       16, 244, 2000, 128: 29, 25, 33, 33 (7 M)     48, 51, 2000, 64: 21, 18, 25, 26 (5 M)
-//   24, 132, 4000, 64: 27, 23, 31, 30 (12 M)             32, 512, 1000, 128: 34, 29, 41, 43 (16 M)    16, 244, 8000, 128: 53, 44, 49, 47 (30 M)
-//   64, 244, 4000, 128: 97, 72, 73, 64 (60 M)            9, 480, 12000, 64: 55, 49, 52, 45 (49 M)     144, 80, 4000, 128: 75, 75, 82, 63 (44 M)
-//   256, 36, 8000, 128: 128, 134, 120, 151 (70 M)        192, 64, 8000, 64: 89, 84, 78, 92 (94 M)     1024, 51, 2047, 128: 213, 172, 139, 170 (102 M)
+// The same over 4 bits, where a tile's keys and values are widened again for each: 16 and 32 rows are tree4_stream_kernel's, 128
+// tree_block_kernel's, all with 16 bits of a probability.  Measured at 16 bits (us a call in a graph; tiles of 16, 32 and 128 rows; lists, rows, positions,
+// head_dim):
+//   32, 51, 2047, 128: 19, 21, 29 (3 M scores)           16, 244, 2000, 128: 29, 25, 33 (7 M)         48, 51, 2000, 64: 21, 18, 26 (5 M)
+//   24, 132, 4000, 64: 27, 23, 30 (12 M)                 32, 512, 1000, 128: 34, 29, 43 (16 M)        16, 244, 8000, 128: 53, 45, 52 (30 M)
+//   9, 480, 12000, 64: 52, 48, 51 (49 M)                 128, 120, 3850, 128: 96, 72, 77 (56 M)       64, 244, 4000, 128: 97, 73, 73 (60 M)
+//   60, 120, 10000, 64: 69, 64, 63 (69 M)                64, 244, 5000, 128: 114, 86, 83 (74 M)       9, 480, 20000, 64: 75, 68, 67 (82 M)
+//   144, 80, 7000, 128: 118, 114, 112 (77 M)             128, 120, 5200, 128: 124, 93, 94 (76 M)      64, 244, 16000, 128: 317, 247, 215 (238 M)
+//   256, 52, 16000, 128: 326, 255, 359 (203 M)           192, 64, 16000, 64: 160, 147, 198 (188 M)    768, 51, 4000, 64: 164, 153, 204 (149 M)
+//   80, 244, 8000, 32: 101, 86, 92 (149 M)               80, 244, 32000, 32: 357, 295, 305 (596 M)
+// (tiles of 64 rows of two waves each, which share the steps: 1024, 51, 2047, 128: 160, of 32 rows 171 (102 M); 512, 51, 4000, 128: 147, 147; 256, 64,
+// 12000, 128: 210, 195; 192, 64, 16000, 64: 151, 147: not kept)
 // and in fp32 (16 and 32 rows; at heads of 128 the latter leaves a SIMD one wave): 64, 244, 4000, 128: 123, 136 (60 M); 24, 132, 4000, 64:
 // 34, 32 (12 M); 128, 100, 2000, 64: 60, 48 (24 M); 32, 40, 9000, 32: 23, 25 (11 M).
-// (What tiles of 64 and 128 rows lose: 8 bits of a probability, where the others have 16.)
 static int tile_rows4(int dtype, int hd, int rows, int64_t lists, int64_t positions) {
   if (rows <= 16) return 16;
   const int64_t scores = lists * positions * rows;
   if (dtype == NGG_F32) return hd == 128 || scores < (hd == 64 ? 8 << 20 : 32 << 20) ? 16 : 32;
-  if (scores >= 40 << 20) return rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  if (hd > 32 && rows > 64 && scores >= 64 << 20) return 128;
   return scores < (hd == 128 ? 6 << 20 : 4 << 20) ? 16 : 32;
 }
 static int step_keys(int rows) { return rows <= 32 ? 128 : 64; }
@@ -831,30 +809,24 @@ static void launch_stream(const TreeArgs &a, hipStream_t s) {
   hipLaunchKernelGGL((tree_stream_kernel<T, CT, HD, QF, NT>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
   merge<T, HD, 16 * QF, 128>(a, s);
 }
-template <typename CT, int HD, int RG>
+template <typename CT, int HD>
 static void launch_block(const TreeArgs &a, hipStream_t s) {
   constexpr size_t lds = (size_t)8 * 32 * HD * 2 + 2 * 64 * 4 + 2 * 4;
-  static const bool once = (allow_lds(&tree_block_kernel<CT, HD, RG>, lds + (NGG_TREE_MAX + 1) * 4), true);
+  static const bool once = (allow_lds(&tree_block_kernel<CT, HD>, lds + (NGG_TREE_MAX + 1) * 4), true);
   (void)once;
-  hipLaunchKernelGGL((tree_block_kernel<CT, HD, RG>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
-  merge<bf16_t, HD, 32 * RG, 64>(a, s);
+  hipLaunchKernelGGL((tree_block_kernel<CT, HD>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
+  merge<bf16_t, HD, 128, 64>(a, s);
 }
-template <int HD>
-static void block4(int rows, const TreeArgs &a, hipStream_t s) {
-  if (rows == 64) launch_block<fp4x2_t, HD, 2>(a, s);
-  else launch_block<fp4x2_t, HD, 4>(a, s);
-}
-void launch_tree_block4(int rows, const TreeArgs &a, hipStream_t s) {
-  if (a.p.hd == 32) block4<32>(rows, a, s);
-  else if (a.p.hd == 64) block4<64>(rows, a, s);
-  else block4<128>(rows, a, s);
+void launch_tree_block4(const TreeArgs &a, hipStream_t s) {
+  if (a.p.hd == 64) launch_block<fp4x2_t, 64>(a, s);
+  else launch_block<fp4x2_t, 128>(a, s);
 }
 template <typename T, typename CT, int HD>
 static void by_rows(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
   if (p.rows == 16 && p.stream) launch_stream<T, CT, HD, 1, true>(a, s);
   else if (p.rows == 16) launch_stream<T, CT, HD, 1, false>(a, s);
   else if (p.rows == 32) launch_stream<T, CT, HD, 2, false>(a, s);
-  else if constexpr (sizeof(T) == 2) launch_block<CT, HD, 4>(a, s);
+  else if constexpr (sizeof(T) == 2) launch_block<CT, HD>(a, s);
 }
 template <typename T, typename CT>
 static void by_head(const TreeArgs &a, const TreePlan &p, hipStream_t s) {

@@ -309,7 +309,7 @@ static void by_head(const TreeArgs &a, const TreePlan &p, hipStream_t s) {
   else by_rows<T, 128>(a, p, s);
 }
 void launch_tree_attention4(int dtype, const TreeArgs &a, const TreePlan &p, hipStream_t s) {
-  if (p.rows >= 64) return launch_tree_block4(p.rows, a, s);
+  if (p.rows == 128) return launch_tree_block4(a, s);
   if (dtype == NGG_F32) by_head<float>(a, p, s);
   else by_head<bf16_t>(a, p, s);
   launch_tree_merge(dtype, p.rows, a, s);

@@ -1,0 +1,109 @@
+"""Attention over a cache of 4 bits by what a launch is planned as: tiles of 16, 32 and 128 rows; lists that go whole, in pieces and in shares.  The
+plan shows in the workspace that a call asks for, which every test here checks, so that another rule cannot leave a kernel untested.  And the
+bits that the kernels keep: bounds that a kernel with a bfloat16 term less would miss, which is shown beside them.  Needs an MI355X."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2411_03786_amd as ngg
+from test_gpu_cache4 import Case4
+from test_gpu_operators import ints, randn
+
+pytestmark = pytest.mark.gpu
+
+
+def workspace(c):
+    """Bytes that the call of a Case4 asks for."""
+    B, T, H, hd = c.q.shape
+    a = ngg.ngg_tree_args(max_pages=c.table.shape[1], batch=B, tree=T, n_heads=H, dtype=ngg.NGG_F32 if c.dtype == "f32" else ngg.NGG_BF16, scale=1.0)
+    need = C.c_int64(-1)
+    assert ngg.load_library().ngg_tree_attention_workspace(c.kv._c, a, need) == ngg.NGG_OK
+    return need.value
+
+
+def held(dtype, hd, rows):
+    """Workgroups that a launch of shares is planned for."""
+    wide = dtype == "f32"
+    if rows == 128:
+        return 512
+    if rows == 32:
+        return 256 * (3 if hd == 32 and not wide else 1 if hd == 128 and wide else 2)
+    return 256 * ((4 if hd == 32 else 3 if hd == 64 else 2) if wide else 3 if hd == 128 else 4)
+
+
+def tiles(c, rows):
+    B, T, H, hd = c.q.shape
+    Hkv = c.kv.n_kv_heads
+    steps = -(-c.table.shape[1] * c.kv.page_size // (64 if rows == 128 else 128))
+    return B * Hkv, -(-T * (H // Hkv) // rows), steps, rows * (hd * 4 + 8)
+
+
+def shares(c, rows):
+    """What a launch of shares asks for: two parts for each."""
+    lists, Z, steps, part = tiles(c, rows)
+    want = -(-held(c.dtype, c.q.shape[-1], rows) // Z)
+    r = max(1, min(want, steps * lists))
+    r = r if r < 8 else -(-r // 8) * 8 if r < want else r // 8 * 8
+    return r * Z * 2 * part
+
+
+def pieces(c, rows, n):
+    """What lists in n pieces ask for."""
+    lists, Z, _, part = tiles(c, rows)
+    return lists * n * Z * part
+
+
+def widen(c, positions):
+    """A page list for so many positions: the call is planned for them."""
+    more = max(-(-positions // c.kv.page_size) - c.table.shape[1], 0)
+    c.table = torch.cat([c.table, torch.full((len(c.table), more), -1, dtype=torch.int32, device="cuda")], 1)
+
+
+def exact(c, b, h, terms=None):
+    """Sequence b's chain under head h in 64 bits: out, sum p |v| / sum p, log sum, and the largest sum of |q k|; terms: with probabilities that are
+    the sum of so many bfloat16 numbers, each the rounding of what the ones before left."""
+    T, H = c.T, c.q.shape[2]
+    n = c.ctx[b] + c.trees[b]
+    k, v = (x[b][:n, h // (H // c.kv.n_kv_heads)].double() for x in (c.ks, c.vs))
+    x = c.q[b, :, h].double()
+    see = torch.arange(n, device="cuda") <= c.ctx[b] + torch.arange(T, device="cuda")[:, None]
+    s = torch.where(see, (x @ k.T.contiguous()) * c.scale, -float("inf"))
+    top = s.amax(-1, keepdim=True)
+    p = torch.exp(s - top)
+    tot = p.sum(-1, keepdim=True)
+    if terms:
+        rest, p = p, torch.zeros_like(p)
+        for _ in range(terms):
+            part = rest.bfloat16().double()
+            p, rest = p + part, rest - part
+    qk = torch.where(see, (x.abs() @ k.abs().T.contiguous()) * abs(c.scale), 0.0).amax(-1)
+    return (p @ v) / tot, (p @ v.abs()) / tot, (top + tot.log()).squeeze(-1), qk
+
+
+@pytest.mark.parametrize("rows,n,H,Hkv,hd,T,positions", [(16, 0, 8, 2, 64, 3, 0), (16, 0, 4, 4, 128, 1, 0), (16, 40, 8, 2, 128, 9, 20000), (32, 61, 8, 2, 128, 9, 70000),
+                                                         (32, 61, 8, 2, 64, 9, 70000), (32, 79, 8, 1, 32, 9, 70000), (128, None, 8, 2, 128, 20, 220000),
+                                                         (128, None, 4, 1, 64, 33, 260000)])
+def test_sixteen_bit_calls_keep_16_bits_of_a_probability(rows, n, H, Hkv, hd, T, positions):
+    """Values of either sign leave little of a row's sum, so that what its terms lose is seen beside the rounding of the output.  Queries of
+    four dimensions: scores off by (4 + 10) 2^-24 of the sum of |q k|, outputs by twice that; two bfloat16 terms of a probability by
+    2^-8 2^-8 of it; sums of n terms, of probabilities and of both terms' products, by 3 n 2^-24; the result's rounding 2^-8 of itself.
+    With one term some outputs are further off than that."""
+    ctx = 60 - T
+    c = Case4([ctx, ctx // 2], [T, T], T, H, Hkv, hd, "bf16", page=64, seed=31)
+    widen(c, positions)
+    c.q[..., 4:] = 0
+    c.scale = 1.0
+    assert workspace(c) == (shares(c, rows) if n is None else pieces(c, rows, n))
+    out, lse = ngg.tree_attention(c.q, c.kv, c.table, ints(c.ctx), scale=1.0, want_lse=True)
+    beyond = 0
+    for b in range(2):
+        keys = c.ctx[b] + T
+        for h in range(H):
+            want, mag, want_lse, qk = exact(c, b, h)
+            tol = mag * (2 * (4 + 10) * 2.0 ** -24 * qk[:, None] + 2.0 ** -16 + 3 * keys * 2.0 ** -24) + want.abs() * 2.0 ** -8
+            assert ((out[b, :, h].double() - want).abs() <= tol).all()
+            assert ((lse[b, :, h].double() - want_lse).abs() <= (4 + 10) * 2.0 ** -24 * qk + (keys + 8) * 2.0 ** -24 + 2.0 ** -23 * want_lse.abs()).all()
+            beyond += int(((exact(c, b, h, 1)[0] - want).abs() > tol).sum())
+            assert ((exact(c, b, h, 2)[0] - want).abs() <= tol).all()
+    assert beyond > 20
