@@ -2,6 +2,8 @@
 // log probabilities (ngg_operators.hip holds their C entry points and argument checks).
 #pragma once
 
+#include <atomic>
+
 #include "ngg.h"
 #include "ngg_internal.h"
 
@@ -15,11 +17,21 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
-// Lets the current device launch a kernel with more than 64 KB of dynamic LDS
-template <typename K>
-inline void allow_lds(K kernel, size_t bytes) {
-  if (bytes > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-}
+// Lets the current device launch a kernel with more than 64 KB of dynamic LDS: one object to a kernel, told the most that any call takes, so that
+// no call lowers what another one, on another thread, is about to launch with.
+class LdsLimit {
+  std::atomic<uint64_t> devices_{0};                       // those that know
+ public:
+  template <typename K>
+  void allow(K kernel, size_t most) {
+    int device = 0;
+    if (most <= 64 * 1024 || hipGetDevice(&device) != hipSuccess) return;
+    const uint64_t bit = (uint64_t)1 << (device & 63);
+    if (devices_.load(std::memory_order_acquire) & bit) return;
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)most) == hipSuccess)
+      devices_.fetch_or(bit, std::memory_order_release);
+  }
+};
 
 // An element of the 8-bit cache: 4 exponent and 3 fraction bits, the encoding without infinities (0x7f and 0xff are NaN).
 struct fp8_t { uint8_t bits; };

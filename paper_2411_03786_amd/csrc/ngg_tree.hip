@@ -804,16 +804,16 @@ static void merge(const TreeArgs &a, hipStream_t s) {
 template <typename T, typename CT, int HD, int QF, bool NT>
 static void launch_stream(const TreeArgs &a, hipStream_t s) {
   constexpr size_t lds = (size_t)4 * QF * (HD / 16 * 256 + 32) * 4;
-  static const bool once = (allow_lds(&tree_stream_kernel<T, CT, HD, QF, NT>, lds + (NGG_TREE_MAX + 1) * 4), true);
-  (void)once;
+  static LdsLimit limit;
+  limit.allow(&tree_stream_kernel<T, CT, HD, QF, NT>, lds + (NGG_TREE_MAX + 1) * 4);
   hipLaunchKernelGGL((tree_stream_kernel<T, CT, HD, QF, NT>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
   merge<T, HD, 16 * QF, 128>(a, s);
 }
 template <typename CT, int HD>
 static void launch_block(const TreeArgs &a, hipStream_t s) {
   constexpr size_t lds = (size_t)8 * 32 * HD * 2 + 2 * 64 * 4 + 2 * 4;
-  static const bool once = (allow_lds(&tree_block_kernel<CT, HD>, lds + (NGG_TREE_MAX + 1) * 4), true);
-  (void)once;
+  static LdsLimit limit;
+  limit.allow(&tree_block_kernel<CT, HD>, lds + (NGG_TREE_MAX + 1) * 4);
   hipLaunchKernelGGL((tree_block_kernel<CT, HD>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
   merge<bf16_t, HD, 128, 64>(a, s);
 }

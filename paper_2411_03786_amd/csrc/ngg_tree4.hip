@@ -290,7 +290,8 @@ __global__ __launch_bounds__(256, stream4_waves(sizeof(T) == 4, HD, QF)) void tr
 template <typename T, int HD, int QF, bool NT, Parts PARTS>
 static void launch_stream(const TreeArgs &a, hipStream_t s) {
   constexpr size_t lds = (size_t)4 * QF * (HD / 16 * 256 + 32) * 4;
-  allow_lds(&tree4_stream_kernel<T, HD, QF, NT, PARTS>, lds + (a.B + 1) * 4);
+  static LdsLimit limit;
+  limit.allow(&tree4_stream_kernel<T, HD, QF, NT, PARTS>, lds + (NGG_TREE_MAX + 1) * 4);
   hipLaunchKernelGGL((tree4_stream_kernel<T, HD, QF, NT, PARTS>), dim3(a.ranges * a.Z), dim3(256), lds + (a.B + 1) * 4, s, a);
 }
 template <typename T, int HD>

@@ -2,6 +2,7 @@
 plan shows in the workspace that a call asks for, which every test here checks, so that another rule cannot leave a kernel untested.  And the
 bits that the kernels keep: bounds that a kernel with a bfloat16 term less would miss, which is shown beside them.  Needs an MI355X."""
 import ctypes as C
+import threading
 
 import pytest
 import torch
@@ -107,3 +108,36 @@ def test_sixteen_bit_calls_keep_16_bits_of_a_probability(rows, n, H, Hkv, hd, T,
             beyond += int(((exact(c, b, h, 1)[0] - want).abs() > tol).sum())
             assert ((exact(c, b, h, 2)[0] - want).abs() <= tol).all()
     assert beyond > 20
+
+
+def test_calls_of_two_host_threads():
+    """Tiles of 32 rows of 128 dimensions take more than 64 KB of LDS, and the more the larger the batch: two threads that call with a batch of 1 and
+    of 1024, each on a stream of its own, through the C entry (which, unlike the binding, lets both in at once)."""
+    lib, calls = ngg.load_library(), []
+    for batch, positions in ((1, 200000), (1024, 256)):
+        c = Case4([20] * min(batch, 8), [1] * min(batch, 8), 1, 32, 1, 128, "bf16", page=64, seed=batch)
+        widen(c, positions)
+        c.table, c.q = (x.repeat(batch // len(x), *[1] * (x.dim() - 1)).contiguous() for x in (c.table, c.q))
+        assert workspace(c) == (pieces(c, 32, 391) if batch == 1 else 0)
+        lens = ints([20] * batch)
+        want = ngg.tree_attention(c.q, c.kv, c.table, lens)
+        out, ws = torch.zeros_like(c.q), torch.empty(max(workspace(c), 16), dtype=torch.uint8, device="cuda")
+        a = ngg.ngg_tree_args(q=c.q.data_ptr(), out=out.data_ptr(), q_batch=32 * 128, q_token=32 * 128, q_head=128, out_batch=32 * 128, out_token=32 * 128, out_head=128,
+                              pages=c.table.data_ptr(), pages_batch=c.table.stride(0), context_lens=lens.data_ptr(), max_pages=c.table.shape[1], batch=batch, tree=1,
+                              n_heads=32, dtype=ngg.NGG_BF16, scale=128 ** -0.5)
+        calls.append((c, a, ws, torch.cuda.Stream(), out, want, lens))
+    torch.cuda.synchronize()
+    bad = []
+
+    def many(c, a, ws, stream, *_):
+        for _ in range(300):
+            if lib.ngg_tree_attention(c.kv._c, a, ws.data_ptr(), ws.numel(), stream.cuda_stream) != ngg.NGG_OK:
+                bad.append(lib.ngg_last_error(None).decode())
+    threads = [threading.Thread(target=many, args=x) for x in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not bad, bad[:3]
+    assert all(torch.equal(x[4], x[5]) for x in calls)
