@@ -83,20 +83,27 @@ __device__ __forceinline__ void move_few(const MoveArgs &a, void *base, int laye
   typedef typename Unit<K::B>::T U;
   const Move m = entry<K>(a, layer, b, threadIdx.x & 63);
   const uint64_t all = __ballot(m.ok);
+  if (all == 0) return;                                    // (of the whole wave)
   const int h = unit / K::N, u = unit - h * K::N;
-  if (h >= a.p.Hkv || all == 0) return;
-  uint8_t *mine = (uint8_t *)base + (int64_t)h * a.p.page_size * K::POS + K::at(0, u);
+  const bool mine_too = h < a.p.Hkv;                       // lanes without a unit stay: they have entries that the others read
+  uint8_t *mine = (uint8_t *)base + (int64_t)(mine_too ? h : 0) * a.p.page_size * K::POS + K::at(0, mine_too ? u : 0);
   U x[kInRegisters];
   uint64_t left = all;
 #pragma unroll
   for (int i = 0; i < kInRegisters; ++i) {
-    if (left) x[i] = *reinterpret_cast<const U *>(mine + of_lane(m.from, __builtin_ctzll(left)));
+    if (left) {
+      const int64_t from = of_lane(m.from, __builtin_ctzll(left));
+      if (mine_too) x[i] = *reinterpret_cast<const U *>(mine + from);
+    }
     left &= left - 1;                                      // (of none: none)
   }
   left = all;
 #pragma unroll
   for (int i = 0; i < kInRegisters; ++i) {
-    if (left) *reinterpret_cast<U *>(mine + of_lane(m.to, __builtin_ctzll(left))) = x[i];
+    if (left) {
+      const int64_t to = of_lane(m.to, __builtin_ctzll(left));
+      if (mine_too) *reinterpret_cast<U *>(mine + to) = x[i];
+    }
     left &= left - 1;
   }
 }
