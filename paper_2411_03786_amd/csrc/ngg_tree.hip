@@ -734,7 +734,8 @@ static int tile_rows(int dtype, int hd, int rows, int64_t lists, int64_t positio
 static int tile_rows4(int dtype, int hd, int rows, int64_t lists, int64_t positions) {
   if (rows <= 16) return 16;
   const int64_t scores = lists * positions * rows;
-  if (dtype == NGG_F32) return hd == 128 || scores < (hd == 64 ? 8 << 20 : 32 << 20) ? 16 : 32;
+  // (tiles are rows of the joining launch's grid, 65535 at most: the largest trees of the most heads have 65536 of 16 rows)
+  if (dtype == NGG_F32) return rows <= 65535 * 16 && (hd == 128 || scores < (hd == 64 ? 8 << 20 : 32 << 20)) ? 16 : 32;
   if (hd > 32 && rows > 64 && scores >= 64 << 20) return 128;
   return scores < (hd == 128 ? 6 << 20 : 4 << 20) ? 16 : 32;
 }

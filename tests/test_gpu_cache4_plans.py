@@ -141,3 +141,30 @@ def test_calls_of_two_host_threads():
     torch.cuda.synchronize()
     assert not bad, bad[:3]
     assert all(torch.equal(x[4], x[5]) for x in calls)
+
+
+def test_the_largest_tree_of_the_most_heads():
+    """1024 tokens of 1024 heads over one key head in fp32: 2^20 rows, which in tiles of 16 would be more than the joining launch can count.  (Tiles of 32,
+    which no other call of heads of 128 in fp32 has.)  Every output, to the bounds of test_gpu_cache4."""
+    T = H = 1024
+    hd, ctx = 128, 1500
+    c = Case4([ctx], [T], T, 1, 1, hd, "f32", page=64, seed=41)
+    c.q = torch.randn(1, T, H, hd, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    assert workspace(c) == shares(c, 32) > 0
+    out, lse = ngg.tree_attention(c.q, c.kv, c.table, ints(c.ctx), want_lse=True)
+    n, at = ctx + T, torch.arange(ctx + T, device="cuda")
+    k, v = (x[0][:n, 0].double() for x in (c.ks, c.vs))
+    kt, kt_abs, v_abs = k.T.contiguous(), k.abs().T.contiguous(), v.abs()
+    for t in range(0, T, 8):
+        x = c.q[0, t:t + 8].double().flatten(0, 1)
+        s = (x @ kt) * c.scale
+        see = (at <= ctx + torch.arange(t, t + 8, device="cuda").repeat_interleave(H)[:, None])
+        s = torch.where(see, s, -float("inf"))
+        top = s.amax(-1, keepdim=True)
+        p = torch.exp(s - top)
+        tot = p.sum(-1, keepdim=True)
+        want, want_lse = (p @ v) / tot, (top + tot.log()).squeeze(-1)
+        err = (hd + 10) * 2.0 ** -24 * ((x.abs() @ kt_abs).amax(-1) * c.scale)
+        tol = (p @ v_abs) / tot * (2 * err + 2.0 ** -15)[:, None] + want.abs() * 2.0 ** -24
+        assert ((out[0, t:t + 8].flatten(0, 1).double() - want).abs() <= tol).all(), t
+        assert ((lse[0, t:t + 8].flatten().double() - want_lse).abs() <= err + 2.0 ** -15 + 2.0 ** -22 * want_lse.abs()).all(), t
