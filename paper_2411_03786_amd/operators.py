@@ -79,6 +79,9 @@ class KVPages:
             raise ValueError(f"unknown cache type {cache!r}")
         if layers < 1:
             raise ValueError(f"{layers} layers")
+        for name, size in (("pages", layers * n_pages), ("page_size", page_size), ("kv heads", n_kv_heads), ("head_dim", head_dim)):
+            if not -2 ** 31 <= size < 2 ** 31:                          # (a C number would be cut without a word)
+                raise ValueError(f"{size} {name} pass 32 bits")
         self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, self.cache = layers * n_pages, page_size, n_kv_heads, head_dim, cache
         self.layers = layers
         self._c = ngg_kv_pages(None, None, None, None, layers * n_pages, page_size, n_kv_heads, head_dim, _CACHES[cache])
