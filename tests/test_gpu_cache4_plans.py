@@ -4,10 +4,12 @@ bits that the kernels keep: bounds that a kernel with a bfloat16 term less would
 import ctypes as C
 import threading
 
+import numpy as np
 import pytest
 import torch
 
 import paper_2411_03786_amd as ngg
+import test_gpu_cache4
 from test_gpu_cache4 import Case4
 from test_gpu_operators import ints, randn
 
@@ -168,3 +170,119 @@ def test_the_largest_tree_of_the_most_heads():
         tol = (p @ v_abs) / tot * (2 * err + 2.0 ** -15)[:, None] + want.abs() * 2.0 ** -24
         assert ((out[0, t:t + 8].flatten(0, 1).double() - want).abs() <= tol).all(), t
         assert ((lse[0, t:t + 8].flatten().double() - want_lse).abs() <= err + 2.0 ** -15 + 2.0 ** -22 * want_lse.abs()).all(), t
+
+
+def ragged(B, T, longest, seed):
+    """Lengths of all kinds: sequences that are not there, contexts of none and one, trees that are missing and short."""
+    rng = np.random.default_rng(seed)
+    ctx = rng.integers(longest // 2, longest - T, B)
+    ctx[::7], ctx[1::11] = 0, 1
+    trees = rng.integers(1, T + 1, B)
+    trees[3::9], trees[0] = 0, T
+    return [int(x) for x in ctx], [int(x) for x in trees]
+
+
+# type, head_dim, tile rows, pieces (None: shares), sequences, query and key heads, tree, planned positions, longest list
+PLANS = [
+    # shares of all lists, single tokens
+    ("bf16", 128, 16, None, 40, 16, 4, 2, 3000, 2900), ("f32", 64, 16, None, 40, 16, 4, 2, 3000, 2900), ("bf16", 32, 16, None, 40, 16, 4, 2, 3000, 2900),
+    ("f32", 128, 16, None, 40, 16, 4, 2, 3000, 2900), ("f32", 32, 16, None, 40, 16, 4, 2, 3000, 2900), ("bf16", 64, 16, None, 40, 16, 4, 2, 3000, 2900),
+    # by non-temporal loads
+    ("bf16", 128, 16, None, 60, 16, 4, 1, 13500, 2000), ("f32", 32, 16, None, 80, 16, 4, 1, 41000, 2000),
+    # shares, trees in tiles of 16 and 32 rows, several a tree
+    ("f32", 128, 16, None, 20, 16, 4, 9, 3000, 2900), ("bf16", 64, 16, None, 20, 16, 4, 9, 1400, 1300), ("bf16", 128, 32, None, 20, 16, 4, 9, 3000, 2900),
+    ("bf16", 64, 32, None, 20, 16, 4, 13, 3000, 2900), ("bf16", 32, 32, None, 20, 16, 4, 13, 3000, 2900), ("f32", 64, 32, None, 20, 16, 4, 9, 3000, 2900),
+    ("f32", 32, 32, None, 20, 16, 4, 9, 12000, 2900),
+    # lists in pieces that are joined: of 16 rows, by non-temporal loads, of 32 rows
+    ("bf16", 128, 16, 33, 3, 4, 1, 13, 4100, 4000), ("f32", 128, 16, 36, 2, 8, 2, 9, 9000, 8900), ("bf16", 128, 16, 4, 40, 16, 4, 1, 20480, 15000),
+    ("bf16", 128, 16, 253, 3, 4, 1, 2, 1100000, 40000), ("f32", 128, 16, 169, 3, 4, 1, 2, 1100000, 40000),
+    ("bf16", 128, 32, 59, 2, 8, 2, 9, 45000, 9000), ("bf16", 64, 32, 59, 2, 8, 2, 9, 45000, 9000), ("f32", 64, 32, 59, 2, 8, 2, 9, 60000, 9000),
+    ("f32", 32, 32, 63, 2, 8, 2, 9, 240000, 30000), ("bf16", 32, 32, 59, 2, 8, 2, 9, 45000, 9000),
+    # shares of tiles of 128 rows
+    ("bf16", 128, 128, None, 3, 8, 2, 20, 150016, 6000), ("bf16", 64, 128, None, 3, 8, 2, 33, 90000, 6000),
+]
+
+
+@pytest.mark.parametrize("plan", PLANS, ids=lambda p: "-".join(map(str, p)))
+def test_plans(plan):
+    """Lists that several workgroups work on, and workgroups that work on several lists."""
+    dtype, hd, rows, n, B, H, Hkv, T, positions, longest = plan
+    ctx, trees = ragged(B, T, longest, B)
+    ctx[0 if B < 7 else 2] = longest - T
+    c = Case4(ctx, trees, T, H, Hkv, hd, dtype, page=64, seed=B + T)
+    widen(c, positions)
+    assert workspace(c) == (shares(c, rows) if n is None else pieces(c, rows, n))
+    see, words = c.masks(seed=B, empty=(T - 1,) if T > 2 else ())
+    out, lse = c.check(words, see)
+    again, lse2 = ngg.tree_attention(c.q, c.kv, c.table, ints(ctx), mask=words, tree_lens=ints(trees), want_lse=True)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("dtype,hd,T", [("bf16", 64, 1), ("f32", 32, 3), ("bf16", 128, 2)])
+def test_shares_among_many_short_sequences(dtype, hd, T):
+    """More sequences than a wave looks through at once, most of them of one step and some not there, between a few long ones."""
+    B = 300
+    ctx, trees = [17 * b % 120 for b in range(B)], [1 + b % T for b in range(B)]
+    for b in (0, 60, 63, 64, 65, 127, 128, 200, 290, 299):
+        ctx[b] = 2300 + b
+    for b in range(130, 199):
+        ctx[b], trees[b] = 0, 0
+    c = Case4(ctx, trees, T, 4, 1, hd, dtype, page=32, seed=T)
+    widen(c, 2700)
+    assert workspace(c) == shares(c, 16)
+    c.check()
+
+
+class Tall(Case4):
+    """As there, with four times the query heads (over 64 rows) and a page list long enough for tiles of 128 rows."""
+
+    def __init__(self, ctx, trees, T, H, Hkv, hd, dtype="bf16", page=32, **more):
+        super().__init__(ctx, trees, T, 4 * H, Hkv, hd, dtype, page=page, **{**more, "wide": False})
+        widen(self, -(-(64 << 20) // (T * 4 * H * len(ctx))))
+        assert workspace(self) == shares(self, 128)
+
+
+@pytest.mark.parametrize("call", [
+    *[(name, dict(T=T, ctx=ctx, H=H, Hkv=Hkv, hd=hd)) for name in ("test_one_sequence",) for H, Hkv, hd in ((6, 2, 64), (8, 2, 128)) for T, ctx in ((6, 0), (17, 65), (70, 300))],
+    *[("test_ragged_batch", dict(hd=hd, page=page)) for hd in (64, 128) for page in (32, 160)],
+    ("test_sharp_scores", {}), ("test_queries_of_many_sizes", dict(hd=64)), ("test_queries_of_many_sizes", dict(hd=128)), ("test_repeats_itself", {}),
+    *[("test_masked_numbers_that_are_not_finite", dict(bad=bad)) for bad in (float("nan"), float("inf"), -float("inf"), 3.2e38)],
+    ("test_a_bad_number_in_the_context_reaches_every_row", dict(T=40))], ids=lambda c: "-".join([c[0][5:], *map(str, c[1].values())]))
+def test_tiles_of_128_rows(monkeypatch, call):
+    """The tests of test_gpu_cache4 that pad their page lists, by more."""
+    monkeypatch.setattr(test_gpu_cache4, "Case4", Tall)
+    getattr(test_gpu_cache4, call[0])(**call[1], dtype="bf16", wide=True)
+
+
+def test_rows_of_tall_tiles_that_see_nothing():
+    c = Tall([0, 40], [9, 9], 9, 8, 2, 64, "bf16", seed=10)
+    see, words = c.masks(seed=10, empty=(0, 4, 8))
+    c.check(words, see)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_pages_out_of_range_under_tall_tiles(hd):
+    """A page outside the pool hides its positions, at each place of a step of two pages."""
+    ctx, T = 150, 20
+    c = Tall([ctx], [T], T, 4, 1, hd, "bf16", seed=13, spare=0)
+    for at in (1, 2, 3):
+        keep = torch.cat([torch.arange(32 * at), torch.arange(32 * at + 32, ctx + T)]).cuda()
+        for wrong in (-1, c.kv.n_pages, 2 ** 31 - 1, -2 ** 31):
+            t = c.table.clone()
+            t[0, at] = wrong
+            out, lse = ngg.tree_attention(c.q, c.kv, t, ints([ctx]), want_lse=True)
+            test_gpu_cache4.check4(out, lse, c.q, [c.ks[0][keep]], [c.vs[0][keep]], [ctx - 32], [T], None, c.scale, "bf16")
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_strides_of_tall_tiles(hd):
+    c = Tall([40, 7, 130], [20] * 3, 20, 4, 2, hd, "bf16", seed=15)
+    want = c.check()[0]
+    for gap in (1, 2, 8):
+        big = torch.zeros(20, 3, 16, hd + gap, dtype=torch.bfloat16, device="cuda")
+        q = big.permute(1, 0, 2, 3)[..., gap:]
+        q.copy_(c.q)
+        dst = torch.full((3, 16, 20, hd + gap), 5.0, dtype=torch.bfloat16, device="cuda")
+        out = dst.permute(0, 2, 1, 3)[..., gap:]
+        ngg.tree_attention(q, c.kv, c.table, ints(c.ctx), out=out)
+        assert torch.equal(out, want) and (dst[..., :gap] == 5.0).all()
