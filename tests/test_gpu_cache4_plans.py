@@ -286,3 +286,69 @@ def test_strides_of_tall_tiles(hd):
         out = dst.permute(0, 2, 1, 3)[..., gap:]
         ngg.tree_attention(q, c.kv, c.table, ints(c.ctx), out=out)
         assert torch.equal(out, want) and (dst[..., :gap] == 5.0).all()
+
+
+def put(c, k, v):
+    """Keys and values [positions, heads, head_dim], which 4 bits hold as they are, for the one sequence of a Case4."""
+    pos = torch.arange(len(k), device="cuda")
+    slots = (c.table[0, pos // 64] * 64 + pos % 64).int()
+    c.kv.write(k.contiguous(), v.contiguous(), slots)
+    c.ks[0], c.vs[0] = c.kv.read(slots, torch.float32)
+    assert torch.equal(c.ks[0], k) and torch.equal(c.vs[0], v)
+
+
+FP32 = [(16, 0, 4, 4, 128, 1, 0), (16, 0, 8, 2, 64, 3, 0), (16, 0, 4, 1, 32, 4, 0), (16, 71, 8, 2, 128, 9, 18000), (16, 71, 8, 2, 64, 9, 18000), (32, 118, 8, 2, 64, 9, 120000),
+        (32, 125, 8, 2, 32, 9, 480000)]
+
+
+@pytest.mark.parametrize("rows,n,H,Hkv,hd,T,positions", FP32)
+def test_fp32_calls_keep_24_bits_of_a_query(rows, n, H, Hkv, hd, T, positions):
+    """Sixteen dimensions that are alike, of which the first two bfloat16 terms leave 2^-17, all of one sign: without the third the scores, and with them
+    the log sums, are off by 2^-17 of themselves.  They may be off by (16 + 14) 2^-24 of the sum of |q k|, sums of n terms by (n + 8) 2^-24 and the
+    logarithm by 2^-23 of itself."""
+    x = 1 + 16448 * 2.0 ** -23
+    c = Case4([5], [T], T, H, Hkv, hd, "f32", page=64, seed=51)
+    widen(c, positions)
+    assert workspace(c) == pieces(c, rows, n)
+    keys = 5 + T
+    k = torch.zeros(keys, Hkv, hd, device="cuda")
+    k[..., :16] = torch.tensor([3.0, 4.0, 6.0], device="cuda")[torch.arange(keys, device="cuda") % 3][:, None, None]
+    put(c, k, torch.ones_like(k))
+    c.q.zero_()
+    c.q[..., :16] = x
+    c.scale = 0.25
+    _, lse = ngg.tree_attention(c.q, c.kv, c.table, ints([5]), scale=0.25, want_lse=True)
+    first = torch.tensor(x, dtype=torch.float64).bfloat16().double()
+    two = (first + (x - first).bfloat16().double()).item()
+    for h in range(H):
+        want, qk = exact(c, 0, h)[2:]
+        tol = (16 + 14) * 2.0 ** -24 * qk + (keys + 8) * 2.0 ** -24 + 2.0 ** -23 * want.abs()
+        assert ((lse[0, :, h].double() - want).abs() <= tol).all()
+    c.q = c.q.double() / x * two
+    assert ((exact(c, 0, 0)[2] - want).abs() > 2 * tol).all()
+
+
+@pytest.mark.parametrize("rows,n,H,Hkv,hd,T,positions", FP32)
+def test_fp32_calls_keep_24_bits_of_a_probability(rows, n, H, Hkv, hd, T, positions):
+    """Keys of two kinds: the first have the row's largest score and values of zero, the others a probability beside them of 0.50224686, of which two
+    bfloat16 terms leave 2^-17, and values of one.  Without the third term outputs are off by 2^-17 of themselves; they may be by 2 (1 + 10) 2^-24 of the
+    sum of |q k| (of one dimension), by 3 n 2^-24 for sums of n terms, and by their rounding."""
+    c = Case4([1], [T], T, H, Hkv, hd, "f32", page=64, seed=52)
+    widen(c, positions)
+    assert workspace(c) == pieces(c, rows, n)
+    keys = 1 + T
+    second = torch.arange(keys, device="cuda") % 2 == 1
+    k, v = (torch.zeros(keys, Hkv, hd, device="cuda") for _ in range(2))
+    k[..., 0] = torch.where(second, 0.5, 1.0)[:, None]
+    v[:] = second.float()[:, None, None]
+    put(c, k, v)
+    c.q.zero_()
+    c.q[..., 0] = 1.0
+    c.scale = float(np.float32(-2 * np.log(0.50224686)))
+    out = ngg.tree_attention(c.q, c.kv, c.table, ints([1]), scale=c.scale)
+    for h in range(H):
+        want, mag, _, qk = exact(c, 0, h)
+        tol = mag * (2 * (1 + 10) * 2.0 ** -24 * qk[:, None] + 3 * keys * 2.0 ** -24) + want.abs() * 2.0 ** -24
+        assert ((out[0, :, h].double() - want).abs() <= tol).all()
+        assert ((exact(c, 0, h, 3)[0] - want).abs() <= tol).all()
+        assert ((exact(c, 0, h, 2)[0] - want).abs() > 1.5 * tol).all()
