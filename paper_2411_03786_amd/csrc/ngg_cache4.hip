@@ -79,7 +79,7 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(const CacheArgs a) {
   row[d1] = from_f32<T>(y);
 }
 
-// Runs of tokens, one workgroup per (32 tokens, head, keys or values), as kv_write_group_kernel.  A key's dimensions go to the pages
+// Runs of tokens, one workgroup per (32 tokens, up to four heads one after the other, keys or values), otherwise as kv_write_group_kernel.  A key's dimensions go to the pages
 // from the registers that they were read into; values pass through LDS, where eight positions of a byte come together.  Bound by the
 // conversions and the turning of bytes beside the memory: 16384 tokens of 8 heads of 128, 16 bits, 23 us, 3.7 TB/s; 976 of 12 of 64, fp32, 8.2.
 template <typename T>
@@ -365,16 +365,17 @@ static dim3 head_groups(const CacheArgs &a) {
 static int64_t launch_tokens(const CacheArgs &a) { return ((1 << 22) / a.p.Hkv - 1) * (int64_t)kGroup; }
 // Calls of few rows (tokens times heads) have 16 lanes for 32 dimensions, whose chain of loads is the shorter one.  Us a call in a graph, so
 // and by groups, of 8 heads of 128, rows:
-//                       512         2048        4096        8192
-//   written, 16 bits    4.6, 5.3    5.0, 5.5    6.0, 5.9    8.6, 6.6
-//            fp32       4.4, 6.4    4.9, 6.5    5.8, 7.3    8.5, 8.8
-//   rotated, 16 bits    4.8, 7.3    5.4, 7.4    6.5, 7.5    9.5, 8.2
-//   read, 16 bits       4.6, 5.3    4.8, 5.4    5.7, 5.7    8.0, 6.3
-//         fp32          4.7, 5.5    4.9, 5.7    5.9, 6.1    8.5, 7.1
+//                       2048        4096        6144        8192
+//   written, 16 bits    5.6, 6.1    6.4, 6.3    7.8, 6.4    9.2, 7.1
+//            fp32       5.4, 6.9    6.3, 7.6    7.7, 7.9    9.1, 8.7
+//   rotated, 16 bits    5.8, 7.7    7.1, 7.8    8.6, 7.8    10.2, 7.8
+//            fp32       5.8, 9.5    6.9, 9.4    8.5, 9.4    10.1, 9.4
+//   read, 16 bits       5.2, 5.8    6.2, 6.1    7.3, 6.2    8.5, 6.6
+//         fp32          5.4, 6.1    6.4, 6.4    7.6, 6.9    9.1, 7.4
 static bool few_rows4(const CacheArgs &a, int most) { return (int64_t)a.n_tokens * a.p.Hkv <= most; }
 template <typename T>
 static void write_type(const CacheArgs &all, hipStream_t s) {
-  if (few_rows4(all, all.cos || sizeof(T) == 4 ? 6144 : 3584)) hipLaunchKernelGGL((kv4_write_kernel<T>), row_blocks(all), dim3(256), 0, s, all);
+  if (few_rows4(all, sizeof(T) == 4 ? 6144 : all.cos ? 5120 : 3584)) hipLaunchKernelGGL((kv4_write_kernel<T>), row_blocks(all), dim3(256), 0, s, all);
   else
     in_parts<T>(all, [s](const CacheArgs &a) {
       hipLaunchKernelGGL((kv4_write_group_kernel<T>), head_groups(a), dim3(256), 0, s, a, (int)rows_of_vectors<T>(a, a.k, a.v), heads_of_group(a));
