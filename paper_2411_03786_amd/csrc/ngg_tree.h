@@ -92,7 +92,8 @@ __device__ __forceinline__ void step_totals(const TreeArgs &a, int *pre) {
 }
 
 // Steps of a share of the list: as many shares as workgroups were launched for, but of 256 keys at least where there are many (us with
-// one step of 128 keys and with two, 16 bits: 88 steps in all 12.4, 14.4; 240 steps 11.4, 12.1; 384 steps 15.9, 13.4; 504 steps 21.1, 18.2)
+// one step of 128 keys and with two, 16 bits: 88 steps in all 12.4, 14.4; 240 steps 11.4, 12.1; 384 steps 15.9, 13.4; 504 steps 21.1, 18.2;
+// over 4 bits 320 steps 12.4, 15.1; 480 steps 14.3, 16.1; 640 steps 15.8, 14.1; 960 steps 19.8, 19.7)
 template <int KS>
 __device__ __forceinline__ int share_steps(const TreeArgs &a, int total) {
   return max((int)((unsigned)(total + a.ranges - 1) / (unsigned)a.ranges), KS == 128 && total < 256 ? 1 : 256 / KS);

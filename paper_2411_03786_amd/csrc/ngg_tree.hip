@@ -730,7 +730,8 @@ static int tile_rows(int dtype, int hd, int rows, int64_t lists, int64_t positio
 // (tiles of 64 rows of two waves each, which share the steps: 1024, 51, 2047, 128: 160, of 32 rows 171 (102 M); 512, 51, 4000, 128: 147, 147; 256, 64,
 // 12000, 128: 210, 195; 192, 64, 16000, 64: 151, 147: not kept)
 // and in fp32 (16 and 32 rows; at heads of 128 the latter leaves a SIMD one wave): 64, 244, 4000, 128: 123, 136 (60 M); 24, 132, 4000, 64:
-// 34, 32 (12 M); 128, 100, 2000, 64: 60, 48 (24 M); 32, 40, 9000, 32: 23, 25 (11 M).
+// 34, 32 (12 M); 128, 100, 2000, 64: 60, 48 (24 M); 32, 40, 9000, 32: 23, 24 (11 M); 64, 40, 9000, 32: 32, 36 (22 M); 8, 244, 16000, 32: 32, 32 (30 M);
+// 4, 512, 16000, 32: 32, 31 (31 M); 32, 244, 8000, 32: 57, 57 (60 M).
 static int tile_rows4(int dtype, int hd, int rows, int64_t lists, int64_t positions) {
   if (rows <= 16) return 16;
   const int64_t scores = lists * positions * rows;
@@ -747,6 +748,11 @@ static int step_keys(int rows) { return rows <= 32 ? 128 : 64; }
 //     256, 16: 24.2, 29.1; 512, 16: 84, 88
 //   fp32: 8 to 48, 2: 12.5, 12.2-13.3; 3: 15.6, 12.6-13.3; 8: 32, 12.3-17.8.  128, 6: 25.9, 25.5; 8: 33, 27.  256, 16: 57, 65;
 //     512, 16: 160, 162
+// Over 4 bits the same bounds (whole and parted, pieces or shares; workgroups, steps):
+//   16 bits: 8, 4: 10.5, 11.0; 6: 12.3, 11.3.  48, 5: 11.6, 11.9; 8: 14.1, 12.9.  128, 6: 14.7, 16.5; 9: 18.0, 18.1; 12: 21.2, 18.7.
+//     256, 12: 22.1, 25.2; 16: 26.3, 31.8; 24: 42.3, 35.7.  512, 16: 40.1, 49.7; 24: 53.1, 60.9 (longer ones would still rather go whole)
+//   fp32: 8, 2: 9.8, 11.6; 4: 11.9, 11.6.  48, 3: 11.0, 12.1; 5: 12.9, 12.5.  128, 6: 16.2, 17.9; 9: 19.7, 19.5.  256, 16: 28.7, 30.8;
+//     20: 35.9, 35.0.  512, 16: 45.4, 49.8; 24: 60.5, 64.2
 // (2^23 workgroups: what a launch can hold of them.)
 static bool whole_lists(int dtype, int64_t steps, int64_t workgroups) {
   const bool wide = dtype == NGG_F32;
