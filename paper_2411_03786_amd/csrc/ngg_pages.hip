@@ -3,6 +3,7 @@
 #include "ngg_operators.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ngg {
 
@@ -83,29 +84,35 @@ __device__ __forceinline__ void move_few(const MoveArgs &a, void *base, int laye
   typedef typename Unit<K::B>::T U;
   const Move m = entry<K>(a, layer, b, threadIdx.x & 63);
   const uint64_t all = __ballot(m.ok);
-  if (all == 0) return;                                    // (of the whole wave)
   const int h = unit / K::N, u = unit - h * K::N;
-  const bool mine_too = h < a.p.Hkv;                       // lanes without a unit stay: they have entries that the others read
+  const bool mine_too = h < a.p.Hkv;
+  const uint64_t with = __ballot(mine_too);
+  if (all == 0 || with == 0) return;                       // (of the whole wave)
   uint8_t *mine = (uint8_t *)base + (int64_t)(mine_too ? h : 0) * a.p.page_size * K::POS + K::at(0, mine_too ? u : 0);
-  U x[kInRegisters];
-  uint64_t left = all;
+  // lanes without a unit stay with their wave, whose other lanes read their entries; waves that have none of them ask no lane
+  auto move = [&](auto whole) {
+    U x[kInRegisters];
+    uint64_t left = all;
 #pragma unroll
-  for (int i = 0; i < kInRegisters; ++i) {
-    if (left) {
-      const int64_t from = of_lane(m.from, __builtin_ctzll(left));
-      if (mine_too) x[i] = *reinterpret_cast<const U *>(mine + from);
+    for (int i = 0; i < kInRegisters; ++i) {
+      if (left) {
+        const int64_t from = of_lane(m.from, __builtin_ctzll(left));
+        if (whole || mine_too) x[i] = *reinterpret_cast<const U *>(mine + from);
+      }
+      left &= left - 1;                                    // (of none: none)
     }
-    left &= left - 1;                                      // (of none: none)
-  }
-  left = all;
+    left = all;
 #pragma unroll
-  for (int i = 0; i < kInRegisters; ++i) {
-    if (left) {
-      const int64_t to = of_lane(m.to, __builtin_ctzll(left));
-      if (mine_too) *reinterpret_cast<U *>(mine + to) = x[i];
+    for (int i = 0; i < kInRegisters; ++i) {
+      if (left) {
+        const int64_t to = of_lane(m.to, __builtin_ctzll(left));
+        if (whole || mine_too) *reinterpret_cast<U *>(mine + to) = x[i];
+      }
+      left &= left - 1;
     }
-    left &= left - 1;
-  }
+  };
+  if (with == ~(uint64_t)0) move(std::true_type{});
+  else move(std::false_type{});
 }
 // More entries wait in LDS, a column for each thread.
 template <typename K>
