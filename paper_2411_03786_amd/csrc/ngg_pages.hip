@@ -77,7 +77,7 @@ __device__ __forceinline__ int64_t of_lane(int64_t x, int l) {
 
 // Up to 16 entries, a lane's each; they wait in the registers of the threads that move their units, so that nothing waits for another wave.
 // Bound by two chains of loads and by the scattered bytes of values: the paths of 16 sequences in 32 layers, 20 MB of whole lines both
-// ways, take 11 us.
+// ways, take 10 us.
 constexpr int kInRegisters = 16;
 template <typename K>
 __device__ __forceinline__ void move_few(const MoveArgs &a, void *base, int layer, int b, int unit) {
@@ -114,7 +114,8 @@ __device__ __forceinline__ void move_few(const MoveArgs &a, void *base, int laye
   if (with == ~(uint64_t)0) move(std::true_type{});
   else move(std::false_type{});
 }
-// More entries wait in LDS, a column for each thread.
+// More entries wait in LDS, a column of 16 bytes an entry for each thread, by workgroups as small as 64 KB ask for: 16 lists of 64 entries in 32 layers of 8 heads of
+// 128, 4 bits, 247 us (29 MB both ways), one of 1024 4.2 ms; fp32 0.84 and 11 ms.
 template <typename K>
 __device__ __forceinline__ void move_many(const MoveArgs &a, void *base, int layer, int b, int unit, uint8_t *wait) {
   typedef typename Unit<K::B>::T U;
