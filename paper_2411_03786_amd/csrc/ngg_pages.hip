@@ -115,7 +115,7 @@ __device__ __forceinline__ void move_few(const MoveArgs &a, void *base, int laye
   else move(std::false_type{});
 }
 // More entries wait in LDS, a column of 16 bytes an entry for each thread, by workgroups as small as 64 KB ask for: 16 lists of 64 entries in 32 layers of 8 heads of
-// 128, 4 bits, 247 us (29 MB both ways), one of 1024 4.2 ms; fp32 0.84 and 11 ms.
+// 128, 4 bits, 247 us (71 MB both ways), one of 1024 4.2 ms; fp32 0.84 and 11 ms.
 template <typename K>
 __device__ __forceinline__ void move_many(const MoveArgs &a, void *base, int layer, int b, int unit, uint8_t *wait) {
   typedef typename Unit<K::B>::T U;
